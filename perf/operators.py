@@ -3,7 +3,8 @@ cache's writer and its inverse (fxp.kv_append, fxp.kv_load), attention over the 
 rows with 4-bit weights (fxp.linear4).
 
 The number format is the framework's: integer mantissas q under one biased exponent e, q standing for q * 2^(e - 127 - (bits - 2)).
-In the cache a block is the 64 tokens of one page and one head (keys [pages, heads, 64, dim], values [pages, heads, dim, 64]), in a
+In the cache a block is the 64 tokens of one page and one head (keys [pages, heads, 64, dim], values [pages, heads, 4, dim, 16]:
+four groups of 16 tokens, each transposed), in a
 weight matrix it is `group` inputs of one output.
 """
 import math
@@ -163,7 +164,7 @@ def _mantissas(shape, bits, g):
 
 def _cache(case, pages, g):
     H, D, bits = case["heads"], case["dim"], case["bits"]
-    return dict(kq=_mantissas((pages, H, PAGE, D), bits, g), vq=_mantissas((pages, H, D, PAGE), bits, g),
+    return dict(kq=_mantissas((pages, H, PAGE, D), bits, g), vq=_mantissas((pages, H, PAGE // 16, D, 16), bits, g),
                 ek=torch.randint(127, 130, (pages, H), dtype=torch.int32, device="cuda", generator=g),
                 ev=torch.randint(124, 129, (pages, H), dtype=torch.int32, device="cuda", generator=g))
 
@@ -328,6 +329,11 @@ def _write(x, q, e, runs, bits):
     return page, torch.where(new, mapped.to(torch.int8), moved.to(torch.int8)).permute(0, 2, 1, 3), e_all.int()
 
 
+def _rows(vq):
+    """Value pages [..., 4, dim, 16] as rows [..., 64, dim]."""
+    return vq.transpose(-1, -2).flatten(-3, -2)
+
+
 def _values(q, e, bits):
     return q.float() * _pow2(e - 125 - bits).float()[:, :, None, None]
 
@@ -343,11 +349,11 @@ def _append(s):
     bits = s["case"]["bits"]
     page, q, e = _write(s["k"], s["kq"], s["ek"], s["runs"], bits)
     s["kq"][page], s["ek"][page] = q, e
-    page, q, e = _write(s["v"], s["vq"].transpose(2, 3), s["ev"], s["runs"], bits)
-    s["vq"][page], s["ev"][page] = q.transpose(2, 3), e
+    page, q, e = _write(s["v"], _rows(s["vq"]), s["ev"], s["runs"], bits)
+    s["vq"][page], s["ev"][page] = q.unflatten(2, (PAGE // 16, 16)).transpose(3, 4), e
     at = s["read"][:, 2].long()
     k = _read(_values(s["kq"][at], s["ek"][at], bits), s["read"])
-    v = _read(_values(s["vq"][at].transpose(2, 3), s["ev"][at], bits), s["read"])
+    v = _read(_values(_rows(s["vq"][at]), s["ev"][at], bits), s["read"])
     return dict(k=k, v=v, ek=s["ek"], ev=s["ev"])
 
 
@@ -359,8 +365,8 @@ def _attend(s):
     at = s["table"].long().clamp(min=0)
     k = s["kq"][at].float() * _pow2(s["ek"][at] - 125 - case["bits"]).float()[..., None, None]        # [B, blocks, H, 64, D]
     k = k.permute(0, 2, 1, 3, 4).reshape(B * H, L, D)
-    v = s["vq"][at].float() * _pow2(s["ev"][at] - 125 - case["bits"]).float()[..., None, None]        # [B, blocks, H, D, 64]
-    v = v.permute(0, 2, 1, 4, 3).reshape(B * H, L, D)
+    v = _rows(s["vq"][at]).float() * _pow2(s["ev"][at] - 125 - case["bits"]).float()[..., None, None]
+    v = v.permute(0, 2, 1, 3, 4).reshape(B * H, L, D)
     first, lens = s["first"].long(), s["lens"].long()
     i = torch.arange(n, device=k.device)
     there = i < (first[1:] - first[:-1])[:, None]
@@ -445,7 +451,7 @@ def exact(case, seed):
     bits, H, D = case["bits"], case["heads"], case["dim"]
     if case["kind"] == "append":
         out = {}
-        for name, x, q, e in (("k", s["k"], s["kq"], s["ek"]), ("v", s["v"], s["vq"].transpose(2, 3), s["ev"])):
+        for name, x, q, e in (("k", s["k"], s["kq"], s["ek"]), ("v", s["v"], s["vq"].permute(0, 1, 2, 4, 3).reshape(-1, H, PAGE, D), s["ev"])):
             x, q, e, rows = x.double().cpu(), q.cpu(), e.cpu(), []
             for t, n, page, off in s["runs"].tolist():
                 if n == 0:
@@ -474,7 +480,8 @@ def exact(case, seed):
         hidden = (j > position) | ((j <= position - case["window"]) if case["window"] else False)
         for h in range(H):
             k = (s["kq"][at, h].double() * (2.0 ** (s["ek"][at, h].double() - 125 - bits))[:, None, None]).reshape(-1, D)[:L]
-            v = (s["vq"][at, h].double() * (2.0 ** (s["ev"][at, h].double() - 125 - bits))[:, None, None]).transpose(1, 2).reshape(-1, D)[:L]
+            v = s["vq"][at, h].double() * (2.0 ** (s["ev"][at, h].double() - 125 - bits))[:, None, None, None]
+            v = v.transpose(2, 3).reshape(-1, D)[:L]
             q = s["q"][first[b]:first[b + 1], h * G:(h + 1) * G].double().transpose(0, 1).reshape(G * n, D)
             a = (q @ k.T.contiguous() * s["scale"]).view(G, n, L).masked_fill(hidden, -math.inf)
             a = torch.exp(a - a.amax(-1, keepdim=True).clamp(min=-1e300))
