@@ -45,8 +45,10 @@ typedef enum fxp_status {
     FXP_ERR_ROUNDING = -5,  /* unknown rounding mode */
     FXP_ERR_BITS = -6,      /* bits outside [2, 8] */
     FXP_ERR_LAUNCH = -7,    /* the HIP runtime refused a launch */
-    FXP_ERR_OVERFLOW = -8   /* contraction longer than an int32 sum is sure to hold (> 133144 terms) where the call has no
+    FXP_ERR_OVERFLOW = -8,  /* contraction longer than an int32 sum is sure to hold (> 133144 terms) where the call has no
                                64-bit path for it: int32 output, a batched product, or no room in ws for the slices */
+    FXP_ERR_TYPE = -9,      /* unknown element type */
+    FXP_ERR_VALUE = -10     /* a scalar argument outside its range */
 } fxp_status;
 
 /* Rounding of the 24-bit shifted mantissa to bits-1 magnitude bits. */
@@ -372,6 +374,118 @@ int fxp_conv2d_fwd(const float* X, const float* W, const fxp_conv2d_shape* shape
 int fxp_conv2d_bwd(const float* dY, const fxp_conv_saved* saved, const fxp_conv2d_shape* shape, float* dX, float* dW,
                    int8_t* dYq, int8_t* dYqT, int32_t* e_dY, uint64_t seed, uint64_t step, int rounding, int bits,
                    void* ws, size_t ws_bytes, void* stream);
+
+/* ---- serving: a paged cache of mapped keys and values, attention over it, products with 4-bit weights ----
+ * The mapping of Sec. 3.1 with one scale per BLOCK instead of one per tensor, rounded to nearest (FXP_ROUND_NEAREST: a
+ * cache is written once and read many times, and a served answer does not depend on a seed). */
+
+/* Element types of the tensors that these calls read and write. */
+enum { FXP_F32 = 0, FXP_BF16 = 1, FXP_F16 = 2 };
+
+/* Tokens of a page: the cache's block, and the contraction of one int8 matrix instruction. */
+#define FXP_KV_PAGE 64
+
+/* A cache of one layer (host struct of device pointers, caller-allocated, 16-byte aligned).  A block is the
+ * FXP_KV_PAGE tokens of one page and one head; it has one scale for its keys and one for its values.
+ *   kq [pages, heads, 64, dim]       keys, a token's row contiguous
+ *   vq [pages, heads, 4, dim, 16]    values in four groups of 16 tokens, each group transposed: what a contraction over
+ *                                    tokens reads without moving a byte, and a new token touches a quarter of the block
+ *   ek, ev [pages, heads]            int32 scales
+ * dim: a multiple of 16, at most 256.  pages < 2^31, heads <= 65535.  bits: width of the mantissas, 2..8 (stored as
+ * int8 whatever the width).  A block's bytes behind its last token are never interpreted; a cache needs no clearing. */
+typedef struct fxp_kv_cache {
+    int8_t* kq;
+    int8_t* vq;
+    int32_t* ek;
+    int32_t* ev;
+    int64_t pages, heads, dim;
+    int bits;
+} fxp_kv_cache;
+
+/* The tables of a step (host struct of device pointers, caller-allocated; slots 8-byte, runs 16-byte aligned, the others 4-byte).
+ * Request b < requests holds lens[b] tokens, in ceil(lens[b] / 64) pages whose numbers are the first entries of
+ * its row of block_table [requests, blocks].  free_pages [pages] is a stack of n_free[0] pages nobody holds.
+ * requests, tokens, pages, blocks * 64 < 2^31.  All a step's calls read the same struct; every layer's cache shares it. */
+typedef struct fxp_kv_step {
+    int64_t requests, blocks, tokens, pages;
+    const int32_t* lens;       /* [requests] */
+    const int32_t* free_pages; /* [pages] */
+    const int32_t* n_free;     /* [1] */
+    int32_t* block_table;      /* [requests, blocks]: the pages taken are entered */
+    int32_t* lens_after;       /* [requests]; may be lens */
+    int32_t* n_free_after;     /* [1]; may be n_free */
+    int32_t* first;            /* [requests + 1]: first new token of each request, and their number */
+    int64_t* slots;            /* [tokens]: page * 64 + place in it of each new token, -1 where it has none */
+    int32_t* positions;        /* [tokens]: place of each new token in its request, -1 behind the last one */
+    int32_t* runs;             /* [fxp_kv_max_runs(requests, tokens), 4]: (first token, count, page, offset) of the new
+                                  tokens that share a page; (0, 0, -1, 0) behind the last run */
+    int32_t* refused;          /* [requests]: 1 = the request's new tokens found no room */
+} fxp_kv_step;
+
+/* Most runs that `tokens` new tokens of `requests` requests can fall into; 0 on bad arguments. */
+int64_t fxp_kv_max_runs(int64_t requests, int64_t tokens);
+
+/* Makes room for n_new[b] (device, >= 0) more tokens of each request and fills the tables of the step.  Pages are
+ * taken from the top of the stack in the order of the requests.  A request that would outgrow its row of
+ * block_table is refused; so is, from the first one that the stack cannot serve on, every request that needs a page.
+ * A refused request keeps its length and its row, its tokens get slot -1 and runs on page -1 (fxp_kv_append skips them).
+ * Tokens and runs beyond `tokens` and the runs' capacity are not written.  Lengths that are negative count as 0.
+ * ws: NULL, or at least 256 bytes, zero before the first call that uses them, which every call leaves zero; required where
+ * lens_after or n_free_after is the input itself. */
+int fxp_kv_tables(const fxp_kv_step* step, const int32_t* n_new, void* ws, size_t ws_bytes, void* stream);
+
+/* Maps new tokens into the cache.  k, v: `tokens` rows of heads x dim elements of `type`, token t and head h at
+ * t * k_token + h * k_head elements (any strides >= 0; fastest where base and strides are multiples of four elements).
+ * runs [n_runs < 2^24, 4], 16-byte aligned: see fxp_kv_step; pages must differ, as those of fxp_kv_tables do.
+ * A block's scale is the largest exponent of the values it holds: where a new token raises it, the tokens
+ * before it are brought to the new scale (magnitude shifted right, rounded half up).  A run at offset 0 begins the block
+ * anew.  A run whose tokens, page or places do not exist is skipped.  Non-finite values: see the top of this file. */
+int fxp_kv_append(const fxp_kv_cache* cache, int type, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                  int64_t v_token, int64_t v_head, int64_t tokens, const int32_t* runs, int64_t n_runs, void* stream);
+
+/* The inverse mapping of cached tokens: row t of k, v [tokens, heads, dim] of `type` receives the values that the
+ * token stands for, rounded once (exact in fp32 and bf16 but for overflow and underflow).  runs as above: the tokens
+ * at places offset .. offset + count - 1 of a page go to rows first ..; rows of no run are left as they are. */
+int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t tokens, const int32_t* runs, int64_t n_runs,
+                void* stream);
+
+/* Attention of new tokens over the cache (the paper's int8 attention products with the softmax in floating point,
+ * Sec. 5).  Request b has step->first[b+1] - step->first[b] rows of q, which are its last ones: row i of n stands at place
+ * lens_after[b] - n + i and sees the tokens at and before it; with window > 0 only the `window` last of them.
+ * out = sum_j softmax_j(scale * q . k_j) v_j with k, v the values that the cache stands for.  Head h of q reads head
+ * h / (q_heads / heads) of the cache; q_heads is a multiple of heads.  q and out: [tokens, q_heads, dim] of `type`, strides
+ * as in fxp_kv_append; rows behind the last request's are left as they are.  A row that sees nothing (no cached
+ * token; all of its pages missing) gives zeros and lse -Inf.  Of *step only requests, blocks, tokens, first,
+ * lens_after and block_table are used; firsts beyond `tokens` count as `tokens`, tokens on a page outside [0, pages) are not seen.
+ * lse: NULL, or [tokens, q_heads] fp32 receiving log sum_j exp(scale * q . k_j).
+ * Arithmetic: rows of q and the weights of 64 tokens are fixed-point numbers of two signed 8-bit digits (three for fp32: 23
+ * bits) under a scale of their own, products are exact int32 sums over 64 terms, sums over more and the
+ * softmax are fp32.  0 < scale < 2^64.  Scores are taken to lie below 2^89 in magnitude.
+ * ws: fxp_kv_attention_workspace_bytes bytes, 256-byte aligned; 0 on bad arguments. */
+size_t fxp_kv_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim);
+int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int type, const void* q, int64_t q_token, int64_t q_head,
+                     int64_t q_heads, float scale, int64_t window, void* out, int64_t out_token, int64_t out_head, float* lse,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* ---- products of a few rows with 4-bit weights ----
+ * A weight matrix W [K, N] as mantissas -7..7 (the mapping with bits = 4, rounded to nearest) with one scale for
+ * each group of `group` (32, 64 or 128) inputs of one output.  Packed layout, made once: tiles of 16 outputs x 128 inputs,
+ * [ceil(N / 16), ceil(K / 128)] tiles of 1024 bytes.  With S = min(group, 64) and k counted in the tile, output r of
+ * the tile and input k are in piece 16 * ((k % S) / (S / 4)) + r of 16 bytes, byte (k / S) * (S / 8) + k % (S / 8) of it, low
+ * half if (k % (S / 4)) < S / 8, else the high half, in two's complement.  scales: uint8 biased exponents
+ * [ceil(N / 16), ceil(K / 128) * 128 / group, 16].  Inputs and outputs past K and N are zero.
+ * K <= 2^20, N <= 2^24; K * ceil16(M) <= 2^34. */
+size_t fxp_w4_packed_bytes(int64_t K, int64_t N);
+size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group);
+/* W: K rows of N elements of `type`, row stride ldw >= N.  packed 16-byte, scales 4-byte aligned. */
+int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales, void* stream);
+/* Y[M,N] = X[M,K] * W.  X, Y of `type`, row strides ldx >= K, ldy >= N.  Made for few rows (one pass over the weights for each 64 of
+ * them); any M is right.  A group of a row of X is a fixed-point number of two signed 8-bit digits (three for fp32)
+ * under its own scale: products are exact int32 sums over a group, sums over groups fp32.
+ * ws: fxp_w4_workspace_bytes bytes (0 on bad arguments), 256-byte aligned. */
+size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group);
+int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, int64_t K, int64_t N, const uint8_t* packed, const uint8_t* scales,
+                  int group, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
 
 /* ---- measurement helper (not a step of the method) ----
  * Core clock while other work runs: enqueues one wave on `stream` (use a stream of its own, next to the kernels

@@ -1,0 +1,451 @@
+// A paged cache of mapped keys and values: the tables of a step, the writer, the inverse mapping.
+//
+// Tables.  Request b with l tokens that receives n more needs ceil((l + n) / 64) - ceil(l / 64) pages; an exclusive sum
+// over the requests gives each its first new token, its place in the stack of free pages and its first run (the new tokens
+// that share a page).  One launch: every workgroup sums over all requests (4 KB per thousand of them, out of the L2) and
+// fills 256 runs of its own, so nothing is exchanged between workgroups.
+//
+// Writer.  q = floor(|x| 2^(125 + bits - e) + 1/2) with e the largest exponent of the block.  A workgroup has one run of one
+// head, keys or values; a thread has blocks of 4 tokens x 4 elements, which is one dword each way for keys (a token's four
+// elements) and, transposed in registers, for values (an element's four tokens).
+#include "fxp_serve_device.h"
+
+namespace fxp {
+
+constexpr int kTabThreads = 1024;
+constexpr int kTabRuns = 256;          // runs a workgroup fills
+
+struct Three {
+    int tokens, need, runs;
+};
+__device__ inline Three add3(const Three& a, const Three& b) { return {a.tokens + b.tokens, a.need + b.need, a.runs + b.runs}; }
+
+// exclusive sums over the workgroup's threads; `total` receives the sum of all
+__device__ inline Three block_scan3(const Three& v, Three* lds, Three& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Three s = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const Three t = {__shfl_up(s.tokens, d), __shfl_up(s.need, d), __shfl_up(s.runs, d)};
+        if (lane >= d) s = add3(s, t);
+    }
+    if (lane == 63) lds[wave] = s;
+    __syncthreads();
+    Three before = {0, 0, 0};
+    total = {0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kTabThreads / 64; ++w) {
+        if (w == wave) before = total;
+        total = add3(total, lds[w]);
+    }
+    __syncthreads();
+    return {before.tokens + s.tokens - v.tokens, before.need + s.need - v.need, before.runs + s.runs - v.runs};
+}
+
+struct Request {
+    int len, had, after, served, first, need0, run0, row;
+};
+
+// what request b asks for; lengths that no device program should hold (negative, sums past 32 bits) only have to stay harmless:
+// every index that comes of them is compared with its array before it is used
+__device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_t b, Request& r, bool& fits) {
+    Three v = {0, 0, 0};
+    fits = false;
+    r.len = r.after = r.had = 0;
+    if (b >= st.requests) return v;
+    const int64_t len = max(st.lens[b], 0), n = min(static_cast<int64_t>(max(n_new[b], 0)), st.tokens), after = len + n;
+    fits = after <= st.blocks * FXP_KV_PAGE;
+    r.len = static_cast<int>(len);
+    r.after = static_cast<int>(min(after, (int64_t{1} << 31) - 1));
+    r.had = static_cast<int>((len + FXP_KV_PAGE - 1) / FXP_KV_PAGE);
+    v.tokens = static_cast<int>(n);
+    v.need = fits ? static_cast<int>((after + FXP_KV_PAGE - 1) / FXP_KV_PAGE) - r.had : 0;
+    v.runs = n ? static_cast<int>((after - 1) / FXP_KV_PAGE - len / FXP_KV_PAGE) + 1 : 0;
+    return v;
+}
+
+// lengths, firsts, refusals and the rest of the stack, of all requests; `outputs`: firsts and refusals too
+__device__ inline void commit_lengths(const fxp_kv_step& st, const int32_t* n_new, Three* lds) {
+    const int n_free = min(static_cast<int64_t>(max(st.n_free[0], 0)), st.pages);
+    __shared__ int taken;
+    if (threadIdx.x == 0) taken = 0;
+    __syncthreads();
+    Three carry = {0, 0, 0}, total;
+    for (int64_t base = 0; base < st.requests; base += kTabThreads) {
+        Request r;
+        bool fits;
+        const Three v = asks(st, n_new, base + threadIdx.x, r, fits);
+        const Three x = add3(carry, block_scan3(v, lds, total));
+        const bool served = fits && (v.need == 0 || x.need + v.need <= n_free);
+        if (base + threadIdx.x < st.requests) st.lens_after[base + threadIdx.x] = served ? r.after : st.lens[base + threadIdx.x];
+        if (served && v.need) atomicMax(&taken, x.need + v.need);
+        carry = add3(carry, total);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) st.n_free_after[0] = n_free - taken;
+}
+
+__global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const int32_t* __restrict__ n_new, int64_t run_rows,
+                                                           uint32_t* ticket) {
+    __shared__ Three lds[kTabThreads / 64];
+    __shared__ Request req[kTabRuns];
+    __shared__ int mark[kTabRuns];          // position of the request that a run belongs to, at the request's first run here
+    __shared__ int64_t slot0[kTabRuns];
+    __shared__ int4 span[kTabRuns];         // first token, count, position of the first token
+    __shared__ int long_runs, last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r0 = blockIdx.x * kTabRuns;
+    const int n_free = min(static_cast<int64_t>(max(st.n_free[0], 0)), st.pages);
+    if (tid < kTabRuns) mark[tid] = -1;
+    if (tid == 0) long_runs = 0;
+    __syncthreads();
+
+    Three carry = {0, 0, 0}, total;
+    for (int64_t base = 0; base < st.requests; base += kTabThreads) {
+        const int64_t b = base + tid;
+        Request r;
+        bool fits;
+        const Three v = asks(st, n_new, b, r, fits);
+        const Three x = add3(carry, block_scan3(v, lds, total));
+        r.served = fits && (v.need == 0 || x.need + v.need <= n_free);
+        r.first = x.tokens;
+        r.need0 = x.need;
+        r.run0 = x.runs;
+        r.row = static_cast<int>(b);
+        // each thousand of requests has a workgroup that writes what belongs to a request
+        if (b < st.requests && (base / kTabThreads) % gridDim.x == blockIdx.x) {
+            st.first[b] = r.first;
+            st.refused[b] = !r.served;
+        }
+        const int lo = max(x.runs, r0);
+        if (v.runs > 0 && lo < x.runs + v.runs && lo < r0 + kTabRuns && x.runs >= 0) {
+            req[lo - r0] = r;
+            mark[lo - r0] = lo - r0;
+        }
+        carry = add3(carry, total);
+    }
+    if (blockIdx.x == 0 && tid == 0) st.first[st.requests] = carry.tokens;
+    __syncthreads();
+
+    // the request of each run: the nearest mark at or before it
+    int owner = -1;
+    if (tid < kTabRuns) {
+        owner = mark[tid];
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int t = __shfl_up(owner, d);
+            if (lane >= d) owner = max(owner, t);
+        }
+        if (lane == 63) mark[tid] = owner;                  // the last of each wave: read below by the waves after it
+    }
+    __syncthreads();
+    if (tid < kTabRuns) {
+        for (int w = 0; w < wave; ++w) owner = max(owner, mark[64 * w + 63]);
+        const int run = r0 + tid;
+        int4 s = make_int4(0, 0, 0, 0);
+        if (run < run_rows) {
+            int4 out = make_int4(0, 0, -1, 0);
+            if (run < carry.runs && owner >= 0) {
+                const Request r = req[owner];
+                const int j = run - r.run0, block = r.len / FXP_KV_PAGE + j, off = j ? 0 : r.len % FXP_KV_PAGE;
+                const int t0 = r.first + (j ? j * FXP_KV_PAGE - r.len % FXP_KV_PAGE : 0);
+                const int count = min(FXP_KV_PAGE - off, r.after - (block * FXP_KV_PAGE + off));
+                int page = -1;
+                if (r.served && block < st.blocks) {
+                    int32_t* entry = st.block_table + int64_t{r.row} * st.blocks + block;
+                    if (block >= r.had) {
+                        const int at = n_free - 1 - (r.need0 + block - r.had);
+                        page = at >= 0 && at < n_free ? st.free_pages[at] : -1;
+                        *entry = page;
+                    } else {
+                        page = *entry;
+                    }
+                }
+                page = max(page, -1);
+                const int64_t slot = page < 0 ? -1 : int64_t{page} * FXP_KV_PAGE + off;
+                const int position = block * FXP_KV_PAGE + off;
+                out = make_int4(t0, count, page, off);
+                s = make_int4(t0, count, position, 0);
+                slot0[tid] = slot;
+                if (t0 >= 0 && t0 < st.tokens) {            // a run's first token here: in a decode step there is no other
+                    st.slots[t0] = slot;
+                    st.positions[t0] = position;
+                }
+                if (count > 1) long_runs = 1;
+            }
+            reinterpret_cast<int4*>(st.runs)[run] = out;
+        }
+        span[tid] = s;
+    }
+    __syncthreads();
+    if (long_runs)
+        for (int i = wave; i < kTabRuns; i += kTabThreads / 64) {
+            const int4 s = span[i];
+            const int64_t t = int64_t{s.x} + lane;
+            if (lane >= 1 && lane < s.y && t >= 0 && t < st.tokens) {
+                st.slots[t] = slot0[i] < 0 ? -1 : slot0[i] + lane;
+                st.positions[t] = s.z + lane;
+            }
+        }
+    for (int64_t t = carry.tokens + int64_t{blockIdx.x} * kTabThreads + tid; t < st.tokens; t += int64_t{gridDim.x} * kTabThreads)
+        if (t >= 0) {
+            st.slots[t] = -1;
+            st.positions[t] = -1;
+        }
+
+    // The lengths and the stack's height may be updated in place: by the workgroup that is last to have read them.
+    if (ticket) {
+        __syncthreads();
+        if (tid == 0) {
+            last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+            if (last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (last) commit_lengths(st, n_new, lds);
+    } else if (blockIdx.x == gridDim.x - 1) {
+        commit_lengths(st, n_new, lds);
+    }
+}
+
+// ---- writer ----
+
+// four tokens x four elements of a [tokens, heads, dim] operand, rows behind `count` zero
+template <int TYPE>
+__device__ inline void load_block(const void* x, int64_t at, int64_t token, int from, int to, bool vec, float (&v)[4][4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= from && i < to) {
+            load_elems<TYPE, 4>(x, at + i * token, vec, v[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i][j] = 0.0f;
+        }
+    }
+}
+
+template <int TYPE, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const void* __restrict__ k, int64_t k_token, int64_t k_head,
+                                                       const void* __restrict__ v, int64_t v_token, int64_t v_head, int64_t tokens,
+                                                       const int4* __restrict__ runs, int vec_k, int vec_v) {
+    __shared__ uint32_t lds[THREADS / 64];
+    const int4 rr = runs[blockIdx.x];
+    const Run run = {rr.x, rr.y, rr.z, rr.w};
+    if (!run_ok(run, tokens, c.pages)) return;
+    const bool values = blockIdx.z != 0;
+    const int head = blockIdx.y, dim = static_cast<int>(c.dim), nd = dim / 4;
+    const void* x = values ? v : k;
+    const int64_t token = values ? v_token : k_token;
+    const bool vec = values ? vec_v : vec_k;
+    const int64_t row0 = int64_t{run.first} * token + head * (values ? v_head : k_head);
+    const int64_t block = int64_t{run.page} * c.heads + head;
+    int32_t* const scale = (values ? c.ev : c.ek) + block;
+    uint32_t* const page = reinterpret_cast<uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
+
+    // the new tokens as quads of places 4 tq .. 4 tq + 3 of the page, with those before the run and behind it left out
+    const int tq0 = run.offset / 4, end = run.offset + run.count, quads = (end + 3) / 4 - tq0, work = quads * nd;
+    const int e_old = run.offset ? min(max(*scale, 1), 255) : 1;
+    constexpr int kKept = 2;             // blocks of 16 values a thread keeps; others are read again, out of the cache
+    float kept[kKept][4][4];
+    uint32_t m = 0;
+    auto fetch = [&](int i, float (&w)[4][4]) {
+        const int tq = tq0 + i / nd, d = i % nd * 4, place = 4 * tq;
+        load_block<TYPE>(x, row0 + (int64_t{place} - run.offset) * token + d, token, max(run.offset - place, 0), min(end - place, 4), vec, w);
+    };
+    auto largest = [&](const float (&w)[4][4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = max(m, __float_as_uint(w[i][j]) & 0x7fffffffu);
+    };
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) {
+            fetch(threadIdx.x + n * THREADS, kept[n]);
+            largest(kept[n]);
+        }
+    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+        float w[4][4];
+        fetch(i, w);
+        largest(w);
+    }
+    m = THREADS == 64 ? wave_max(m) : block_max<THREADS / 64>(m, lds);
+    const int e = max(e_old, min(max(static_cast<int>(m >> 23), 1), 255)), grown = e - e_old, cut = 25 - c.bits;
+    if (threadIdx.x == 0) *scale = e;
+
+    // address (in dwords) of a block of values' element j, or of keys' token j
+    auto place_of = [&](int tq, int d, int j) {
+        return values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4;
+    };
+    auto write = [&](int i, const float (&w)[4][4]) {
+        const int tq = tq0 + i / nd, d = i % nd * 4, from = max(run.offset - 4 * tq, 0), to = min(end - 4 * tq, 4);
+        uint32_t o[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            o[a] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[a] |= (static_cast<uint32_t>(map_nearest(w[a][j], e, cut)) & 0xffu) << (8 * j);
+        }
+        if (values) {
+            uint32_t t[4];
+            transpose4x4(o, t);
+            const uint32_t old = from ? (1u << (8 * from)) - 1u : 0u;        // bytes of the tokens before the run
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t* p = page + place_of(tq, d, j);
+                if (from) {
+                    const uint32_t b = *p;
+                    t[j] = (t[j] & ~old) | ((grown ? remap_nearest4(b, grown) : b) & old);
+                }
+                *p = t[j];
+            }
+        } else {
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                uint32_t* p = page + place_of(tq, d, a);
+                if (a >= from && a < to) *p = o[a];
+                else if (a < from && grown) *p = remap_nearest4(*p, grown);
+            }
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) write(threadIdx.x + n * THREADS, kept[n]);
+    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+        float w[4][4];
+        fetch(i, w);
+        write(i, w);
+    }
+    // quads of old tokens alone
+    if (run.offset && grown)
+        for (int i = threadIdx.x; i < tq0 * nd; i += THREADS)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t* p = page + place_of(i / nd, i % nd * 4, j);
+                *p = remap_nearest4(*p, grown);
+            }
+}
+
+// ---- inverse mapping: a wave has 4 tokens x 64 quads of elements at a time ----
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_kv_load(fxp_kv_cache c, void* __restrict__ k, void* __restrict__ v, int64_t tokens,
+                                                 const int4* __restrict__ runs) {
+    const int4 rr = runs[blockIdx.x];
+    const Run run = {rr.x, rr.y, rr.z, rr.w};
+    if (!run_ok(run, tokens, c.pages)) return;
+    const bool values = blockIdx.z != 0;
+    const int head = blockIdx.y, dim = static_cast<int>(c.dim), nd = dim / 4;
+    const int64_t block = int64_t{run.page} * c.heads + head;
+    const int unit = min(max((values ? c.ev : c.ek)[block], 1), 255) - 125 - c.bits;
+    const uint32_t* page = reinterpret_cast<const uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
+    const int tq0 = run.offset / 4, end = run.offset + run.count, work = ((end + 3) / 4 - tq0) * nd;
+    for (int i = threadIdx.x; i < work; i += 256) {
+        const int tq = tq0 + i / nd, d = i % nd * 4;
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) b[j] = page[values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4];
+        if (values) {
+            uint32_t t[4];
+            transpose4x4(b, t);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = t[j];
+        }
+#pragma unroll
+        for (int a = 0; a < 4; ++a) {
+            const int place = 4 * tq + a;
+            if (place < run.offset || place >= end) continue;
+            float x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[j] = unmap_value(static_cast<int8_t>(b[a] >> (8 * j)), unit);
+            store4<TYPE>(values ? v : k, ((int64_t{run.first} + place - run.offset) * c.heads + head) * dim + d, true, x);
+        }
+    }
+}
+
+constexpr int64_t kMostRuns = (int64_t{1} << 24) - 1;      // 256 threads each, fewer than 2^32 in all
+
+static bool multiple_of_4(const void* p, int64_t token, int64_t head, int type) {
+    return aligned(p, 4 * elem_size(type)) && token % 4 == 0 && head % 4 == 0;
+}
+
+}  // namespace fxp
+
+extern "C" int64_t fxp_kv_max_runs(int64_t requests, int64_t tokens) {
+    if (requests < 0 || tokens < 0 || requests >= (int64_t{1} << 31) || tokens >= (int64_t{1} << 31)) return 0;
+    // n tokens of one request touch at most (n + 126) / 64 pages, and at least one token each
+    const int64_t most = (tokens + 2 * (FXP_KV_PAGE - 1) * requests) / FXP_KV_PAGE;
+    return most < tokens ? most : tokens;
+}
+
+extern "C" int fxp_kv_tables(const fxp_kv_step* st, const int32_t* n_new, void* ws, size_t ws_bytes, void* stream) {
+    if (!st) return FXP_ERR_NULL;
+    constexpr int64_t kMost = int64_t{1} << 31;
+    if (st->requests <= 0 || st->blocks <= 0 || st->tokens < 0 || st->pages <= 0 || st->requests >= kMost || st->tokens >= kMost ||
+        st->pages >= kMost || st->blocks * FXP_KV_PAGE >= kMost || st->blocks >= kMost)
+        return FXP_ERR_DIMS;
+    if (!n_new || !st->lens || !st->free_pages || !st->n_free || !st->block_table || !st->lens_after || !st->n_free_after || !st->first ||
+        !st->refused || (st->tokens && (!st->slots || !st->positions || !st->runs)))
+        return FXP_ERR_NULL;
+    for (const void* p : {static_cast<const void*>(n_new), static_cast<const void*>(st->lens), static_cast<const void*>(st->free_pages),
+                          static_cast<const void*>(st->n_free), static_cast<const void*>(st->block_table),
+                          static_cast<const void*>(st->lens_after), static_cast<const void*>(st->n_free_after),
+                          static_cast<const void*>(st->first), static_cast<const void*>(st->positions), static_cast<const void*>(st->refused)})
+        if (!fxp::aligned(p, 4)) return FXP_ERR_ALIGN;
+    if (!fxp::aligned(st->slots, 8) || !fxp::aligned(st->runs, 16)) return FXP_ERR_ALIGN;
+    const bool in_place = st->lens_after == st->lens || st->n_free_after == st->n_free;
+    if (in_place && (!ws || ws_bytes < 256)) return FXP_ERR_WORKSPACE;
+    if (in_place && !fxp::aligned(ws, 4)) return FXP_ERR_ALIGN;
+    const int64_t rows = fxp_kv_max_runs(st->requests, st->tokens);
+    const int64_t grid = rows > fxp::kTabRuns ? (rows + fxp::kTabRuns - 1) / fxp::kTabRuns : 1;
+    hipLaunchKernelGGL(fxp::k_kv_tables, dim3(static_cast<unsigned>(grid)), dim3(fxp::kTabThreads), 0, static_cast<hipStream_t>(stream), *st,
+                       n_new, rows, in_place ? static_cast<uint32_t*>(ws) : nullptr);
+    return fxp::launch_status();
+}
+
+extern "C" int fxp_kv_append(const fxp_kv_cache* cache, int type, const void* k, int64_t k_token, int64_t k_head, const void* v,
+                             int64_t v_token, int64_t v_head, int64_t tokens, const int32_t* runs, int64_t n_runs, void* stream) {
+    const int rc = fxp::check_cache(cache);
+    if (rc) return rc;
+    if (!fxp::known_type(type)) return FXP_ERR_TYPE;
+    if (tokens < 0 || n_runs < 0 || tokens >= (int64_t{1} << 31) || n_runs > fxp::kMostRuns || !fxp::strides_ok(k_token, k_head) ||
+        !fxp::strides_ok(v_token, v_head))
+        return FXP_ERR_DIMS;
+    if (tokens == 0 || n_runs == 0) return FXP_OK;
+    if (!k || !v || !runs) return FXP_ERR_NULL;
+    if (!fxp::aligned(k, fxp::elem_size(type)) || !fxp::aligned(v, fxp::elem_size(type)) || !fxp::aligned(runs, 16)) return FXP_ERR_ALIGN;
+    const int vk = fxp::multiple_of_4(k, k_token, k_head, type), vv = fxp::multiple_of_4(v, v_token, v_head, type);
+    const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), 2);
+    const bool few = tokens <= 4 * n_runs;
+    auto go = [&](auto type_c) {
+        constexpr int TYPE = decltype(type_c)::value;
+        if (few)
+            hipLaunchKernelGGL((fxp::k_kv_append<TYPE, 64>), grid, dim3(64), 0, static_cast<hipStream_t>(stream), *cache, k, k_token, k_head, v,
+                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv);
+        else
+            hipLaunchKernelGGL((fxp::k_kv_append<TYPE, 256>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), *cache, k, k_token, k_head, v,
+                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv);
+    };
+    if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
+    else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
+    else go(std::integral_constant<int, FXP_F16>{});
+    return fxp::launch_status();
+}
+
+extern "C" int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t tokens, const int32_t* runs, int64_t n_runs,
+                           void* stream) {
+    const int rc = fxp::check_cache(cache);
+    if (rc) return rc;
+    if (!fxp::known_type(type)) return FXP_ERR_TYPE;
+    if (tokens < 0 || n_runs < 0 || tokens >= (int64_t{1} << 31) || n_runs > fxp::kMostRuns) return FXP_ERR_DIMS;
+    if (tokens == 0 || n_runs == 0) return FXP_OK;
+    if (!k || !v || !runs) return FXP_ERR_NULL;
+    if (!fxp::aligned(k, 16) || !fxp::aligned(v, 16) || !fxp::aligned(runs, 16)) return FXP_ERR_ALIGN;
+    const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), 2);
+    auto go = [&](auto type_c) {
+        hipLaunchKernelGGL((fxp::k_kv_load<decltype(type_c)::value>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), *cache, k, v, tokens,
+                           reinterpret_cast<const int4*>(runs));
+    };
+    if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
+    else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
+    else go(std::integral_constant<int, FXP_F16>{});
+    return fxp::launch_status();
+}

@@ -79,11 +79,13 @@ extern "C" const char* fxp_strerror(int status) {
         case FXP_ERR_BITS: return "bits outside [2, 8]";
         case FXP_ERR_LAUNCH: return "kernel launch failed";
         case FXP_ERR_OVERFLOW: return "contraction too long for int32 accumulation";
+        case FXP_ERR_TYPE: return "unknown element type";
+        case FXP_ERR_VALUE: return "a scalar argument outside its range";
         default: return "unknown status";
     }
 }
 
-extern "C" int fxp_version(void) { return 111; }
+extern "C" int fxp_version(void) { return 112; }
 
 extern "C" size_t fxp_workspace_bytes(int op, int64_t M, int64_t N, int64_t K) {
     if (M < 0 || N < 0 || K < 0) return 0;

@@ -1,0 +1,159 @@
+// Device code that the serving kernels share: element types, the mapping rounded to nearest, digits of a float row.
+#pragma once
+#include "fxp_internal.h"
+
+namespace fxp {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+
+template <int TYPE>
+struct Elem;
+template <>
+struct Elem<FXP_F32> {
+    using T = float;
+};
+template <>
+struct Elem<FXP_BF16> {
+    using T = __bf16;
+};
+template <>
+struct Elem<FXP_F16> {
+    using T = _Float16;
+};
+
+inline int elem_size(int type) { return type == FXP_F32 ? 4 : 2; }
+inline bool known_type(int type) { return type == FXP_F32 || type == FXP_BF16 || type == FXP_F16; }
+
+// N consecutive elements as floats (exact); `vec`: the address is a multiple of N elements, so N of them are one load
+// or, from 32 bytes on, several
+template <int TYPE, int N>
+__device__ inline void load_elems(const void* base, int64_t at, bool vec, float (&out)[N]) {
+    using T = typename Elem<TYPE>::T;
+    const T* p = static_cast<const T*>(base) + at;
+    if (vec) {
+        constexpr int kPiece = N * sizeof(T) < 16 ? N : 16 / static_cast<int>(sizeof(T));
+        typedef T Vec __attribute__((ext_vector_type(kPiece)));
+#pragma unroll
+        for (int i = 0; i < N; i += kPiece) {
+            const Vec v = *reinterpret_cast<const Vec*>(p + i);
+#pragma unroll
+            for (int j = 0; j < kPiece; ++j) out[i + j] = static_cast<float>(v[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) out[i] = static_cast<float>(p[i]);
+    }
+}
+
+// four floats rounded to nearest, to an address that is a multiple of four elements
+template <int TYPE>
+__device__ inline void store4(void* base, int64_t at, bool vec, const float (&x)[4]) {
+    using T = typename Elem<TYPE>::T;
+    T* p = static_cast<T*>(base) + at;
+    typedef T Vec __attribute__((ext_vector_type(4)));
+    if (vec) {
+        Vec v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = static_cast<T>(x[j]);
+        *reinterpret_cast<Vec*>(p) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = static_cast<T>(x[j]);
+    }
+}
+
+// The mapping of one value under scale e with `cut` = 25 - bits low bits dropped, half up on the magnitude (what
+// fxp_map does with FXP_ROUND_NEAREST), as a signed byte.
+__device__ inline int map_nearest(float x, int e, int cut) {
+    const uint32_t b = __float_as_uint(x), field = (b >> 23) & 0xffu, f = b & 0x7fffffu, sat = (1u << (24 - cut)) - 1u;
+    const int d = e - static_cast<int>(max(field, 1u));
+    const uint32_t m = (f | (field ? 0x800000u : 0u)) >> min(max(d, 0), 31);
+    uint32_t q = min((m + (1u << (cut - 1))) >> cut, sat);
+    if (d < 0) q = sat;
+    if (field == 255u) q = f == 0u ? sat : 0u;
+    return (b >> 31) ? -static_cast<int>(q) : static_cast<int>(q);
+}
+
+// a mapped byte brought to a scale larger by d >= 1: half up on the magnitude
+__device__ inline int remap_nearest(int q, int d) {
+    const int s = min(d, 9);                             // 9: every magnitude becomes 0
+    const int m = (abs(q) + (1 << (s - 1))) >> s;
+    return q < 0 ? -m : m;
+}
+__device__ inline uint32_t remap_nearest4(uint32_t four, int d) {
+    uint32_t r = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        r |= (static_cast<uint32_t>(remap_nearest(static_cast<int8_t>(four >> (8 * i)), d)) & 0xffu) << (8 * i);
+    return r;
+}
+
+// bytes j of four words, one after the other
+__device__ inline uint32_t bytes_of(uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3, int j) {
+    const uint32_t s = static_cast<uint32_t>(j) | (static_cast<uint32_t>(j + 4) << 8);
+    return perm(perm(w3, w2, s), perm(w1, w0, s), 0x05040100u);
+}
+
+// Digits of 16 integers, most significant first.  Adding 128 in every lower byte makes each lower digit its byte minus 128 (the byte
+// with its top bit turned), and carries the rest into the one above it.
+template <int ND>
+__device__ inline void digits16(const int (&v)[16], v4i (&d)[ND]) {
+    constexpr int kBias = ND == 2 ? 0x80 : 0x8080;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = static_cast<uint32_t>(v[4 * t + i] + kBias);
+#pragma unroll
+        for (int j = 0; j < ND; ++j) {
+            const uint32_t by = bytes_of(w[0], w[1], w[2], w[3], ND - 1 - j);
+            d[j][t] = static_cast<int>(j == 0 ? by : by ^ 0x80808080u);
+        }
+    }
+}
+
+template <int ND>
+struct Digits {
+    // largest magnitude: 127 in every digit
+    static constexpr int kMost = ND == 2 ? 32639 : 8355711;
+    static constexpr int kBits = ND == 2 ? 15 : 23;
+};
+
+// exponent of one unit of a row (or group) of floats whose largest magnitude has the bits m: the row stays below 127/128 of the binade
+// (2^-7 and a little short of it: rounding must not reach 128 in a digit)
+template <int ND>
+__device__ inline int unit_of(uint32_t m) {
+    return min(max(static_cast<int>((m + 0x10200u) >> 23), 1), 255) - 126 - Digits<ND>::kBits;
+}
+template <int ND>
+__device__ inline int fixed_point(float x, int unit) {
+    return min(max(static_cast<int>(rintf(ldexpf(x, -unit))), -Digits<ND>::kMost), Digits<ND>::kMost);
+}
+
+__device__ inline v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+
+struct Run {
+    int first, count, page, offset;
+};
+// whether the tokens, the page and the places of a run exist
+__device__ inline bool run_ok(const Run& r, int64_t tokens, int64_t pages) {
+    return r.count > 0 && r.count <= FXP_KV_PAGE && r.offset >= 0 && r.offset + r.count <= FXP_KV_PAGE && r.first >= 0 &&
+           int64_t{r.first} + r.count <= tokens && r.page >= 0 && r.page < pages;
+}
+
+inline int check_cache(const fxp_kv_cache* c) {
+    if (!c || !c->kq || !c->vq || !c->ek || !c->ev) return FXP_ERR_NULL;
+    if (c->pages <= 0 || c->pages >= (int64_t{1} << 31) || c->heads <= 0 || c->heads > 65535 || c->dim <= 0 || c->dim > 256 ||
+        c->dim % 16)
+        return FXP_ERR_DIMS;
+    if (c->bits < 2 || c->bits > 8) return FXP_ERR_BITS;
+    if (!aligned(c->kq, 16) || !aligned(c->vq, 16) || !aligned(c->ek, 4) || !aligned(c->ev, 4)) return FXP_ERR_ALIGN;
+    return FXP_OK;
+}
+
+// strides of a [tokens, heads, dim] operand; sizes stay far from 2^63
+inline bool strides_ok(int64_t token, int64_t head) {
+    return token >= 0 && head >= 0 && token < (int64_t{1} << 31) && head < (int64_t{1} << 40);
+}
+
+}  // namespace fxp

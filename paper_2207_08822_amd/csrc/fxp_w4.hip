@@ -1,0 +1,294 @@
+// Products of a few rows with 4-bit weights: y[m,n] = sum over groups of 2^(e[group,n] - 129) * sum_k x[m,k] q[k,n].
+//
+// A 16 x 16 x 64 int8 matrix instruction has 16 outputs' weights as A (the lane's 16 mantissas of one output: 8 bytes) and the digits
+// of up to 16 rows of x as B.  A mantissa is used in the upper half of its byte, 16 q, so that unpacking is a shift and two masks for
+// eight of them; the factor 16 is taken out with the scales.  The int32 sums of a group are exact; group by group
+// they are scaled into fp32 sums.
+#include "fxp_serve_device.h"
+
+namespace fxp {
+
+constexpr int kW4Waves = 8;
+constexpr int kW4Threads = 64 * kW4Waves;
+
+struct W4Args {
+    const void* x;
+    int64_t ldx;
+    int M, K, N, k_tiles, n_tiles, m_tiles;
+    const uint8_t* packed;
+    const uint8_t* scales;
+    void* y;
+    int64_t ldy;
+    uint8_t* digits;     // [k_tiles][m_tiles][ND][128 / S][64][S / 4] bytes
+    float* units;        // [k_tiles * 128 / group][16 m_tiles]: 2^(exponent of one unit - 6)
+    int vec_x;
+};
+
+// The digits of x in the order of the B operand.  A thread has 16 inputs of one row; group / 16 neighbours share a scale.
+template <int TYPE, int GROUP>
+__global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64;
+    const int i = blockIdx.x * 256 + threadIdx.x, pieces = a.k_tiles * 8, row = i / pieces, piece = i % pieces, k = piece * 16;
+    if (row >= 16 * a.m_tiles) return;                     // whole groups of neighbours: pieces is a multiple of 8
+    float x[16];
+    if (row < a.M && k + 16 <= a.K) {
+        load_elems<TYPE, 16>(a.x, row * a.ldx + k, a.vec_x, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            x[j] = row < a.M && k + j < a.K ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(a.x)[row * a.ldx + k + j]) : 0.0f;
+    }
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) m = max(m, __float_as_uint(x[j]) & 0x7fffffffu);
+#pragma unroll
+    for (int d = 1; d < GROUP / 16; d <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
+    const int unit = unit_of<ND>(m);
+    int v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[j], unit);
+    v4i d[ND];
+    digits16<ND>(v, d);
+    const int tile = k / 128, s = k % 128 / S, g = k % S / (S / 4), mt = row / 16, r = row % 16;
+    uint8_t* base = a.digits + (static_cast<int64_t>(tile) * a.m_tiles + mt) * (ND * 2048);
+#pragma unroll
+    for (int j = 0; j < ND; ++j) {
+        uint8_t* p = base + ((j * (128 / S) + s) * 64 + 16 * g + r) * (S / 4);
+        if constexpr (S == 64) {
+            *reinterpret_cast<v4i*>(p) = d[j];
+        } else {
+            *reinterpret_cast<int2*>(p) = make_int2(d[j][0], d[j][1]);
+            *reinterpret_cast<int2*>(p + 16 * (S / 4)) = make_int2(d[j][2], d[j][3]);          // the next piece: 16 (g + 1) + r
+        }
+    }
+    if (k % GROUP == 0) a.units[static_cast<int64_t>(k / GROUP) * (16 * a.m_tiles) + row] = ldexpf(1.0f, unit - 6);
+}
+
+template <int TYPE, int GROUP, int NT, int MT>
+__global__ __launch_bounds__(kW4Threads) void k_w4_linear(W4Args a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S;
+    __shared__ float red[kW4Waves][NT * 16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int nt0 = blockIdx.x * NT, mt0 = blockIdx.y * MT;
+    float sum[MT][NT][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[i][n][j] = 0.0f;
+
+    constexpr int GT = 128 / GROUP;                       // groups of a tile
+    for (int kt = wave; kt < a.k_tiles; kt += kW4Waves) {
+        v4i w[NT];
+        uint32_t e[NT][GT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int nt = min(nt0 + n, a.n_tiles - 1);
+            w[n] = *reinterpret_cast<const v4i*>(a.packed + (static_cast<int64_t>(nt) * a.k_tiles + kt) * 1024 + lane * 16);
+#pragma unroll
+            for (int j = 0; j < GT; ++j)
+                e[n][j] = *reinterpret_cast<const uint32_t*>(a.scales + ((static_cast<int64_t>(nt) * a.k_tiles + kt) * GT + j) * 16 + 4 * g);
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int mt = min(mt0 + i, a.m_tiles - 1);
+            const uint8_t* dig = a.digits + (static_cast<int64_t>(kt) * a.m_tiles + mt) * (ND * 2048);
+#pragma unroll
+            for (int j = 0; j < GT; ++j) {
+                constexpr int SG = STEPS / GT;            // steps of a group
+                const float unit = a.units[(static_cast<int64_t>(kt) * GT + j) * (16 * a.m_tiles) + mt * 16 + col];
+                v4i acc[NT][ND];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[n][d] = v4i{0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < SG; ++t) {
+                    const int s = j * SG + t;
+                    if constexpr (S == 64) {
+                        v4i b[ND];
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) b[d] = *reinterpret_cast<const v4i*>(dig + ((d * STEPS + s) * 64 + lane) * 16);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const int w0 = w[n][2 * s], w1 = w[n][2 * s + 1];
+                            const int mask = static_cast<int>(0xf0f0f0f0u);
+                            const v4i q = {(w0 << 4) & mask, (w1 << 4) & mask, w0 & mask, w1 & mask};
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) acc[n][d] = mfma_i8(q, b[d], acc[n][d]);
+                        }
+                    } else {
+                        long b[ND];
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) b[d] = *reinterpret_cast<const long*>(dig + ((d * STEPS + s) * 64 + lane) * 8);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const uint32_t w0 = static_cast<uint32_t>(w[n][s]), mask = 0xf0f0f0f0u;
+                            const long q = static_cast<long>(static_cast<uint64_t>(w0 & mask) << 32 | ((w0 << 4) & mask));
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) acc[n][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, b[d], acc[n][d], 0, 0, 0);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float v = static_cast<float>(acc[n][0][r] * 256 + acc[n][1][r]);
+                        if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[n][2][r]));
+                        const float scale = __uint_as_float(((e[n][j] >> (8 * r)) & 0xffu) << 23);
+                        sum[i][n][r] = fmaf(v * unit, scale, sum[i][n][r]);
+                    }
+            }
+        }
+    }
+
+    // the waves' shares of the contraction
+    using T = typename Elem<TYPE>::T;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        if (i) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) red[wave][n * 16 + 4 * g + r][col] = sum[i][n][r];
+        __syncthreads();
+        for (int j = threadIdx.x; j < NT * 256; j += kW4Threads) {
+            const int n = j % (NT * 16), m = j / (NT * 16);
+            float v = 0.0f;
+#pragma unroll
+            for (int w = 0; w < kW4Waves; ++w) v += red[w][n][m];
+            const int row = (mt0 + i) * 16 + m, out = nt0 * 16 + n;
+            if (row < a.M && out < a.N) static_cast<T*>(a.y)[row * a.ldy + out] = static_cast<T>(v);
+        }
+    }
+}
+
+// W -> mantissas and scales: a thread has one group of one output.
+template <int TYPE, int GROUP>
+__global__ __launch_bounds__(256) void k_w4_pack(const void* __restrict__ W, int64_t ldw, int64_t K, int64_t N, int k_tiles, int n_tiles,
+                                                 uint8_t* __restrict__ packed, uint8_t* __restrict__ scales) {
+    using T = typename Elem<TYPE>::T;
+    constexpr int S = GROUP < 64 ? GROUP : 64, GT = 128 / GROUP;
+    const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t kg = blockIdx.y, k0 = kg * GROUP;
+    if (n >= static_cast<int64_t>(n_tiles) * 16) return;
+    const T* w = static_cast<const T*>(W);
+    auto value = [&](int64_t k) { return n < N && k < K ? static_cast<float>(w[k * ldw + n]) : 0.0f; };
+    uint32_t m = 0;
+    for (int k = 0; k < GROUP; ++k) m = max(m, __float_as_uint(value(k0 + k)) & 0x7fffffffu);
+    // a scale byte is the exponent field of a power of two that multiplies in fp32: 254 at most
+    const int e = min(max(static_cast<int>(m >> 23), 1), 254);
+    const int64_t nt = n / 16, tile = nt * k_tiles + k0 / 128;
+    const int r = static_cast<int>(n % 16);
+    scales[(tile * GT + k0 % 128 / GROUP) * 16 + r] = static_cast<uint8_t>(e);
+    for (int k = 0; k < GROUP; k += S / 4) {               // a lane's piece of a step: S / 4 inputs, S / 8 bytes
+        const int kk = static_cast<int>((k0 + k) % 128), s = kk / S, g = kk % S / (S / 4);
+        uint8_t* p = packed + tile * 1024 + (16 * g + r) * 16 + s * (S / 8);
+#pragma unroll
+        for (int j = 0; j < S / 8; j += 4) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int lo = map_nearest(value(k0 + k + j + b), e, 21), hi = map_nearest(value(k0 + k + j + b + S / 8), e, 21);
+                word |= static_cast<uint32_t>((lo & 15) | ((hi & 15) << 4)) << (8 * b);
+            }
+            *reinterpret_cast<uint32_t*>(p + j) = word;
+        }
+    }
+}
+
+static bool w4_group_ok(int group) { return group == 32 || group == 64 || group == 128; }
+static bool w4_sizes_ok(int64_t K, int64_t N) { return K > 0 && N > 0 && K <= (int64_t{1} << 20) && N <= (int64_t{1} << 24); }
+
+template <typename F>
+static void w4_of_type(int type, F f) {
+    if (type == FXP_F32) f(std::integral_constant<int, FXP_F32>{});
+    else if (type == FXP_BF16) f(std::integral_constant<int, FXP_BF16>{});
+    else f(std::integral_constant<int, FXP_F16>{});
+}
+template <typename F>
+static void w4_of_group(int group, F f) {
+    if (group == 32) f(std::integral_constant<int, 32>{});
+    else if (group == 64) f(std::integral_constant<int, 64>{});
+    else f(std::integral_constant<int, 128>{});
+}
+
+}  // namespace fxp
+
+extern "C" size_t fxp_w4_packed_bytes(int64_t K, int64_t N) {
+    return fxp::w4_sizes_ok(K, N) ? static_cast<size_t>((N + 15) / 16) * ((K + 127) / 128) * 1024 : 0;
+}
+extern "C" size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group) {
+    return fxp::w4_sizes_ok(K, N) && fxp::w4_group_ok(group) ? static_cast<size_t>((N + 15) / 16) * ((K + 127) / 128) * (128 / group) * 16 : 0;
+}
+extern "C" size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group) {
+    if (!fxp::known_type(type) || !fxp::w4_group_ok(group) || !fxp::w4_sizes_ok(K, 1) || M <= 0 || M >= (int64_t{1} << 20)) return 0;
+    const size_t rows = (M + 15) / 16 * 16, tiles = (K + 127) / 128;
+    return rows * tiles * 128 * (type == FXP_F32 ? 3 : 2) + rows * tiles * (128 / group) * sizeof(float);
+}
+
+extern "C" int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales,
+                           void* stream) {
+    using namespace fxp;
+    if (!known_type(type)) return FXP_ERR_TYPE;
+    if (!w4_group_ok(group)) return FXP_ERR_VALUE;
+    if (!w4_sizes_ok(K, N) || ldw < N || ldw >= (int64_t{1} << 32)) return FXP_ERR_DIMS;
+    if (!W || !packed || !scales) return FXP_ERR_NULL;
+    if (!aligned(W, elem_size(type)) || !aligned(packed, 16) || !aligned(scales, 4)) return FXP_ERR_ALIGN;
+    const int64_t k_tiles = (K + 127) / 128, n_tiles = (N + 15) / 16;
+    const dim3 grid(static_cast<unsigned>((n_tiles * 16 + 255) / 256), static_cast<unsigned>(k_tiles * (128 / group)));
+    w4_of_type(type, [&](auto t) {
+        w4_of_group(group, [&](auto g) {
+            hipLaunchKernelGGL((k_w4_pack<decltype(t)::value, decltype(g)::value>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), W, ldw,
+                               K, N, static_cast<int>(k_tiles), static_cast<int>(n_tiles), packed, scales);
+        });
+    });
+    return launch_status();
+}
+
+extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, int64_t K, int64_t N, const uint8_t* packed,
+                             const uint8_t* scales, int group, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
+    using namespace fxp;
+    if (!known_type(type)) return FXP_ERR_TYPE;
+    if (!w4_group_ok(group)) return FXP_ERR_VALUE;
+    if (!w4_sizes_ok(K, N) || M < 0 || M >= (int64_t{1} << 20) || ldx < K || ldy < N || ldx >= (int64_t{1} << 32) || ldy >= (int64_t{1} << 32))
+        return FXP_ERR_DIMS;
+    if (M == 0) return FXP_OK;
+    if (!X || !packed || !scales || !Y) return FXP_ERR_NULL;
+    const size_t size = elem_size(type);
+    if (!aligned(X, size) || !aligned(Y, size) || !aligned(packed, 16) || !aligned(scales, 4)) return FXP_ERR_ALIGN;
+    if (!ws || ws_bytes < fxp_w4_workspace_bytes(type, M, K, group)) return FXP_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    W4Args a;
+    a.x = X;
+    a.ldx = ldx;
+    a.M = static_cast<int>(M);
+    a.K = static_cast<int>(K);
+    a.N = static_cast<int>(N);
+    a.k_tiles = static_cast<int>((K + 127) / 128);
+    a.n_tiles = static_cast<int>((N + 15) / 16);
+    a.m_tiles = static_cast<int>((M + 15) / 16);
+    a.packed = packed;
+    a.scales = scales;
+    a.y = Y;
+    a.ldy = ldy;
+    a.digits = static_cast<uint8_t*>(ws);
+    a.units = reinterpret_cast<float*>(a.digits + static_cast<size_t>(a.m_tiles) * 16 * a.k_tiles * 128 * (type == FXP_F32 ? 3 : 2));
+    a.vec_x = aligned(X, 16) && ldx * size % 16 == 0;
+    const int64_t pieces = int64_t{16} * a.m_tiles * a.k_tiles * 8;
+    if (pieces > (int64_t{1} << 30)) return FXP_ERR_DIMS;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    w4_of_type(type, [&](auto t) {
+        w4_of_group(group, [&](auto g) {
+            constexpr int TYPE = decltype(t)::value, GROUP = decltype(g)::value;
+            hipLaunchKernelGGL((k_w4_digits<TYPE, GROUP>), dim3(static_cast<unsigned>((pieces + 255) / 256)), dim3(256), 0, s, a);
+            if (a.m_tiles == 1)
+                hipLaunchKernelGGL((k_w4_linear<TYPE, GROUP, 1, 1>), dim3(a.n_tiles), dim3(kW4Threads), 0, s, a);
+            else
+                hipLaunchKernelGGL((k_w4_linear<TYPE, GROUP, 2, 4>), dim3((a.n_tiles + 1) / 2, (a.m_tiles + 3) / 4), dim3(kW4Threads), 0, s, a);
+        });
+    });
+    return launch_status();
+}

@@ -46,6 +46,17 @@ class _ConvSaved(ctypes.Structure):
                 ("eX", ctypes.c_void_p), ("eW", ctypes.c_void_p)]
 
 
+class _KvCache(ctypes.Structure):
+    _fields_ = [("kq", ctypes.c_void_p), ("vq", ctypes.c_void_p), ("ek", ctypes.c_void_p), ("ev", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("heads", ctypes.c_int64), ("dim", ctypes.c_int64), ("bits", ctypes.c_int)]
+
+
+class _KvStep(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("requests", "blocks", "tokens", "pages")] +
+                [(n, ctypes.c_void_p) for n in ("lens", "free_pages", "n_free", "block_table", "lens_after", "n_free_after", "first",
+                                                "slots", "positions", "runs", "refused")])
+
+
 _lib = None
 
 
@@ -120,6 +131,25 @@ def lib():
     L.fxp_sgd16_step.argtypes = [vp, vp, vp, sz, c.c_float, c.c_float, c.c_float, vp, u64, u64, ci, vp, sz, vp]
     L.fxp_axpy16.restype = ci
     L.fxp_sgd16_step.restype = ci
+    cache, step = c.POINTER(_KvCache), c.POINTER(_KvStep)
+    L.fxp_kv_max_runs.argtypes = [i64, i64]
+    L.fxp_kv_max_runs.restype = i64
+    L.fxp_kv_tables.argtypes = [step, vp, vp, sz, vp]
+    L.fxp_kv_append.argtypes = [cache, ci, vp, i64, i64, vp, i64, i64, i64, vp, i64, vp]
+    L.fxp_kv_load.argtypes = [cache, ci, vp, vp, i64, vp, i64, vp]
+    L.fxp_kv_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    L.fxp_kv_attention_workspace_bytes.restype = sz
+    L.fxp_kv_attention.argtypes = [cache, step, ci, vp, i64, i64, i64, c.c_float, i64, vp, i64, i64, vp, vp, sz, vp]
+    L.fxp_w4_packed_bytes.argtypes = [i64, i64]
+    L.fxp_w4_packed_bytes.restype = sz
+    L.fxp_w4_scale_bytes.argtypes = [i64, i64, ci]
+    L.fxp_w4_scale_bytes.restype = sz
+    L.fxp_w4_workspace_bytes.argtypes = [ci, i64, i64, ci]
+    L.fxp_w4_workspace_bytes.restype = sz
+    L.fxp_w4_pack.argtypes = [ci, vp, i64, i64, i64, ci, vp, vp, vp]
+    L.fxp_w4_linear.argtypes = [ci, vp, i64, i64, i64, i64, vp, vp, ci, vp, i64, vp, sz, vp]
+    for name in ("fxp_kv_tables", "fxp_kv_append", "fxp_kv_load", "fxp_kv_attention", "fxp_w4_pack", "fxp_w4_linear"):
+        getattr(L, name).restype = ci
     for name in ("fxp_scale", "fxp_map", "fxp_scale_map", "fxp_gemm", "fxp_unmap", "fxp_unmap_i8", "fxp_gemm_unmap",
                  "fxp_gemm_unmap_absmax", "fxp_map_absmax",
                  "fxp_linear_fwd", "fxp_linear_bwd", "fxp_gemm_batched", "fxp_gemm_unmap_batched", "fxp_bmm_fwd",
@@ -533,3 +563,210 @@ def sgd16_step_multi(buf, lr, momentum=0.0, weight_decay=0.0, seed=0, step=0, ro
     """In-place SGD step on every tensor of buf (own scales per tensor), a handful of launches in all."""
     _check(lib().fxp_sgd16_step_multi(buf.table, buf.count, float(lr), float(momentum), float(weight_decay), seed, step,
                                       rounding, _p(buf.ws), buf.ws.numel(), _stream()), "fxp_sgd16_step_multi")
+
+
+# ---- serving: a paged cache of mapped keys and values, attention over it, products with 4-bit weights ----
+
+KV_PAGE = 64            # tokens of a page (FXP_KV_PAGE)
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _served(t, what, dims):
+    """The type code of a float tensor of `dims` dimensions on the current device whose last dimension is contiguous."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise FxpError(f"{what} must be a CUDA tensor: libfxp has no CPU path")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise FxpError(f"{what} is on another device than the current one")
+    code = _TYPES.get(t.dtype)
+    if code is None or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise FxpError(f"{what} must be a {dims}-dimensional float32, bfloat16 or float16 tensor with a contiguous last dimension")
+    return code
+
+
+def _index(t, what, shape=None, dtype=torch.int32):
+    t = _dev(t, dtype, what)
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise FxpError(f"{what} is on another device than the current one")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise FxpError(f"{what} must have the shape {tuple(shape)}")
+    return t
+
+
+def _row_stride(t, what):
+    """Elements from one row of a matrix to the next; rows may not overlap."""
+    rows, cols = t.shape
+    if rows <= 1:
+        return cols
+    if t.stride(0) < cols:
+        raise FxpError(f"the rows of {what} overlap")
+    return t.stride(0)
+
+
+class KvCache:
+    """Caller-owned cache of one layer: int8 keys [pages, heads, 64, dim], values [pages, heads, 4, dim, 16], scales [pages, heads]."""
+
+    def __init__(self, pages, heads, dim, bits=8, device="cuda"):
+        i8, i32 = dict(dtype=torch.int8, device=device), dict(dtype=torch.int32, device=device)
+        self._set(torch.empty((pages, heads, KV_PAGE, dim), **i8), torch.empty((pages, heads, KV_PAGE // 16, dim, 16), **i8),
+                  torch.ones((pages, heads), **i32), torch.ones((pages, heads), **i32), bits)
+
+    @classmethod
+    def of(cls, kq, vq, ek, ev, bits=8):
+        """The cache that four tensors of these shapes are."""
+        self = cls.__new__(cls)
+        self._set(kq, vq, ek, ev, bits)
+        return self
+
+    def _set(self, kq, vq, ek, ev, bits):
+        if kq.dim() != 4 or kq.shape[2] != KV_PAGE:
+            raise FxpError(f"kq must be [pages, heads, {KV_PAGE}, dim]")
+        pages, heads, _, dim = kq.shape
+        _index(kq, "kq", dtype=torch.int8)
+        _index(vq, "vq", (pages, heads, KV_PAGE // 16, dim, 16), torch.int8)
+        _index(ek, "ek", (pages, heads))
+        _index(ev, "ev", (pages, heads))
+        if dim % 16 or dim > 256 or not 2 <= bits <= 8:
+            raise FxpError("dim must be a multiple of 16, at most 256, and bits in 2..8")
+        self.kq, self.vq, self.ek, self.ev, self.bits = kq, vq, ek, ev, bits
+        self.pages, self.heads, self.dim, self.device = pages, heads, dim, kq.device
+        self.c = _KvCache(_p(kq), _p(vq), _p(ek), _p(ev), pages, heads, dim, bits)
+        self.ref = ctypes.byref(self.c)
+
+
+class KvTables:
+    """Caller-owned tables of up to `requests` requests of `blocks` pages and of a step of up to `tokens` new tokens; all layers of
+    a model share them.  The caller frees a finished request by pushing its pages on `free` (free[n_free] and up), raising
+    n_free and setting its length to 0.  in_place: a step moves lens and n_free on (lens_after is lens); otherwise it leaves them and
+    writes lens_after and n_free_after."""
+
+    def __init__(self, requests, blocks, tokens, pages, in_place=True, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.requests, self.blocks, self.tokens, self.pages = requests, blocks, tokens, pages
+        self.block_table = torch.full((requests, blocks), -1, **i32)
+        self.lens = torch.zeros(requests, **i32)
+        self.free = torch.arange(pages - 1, -1, -1, **i32)          # page 0 is taken first
+        self.n_free = torch.full((1,), pages, **i32)
+        self.lens_after = self.lens if in_place else torch.zeros(requests, **i32)
+        self.n_free_after = self.n_free if in_place else torch.zeros(1, **i32)
+        self.first = torch.zeros(requests + 1, **i32)
+        self.slots = torch.full((tokens,), -1, dtype=torch.int64, device=device)
+        self.positions = torch.full((tokens,), -1, **i32)
+        self.runs = torch.zeros((int(lib().fxp_kv_max_runs(requests, tokens)), 4), **i32)
+        self.runs[:, 2] = -1
+        self.refused = torch.zeros(requests, **i32)
+        self.ws = torch.zeros(256, dtype=torch.uint8, device=device)
+        self.c = _KvStep(requests, blocks, tokens, pages, _p(self.lens), _p(self.free), _p(self.n_free), _p(self.block_table), _p(self.lens_after),
+                         _p(self.n_free_after), _p(self.first), _p(self.slots), _p(self.positions), _p(self.runs), _p(self.refused))
+        self.ref = ctypes.byref(self.c)
+
+
+def kv_tables(n_new, tab):
+    """Room for n_new[b] more tokens of each request, and the step's tables (tab.first, slots, positions, runs, refused); returns tab."""
+    _index(n_new, "n_new", (tab.requests,))
+    _check(lib().fxp_kv_tables(tab.ref, n_new.data_ptr(), tab.ws.data_ptr(), 256, _stream()), "fxp_kv_tables")
+    return tab
+
+
+def _runs(runs):
+    runs = _index(runs, "runs")
+    if runs.dim() != 2 or runs.shape[1] != 4:
+        raise FxpError("runs must be [n, 4]")
+    return runs
+
+
+def kv_append(k, v, cache, runs):
+    """Maps the new tokens k, v [tokens, heads, dim] (any strides of the first two) into the cache; runs: KvTables.runs."""
+    code = _served(k, "k", 3)
+    if _served(v, "v", 3) != code or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.dim):
+        raise FxpError("k and v must be [tokens, heads, dim] of the cache and of one type")
+    runs = _runs(runs)
+    _check(lib().fxp_kv_append(cache.ref, code, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), k.shape[0],
+                               runs.data_ptr(), runs.shape[0], _stream()), "fxp_kv_append")
+
+
+def kv_load(cache, runs, tokens, dtype=torch.float32, out=None):
+    """(k, v) [tokens, heads, dim]: the values that the cached tokens of `runs` stand for; out: the two tensors to fill."""
+    runs = _runs(runs)
+    shape = (tokens, cache.heads, cache.dim)
+    k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
+    code = _served(k, "k", 3)
+    for t, name in ((k, "k"), (v, "v")):
+        if tuple(t.shape) != shape or not t.is_contiguous() or _served(t, name, 3) != code:
+            raise FxpError("the outputs must be contiguous [tokens, heads, dim] tensors of one type")
+    _check(lib().fxp_kv_load(cache.ref, code, k.data_ptr(), v.data_ptr(), tokens, runs.data_ptr(), runs.shape[0], _stream()), "fxp_kv_load")
+    return k, v
+
+
+class AttentionBuffers:
+    """Scratch of kv_attention for up to `requests` requests with `tokens` rows in all; one call at a time."""
+
+    def __init__(self, requests, tokens, q_heads, cache):
+        self.nbytes = int(lib().fxp_kv_attention_workspace_bytes(requests, tokens, q_heads, cache.heads, cache.dim))
+        if self.nbytes == 0:
+            raise FxpError("bad sizes: q_heads must be a multiple of the cache's heads")
+        self.ws = torch.zeros(self.nbytes, dtype=torch.uint8, device=cache.device)
+
+
+def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=None):
+    """Attention of the step's rows q [tokens, q_heads, dim] over the cache: causal, over the last `window` tokens where it is > 0.
+    scale: dim ** -0.5 by default; lse: [tokens, q_heads] fp32 to fill with the logarithms of the softmax's sums."""
+    code = _served(q, "q", 3)
+    tokens, q_heads, dim = q.shape
+    if tokens != tab.tokens or dim != cache.dim:
+        raise FxpError("q must be [tokens, q_heads, dim] of the tables and the cache")
+    if out is None:
+        out = torch.empty((tokens, q_heads, dim), dtype=q.dtype, device=q.device)
+    elif _served(out, "out", 3) != code or out.shape != q.shape or (tokens > 1 and out.stride(0) < dim) or (q_heads > 1 and out.stride(1) < dim):
+        raise FxpError("out must have the shape and type of q, and rows that do not overlap")
+    if lse is not None:
+        _dev(lse, torch.float32, "lse")
+        if tuple(lse.shape) != (tokens, q_heads):
+            raise FxpError("lse must be [tokens, q_heads]")
+    if buf is None:
+        buf = AttentionBuffers(tab.requests, tokens, q_heads, cache)
+    _check(lib().fxp_kv_attention(cache.ref, tab.ref, code, q.data_ptr(), q.stride(0), q.stride(1), q_heads, dim ** -0.5 if scale is None else scale,
+                                  window, out.data_ptr(), out.stride(0), out.stride(1), _p(lse), buf.ws.data_ptr(), buf.nbytes, _stream()),
+           "fxp_kv_attention")
+    return out
+
+
+class W4Weights:
+    """A weight matrix [K, N] as packed 4-bit mantissas and scales (the layout of include/fxp.h)."""
+
+    def __init__(self, packed, scales, K, N, group=64):
+        if int(lib().fxp_w4_scale_bytes(K, N, group)) == 0:
+            raise FxpError("group must be 32, 64 or 128, and K and N in range")
+        _index(packed, "packed", dtype=torch.uint8)
+        _index(scales, "scales", dtype=torch.uint8)
+        if packed.numel() != lib().fxp_w4_packed_bytes(K, N) or scales.numel() != lib().fxp_w4_scale_bytes(K, N, group):
+            raise FxpError("packed or scales have another size than K, N and group ask for")
+        self.packed, self.scales, self.K, self.N, self.group = packed, scales, K, N, group
+        self.pointers = packed.data_ptr(), scales.data_ptr()
+
+
+def pack4(W, group=64):
+    """W4Weights of a float matrix W [K, N]: mantissas -7..7 rounded to nearest, a scale for each `group` inputs of an output."""
+    code = _served(W, "W", 2)
+    K, N = W.shape
+    nbytes = int(lib().fxp_w4_packed_bytes(K, N)), int(lib().fxp_w4_scale_bytes(K, N, group))
+    packed, scales = (torch.empty(max(n, 1), dtype=torch.uint8, device=W.device) for n in nbytes)
+    _check(lib().fxp_w4_pack(code, _p(W), _row_stride(W, "W"), K, N, group, _p(packed), _p(scales), _stream()), "fxp_w4_pack")
+    return W4Weights(packed, scales, K, N, group)
+
+
+def linear4(x, w, out=None, ws=None):
+    """y [M, N] = x [M, K] W of x's type, W the 4-bit weights w; made for a few rows."""
+    code = _served(x, "x", 2)
+    M, K = x.shape
+    if K != w.K:
+        raise FxpError("x must be [M, K] of the weights")
+    if out is None:
+        out = torch.empty((M, w.N), dtype=x.dtype, device=x.device)
+    elif _served(out, "out", 2) != code or tuple(out.shape) != (M, w.N):
+        raise FxpError("out must be [M, N] of x's type")
+    if ws is None:
+        ws = torch.empty(max(256, int(lib().fxp_w4_workspace_bytes(code, M, K, w.group))), dtype=torch.uint8, device=x.device)
+    packed, scales = w.pointers
+    _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), _row_stride(out, "out"),
+                               ws.data_ptr(), ws.numel(), _stream()), "fxp_w4_linear")
+    return out

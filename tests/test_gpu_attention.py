@@ -1,0 +1,215 @@
+"""Attention over the paged 8-bit cache against its definition in 64 bits, within bounds that follow from the stated arithmetic."""
+import numpy as np
+import pytest
+
+from tests import serve_ref as ref
+from tests.gpu_util import dev, host, say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+TYPES = {"fp32": (torch.float32, 23, 2.0 ** -24), "bf16": (torch.bfloat16, 15, 2.0 ** -8), "fp16": (torch.float16, 15, 2.0 ** -11)}
+
+
+@pytest.fixture(scope="module")
+def fxp():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU path in libfxp")
+    from paper_2207_08822_amd import fxp as binding
+    binding.lib()
+    return binding
+
+
+class Case:
+    """A cache, tables and queries on the device and as arrays."""
+
+    def __init__(self, fxp, lens, news, QH, H, D, kind, bits=8, seed=0, behind=0, missing=(), sharp=1.0, sink=False, spare=0):
+        rng = np.random.default_rng(seed + 1000 * D + QH)
+        self.lens, self.T = np.array(lens), int(sum(news)) + behind
+        self.first = np.concatenate([[0], np.cumsum(news)])
+        held = [-(-n // 64) for n in lens]
+        self.blocks, pages = max(max(held), 1) + 1, sum(held) + 2 + spare
+        order = (rng.permutation(pages - spare) + spare).astype(np.int32)
+        self.table, at = np.full((len(lens), self.blocks), -1, np.int32), 0
+        for b, n in enumerate(held):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        for b, j, page in missing:
+            self.table[b, j] = page
+        top = 2 ** (bits - 1)
+        bell = lambda shape: np.clip(np.round(rng.standard_normal(shape) * top / 3), 1 - top, top - 1).astype(np.int8)  # noqa: E731
+        kq, vq = bell((pages - spare, H, 64, D)), bell((pages - spare, H, 4, D, 16))
+        ek, ev = rng.integers(126, 129, (pages - spare, H)), rng.integers(120, 130, (pages - spare, H))
+        if sink:                              # the first token of each request outweighs all others by far
+            for b, n in enumerate(held):
+                if n:
+                    kq[self.table[b, 0] - spare, :, 0] = np.sign(kq[self.table[b, 0] - spare, :, 0]) * (top - 1)
+        self.k, self.v = ref.Cache(kq, ek, bits), ref.Cache(ref.rows_of(vq), ev, bits)
+        self.spare = spare
+        if spare:
+            self.cache = fxp.KvCache(pages, H, D, bits)
+            for mine, theirs in ((self.cache.kq, kq), (self.cache.vq, vq), (self.cache.ek, ek), (self.cache.ev, ev)):
+                mine[spare:].copy_(torch.tensor(theirs))
+        else:
+            self.cache = fxp.KvCache.of(dev(kq), dev(vq), dev(ek.astype(np.int32)), dev(ev.astype(np.int32)), bits)
+        self.tab = fxp.KvTables(len(lens), self.blocks, self.T, 4, in_place=False)
+        self.tab.block_table.copy_(torch.tensor(self.table))
+        self.tab.lens_after.copy_(torch.tensor(self.lens.astype(np.int32)))
+        self.tab.first.copy_(torch.tensor(self.first.astype(np.int32)))
+        dtype, self.unit_bits, self.half = TYPES[kind]
+        q = torch.tensor((rng.standard_normal((self.T, QH, D)) * sharp).astype(np.float32)).to(dtype)
+        if sink:
+            for b, n in enumerate(held):
+                if n:
+                    for h in range(QH):
+                        row = torch.tensor(np.sign(kq[self.table[b, 0] - spare, h // (QH // H), 0]).astype(np.float32)).to(dtype)
+                        q[self.first[b]:self.first[b + 1], h] += row * sharp
+        self.q, self.dq = q, q.cuda()
+        self.scale = float(np.float32(D ** -0.5))
+
+    def want(self, window=0):
+        table = np.where((self.table >= self.spare) & (self.table < self.spare + len(self.k.q)), self.table - self.spare, -1)
+        return ref.attention(self.q.double().numpy(), self.k.values(), self.v.values(), self.first, self.lens, table, self.scale, window,
+                             self.unit_bits, self.half)
+
+    def check(self, out, lse=None, window=0, want=None):
+        o, logs, off = want or self.want(window)
+        rows = self.first[-1]
+        got = out.double().cpu().numpy()
+        far = np.abs(got - o)[:rows]
+        assert (far <= off[:rows]).all(), f"off by {np.max(far / np.maximum(off[:rows], 1e-300))} of what it may be"
+        if lse is not None:
+            got = lse.double().cpu().numpy()[:rows]
+            assert np.array_equal(np.isinf(got), np.isinf(logs[:rows]))
+            m = np.isfinite(logs[:rows])
+            # the weights' factor, plus fp32 roundings of the logarithm, its sum with the largest score and that score
+            assert (np.abs(got[m] - logs[:rows][m]) <= 2e-3 * (self.unit_bits < 20) + 4e-6 * (1 + np.abs(logs[:rows][m]))).all()
+
+
+# lengths, new tokens, query heads, heads, dim
+CASES = [([1], [1], 1, 1, 16), ([64], [1], 4, 4, 64), ([65, 1, 200, 63], [1, 1, 1, 1], 8, 2, 128), ([300, 5, 0, 129], [5, 5, 0, 3], 14, 2, 80),
+         ([257], [17], 6, 2, 48), ([1000, 640], [1, 2], 16, 1, 256), ([40, 700], [40, 33], 3, 3, 112), ([100, 0, 77], [1, 2, 9], 4, 2, 192),
+         ([2, 3, 64, 128], [2, 3, 64, 70], 2, 1, 64), ([3000], [1], 32, 8, 128)]
+
+
+@pytest.mark.parametrize("lens,news,QH,H,D", CASES)
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("window", [0, 70])
+def test_attention(fxp, lens, news, QH, H, D, kind, window):
+    say("kv_attention", (lens, news, QH, H, D, kind, window))
+    c = Case(fxp, lens, news, QH, H, D, kind, behind=2)
+    out = torch.full((c.T, QH, D), 9.0, dtype=c.dq.dtype, device="cuda")
+    lse = torch.full((c.T, QH), 9.0, device="cuda")
+    got = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, window=window, out=out, lse=lse)
+    assert got is out
+    c.check(out, lse, window)
+    assert (out[c.first[-1]:] == 9).all() and (lse[c.first[-1]:] == 9).all()      # rows behind the last request
+
+
+@pytest.mark.parametrize("bits", [2, 4, 7])
+def test_attention_over_other_widths(fxp, bits):
+    say("kv_attention, bits", bits)
+    c = Case(fxp, [500, 31], [2, 1], 8, 4, 64, "bf16", bits=bits)
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_attention_with_a_token_that_outweighs_thousands(fxp, kind):
+    say("kv_attention, one large weight and a long tail", kind)
+    c = Case(fxp, [4000], [1], 2, 1, 64, kind, sink=True, sharp=2.0)
+    lse = torch.empty((1, 2), device="cuda")
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, lse=lse), lse)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_attention_is_the_value_where_all_values_are_one(fxp, kind):
+    """Weights rounded to half a unit of 1/32639 of the page's largest: 64 of them are off by 64 * 0.5 / 32639 of it at most."""
+    say("kv_attention over constant values", kind)
+    c = Case(fxp, [1500, 3], [1, 1], 4, 2, 64, kind)
+    c.cache.vq.fill_(64)
+    c.cache.ev.fill_(127)                                     # 64 * 2^(127 - 133) = 1
+    out = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale).double()
+    most = 32639 if c.unit_bits == 15 else 8355711
+    assert float((out - 1).abs().max()) <= 32 / most + c.half + 2.0 ** -20
+
+
+@pytest.mark.parametrize("window", [0, 100])
+def test_attention_with_pages_that_do_not_exist(fxp, window):
+    say("kv_attention, bad pages")
+    c = Case(fxp, [500, 64, 130], [3, 1, 1], 4, 2, 64, "bf16", missing=[(0, 2, -1), (0, 5, 10 ** 9), (1, 0, -(2 ** 31)), (2, 2, 17)])
+    lse = torch.empty((c.T, 4), device="cuda")
+    out = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, window=window, lse=lse)
+    c.check(out, lse, window)
+    assert not out[3].any() and torch.isinf(lse[3]).all()     # the only page of the second request is missing
+
+
+def test_attention_layouts_and_types_of_rows(fxp):
+    say("kv_attention, strided q and out")
+    c = Case(fxp, [200, 90], [3, 2], 6, 2, 80, "bf16")
+    want = c.want()
+    fused = torch.zeros((c.T, 6, 3 * 80 + 1), dtype=torch.bfloat16, device="cuda")
+    fused[:, :, 1:81] = c.dq
+    c.check(fxp.kv_attention(fused[:, :, 1:81], c.cache, c.tab, scale=c.scale, out=fused[:, :, 81:161]), want=want)
+    assert not fused[:, :, 0].any() and not fused[:, :, 161:].any() and torch.equal(fused[:, :, 1:81], c.dq)
+    first = c.dq.transpose(0, 1).contiguous().transpose(0, 1)
+    c.check(fxp.kv_attention(first, c.cache, c.tab, scale=c.scale, out=torch.empty_like(first)), want=want)
+    assert torch.equal(fxp.kv_attention(first, c.cache, c.tab, scale=c.scale), fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+def test_attention_many_requests(fxp):
+    say("kv_attention, 600 requests, most of them short")
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 40, 600)
+    lens[::100] = 600
+    c = Case(fxp, lens.tolist(), np.minimum(rng.integers(0, 3, 600), 2).tolist(), 2, 2, 16, "fp32")
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+def test_attention_from_a_graph_and_on_another_stream(fxp):
+    say("kv_attention captured, replayed with other lengths")
+    c = Case(fxp, [700, 64, 5], [1, 1, 1], 8, 4, 128, "fp16")
+    buf = fxp.AttentionBuffers(3, 3, 8, c.cache)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = fxp.kv_attention(c.dq, c.cache, c.tab, buf, scale=c.scale)
+    side.synchronize()
+    c.check(out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = fxp.kv_attention(c.dq, c.cache, c.tab, buf, scale=c.scale)
+    for lens in ([700, 64, 5], [1, 2, 3], [320, 0, 5], [700, 64, 5]):
+        c.lens = np.array(lens)
+        c.tab.lens_after.copy_(torch.tensor(lens, dtype=torch.int32))
+        out.fill_(5.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        c.check(out)
+        assert torch.equal(out, fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+def test_attention_answers_alike_every_time(fxp):
+    say("kv_attention, twenty calls")
+    c = Case(fxp, [5000, 900], [1, 3], 16, 2, 128, "bf16")
+    want = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale)
+    for _ in range(20):
+        assert torch.equal(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale), want)
+
+
+def test_attention_over_a_cache_past_32_bits(fxp):
+    say("kv_attention behind 4 GiB of keys")
+    c = Case(fxp, [130, 64], [1, 2], 16, 8, 256, "bf16", spare=33000)
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+def test_attention_of_rows_that_are_not_finite(fxp):
+    """As everywhere in the library: NaN maps to 0, Inf to the largest magnitude; other rows are not touched by it."""
+    say("kv_attention, Inf and NaN in q, the largest scales in the cache")
+    c = Case(fxp, [100, 100], [1, 1], 2, 2, 64, "fp32")
+    want = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale)
+    q = c.dq.clone()
+    q[0, 0, 3], q[0, 1, :] = float("inf"), float("nan")
+    out = fxp.kv_attention(q, c.cache, c.tab, scale=c.scale)
+    assert torch.equal(out[1], want[1]) and torch.isfinite(out).all()
+    c.cache.ek.fill_(255)
+    assert torch.isfinite(fxp.kv_attention(c.dq * 1e30, c.cache, c.tab, scale=c.scale)).all()

@@ -1,0 +1,155 @@
+"""Products with 4-bit weights: the packing bit for bit, the products against 64-bit sums within bounds that follow from the arithmetic."""
+import numpy as np
+import pytest
+
+from tests import serve_ref as ref
+from tests.gpu_util import dev, host, say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+TYPES = {"fp32": (torch.float32, 23, 2.0 ** -24), "bf16": (torch.bfloat16, 15, 2.0 ** -8), "fp16": (torch.float16, 15, 2.0 ** -11)}
+
+
+@pytest.fixture(scope="module")
+def fxp():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU path in libfxp")
+    from paper_2207_08822_amd import fxp as binding
+    binding.lib()
+    return binding
+
+
+def groups_of(a, group):
+    """[K, ...] cut into [groups, group, ...], zero behind K."""
+    pad = np.zeros((-(-a.shape[0] // group) * group,) + a.shape[1:])
+    pad[:a.shape[0]] = a
+    return pad.reshape((-1, group) + a.shape[1:])
+
+
+@pytest.mark.parametrize("K,N,group", [(1, 1, 64), (64, 16, 64), (130, 33, 32), (257, 100, 128), (1000, 48, 64), (128, 300, 32)])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_pack4(fxp, K, N, group, kind):
+    say("w4_pack", (K, N, group, kind))
+    rng = np.random.default_rng(K + N)
+    W = rng.standard_normal((K, N)) * 2.0 ** rng.integers(-5, 3, (1, N))
+    W[:, ::3] = np.round(W[:, ::3] * 8) / 8                       # halves among them
+    if N > 4:
+        W[:, 4] = 0
+    W = torch.tensor(W.astype(np.float32)).to(TYPES[kind][0])
+    wide = torch.zeros((K, N + 3), dtype=W.dtype, device="cuda")
+    wide[:, 1:N + 1] = W.cuda()
+    w = fxp.pack4(wide[:, 1:N + 1], group)
+    q, unit = ref.unpack4(host(w.packed), host(w.scales), K, N, group)
+    parts = groups_of(W.double().numpy(), group)
+    e = np.array([[ref.exponent(parts[i, :, n]) for n in range(N)] for i in range(len(parts))])
+    want = np.stack([ref.to_units(parts[i], e[i], 4) for i in range(len(parts))]).reshape(-1, N)[:K]
+    assert np.array_equal(unit, np.repeat(2.0 ** (e - 129.0), group, 0)[:K])
+    assert np.array_equal(q, want)
+    # what lies behind K and N is zero
+    kt, nt = -(-K // 128), -(-N // 16)
+    q, _ = ref.unpack4(host(w.packed), host(w.scales), kt * 128, nt * 16, group)
+    assert not q[K:].any() and not q[:, N:].any()
+
+
+def weights(fxp, rng, K, N, group):
+    """Packed weights with random mantissas (zero behind K and N) and scales, and their values."""
+    W = torch.tensor((rng.standard_normal((K, N)) * 2.0 ** rng.integers(-3, 4, (1, N))).astype(np.float32))
+    w = fxp.pack4(W.cuda(), group)
+    q, unit = ref.unpack4(host(w.packed), host(w.scales), K, N, group)
+    return w, q * unit
+
+
+def bound(x, W, y, group, unit_bits, half):
+    """x's groups are rounded to half a unit 2^(e - 126 - unit_bits), e the exponent of the group's largest element (one more within 2^-7
+    of the next binade); a group's integer sum becomes fp32 once (three times with a third digit), is scaled twice and added in: five roundings
+    of 2^-24 of the group's sum of magnitudes, and one of the whole sum for each group and each of the eight partial sums joined."""
+    gx, gw = groups_of(x.T, group), groups_of(W, group)               # [G, group, M], [G, group, N]
+    top = np.abs(gx).max(1) * (1 + 2.0 ** -6)
+    e = np.maximum(np.frexp(top)[1] + 126, 1)
+    unit = 2.0 ** (e - 126.0 - unit_bits) * (top > 0)
+    mass = np.abs(x) @ np.abs(W)
+    inner = unit.T / 2 @ np.abs(gw).sum(1) + 2.0 ** -24 * (5 + len(gx) + 40) * mass
+    return half * (np.abs(y) + inner) + inner
+
+
+SIZES = [(1, 1, 1), (1, 64, 16), (2, 130, 33), (16, 128, 48), (17, 1000, 100), (1, 4096, 20), (5, 768, 2304), (64, 300, 70), (65, 257, 17),
+         (130, 640, 40), (3, 20000, 5)]
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_linear4(fxp, M, K, N, group, kind):
+    say("w4_linear", (M, K, N, group, kind))
+    rng = np.random.default_rng(M * 3 + K + N)
+    w, W = weights(fxp, rng, K, N, group)
+    dtype, unit_bits, half = TYPES[kind]
+    x = rng.standard_normal((M, K)) * np.exp2(rng.standard_normal((1, K)) * 2)
+    x[:, :K // 3] = 0 if M == 2 else x[:, :K // 3]                    # whole groups of zeros
+    x = torch.tensor(x.astype(np.float32)).to(dtype)
+    y = x.double().numpy() @ W
+    got = fxp.linear4(x.cuda(), w).double().cpu().numpy()
+    off = bound(x.double().numpy(), W, y, group, unit_bits, half)
+    assert (np.abs(got - y) <= off).all(), np.max(np.abs(got - y) / np.maximum(off, 1e-300))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_linear4_of_whole_numbers_is_exact(fxp, kind):
+    """x in -8..8 and scales of one power of two: every product and sum fits fp32, and the result is rounded once."""
+    say("w4_linear of whole numbers", kind)
+    rng = np.random.default_rng(4)
+    x = torch.tensor(rng.integers(-8, 9, (7, 500)).astype(np.float32)).to(TYPES[kind][0])
+    W = rng.integers(-7, 8, (500, 90)).astype(np.float32)
+    W[::32] = 7                                                      # every group's scale is that of 7
+    w = fxp.pack4(torch.tensor(W).cuda(), 64)
+    want = torch.tensor(x.double().numpy() @ W.astype(np.float64)).to(x.dtype)
+    assert torch.equal(fxp.linear4(x.cuda(), w).cpu(), want)
+
+
+def test_linear4_strides_and_rows(fxp):
+    say("w4_linear, strided x and out, row by row")
+    rng = np.random.default_rng(6)
+    w, W = weights(fxp, rng, 333, 50, 64)
+    wide = torch.randn((20, 400), device="cuda").to(torch.bfloat16)
+    x = wide[:, 7:340]
+    out = torch.full((20, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    fxp.linear4(x, w, out=out[:, 5:55])
+    assert (out[:, :5] == 3).all() and (out[:, 55:] == 3).all()
+    assert torch.equal(out[:, 5:55], fxp.linear4(x.contiguous(), w))
+    for m in (0, 19):                                                # a row does not depend on the rows beside it
+        assert torch.equal(out[m, 5:55], fxp.linear4(x[m:m + 1], w)[0])
+    assert fxp.linear4(x[:0], w).shape == (0, 50)
+    with pytest.raises(fxp.FxpError):
+        fxp.linear4(wide[:1, :333].expand(4, 333), w)
+
+
+def test_linear4_of_values_that_are_not_finite_or_tiny(fxp):
+    say("w4_linear, Inf, NaN, sub-normal")
+    rng = np.random.default_rng(7)
+    w, W = weights(fxp, rng, 256, 32, 64)
+    x = torch.randn((4, 256), device="cuda")
+    want = fxp.linear4(x, w)
+    bad = x.clone()
+    bad[1, 70], bad[2, 3] = float("inf"), float("nan")
+    got = fxp.linear4(bad, w)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[3], want[3]) and not torch.isnan(got).any()
+    tiny = torch.full((1, 256), 1e-40, device="cuda")
+    assert (fxp.linear4(tiny, w).abs() < 1e-36).all()
+
+
+def test_linear4_from_a_graph(fxp):
+    say("w4_linear captured")
+    rng = np.random.default_rng(8)
+    w, W = weights(fxp, rng, 1024, 200, 64)
+    x = torch.randn((3, 1024), device="cuda").to(torch.float16)
+    fxp.linear4(x, w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = fxp.linear4(x, w)
+    for i in range(4):
+        x.copy_(torch.randn((3, 1024), device="cuda"))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, fxp.linear4(x, w))
