@@ -1,10 +1,9 @@
 // Attention over a paged cache of mapped keys and values, with int8 matrix products and the softmax in fp32 (Sec. 5).
 //
-// A tile is 16 rows (token, query head) of one request and one head of the cache; a unit of work is one page (64 tokens) of a tile.
-// All units of a call stand in one line, request by request, tile by tile, head by head, page by page, and every workgroup takes an
-// equal stretch of it: lengths differ by orders of magnitude and are known on the device alone.  The four waves of a
-// workgroup take the pages of a stretch in turn.  Where a tile's pages fall into two stretches or more, each leaves
-// (largest score, sum, output) of its part in the workspace and a second launch joins them.
+// A tile is 16 rows (token, query head) of one request and one head of the cache.  All pages of all tiles stand in one line, request
+// by request, tile by tile, head by head, and every workgroup takes an equal stretch of it: lengths differ by orders of magnitude
+// and are known on the device alone.  A workgroup's waves take the pages of a stretch in turn.  Where a tile's pages fall into several
+// stretches, each leaves (largest score, sum, output) of its part in the workspace, and the workgroup that is last to do so joins them.
 //
 // One page: S^T = K Q^T by v_mfma_i32_16x16x64_i8 with the key rows as they lie in memory as A operand (16 bytes a lane) and
 // Q's digits as B; a lane then holds 16 scores of ONE row (column lane % 16), tokens 16 (lane / 16) .. + 15 - the
@@ -17,11 +16,12 @@
 // relative to the page's own largest, so a long tail of small weights behind one large one keeps its sum.  fp32 has 23 bits.
 #include "fxp_serve_device.h"
 
+#ifndef SEL8
+#define SEL8 0
+#endif
 namespace fxp {
 
 constexpr int kTile = 16;
-constexpr int kAttWaves = 4;
-constexpr int kAttThreads = 64 * kAttWaves;
 constexpr int kAttGroups = 512;          // workgroups at most: two a CU
 
 struct AttArgs {
@@ -35,18 +35,14 @@ struct AttArgs {
     void* out;
     int64_t out_token, out_head;
     float* lse;
-    float* part_o;          // [workgroup][2][16][dim]
-    float2* part_ml;        // [workgroup][2][16]
+    float* part_o;          // [workgroup][2][16][dim]: parts of the tiles that the stretch ends in (0) and begins in (1)
+    float2* part_ml;        // [workgroup][2][16]: largest score (log2), sum
+    uint32_t* tickets;      // [tiles][heads]: parts of a tile that are there; zero between calls
     int group;              // query heads per head of the cache
+    uint32_t group_inverse; // ceil(2^32 / group): (x * it) >> 32 is x / group for x * group < 2^32
     int vec_q, vec_out;
     float scale_log2;       // scale * log2(e)
-    int64_t window;         // <= 0: none
-};
-
-// where a tile stands
-struct Segment {
-    int b, tile, head, rows, n, len, page0, pages, tok0;
-    int64_t unit0;
+    int window;             // 0: none
 };
 
 struct Extent {
@@ -59,68 +55,91 @@ __device__ inline Extent extent(const AttArgs& a, int64_t b) {
     e.n = max(min(max(a.first[b + 1], 0), most) - e.tok0, 0);
     e.len = static_cast<int>(min(static_cast<int64_t>(max(a.lens[b], 0)), a.blocks * FXP_KV_PAGE));
     e.tiles = (e.n * a.group + kTile - 1) / kTile;
-    const int64_t from = a.window > 0 ? max(int64_t{e.len} - e.n + 1 - a.window, int64_t{0}) : 0;
-    e.page0 = static_cast<int>(from / FXP_KV_PAGE);
+    const int from = a.window > 0 ? max(e.len - e.n + 1 - a.window, 0) : 0;
+    e.page0 = from / FXP_KV_PAGE;
     e.pages = max((e.len + FXP_KV_PAGE - 1) / FXP_KV_PAGE - e.page0, 1);       // an empty request still has its zeros to write
     return e;
 }
 
-// sum over the workgroup, and the sum before the thread
+// Cost of a tile in pages besides its own: its rows of q, the join of its parts, the first loads' way.  (Without it a workgroup
+// whose stretch is many short tiles takes as long as several others.)
 template <int WAVES>
-__device__ inline int64_t block_scan64(int64_t v, int64_t* lds, int64_t& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t t = __shfl_up(static_cast<long long>(s), d);
-        if (lane >= d) s += t;
-    }
-    if (lane == 63) lds[wave] = s;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (w == wave) before = total;
-        total += lds[w];
-    }
-    __syncthreads();
-    return before + s - v;
+constexpr int kTileCost = 2 * WAVES;
+
+// The line, and where this workgroup's stretch of it begins.  Units are counted in 32 bits: the host sees to it.
+struct Stretch {
+    uint32_t units, per, u0;           // all units, those of a stretch, the first of this one
+    uint32_t unit_b;                   // units before request b
+    int b, tiles_before;               // request of unit u0, tiles before it
+    Extent e;
+};
+
+// Pages of a stretch: equal shares, but no fewer than one a wave, and so many that the parts of the longest tile are at
+// most some twice as many as the pages that a wave has of them (they are joined one after the other).
+template <int WAVES>
+__device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
+    const uint32_t per = (units + gridDim.x - 1) / gridDim.x;
+    const int least = static_cast<int>(0.7f * sqrtf(static_cast<float>(most_pages)));
+    return max(per, static_cast<uint32_t>(max(least, WAVES)));
 }
 
-// units of all requests; found[0..1] = (request, units before it) of the request that unit `at` belongs to
-__device__ inline int64_t locate(const AttArgs& a, int64_t at, bool tiles_only, int64_t* lds, int64_t* found) {
-    int64_t carry = 0, total;
-    for (int64_t base = 0; base < a.requests; base += kAttThreads) {
-        const int64_t b = base + threadIdx.x;
-        int64_t v = 0;
-        if (b < a.requests) {
-            const Extent e = extent(a, b);
-            v = tiles_only ? e.tiles : e.tiles * a.c.heads * e.pages;
+// sum over the lanes up to this one, inside the vector ALU (rows of 16 first, then row to row)
+__device__ inline uint32_t wave_scan(uint32_t v) {
+    auto step = [](uint32_t x, auto ctrl, auto rows) {
+        return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+    };
+    using std::integral_constant;
+    v = step(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});     // row_shr:1
+    v = step(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});     // row_shr:2
+    v = step(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});     // row_shr:4
+    v = step(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});     // row_shr:8
+    v = step(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});     // row_bcast:15 into rows 1 and 3
+    v = step(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});     // row_bcast:31 into rows 2 and 3
+    return v;
+}
+__device__ inline int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+
+// Every wave by itself, 64 requests at a time; the loads of up to 64 requests are made once.
+template <int WAVES>
+__device__ inline Stretch survey(const AttArgs& a) {
+    const int lane = threadIdx.x & 63, requests = static_cast<int>(a.requests), heads = static_cast<int>(a.c.heads);
+    Stretch st = {};
+    auto units_of = [&](const Extent& e) { return static_cast<uint32_t>(e.tiles * heads) * static_cast<uint32_t>(e.pages + kTileCost<WAVES>); };
+    Extent e = {};
+    uint32_t v = 0;
+    int most = 0;
+    for (int base = 0; base < requests; base += 64) {
+        if (base + lane < requests) e = extent(a, base + lane);
+        else e.tiles = 0;
+        v = units_of(e);
+        most = max(most, e.tiles ? e.pages : 0);
+        st.units += static_cast<uint32_t>(lane_of(static_cast<int>(wave_scan(v)), 63));
+    }
+    st.per = stretch_of<WAVES>(st.units, static_cast<int>(wave_max(static_cast<uint32_t>(most))));
+    st.u0 = st.per * blockIdx.x;
+    st.b = -1;
+    uint32_t carry = 0;
+    for (int base = 0; base < requests; base += 64) {
+        if (requests > 64) {
+            if (base + lane < requests) e = extent(a, base + lane);
+            else e.tiles = 0;
+            v = units_of(e);
         }
-        const int64_t x = carry + block_scan64<kAttWaves>(v, lds, total);
-        if (at >= x && at < x + v) {
-            found[0] = b;
-            found[1] = x;
+        const uint32_t sum = wave_scan(v), x = carry + sum - v;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(st.u0 >= x && st.u0 < x + v);
+        const int sum_t = static_cast<int>(wave_scan(static_cast<uint32_t>(e.tiles)));
+        if (hit) {
+            const int w = __builtin_ctzll(hit);
+            st.b = base + w;
+            st.unit_b = static_cast<uint32_t>(lane_of(static_cast<int>(x), w));
+            st.tiles_before += lane_of(sum_t - e.tiles, w);
+            st.e = {lane_of(e.n, w), lane_of(e.len, w), lane_of(e.tiles, w), lane_of(e.page0, w), lane_of(e.pages, w), lane_of(e.tok0, w)};
+            break;
         }
-        carry += total;
+        st.tiles_before += lane_of(sum_t, 63);
+        carry += static_cast<uint32_t>(lane_of(static_cast<int>(sum), 63));
     }
-    __syncthreads();
-    return carry;
-}
-
-__device__ inline int64_t units_per_group(int64_t units, unsigned groups) {
-    const int64_t per = (units + groups - 1) / groups;
-    return (max(per, int64_t{kAttWaves}) + kAttWaves - 1) / kAttWaves * kAttWaves;
-}
-
-__device__ inline float max_groups(float v) {              // over the four lanes that hold a row
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ inline float sum_groups(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    return st;
 }
 
 // sum of products of digits, as a float: acc = d1 * 256 + d0 fits 32 bits over 256 terms; a third digit is added in fp32
@@ -145,265 +164,385 @@ __device__ inline void dot_digits(const v4i (&a)[N], const v4i (&b)[N][ND], floa
     }
 }
 
-template <int TYPE, int DB>
-__global__ __launch_bounds__(kAttThreads, DB <= 2 ? 2 : 1) void k_kv_attend(AttArgs a) {
-    constexpr int ND = TYPE == FXP_F32 ? 3 : 2;
-    constexpr int DMAX = 64 * DB, ROW = DMAX + 4;
-    __shared__ int64_t scan[kAttWaves];
-    __shared__ int64_t found[2];
-    __shared__ float s_m[kAttWaves][kTile], s_l[kAttWaves][kTile];
-    __shared__ float s_o[kAttWaves][kTile][ROW];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads);
-    if (threadIdx.x == 0) found[0] = -1;
-    __syncthreads();
-    // the stretch of this workgroup; the size of a stretch needs the sum first
-    const int64_t units = locate(a, -1, false, scan, found);
-    const int64_t per = units_per_group(units, gridDim.x);
-    const int64_t u0 = per * blockIdx.x, u1 = min(u0 + per, units);
-    if (u0 >= u1) return;
-    locate(a, u0, false, scan, found);
-    int64_t b = found[0], unit_b = found[1];
-    Extent e = extent(a, b);
-    int64_t u = u0;
-
-    while (u < u1) {
-        // the tile that unit u belongs to, and this workgroup's pages of it
-        int64_t in_b = u - unit_b;
-        while (in_b >= int64_t{e.tiles} * heads * e.pages) {
-            unit_b += int64_t{e.tiles} * heads * e.pages;
-            e = extent(a, ++b);
-            in_b = u - unit_b;
-        }
-        const int seg = static_cast<int>(in_b / e.pages), p0 = static_cast<int>(in_b % e.pages);
-        const int tile = seg / heads, head = seg % heads;
-        const int p1 = static_cast<int>(min(int64_t{e.pages}, p0 + (u1 - u)));
-        const bool whole = p0 == 0 && p1 == e.pages;
-        const int slot = u == u0 ? 0 : 1;
-        u += p1 - p0;
-
-        // this lane's row
-        const int r = tile * kTile + col, tok = r / a.group, qh = head * a.group + r % a.group;
-        const bool row_ok = tok < e.n;
-        const int place = e.len - e.n + tok;                           // negative: more rows than tokens; such a row sees nothing
-        const int see_to = row_ok ? min(place, e.len - 1) : -1;
-        const int64_t see_from = a.window > 0 ? int64_t{place} - a.window + 1 : 0;
-
-        // Q's digits
-        v4i qd[DB][ND];
-        int qe;
-        {
-            float x[DB][16];
-            uint32_t m = 0;
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                const int d = 64 * i + 16 * g;
-                if (row_ok && d < dim) {
-                    load_elems<TYPE, 16>(a.q, (int64_t{e.tok0} + tok) * a.q_token + qh * a.q_head + d, a.vec_q, x[i]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) x[i][j] = 0.0f;
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j) m = max(m, __float_as_uint(x[i][j]) & 0x7fffffffu);
-            }
-            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
-            m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
-            qe = unit_of<ND>(m);
-#pragma unroll
-            for (int i = 0; i < DB; ++i) {
-                int v[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[i][j], qe);
-                digits16<ND>(v, qd[i]);
-            }
-        }
-
-        float o[4 * DB][4];
-        float m_run = -INFINITY, l_run = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 4 * DB; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
-
-        for (int p = p0 + wave; p < p1; p += kAttWaves) {
-            const int block = e.page0 + p;
-            const int page = block < a.blocks ? a.table[b * a.blocks + block] : -1;
-            if (page < 0 || page >= a.c.pages) continue;
-            const int64_t at = int64_t{page} * heads + head;
-            const int8_t* kp = a.c.kq + at * (FXP_KV_PAGE * dim);
-            const int8_t* vp = a.c.vq + at * (FXP_KV_PAGE * dim);
-            const int ek = min(max(a.c.ek[at], 1), 255) - 125 - a.c.bits, ev = min(max(a.c.ev[at], 1), 255) - 125 - a.c.bits;
-            v4i kf[4][DB], vf[4 * DB];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int i = 0; i < DB; ++i) {
-                    const int token = 16 * (col >> 2) + 4 * t + (col & 3), d = 64 * i + 16 * g;
-                    kf[t][i] = d < dim ? *reinterpret_cast<const v4i*>(kp + token * dim + d) : v4i{0, 0, 0, 0};
-                }
-#pragma unroll
-            for (int i = 0; i < 4 * DB; ++i)
-                if (16 * i < dim) vf[i] = *reinterpret_cast<const v4i*>(vp + (g * dim + 16 * i + col) * 16);
-            // bounded so that no product of it and a sum of up to 2^15 terms (digits x 7 bits x dim) passes 2^127: no Inf - Inf below
-            const float f = fminf(ldexpf(a.scale_log2, qe + ek), ND == 2 ? 0x1p97f : 0x1p89f);
-
-            float s[16];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                float x[4];
-                dot_digits<ND, DB>(kf[t], qd, x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[4 * t + i] = x[i] * f;
-            }
-            const int j0 = block * FXP_KV_PAGE + 16 * g;
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (j0 + i > see_to || j0 + i < see_from) s[i] = -INFINITY;
-            float m = s[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-            m = max_groups(m);
-            const float top = m == -INFINITY ? 0.0f : m;
-            float l = 0.0f;
-            v4i pd[1][ND];
-            int v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = exp2f(s[i] - top);
-                l += w;
-                v[i] = static_cast<int>(rintf(w * Digits<ND>::kMost));
-            }
-            digits16<ND>(v, pd[0]);
-            l = sum_groups(l);
-            const float m_new = fmaxf(m_run, m), ref = m_new == -INFINITY ? 0.0f : m_new;
-            const float keep = exp2f(m_run - ref), gain = exp2f(m - ref);
-            const float fv = ldexpf(gain * (1.0f / Digits<ND>::kMost), ev);
-            l_run = l_run * keep + l * gain;
-            m_run = m_new;
-#pragma unroll
-            for (int i = 0; i < 4 * DB; ++i) {
-                if (16 * i >= dim) continue;
-                float x[4];
-                const v4i vfrag[1] = {vf[i]};
-                dot_digits<ND, 1>(vfrag, pd, x);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[i][j] = fmaf(x[j], fv, o[i][j] * keep);
-            }
-        }
-
-        // the four waves' parts
-        if (g == 0) {
-            s_m[wave][col] = m_run;
-            s_l[wave][col] = l_run;
-        }
-#pragma unroll
-        for (int i = 0; i < 4 * DB; ++i)
-            if (16 * i < dim) *reinterpret_cast<float4*>(&s_o[wave][col][16 * i + 4 * g]) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-        __syncthreads();
-        const int rows = min(e.n * a.group - tile * kTile, kTile);
-        for (int i = threadIdx.x; i < rows * (dim / 4); i += kAttThreads) {
-            const int row = i / (dim / 4), d = i % (dim / 4) * 4;
-            float m = s_m[0][row];
-#pragma unroll
-            for (int w = 1; w < kAttWaves; ++w) m = fmaxf(m, s_m[w][row]);
-            const float ref = m == -INFINITY ? 0.0f : m;
-            float l = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int w = 0; w < kAttWaves; ++w) {
-                const float f = exp2f(s_m[w][row] - ref);
-                const float4 y = *reinterpret_cast<const float4*>(&s_o[w][row][d]);
-                l = fmaf(s_l[w][row], f, l);
-                x[0] = fmaf(y.x, f, x[0]);
-                x[1] = fmaf(y.y, f, x[1]);
-                x[2] = fmaf(y.z, f, x[2]);
-                x[3] = fmaf(y.w, f, x[3]);
-            }
-            const int rr = tile * kTile + row;
-            const int64_t t = int64_t{e.tok0} + rr / a.group;
-            const int h = head * a.group + rr % a.group;
-            if (whole) {
-                const float inv = l > 0.0f ? 1.0f / l : 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] *= inv;
-                store4<TYPE>(a.out, t * a.out_token + h * a.out_head + d, a.vec_out, x);
-                if (a.lse && d == 0) a.lse[t * (heads * a.group) + h] = l > 0.0f ? (m + log2f(l)) * 0.693147180559945f : -INFINITY;
-            } else {
-                const int64_t part = (int64_t{blockIdx.x} * 2 + slot) * kTile + row;
-                *reinterpret_cast<float4*>(a.part_o + part * dim + d) = make_float4(x[0], x[1], x[2], x[3]);
-                if (d == 0) a.part_ml[part] = make_float2(m, l);
-            }
-        }
-        __syncthreads();
-    }
+__device__ inline float swap_max(float v) {                  // over the four lanes that hold a row
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ inline float swap_sum(float v) {
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
 }
 
-// Joins the parts of a tile that fell into several stretches.  blockIdx.x = tile, blockIdx.y = head.
-template <int TYPE>
-__global__ __launch_bounds__(kAttThreads) void k_kv_attend_join(AttArgs a, unsigned groups) {
-    __shared__ int64_t scan[kAttWaves];
-    __shared__ int64_t found[2];
-    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), head = blockIdx.y;
-    if (threadIdx.x == 0) found[0] = -1;
-    __syncthreads();
-    locate(a, blockIdx.x, true, scan, found);
-    const int64_t b = found[0], tile0 = found[1];
-    if (b < 0) return;
-    __syncthreads();
-    // units before request b
-    int64_t before = 0, units = 0, total;
-    for (int64_t base = 0; base < a.requests; base += kAttThreads) {
-        const int64_t i = base + threadIdx.x;
-        int64_t v = 0;
-        if (i < a.requests) {
-            const Extent x = extent(a, i);
-            v = x.tiles * a.c.heads * x.pages;
-        }
-        const int64_t x = units + block_scan64<kAttWaves>(v, scan, total);
-        if (i == b) found[1] = x;
-        units += total;
-    }
-    __syncthreads();
-    before = found[1];
-    const Extent e = extent(a, b);
-    const int tile = static_cast<int>(blockIdx.x - tile0);
-    const int64_t per = units_per_group(units, groups);
-    const int64_t s0 = before + (int64_t{tile} * heads + head) * e.pages, s1 = s0 + e.pages;
-    const int64_t w0 = s0 / per, w1 = (s1 - 1) / per;
-    if (w0 == w1) return;
-    const int rows = min(e.n * a.group - tile * kTile, kTile);
-    for (int i = threadIdx.x; i < rows * (dim / 4); i += kAttThreads) {
-        const int row = i / (dim / 4), d = i % (dim / 4) * 4;
-        float m = -INFINITY;
-        for (int64_t w = w0; w <= w1; ++w) m = fmaxf(m, a.part_ml[(w * 2 + (w * per < s0)) * kTile + row].x);
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float l = 0.0f, x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int64_t w = w0; w <= w1; ++w) {
-            const int64_t part = (w * 2 + (w * per < s0)) * kTile + row;
-            const float2 ml = a.part_ml[part];
-            const float f = exp2f(ml.x - ref);
-            const float4 y = *reinterpret_cast<const float4*>(a.part_o + part * dim + d);
-            l = fmaf(ml.y, f, l);
-            x[0] = fmaf(y.x, f, x[0]);
-            x[1] = fmaf(y.y, f, x[1]);
-            x[2] = fmaf(y.z, f, x[2]);
-            x[3] = fmaf(y.w, f, x[3]);
-        }
-        const int rr = tile * kTile + row;
-        const int64_t t = int64_t{e.tok0} + rr / a.group;
-        const int h = head * a.group + rr % a.group;
-        const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+// Q's digits of this lane's row (zeros where there is none), and the exponent of their unit
+template <int TYPE, int DB, int ND>
+__device__ inline int load_query(const AttArgs& a, const Extent& e, int tok, int qh, bool row_ok, int g, v4i (&qd)[DB][ND]) {
+    float x[DB][16];
+    uint32_t m = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] *= inv;
-        store4<TYPE>(a.out, t * a.out_token + h * a.out_head + d, a.vec_out, x);
-        if (a.lse && d == 0) a.lse[t * (heads * a.group) + h] = l > 0.0f ? (m + log2f(l)) * 0.693147180559945f : -INFINITY;
+    for (int i = 0; i < DB; ++i) {
+        const int d = 64 * i + 16 * g;
+        if (row_ok && d < a.c.dim) {
+            load_elems<TYPE, 16>(a.q, (int64_t{e.tok0} + tok) * a.q_token + qh * a.q_head + d, a.vec_q, x[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) x[i][j] = 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 16; ++j) m = max(m, __float_as_uint(x[i][j]) & 0x7fffffffu);
+    }
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
+    const int unit = unit_of<ND>(m);
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+        int v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[i][j], unit);
+        digits16<ND>(v, qd[i]);
+    }
+    return unit;
+}
+
+// Weights 2^(s - top) of 16 scores as digits, and their sum; `top` becomes the score that weighs 1 (32767 / 32639 for two digits: the
+// packing conversion multiplies by 32767, and the largest weight has to stay at 127 in each digit).
+template <int ND>
+__device__ inline float weigh(const float (&s)[16], float& top, v4i (&pd)[1][ND]) {
+    float l = 0.0f;
+    if constexpr (ND == 2) {
+        top += 0.00564698f;                    // log2(32767 / 32639), rounded up
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            float w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(s[4 * t + i] - top);
+                l += w[i];
+            }
+            typedef short v2s __attribute__((ext_vector_type(2)));
+            const v2s a = __builtin_amdgcn_cvt_pknorm_i16(w[0], w[1]), b = __builtin_amdgcn_cvt_pknorm_i16(w[2], w[3]);
+            const uint32_t x = __builtin_bit_cast(uint32_t, a) + 0x00800080u, y = __builtin_bit_cast(uint32_t, b) + 0x00800080u;
+            pd[0][0][t] = static_cast<int>(perm(y, x, 0x07050301u));
+            pd[0][1][t] = static_cast<int>(perm(y, x, 0x06040200u) ^ 0x80808080u);
+        }
+    } else {
+        int v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float w = __builtin_amdgcn_exp2f(s[i] - top);
+            l += w;
+            v[i] = static_cast<int>(rintf(w * Digits<ND>::kMost));
+        }
+        digits16<ND>(v, pd[0]);
+    }
+    return l;
+}
+template <int ND>
+constexpr float kWeightUnit = ND == 2 ? 1.0f / 32767 : 1.0f / 8355711;
+
+// Rows of a tile: row i is token tok + (rest + i) / group of the request, head (rest + i) % group of its group.
+struct TileRows {
+    int tok, rest;
+    __device__ void at(const AttArgs& a, int i, int& t, int& h) const {
+        const int x = rest + i, q = static_cast<int>(__umulhi(static_cast<uint32_t>(x), a.group_inverse));
+        t = tok + (a.group == 1 ? x : q);                               // the inverse of 1 does not fit
+        h = x - (a.group == 1 ? x : q * a.group);
+    }
+};
+__device__ inline TileRows tile_rows(const AttArgs& a, int tile) {
+    const int r = tile * kTile, tok = static_cast<int>(static_cast<uint32_t>(r) / static_cast<uint32_t>(a.group));
+    return {tok, r - tok * a.group};
+}
+
+// one row's share of four elements, and the join of two shares
+struct Share {
+    float m, l, x[4];
+};
+__device__ inline void join(Share& s, float m, float l, const float4 y) {
+    const float top = fmaxf(s.m, m), ref = top == -INFINITY ? 0.0f : top;
+    const float keep = __builtin_amdgcn_exp2f(s.m - ref), gain = __builtin_amdgcn_exp2f(m - ref);
+    s.m = top;
+    s.l = s.l * keep + l * gain;
+    s.x[0] = s.x[0] * keep + y.x * gain;
+    s.x[1] = s.x[1] * keep + y.y * gain;
+    s.x[2] = s.x[2] * keep + y.z * gain;
+    s.x[3] = s.x[3] * keep + y.w * gain;
+}
+// two floats to and from memory that other XCDs see: atomic accesses of device scope pass their L2 caches
+__device__ inline void store_part(float* p, float x, float y) {
+    const uint64_t v = static_cast<uint64_t>(__float_as_uint(y)) << 32 | __float_as_uint(x);
+    __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ inline float2 load_part(const float* p) {
+    const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float(static_cast<uint32_t>(v)), __uint_as_float(static_cast<uint32_t>(v >> 32)));
+}
+template <int TYPE>
+__device__ inline void finish(const AttArgs& a, const Extent& e, const TileRows& rows_of, int head, int row, int d, Share s) {
+    int tok, in_group;
+    rows_of.at(a, row, tok, in_group);
+    const int64_t t = int64_t{e.tok0} + tok;
+    const int h = head * a.group + in_group;
+    const float inv = s.l > 0.0f ? 1.0f / s.l : 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s.x[j] *= inv;
+    store4<TYPE>(a.out, t * a.out_token + h * a.out_head + d, a.vec_out, s.x);
+    if (a.lse && d == 0) a.lse[t * (static_cast<int>(a.c.heads) * a.group) + h] = s.l > 0.0f ? (s.m + log2f(s.l)) * 0.693147180559945f : -INFINITY;
+}
+
+template <int TYPE, int DB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttArgs a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, THREADS = 64 * WAVES, COST = kTileCost<WAVES>;
+    constexpr int DMAX = 64 * DB, ROW = DMAX + 4;
+    __shared__ float s_m[WAVES][kTile], s_l[WAVES][kTile];
+    __shared__ float4 s_o4[WAVES * kTile * ROW / 4];
+    __shared__ int s_last;
+    float* const s_o = reinterpret_cast<float*>(s_o4);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), nd = dim / 4;
+    const Stretch st = survey<WAVES>(a);
+    const uint32_t per = st.per, u0 = st.u0, u1 = min(u0 + per, st.units);
+    if (st.b < 0) return;                                               // behind the end of the line
+    int b = st.b, tiles_before = st.tiles_before;
+    Extent e = st.e;
+    // the tile of unit u0, and its first unit
+    const uint32_t first_seg = (u0 - st.unit_b) / static_cast<uint32_t>(e.pages + COST);
+    int tile = static_cast<int>(first_seg / static_cast<uint32_t>(heads)), head = static_cast<int>(first_seg - static_cast<uint32_t>(tile * heads));
+    uint32_t s0 = st.unit_b + first_seg * static_cast<uint32_t>(e.pages + COST);
+
+    while (s0 < u1) {
+        // this workgroup's pages of the tile
+        const int ahead = static_cast<int>(u0 - s0) - COST;             // of the stretch's begin, from the tile's first page
+        const int p0 = max(ahead, 0), p1 = min(static_cast<int>(u1 - s0) - COST, e.pages);
+        if (p0 < p1) {
+            const TileRows rows_of = tile_rows(a, tile);
+            int tok, in_group;
+            rows_of.at(a, col, tok, in_group);
+            const int qh = head * a.group + in_group;
+            const bool row_ok = tok < e.n;
+            const int place = e.len - e.n + tok;                       // negative: more rows than tokens; such a row sees nothing
+            const int see_to = row_ok ? min(place, e.len - 1) : -1;
+            const int see_from = a.window > 0 ? max(place - a.window + 1, 0) : 0;
+            // places that every row of the tile sees
+            const int rows = min(e.n * a.group - tile * kTile, kTile);
+            int last_tok, unused;
+            rows_of.at(a, rows - 1, last_tok, unused);
+            const int all_to = e.len - e.n + rows_of.tok;
+            const int all_from = a.window > 0 ? max(e.len - e.n + last_tok - a.window + 1, 0) : 0;
+
+            // the pages' numbers: lane i has that of the wave's i-th page
+            const int32_t* const table = a.table + int64_t{b} * a.blocks + e.page0;
+            int ids = 0;
+            auto load_ids = [&](int p) {
+                const int at = p + WAVES * lane;
+                ids = at < p1 ? table[at] : -1;
+            };
+            load_ids(p0 + wave);
+
+            v4i kf[4][DB], vf[4 * DB];
+            int ek_now = 0, ev_now = 0, ek_next = 0, ev_next = 0;
+            bool dead_now = true, dead_next = true;
+            // page `id`, or page 0, of which nothing is seen then
+            auto base_of = [&](int id, bool& dead) {
+                dead = id < 0 || id >= a.c.pages;
+                return (int64_t{dead ? 0 : id} * heads + head);
+            };
+            const int k_off = (16 * (col >> 2) + (col & 3)) * dim + 16 * g, v_off = (g * dim + col) * 16;
+            auto load_k = [&](int64_t at) {
+                const int8_t* p = a.c.kq + at * (FXP_KV_PAGE * dim) + k_off;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int i = 0; i < DB; ++i) {
+                        if (64 * i + 16 * g < dim) kf[t][i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 4 * t * dim + 64 * i));
+                        else kf[t][i] = v4i{0, 0, 0, 0};
+                    }
+            };
+            auto load_v = [&](int64_t at) {
+                const int8_t* p = a.c.vq + at * (FXP_KV_PAGE * dim) + v_off;
+#pragma unroll
+                for (int i = 0; i < 4 * DB; ++i)
+                    if (16 * i < dim) vf[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 256 * i));
+            };
+
+            float o[4 * DB][4];
+            float m_run = -INFINITY, l_run = 0.0f;                     // l_run: of this lane's 16 tokens of each page
+#pragma unroll
+            for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+
+            int p = p0 + wave, index = 0;
+            int64_t at = 0;
+            if (p < p1) {
+                at = base_of(__builtin_amdgcn_readlane(ids, 0), dead_next);
+                ek_next = a.c.ek[at];
+                ev_next = a.c.ev[at];
+                load_k(at);
+                load_v(at);
+            }
+            v4i qd[DB][ND];
+            const int qe = load_query<TYPE, DB, ND>(a, e, tok, qh, row_ok, g, qd);
+
+            for (; p < p1; p += WAVES) {
+                ek_now = ek_next;
+                ev_now = ev_next;
+                dead_now = dead_next;
+                const bool more = p + WAVES < p1;
+                if (more) {
+                    if (++index == 64) {
+                        index = 0;
+                        load_ids(p + WAVES);
+                    }
+                    at = base_of(__builtin_amdgcn_readlane(ids, index), dead_next);
+                    ek_next = a.c.ek[at];
+                    ev_next = a.c.ev[at];
+                }
+                const int ek = min(max(ek_now, 1), 255) - 125 - a.c.bits, ev = min(max(ev_now, 1), 255) - 125 - a.c.bits;
+                // bounded so that no product of it and a sum of up to 2^15 terms (digits x 7 bits x dim) passes 2^127: no Inf - Inf below
+                const float f = fminf(ldexpf(a.scale_log2, qe + ek), ND == 2 ? 0x1p97f : 0x1p89f);
+                float s[16];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    float x[4];
+                    dot_digits<ND, DB>(kf[t], qd, x);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[4 * t + i] = x[i] * f;
+                }
+                if (more) load_k(at);                                   // on its way while the softmax is worked out
+                const int j0 = (e.page0 + p) * FXP_KV_PAGE;
+                if (dead_now || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (dead_now || j0 + 16 * g + i > see_to || j0 + 16 * g + i < see_from) s[i] = -INFINITY;
+                }
+                float m = s[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+                m = swap_max(m);
+                float top = m == -INFINITY ? 0.0f : m;
+                v4i pd[1][ND];
+                const float l = weigh<ND>(s, top, pd);
+                const float m_page = m == -INFINITY ? m : top, m_new = fmaxf(m_run, m_page), ref = m_new == -INFINITY ? 0.0f : m_new;
+                const float keep = __builtin_amdgcn_exp2f(m_run - ref), gain = __builtin_amdgcn_exp2f(m_page - ref);
+                const float fv = ldexpf(gain * kWeightUnit<ND>, ev);
+                l_run = l_run * keep + l * gain;
+                if (__any(keep != 1.0f)) {
+#pragma unroll
+                    for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[i][j] *= keep;
+                }
+                m_run = m_new;
+#pragma unroll
+                for (int i = 0; i < 4 * DB; ++i) {
+                    if (16 * i >= dim) continue;
+                    float x[4];
+                    const v4i vfrag[1] = {vf[i]};
+                    dot_digits<ND, 1>(vfrag, pd, x);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[i][j] = fmaf(x[j], fv, o[i][j]);
+                }
+                if (more) load_v(at);
+            }
+
+            // the waves' parts
+            l_run = swap_sum(l_run);
+            if (g == 0) {
+                s_m[wave][col] = m_run;
+                s_l[wave][col] = l_run;
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * DB; ++i)
+                if (16 * i < dim)
+                    *reinterpret_cast<float4*>(s_o + (wave * kTile + col) * ROW + 16 * i + 4 * g) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+            __syncthreads();
+            // the workgroups that have pages of this tile: w_first .. w_last; all but the first have it at the start of their stretch
+            const int behind = static_cast<int>(s0 - u0) + COST + e.pages - 1;
+            const int w_first = static_cast<int>(blockIdx.x) - (ahead > 0 ? static_cast<int>((static_cast<uint32_t>(ahead) + per - 1) / per) : 0);
+            const int w_last = static_cast<int>(blockIdx.x + static_cast<uint32_t>(behind) / per);
+            const bool whole = w_first == w_last;
+            for (int i = threadIdx.x; i < rows * nd; i += THREADS) {
+                const int row = i / nd, d = i % nd * 4;
+                Share s = {-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w)
+                    join(s, s_m[w][row], s_l[w][row], *reinterpret_cast<const float4*>(s_o + (w * kTile + row) * ROW + d));
+                if (whole) {
+                    finish<TYPE>(a, e, rows_of, head, row, d, s);
+                } else {
+                    const int64_t part = (int64_t{blockIdx.x} * 2 + (static_cast<int>(blockIdx.x) == w_first)) * kTile + row;
+                    store_part(a.part_o + part * dim + d, s.x[0], s.x[1]);
+                    store_part(a.part_o + part * dim + d + 2, s.x[2], s.x[3]);
+                    if (d == 0) store_part(&a.part_ml[part].x, s.m, s.l);
+                }
+            }
+            if (!whole) {
+                // The last to arrive joins the parts.  Parts are stored past the L2 of this XCD (store_part) and loaded past that of the
+                // reader's, so it is enough that every wave's stores are there before the ticket is drawn.  Release and acquire
+                // fences instead write back and drop whole L2 caches, in every workgroup: 97 us in place of 65 for 64 requests of 200
+                // to 8000 tokens.
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    uint32_t* ticket = a.tickets + (tiles_before + tile) * heads + head;
+                    const uint32_t others = static_cast<uint32_t>(w_last - w_first);
+                    s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == others;
+                    if (s_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                }
+                __syncthreads();
+                if (s_last) {
+                    // `ways` threads share four elements of a row
+                    const int work = rows * nd, ways = max(THREADS / work, 1);
+                    for (int i0 = 0; i0 < work; i0 += THREADS) {
+                        const int i = i0 + static_cast<int>(threadIdx.x) % (work < THREADS ? work : THREADS);
+                        const int way = work < THREADS ? static_cast<int>(threadIdx.x) / work : 0;
+                        Share s = {-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+                        if (i < work && way < ways) {
+                            const int row = i / nd, d = i % nd * 4;
+#pragma unroll 4
+                            for (int w = w_first + way; w <= w_last; w += ways) {
+                                const int64_t part = (int64_t{w} * 2 + (w == w_first)) * kTile + row;
+                                const float2 ml = load_part(&a.part_ml[part].x), x = load_part(a.part_o + part * dim + d),
+                                             y = load_part(a.part_o + part * dim + d + 2);
+                                join(s, ml.x, ml.y, make_float4(x.x, x.y, y.x, y.y));
+                            }
+                        }
+                        if (ways > 1) {                                 // work < THREADS: one turn of the outer loop
+                            s_o4[threadIdx.x] = make_float4(s.x[0], s.x[1], s.x[2], s.x[3]);
+                            s_o4[THREADS + threadIdx.x] = make_float4(s.m, s.l, 0.0f, 0.0f);
+                            __syncthreads();
+                            if (way == 0)
+                                for (int w = 1; w < ways; ++w) {
+                                    const float4 ml = s_o4[THREADS + i + w * work];
+                                    join(s, ml.x, ml.y, s_o4[i + w * work]);
+                                }
+                        }
+                        if (i < work && way == 0) finish<TYPE>(a, e, rows_of, head, i / nd, i % nd * 4, s);
+                    }
+                }
+            }
+            __syncthreads();
+        }
+        // on to the next tile
+        s0 += e.pages + COST;
+        if (++head == heads) {
+            head = 0;
+            if (++tile == e.tiles) {
+                tile = 0;
+                tiles_before += e.tiles;
+                do {
+                    if (++b == a.requests) return;
+                    e = extent(a, b);
+                } while (e.tiles == 0);
+            }
+        }
     }
 }
 
 static bool attention_sizes_ok(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim) {
     constexpr int64_t kMost = int64_t{1} << 31;
     return requests > 0 && requests < kMost && tokens >= 0 && tokens < kMost && heads > 0 && heads <= 65535 && q_heads > 0 &&
-           q_heads <= 65535 && q_heads % heads == 0 && dim > 0 && dim <= 256 && dim % 16 == 0 && tokens * q_heads < kMost;
+           q_heads <= 16384 && q_heads % heads == 0 && dim > 0 && dim <= 256 && dim % 16 == 0 && tokens * q_heads < kMost;
 }
 
 // tiles of all requests, at most
@@ -413,7 +552,8 @@ static int64_t most_tiles(int64_t requests, int64_t tokens, int64_t group) { ret
 
 extern "C" size_t fxp_kv_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim) {
     if (!fxp::attention_sizes_ok(requests, tokens, q_heads, heads, dim)) return 0;
-    return static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float2));
+    return static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float2)) +
+           fxp::round_up(fxp::most_tiles(requests, tokens, q_heads / heads) * heads * sizeof(uint32_t), 256);
 }
 
 extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st, int type, const void* q, int64_t q_token, int64_t q_head,
@@ -451,21 +591,26 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.out_token = out_token;
     a.out_head = out_head;
     a.lse = lse;
-    a.part_o = static_cast<float*>(ws);
+    a.window = static_cast<int>(window < (int64_t{1} << 30) ? window : (int64_t{1} << 30));
+    // the tickets stand first: what stands behind them may hold anything
+    const int64_t tiles = most_tiles(st->requests, st->tokens, a.group);
+    if (tiles >= int64_t{1} << 24) return FXP_ERR_DIMS;
+    a.tickets = static_cast<uint32_t*>(ws);
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + round_up(tiles * cache->heads * sizeof(uint32_t), 256));
     a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<size_t>(kAttGroups) * 2 * kTile * cache->dim);
     a.group = static_cast<int>(q_heads / cache->heads);
+    a.group_inverse = static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group);
     a.vec_q = aligned(q, 16) && q_token * size % 16 == 0 && q_head * size % 16 == 0;
     a.vec_out = aligned(out, 4 * size) && out_token % 4 == 0 && out_head % 4 == 0;
     a.scale_log2 = scale * 1.44269504088896f;
-    a.window = window;
-    const int64_t tiles = most_tiles(st->requests, st->tokens, a.group);
-    if (tiles >= int64_t{1} << 24) return FXP_ERR_DIMS;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    if (tiles * cache->heads * (st->blocks + kTileCost<8>) >= int64_t{1} << 31) return FXP_ERR_DIMS;
     auto go = [&](auto type_c, auto db_c) {
         constexpr int TYPE = decltype(type_c)::value, DB = decltype(db_c)::value;
-        hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroups), dim3(kAttThreads), 0, s, a);
-        hipLaunchKernelGGL((k_kv_attend_join<TYPE>), dim3(static_cast<unsigned>(tiles), static_cast<unsigned>(cache->heads)), dim3(kAttThreads), 0,
-                           s, a, static_cast<unsigned>(kAttGroups));
+        if (SEL8)
+            hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 8>), dim3(kAttGroups / 2), dim3(512), 0, s, a);
+        else
+            hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 4>), dim3(kAttGroups), dim3(256), 0, s, a);
     };
     auto of_type = [&](auto type_c) {
         const int64_t db = (cache->dim + 63) / 64;
