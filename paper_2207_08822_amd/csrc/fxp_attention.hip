@@ -79,6 +79,9 @@ struct Stretch {
 template <int WAVES>
 __device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
     const uint32_t per = (units + gridDim.x - 1) / gridDim.x;
+#ifdef WHOLE
+    if (most_pages <= WHOLE) return max(per, static_cast<uint32_t>(most_pages + kTileCost<WAVES>));
+#endif
     const int least = static_cast<int>(0.7f * sqrtf(static_cast<float>(most_pages)));
     return max(per, static_cast<uint32_t>(max(least, WAVES)));
 }
@@ -203,10 +206,10 @@ __device__ inline int load_query(const AttArgs& a, const Extent& e, int tok, int
     return unit;
 }
 
-// Weights 2^(s - top) of 16 scores as digits, and their sum; `top` becomes the score that weighs 1 (32767 / 32639 for two digits: the
+// Weights 2^(f s - top) of 16 scores as digits, and their sum; `top` becomes the score that weighs 1 (32767 / 32639 for two digits: the
 // packing conversion multiplies by 32767, and the largest weight has to stay at 127 in each digit).
 template <int ND>
-__device__ inline float weigh(const float (&s)[16], float& top, v4i (&pd)[1][ND]) {
+__device__ inline float weigh(const float (&s)[16], float f, float& top, v4i (&pd)[1][ND]) {
     float l = 0.0f;
     if constexpr (ND == 2) {
         top += 0.00564698f;                    // log2(32767 / 32639), rounded up
@@ -215,7 +218,7 @@ __device__ inline float weigh(const float (&s)[16], float& top, v4i (&pd)[1][ND]
             float w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(s[4 * t + i] - top);
+                w[i] = __builtin_amdgcn_exp2f(fmaf(s[4 * t + i], f, -top));
                 l += w[i];
             }
             typedef short v2s __attribute__((ext_vector_type(2)));
@@ -228,7 +231,7 @@ __device__ inline float weigh(const float (&s)[16], float& top, v4i (&pd)[1][ND]
         int v[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const float w = __builtin_amdgcn_exp2f(s[i] - top);
+            const float w = __builtin_amdgcn_exp2f(fmaf(s[i], f, -top));
             l += w;
             v[i] = static_cast<int>(rintf(w * Digits<ND>::kMost));
         }
@@ -346,22 +349,22 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 dead = id < 0 || id >= a.c.pages;
                 return (int64_t{dead ? 0 : id} * heads + head);
             };
-            const int k_off = (16 * (col >> 2) + (col & 3)) * dim + 16 * g, v_off = (g * dim + col) * 16;
+            // elements behind dim: Q's digits are zero there, whatever is loaded, and outputs are not stored; loads stay in the block
+            const int k_off = (16 * (col >> 2) + (col & 3)) * dim, v_off = (g * dim + col) * 16;
+            const int k_last = 64 * (DB - 1) + 16 * g < dim ? 64 * (DB - 1) + 16 * g : 0;
             auto load_k = [&](int64_t at) {
-                const int8_t* p = a.c.kq + at * (FXP_KV_PAGE * dim) + k_off;
+                const int8_t* p = a.c.kq + at * (FXP_KV_PAGE * dim);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
-                    for (int i = 0; i < DB; ++i) {
-                        if (64 * i + 16 * g < dim) kf[t][i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 4 * t * dim + 64 * i));
-                        else kf[t][i] = v4i{0, 0, 0, 0};
-                    }
+                    for (int i = 0; i < DB; ++i)
+                        kf[t][i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 4 * t * dim + (k_off + (i < DB - 1 ? 64 * i + 16 * g : k_last))));
             };
             auto load_v = [&](int64_t at) {
-                const int8_t* p = a.c.vq + at * (FXP_KV_PAGE * dim) + v_off;
+                const int8_t* p = a.c.vq + at * (FXP_KV_PAGE * dim);
 #pragma unroll
                 for (int i = 0; i < 4 * DB; ++i)
-                    if (16 * i < dim) vf[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 256 * i));
+                    vf[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + (i < 4 * (DB - 1) ? 256 * i : min(256 * i, 16 * (dim - 16))) + v_off));
             };
 
             float o[4 * DB][4];
@@ -398,30 +401,32 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                     ev_next = a.c.ev[at];
                 }
                 const int ek = min(max(ek_now, 1), 255) - 125 - a.c.bits, ev = min(max(ev_now, 1), 255) - 125 - a.c.bits;
-                // bounded so that no product of it and a sum of up to 2^15 terms (digits x 7 bits x dim) passes 2^127: no Inf - Inf below
-                const float f = fminf(ldexpf(a.scale_log2, qe + ek), ND == 2 ? 0x1p97f : 0x1p89f);
+                // bounded so that no product of it and a sum of up to 2^15 terms (digits x 7 bits x dim) passes 2^127, and not zero: no
+                // Inf - Inf and no 0 * Inf below
+                const float f = fminf(fmaxf(ldexpf(a.scale_log2, qe + ek), 0x1p-126f), ND == 2 ? 0x1p97f : 0x1p89f);
                 float s[16];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     float x[4];
                     dot_digits<ND, DB>(kf[t], qd, x);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) s[4 * t + i] = x[i] * f;
+                    for (int i = 0; i < 4; ++i) s[4 * t + i] = x[i];
                 }
                 if (more) load_k(at);                                   // on its way while the softmax is worked out
                 const int j0 = (e.page0 + p) * FXP_KV_PAGE;
                 if (dead_now || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) {
+                    const int to = dead_now ? -1 : see_to - j0 - 16 * g, from = see_from - j0 - 16 * g;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (dead_now || j0 + 16 * g + i > see_to || j0 + 16 * g + i < see_from) s[i] = -INFINITY;
+                    for (int i = 0; i < 16; ++i) s[i] = (i > to) | (i < from) ? -INFINITY : s[i];
                 }
                 float m = s[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-                m = swap_max(m);
-                float top = m == -INFINITY ? 0.0f : m;
+                m = swap_max(m) * f;
+                // a little above the largest score: f s - top rounds once, and must not come out above 0
+                float top = m == -INFINITY ? 0.0f : fmaf(fabsf(m), 0x1p-22f, m);
                 v4i pd[1][ND];
-                const float l = weigh<ND>(s, top, pd);
+                const float l = weigh<ND>(s, f, top, pd);
                 const float m_page = m == -INFINITY ? m : top, m_new = fmaxf(m_run, m_page), ref = m_new == -INFINITY ? 0.0f : m_new;
                 const float keep = __builtin_amdgcn_exp2f(m_run - ref), gain = __builtin_amdgcn_exp2f(m_page - ref);
                 const float fv = ldexpf(gain * kWeightUnit<ND>, ev);
@@ -435,7 +440,6 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 m_run = m_new;
 #pragma unroll
                 for (int i = 0; i < 4 * DB; ++i) {
-                    if (16 * i >= dim) continue;
                     float x[4];
                     const v4i vfrag[1] = {vf[i]};
                     dot_digits<ND, 1>(vfrag, pd, x);
@@ -453,8 +457,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
             }
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i)
-                if (16 * i < dim)
-                    *reinterpret_cast<float4*>(s_o + (wave * kTile + col) * ROW + 16 * i + 4 * g) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+                *reinterpret_cast<float4*>(s_o + (wave * kTile + col) * ROW + 16 * i + 4 * g) = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
             __syncthreads();
             // the workgroups that have pages of this tile: w_first .. w_last; all but the first have it at the start of their stretch
             const int behind = static_cast<int>(s0 - u0) + COST + e.pages - 1;
@@ -463,10 +466,20 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
             const bool whole = w_first == w_last;
             for (int i = threadIdx.x; i < rows * nd; i += THREADS) {
                 const int row = i / nd, d = i % nd * 4;
-                Share s = {-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+                Share s = {s_m[0][row], 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w)
-                    join(s, s_m[w][row], s_l[w][row], *reinterpret_cast<const float4*>(s_o + (w * kTile + row) * ROW + d));
+                for (int w = 1; w < WAVES; ++w) s.m = fmaxf(s.m, s_m[w][row]);
+                const float ref = s.m == -INFINITY ? 0.0f : s.m;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(s_m[w][row] - ref);
+                    const float4 y = *reinterpret_cast<const float4*>(s_o + (w * kTile + row) * ROW + d);
+                    s.l = fmaf(s_l[w][row], f, s.l);
+                    s.x[0] = fmaf(y.x, f, s.x[0]);
+                    s.x[1] = fmaf(y.y, f, s.x[1]);
+                    s.x[2] = fmaf(y.z, f, s.x[2]);
+                    s.x[3] = fmaf(y.w, f, s.x[3]);
+                }
                 if (whole) {
                     finish<TYPE>(a, e, rows_of, head, row, d, s);
                 } else {

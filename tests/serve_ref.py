@@ -91,7 +91,8 @@ def attention(q, k, v, first, lens, table, scale, window, unit_bits, half_step):
     of its row's largest element (one more where that is within 2^-7 of the next binade), so a score is off by at most scale * u/2 * sum|k|, and by
     a few fp32 roundings of a value of its size; a weight w_j = exp(s_j) then by a factor within exp(+-d).  The weights of a page are rounded to
     half a unit of 1/32639 (1/8355711) of the page's largest weight.  fp32 sums of a page's products and of the pages add roundings of 2^-24 each,
-    counted once per page and then some.  The output is rounded once, by half a step."""
+    counted once per page and then some.  A weight below 2^-126 of the largest is no normal fp32 number: 2^-126 |v| each may be lost (a token
+    that weighs 1e-44 gives 0, not 1e-44 v).  The output is rounded once, by half a step."""
     T, QH, D = q.shape
     H = k.shape[1]
     G, most = QH // H, 32639 if unit_bits == 15 else 8355711
@@ -122,7 +123,7 @@ def attention(q, k, v, first, lens, table, scale, window, unit_bits, half_step):
                 mass = w @ np.abs(vv) / l
                 tops = np.array([w[p * PAGE:(p + 1) * PAGE].max() for p in range(len(pages))])
                 rounded = sum(tops[p] * np.abs(vv[p * PAGE:(p + 1) * PAGE][w[p * PAGE:(p + 1) * PAGE] > 0]).sum(0) for p in range(len(pages))) * 0.5 / most / l
-                inner = (math.expm1(2 * d) + 2.0 ** -24 * (2 * len(pages) + 80)) * mass + rounded * math.exp(2 * d)
+                inner = (math.expm1(2 * d) + 2.0 ** -24 * (2 * len(pages) + 80)) * mass + rounded * math.exp(2 * d) + 2.0 ** -126 * np.abs(vv).sum(0)
                 off[t, h] = half_step * (np.abs(out[t, h]) + inner) + inner
     return out, lse, off
 

@@ -122,6 +122,15 @@ def test_attention_with_a_token_that_outweighs_thousands(fxp, kind):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("sharp", [30.0, 1000.0])
+def test_attention_with_large_scores(fxp, kind, sharp):
+    """Scores in the hundreds and tens of thousands: their fp32 roundings must not lift a weight above the largest digit."""
+    say("kv_attention, large scores", kind, sharp)
+    c = Case(fxp, [900, 64], [2, 1], 8, 4, 64, kind, sharp=sharp)
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
 def test_attention_is_the_value_where_all_values_are_one(fxp, kind):
     """Weights rounded to half a unit of 1/32639 of the page's largest: 64 of them are off by 64 * 0.5 / 32639 of it at most."""
     say("kv_attention over constant values", kind)
