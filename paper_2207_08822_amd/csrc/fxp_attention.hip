@@ -16,12 +16,10 @@
 // relative to the page's own largest, so a long tail of small weights behind one large one keeps its sum.  fp32 has 23 bits.
 #include "fxp_serve_device.h"
 
-#ifndef SEL8
-#define SEL8 0
-#endif
 namespace fxp {
 
 constexpr int kTile = 16;
+constexpr int kFewRows = 2 * kTile;
 constexpr int kAttGroups = 512;          // workgroups at most: two a CU
 
 struct AttArgs {
@@ -43,6 +41,7 @@ struct AttArgs {
     int vec_q, vec_out;
     float scale_log2;       // scale * log2(e)
     int window;             // 0: none
+    int few_rows;           // requests of more rows are the other kernel's; 0: one kernel has all
 };
 
 struct Extent {
@@ -55,6 +54,7 @@ __device__ inline Extent extent(const AttArgs& a, int64_t b) {
     e.n = max(min(max(a.first[b + 1], 0), most) - e.tok0, 0);
     e.len = static_cast<int>(min(static_cast<int64_t>(max(a.lens[b], 0)), a.blocks * FXP_KV_PAGE));
     e.tiles = (e.n * a.group + kTile - 1) / kTile;
+    if (a.few_rows > 0 && e.n * a.group > a.few_rows) e.tiles = 0;
     const int from = a.window > 0 ? max(e.len - e.n + 1 - a.window, 0) : 0;
     e.page0 = from / FXP_KV_PAGE;
     e.pages = max((e.len + FXP_KV_PAGE - 1) / FXP_KV_PAGE - e.page0, 1);       // an empty request still has its zeros to write
@@ -79,9 +79,6 @@ struct Stretch {
 template <int WAVES>
 __device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
     const uint32_t per = (units + gridDim.x - 1) / gridDim.x;
-#ifdef WHOLE
-    if (most_pages <= WHOLE) return max(per, static_cast<uint32_t>(most_pages + kTileCost<WAVES>));
-#endif
     const int least = static_cast<int>(0.7f * sqrtf(static_cast<float>(most_pages)));
     return max(per, static_cast<uint32_t>(max(least, WAVES)));
 }
@@ -145,26 +142,31 @@ __device__ inline Stretch survey(const AttArgs& a) {
     return st;
 }
 
-// sum of products of digits, as a float: acc = d1 * 256 + d0 fits 32 bits over 256 terms; a third digit is added in fp32
-template <int ND, int N>
-__device__ inline void dot_digits(const v4i (&a)[N], const v4i (&b)[N][ND], float (&out)[4]) {
-    v4i acc = {0, 0, 0, 0};
+// T tiles of sums of products of digits, as floats: acc = d1 * 256 + d0 fits 32 bits over 256 terms, a third digit is added in fp32.
+// The tiles go through each stage together: a matrix instruction's result can be used some 10 instructions later, and one tile after
+// the other (what the compiler makes of a loop over tiles) waits for each.
+template <int ND, int N, int T>
+__device__ inline void dot_digits(const v4i (&a)[T][N], const v4i (&b)[N][ND], float (&out)[T][4]) {
+    v4i acc[ND][T];
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc = mfma_i8(a[i], b[i][0], acc);
+    for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[j] <<= 8;
+        for (int t = 0; t < T; ++t) acc[d][t] = mfma_i8(a[t][0], b[0][d], v4i{0, 0, 0, 0});
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc = mfma_i8(a[i], b[i][1], acc);
-    if constexpr (ND == 3) {
-        v4i low = {0, 0, 0, 0};
+    for (int i = 1; i < N; ++i)
 #pragma unroll
-        for (int i = 0; i < N; ++i) low = mfma_i8(a[i], b[i][2], low);
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) out[j] = fmaf(static_cast<float>(acc[j]), 256.0f, static_cast<float>(low[j]));
-    } else {
+            for (int t = 0; t < T; ++t) acc[d][t] = mfma_i8(a[t][i], b[i][d], acc[d][t]);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) out[j] = static_cast<float>(acc[j]);
-    }
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float top = static_cast<float>((acc[0][t][j] << 8) + acc[1][t][j]);
+            if constexpr (ND == 3) out[t][j] = fmaf(top, 256.0f, static_cast<float>(acc[2][t][j]));
+            else out[t][j] = top;
+        }
 }
 
 __device__ inline float swap_max(float v) {                  // over the four lanes that hold a row
@@ -242,6 +244,45 @@ __device__ inline float weigh(const float (&s)[16], float f, float& top, v4i (&p
 template <int ND>
 constexpr float kWeightUnit = ND == 2 ? 1.0f / 32767 : 1.0f / 8355711;
 
+// The score that a row's sums are relative to: the first page's largest, and a new one where a page's is 8 (in log2) above it.  Sums
+// grow by 2^8 at most in between, which fp32 has room for, and rescaling the outputs (a fifth of a page's vector work) is rare;
+// a running maximum rises for some row of a tile on most pages.
+struct Turn {
+    float ref, keep, gain;
+};
+__device__ inline Turn next_reference(float ref, float page) {
+    const float next = page > ref + 8.0f ? page : ref, r = next == -INFINITY ? 0.0f : next;     // -Inf + 8 = -Inf: the first page takes it
+    return {next, __builtin_amdgcn_exp2f(ref - r), __builtin_amdgcn_exp2f(page - r)};
+}
+
+// What a sum of products of digits is multiplied with (2^`unit` is that of the sum).  Bounded so that no product of it and a sum (2^15 or 2^23,
+// 7 bits, up to 256 terms) passes 2^127, and not zero: no Inf - Inf and no 0 * Inf in the softmax.
+template <int ND>
+__device__ inline float score_unit(const AttArgs& a, int unit) {
+    return fminf(fmaxf(ldexpf(a.scale_log2, unit), 0x1p-126f), ND == 2 ? 0x1p97f : 0x1p89f);
+}
+// scores of places that this lane's row does not see: those behind `to` and before `from`, or all
+__device__ inline void hide(float (&s)[16], bool all, int to, int from) {
+    const int last = all ? -1 : to;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = ((i > last) | (i < from)) ? -INFINITY : s[i];
+}
+// One page of a row: the weights of this lane's 16 scores f * s as digits, the row's reference and sum (of this lane's tokens) moved on.
+template <int ND>
+__device__ inline Turn softmax_page(const float (&s)[16], float f, float& ref, float& l, v4i (&pd)[1][ND]) {
+    float m = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
+    m = swap_max(m) * f;
+    // a little above the largest score: f s - top rounds once, and must not come out above 0
+    float top = m == -INFINITY ? 0.0f : fmaf(fabsf(m), 0x1p-22f, m);
+    const float sum = weigh<ND>(s, f, top, pd);
+    const Turn turn = next_reference(ref, m == -INFINITY ? m : top);
+    l = l * turn.keep + sum * turn.gain;
+    ref = turn.ref;
+    return turn;
+}
+
 // Rows of a tile: row i is token tok + (rest + i) / group of the request, head (rest + i) % group of its group.
 struct TileRows {
     int tok, rest;
@@ -300,7 +341,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
     __shared__ float4 s_o4[WAVES * kTile * ROW / 4];
     __shared__ int s_last;
     float* const s_o = reinterpret_cast<float*>(s_o4);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), nd = dim / 4;
     const Stretch st = survey<WAVES>(a);
     const uint32_t per = st.per, u0 = st.u0, u1 = min(u0 + per, st.units);
@@ -341,6 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
             };
             load_ids(p0 + wave);
 
+            constexpr bool kAhead = DB * ND <= 4;                       // values too are loaded a page ahead, where there are registers for it
             v4i kf[4][DB], vf[4 * DB];
             int ek_now = 0, ev_now = 0, ek_next = 0, ev_next = 0;
             bool dead_now = true, dead_next = true;
@@ -350,18 +392,20 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 return (int64_t{dead ? 0 : id} * heads + head);
             };
             // elements behind dim: Q's digits are zero there, whatever is loaded, and outputs are not stored; loads stay in the block
-            const int k_off = (16 * (col >> 2) + (col & 3)) * dim, v_off = (g * dim + col) * 16;
-            const int k_last = 64 * (DB - 1) + 16 * g < dim ? 64 * (DB - 1) + 16 * g : 0;
+            // (a block's address is uniform and the lane's offsets are unsigned: loads then take a scalar base)
+            const uint32_t k_row = static_cast<uint32_t>((16 * (col >> 2) + (col & 3)) * dim), k_off = k_row + 16u * g;
+            const uint32_t k_last = 64 * (DB - 1) + 16 * g < dim ? k_row + 64u * (DB - 1) + 16u * g : k_row, v_off = static_cast<uint32_t>((g * dim + col) * 16);
             auto load_k = [&](int64_t at) {
-                const int8_t* p = a.c.kq + at * (FXP_KV_PAGE * dim);
+                const int8_t* const p = a.c.kq + at * (FXP_KV_PAGE * dim);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int i = 0; i < DB; ++i)
-                        kf[t][i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + 4 * t * dim + (k_off + (i < DB - 1 ? 64 * i + 16 * g : k_last))));
+                        kf[t][i] = __builtin_nontemporal_load(
+                            reinterpret_cast<const v4i*>(p + 4 * t * dim + (i < DB - 1 ? 64 * i : 0) + (i < DB - 1 ? k_off : k_last)));
             };
             auto load_v = [&](int64_t at) {
-                const int8_t* p = a.c.vq + at * (FXP_KV_PAGE * dim);
+                const int8_t* const p = a.c.vq + at * (FXP_KV_PAGE * dim);
 #pragma unroll
                 for (int i = 0; i < 4 * DB; ++i)
                     vf[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(p + (i < 4 * (DB - 1) ? 256 * i : min(256 * i, 16 * (dim - 16))) + v_off));
@@ -381,7 +425,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 ek_next = a.c.ek[at];
                 ev_next = a.c.ev[at];
                 load_k(at);
-                load_v(at);
+                if (kAhead) load_v(at);
             }
             v4i qd[DB][ND];
             const int qe = load_query<TYPE, DB, ND>(a, e, tok, qh, row_ok, g, qd);
@@ -391,6 +435,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 ev_now = ev_next;
                 dead_now = dead_next;
                 const bool more = p + WAVES < p1;
+                if (!kAhead) load_v(at);
                 if (more) {
                     if (++index == 64) {
                         index = 0;
@@ -401,52 +446,34 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                     ev_next = a.c.ev[at];
                 }
                 const int ek = min(max(ek_now, 1), 255) - 125 - a.c.bits, ev = min(max(ev_now, 1), 255) - 125 - a.c.bits;
-                // bounded so that no product of it and a sum of up to 2^15 terms (digits x 7 bits x dim) passes 2^127, and not zero: no
-                // Inf - Inf and no 0 * Inf below
-                const float f = fminf(fmaxf(ldexpf(a.scale_log2, qe + ek), 0x1p-126f), ND == 2 ? 0x1p97f : 0x1p89f);
+                float s4[4][4];
+                dot_digits<ND, DB, 4>(kf, qd, s4);
                 float s[16];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    float x[4];
-                    dot_digits<ND, DB>(kf[t], qd, x);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s[4 * t + i] = x[i];
-                }
+                for (int i = 0; i < 16; ++i) s[i] = s4[i / 4][i % 4];
                 if (more) load_k(at);                                   // on its way while the softmax is worked out
                 const int j0 = (e.page0 + p) * FXP_KV_PAGE;
-                if (dead_now || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) {
-                    const int to = dead_now ? -1 : see_to - j0 - 16 * g, from = see_from - j0 - 16 * g;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = (i > to) | (i < from) ? -INFINITY : s[i];
-                }
-                float m = s[0];
-#pragma unroll
-                for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
-                m = swap_max(m) * f;
-                // a little above the largest score: f s - top rounds once, and must not come out above 0
-                float top = m == -INFINITY ? 0.0f : fmaf(fabsf(m), 0x1p-22f, m);
+                if (dead_now || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) hide(s, dead_now, see_to - j0 - 16 * g, see_from - j0 - 16 * g);
                 v4i pd[1][ND];
-                const float l = weigh<ND>(s, f, top, pd);
-                const float m_page = m == -INFINITY ? m : top, m_new = fmaxf(m_run, m_page), ref = m_new == -INFINITY ? 0.0f : m_new;
-                const float keep = __builtin_amdgcn_exp2f(m_run - ref), gain = __builtin_amdgcn_exp2f(m_page - ref);
-                const float fv = ldexpf(gain * kWeightUnit<ND>, ev);
-                l_run = l_run * keep + l * gain;
-                if (__any(keep != 1.0f)) {
+                const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd);
+                const float fv = ldexpf(turn.gain * kWeightUnit<ND>, ev);
+                if (__any(turn.keep != 1.0f)) {
 #pragma unroll
                     for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) o[i][j] *= keep;
+                        for (int j = 0; j < 4; ++j) o[i][j] *= turn.keep;
                 }
-                m_run = m_new;
 #pragma unroll
-                for (int i = 0; i < 4 * DB; ++i) {
-                    float x[4];
-                    const v4i vfrag[1] = {vf[i]};
-                    dot_digits<ND, 1>(vfrag, pd, x);
+                for (int i = 0; i < 4 * DB; i += 4) {
+                    float x[4][4];
+                    const v4i four[4][1] = {{vf[i]}, {vf[i + 1]}, {vf[i + 2]}, {vf[i + 3]}};
+                    dot_digits<ND, 1, 4>(four, pd, x);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) o[i][j] = fmaf(x[j], fv, o[i][j]);
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) o[i + t][j] = fmaf(x[t][j], fv, o[i + t][j]);
                 }
-                if (more) load_v(at);
+                if (kAhead && more) load_v(at);
             }
 
             // the waves' parts
@@ -552,6 +579,180 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
     }
 }
 
+// ---- many rows of one request (prompts) ----
+//
+// A workgroup has 64 consecutive rows of one request and head, each of its four waves a tile of 16.  The waves share the pages:
+// each page goes through LDS once (two buffers, the next page's loads in registers meanwhile).  Per page a wave issues 16 DB
+// matrix instructions of 16 cycles (two digits) and, at DB = 2, some 270 vector instructions of 4; they follow one another rather than
+// overlap (1650 cycles a page and SIMD measured, 1140 + 512), which is what bounds it.  32 rows a wave, which halves the LDS
+// reads, took 303 us in place of 249 for 4600 tokens behind up to 7000 (16 heads over 4 of 128): fewer, longer workgroups.
+// In LDS the keys stand by pieces of 16 elements, [dim / 16][64 places][16], the places in the order that the A operand takes
+// them, turned by twice the piece's number: 16 lanes then read 256 consecutive bytes, and the 16 pieces that 16
+// lanes write (8 of a token, two tokens) fall on 16 different ones.
+constexpr int kRowWaves = 4;
+
+template <int TYPE, int DB>
+__global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_rows(AttArgs a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, PAGE_BYTES = 64 * 64 * DB, THREADS = 64 * kRowWaves;
+    __shared__ v4i lds[2][2][PAGE_BYTES / 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
+    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), head = blockIdx.x;
+    constexpr int ROWS = kRowWaves * kTile;
+
+    // the request and the block of its rows; the last blocks come first, because they see the most pages
+    const int want = static_cast<int>(gridDim.y - 1 - blockIdx.y);
+    int b = -1, block = 0;
+    Extent e = {};
+    {
+        int carry = 0;
+        for (int base = 0; base < a.requests; base += 64) {
+            Extent x_e = {};
+            if (base + lane < a.requests) x_e = extent(a, base + lane);
+            const int v = x_e.n * a.group > a.few_rows ? (x_e.n * a.group + ROWS - 1) / ROWS : 0;
+            const int sum = static_cast<int>(wave_scan(static_cast<uint32_t>(v))), x = carry + sum - v;
+            const uint64_t hit = __builtin_amdgcn_ballot_w64(want >= x && want < x + v);
+            if (hit) {
+                const int w = __builtin_ctzll(hit);
+                b = base + w;
+                block = want - lane_of(x, w);
+                e = {lane_of(x_e.n, w), lane_of(x_e.len, w), lane_of(x_e.tiles, w), lane_of(x_e.page0, w), lane_of(x_e.pages, w), lane_of(x_e.tok0, w)};
+                break;
+            }
+            carry += lane_of(sum, 63);
+        }
+    }
+    if (b < 0) return;
+
+    // this lane's rows
+    int tok, in_group;
+    const TileRows wave_of = tile_rows(a, block * kRowWaves + wave);
+    wave_of.at(a, col, tok, in_group);
+    const bool row_ok = tok < e.n;
+    const int shift = e.len - e.n, place = shift + tok;
+    const int see_to = row_ok ? min(place, e.len - 1) : -1;
+    const int see_from = a.window > 0 ? max(place - a.window + 1, 0) : 0;
+    v4i qd[DB][ND];
+    const int qe = load_query<TYPE, DB, ND>(a, e, tok, head * a.group + in_group, row_ok, g, qd);
+    // pages that any row of the workgroup sees, places that every and any row of the wave does
+    const TileRows first_of = tile_rows(a, block * kRowWaves);
+    int last_tok, wave_last, unused;
+    first_of.at(a, ROWS - 1, last_tok, unused);
+    wave_of.at(a, kTile - 1, wave_last, unused);
+    last_tok = min(last_tok, e.n - 1);
+    wave_last = min(wave_last, e.n - 1);
+    const int p_end = min((max(shift + last_tok + 1, 0) + FXP_KV_PAGE - 1) / FXP_KV_PAGE, (e.len + FXP_KV_PAGE - 1) / FXP_KV_PAGE);
+    const int p_begin = a.window > 0 ? max(shift + first_of.tok - a.window + 1, 0) / FXP_KV_PAGE : 0;
+    const int all_to = shift + wave_of.tok, any_to = shift + wave_last;
+    const int all_from = a.window > 0 ? max(shift + wave_last - a.window + 1, 0) : 0;
+
+    // pieces of 16 bytes that this thread brings in, and where the keys among them go
+    const int pieces = 4 * dim, per_row = dim / 16;
+    int k_to[DB];
+#pragma unroll
+    for (int j = 0; j < DB; ++j) {
+        const int piece = threadIdx.x + THREADS * j, token = piece / per_row, c = piece - token * per_row;
+        k_to[j] = c * 64 + ((((token >> 2) & 3) * 16 + (token >> 4) * 4 + (token & 3)) ^ ((2 * c) & 15));
+    }
+    v4i kin[DB], vin[DB];
+    const int32_t* const table = a.table + int64_t{b} * a.blocks;
+    int ek_next = 0, ev_next = 0;
+    bool dead_next = true;
+    int id_next = p_begin < p_end ? table[p_begin] : -1;          // of the page that is fetched next
+    auto fetch = [&](int p) {
+        const int id = __builtin_amdgcn_readfirstlane(id_next);
+        id_next = table[min(p + 1, p_end - 1)];
+        dead_next = id < 0 || id >= a.c.pages;
+        const int64_t at = int64_t{dead_next ? 0 : id} * heads + head;
+        ek_next = a.c.ek[at];
+        ev_next = a.c.ev[at];
+        const v4i* const kp = reinterpret_cast<const v4i*>(a.c.kq + at * (FXP_KV_PAGE * dim));
+        const v4i* const vp = reinterpret_cast<const v4i*>(a.c.vq + at * (FXP_KV_PAGE * dim));
+#pragma unroll
+        for (int j = 0; j < DB; ++j) {
+            const int piece = min(static_cast<int>(threadIdx.x) + THREADS * j, pieces - 1);
+            kin[j] = kp[piece];
+            vin[j] = vp[piece];
+        }
+    };
+    auto put = [&](int buffer) {
+#pragma unroll
+        for (int j = 0; j < DB; ++j) {
+            const int piece = threadIdx.x + THREADS * j;
+            if (piece < pieces) {
+                lds[buffer][0][k_to[j]] = kin[j];
+                lds[buffer][1][piece] = vin[j];
+            }
+        }
+    };
+
+    float o[4 * DB][4], m_run = -INFINITY, l_run = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = 0.0f;
+    if (p_begin < p_end) {
+        fetch(p_begin);
+        put(0);
+    }
+    __syncthreads();
+    int buffer = 0;
+    for (int p = p_begin; p < p_end; ++p, buffer ^= 1) {
+        const bool dead = dead_next;
+        const int ek = min(max(ek_next, 1), 255) - 125 - a.c.bits, ev = min(max(ev_next, 1), 255) - 125 - a.c.bits;
+        if (p + 1 < p_end) fetch(p + 1);
+        const int j0 = p * FXP_KV_PAGE;
+        if (j0 <= any_to && j0 + FXP_KV_PAGE - 1 >= (a.window > 0 ? shift + wave_of.tok - a.window + 1 : 0)) {
+            const v4i* const kl = lds[buffer][0];
+            const v4i* const vl = lds[buffer][1];
+            v4i kf[4][DB];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < DB; ++i) kf[t][i] = kl[(4 * i + g) * 64 + ((16 * t + col) ^ ((2 * (4 * i + g)) & 15))];
+            float s4[4][4], s[16];
+            dot_digits<ND, DB, 4>(kf, qd, s4);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = s4[i / 4][i % 4];
+            if (dead || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) hide(s, dead, see_to - j0 - 16 * g, see_from - j0 - 16 * g);
+            v4i pd[1][ND];
+            const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd);
+            const float fv = ldexpf(turn.gain * kWeightUnit<ND>, ev);
+            if (__any(turn.keep != 1.0f)) {
+#pragma unroll
+                for (int i = 0; i < 4 * DB; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[i][j] *= turn.keep;
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * DB; i += 4) {
+                const v4i* const vt = vl + g * dim + 16 * i + col;
+                const v4i vf[4][1] = {{vt[0]}, {vt[16]}, {vt[32]}, {vt[48]}};
+                float x[4][4];
+                dot_digits<ND, 1, 4>(vf, pd, x);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[i + t][j] = fmaf(x[t][j], fv, o[i + t][j]);
+            }
+        }
+        if (p + 1 < p_end) put(buffer ^ 1);
+        __syncthreads();
+    }
+    const float l = swap_sum(l_run), inv = l > 0.0f ? 1.0f / l : 0.0f;
+    if (!row_ok) return;
+    const int64_t t = int64_t{e.tok0} + tok;
+    const int h = head * a.group + in_group;
+#pragma unroll
+    for (int i = 0; i < 4 * DB; ++i) {
+        if (16 * i >= dim) continue;
+        float x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = o[i][j] * inv;
+        store4<TYPE>(a.out, t * a.out_token + h * a.out_head + 16 * i + 4 * g, a.vec_out, x);
+    }
+    if (a.lse && g == 0) a.lse[t * (heads * a.group) + h] = l > 0.0f ? (m_run + log2f(l)) * 0.693147180559945f : -INFINITY;
+}
+
 static bool attention_sizes_ok(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim) {
     constexpr int64_t kMost = int64_t{1} << 31;
     return requests > 0 && requests < kMost && tokens >= 0 && tokens < kMost && heads > 0 && heads <= 65535 && q_heads > 0 &&
@@ -617,13 +818,21 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.vec_out = aligned(out, 4 * size) && out_token % 4 == 0 && out_head % 4 == 0;
     a.scale_log2 = scale * 1.44269504088896f;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (tiles * cache->heads * (st->blocks + kTileCost<8>) >= int64_t{1} << 31) return FXP_ERR_DIMS;
+    if (tiles * cache->heads * (st->blocks + kTileCost<4>) >= int64_t{1} << 31) return FXP_ERR_DIMS;
     auto go = [&](auto type_c, auto db_c) {
         constexpr int TYPE = decltype(type_c)::value, DB = decltype(db_c)::value;
-        if (SEL8)
-            hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 8>), dim3(kAttGroups / 2), dim3(512), 0, s, a);
-        else
-            hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 4>), dim3(kAttGroups), dim3(256), 0, s, a);
+        // Many rows a request, and enough blocks of 64 for every CU: the kernel that shares pages among rows (16 heads, 4 of the cache,
+        // 128 elements, one request: 1024 rows of 0 earlier tokens 12 us against 13 of the other kernel, 2048 18 / 24, 8192 68 / 219).  It has no
+        // way to split a context: with half as many blocks as CUs, 1024 rows behind 4000 tokens take 92 us against 53.  Requests of up to two
+        // tiles stay with the other kernel (32 rows: 24 us against 30; 35 rows, three tiles: 36 / 28).
+        constexpr int kRows = kRowWaves * kTile;
+        const int64_t row_blocks = (st->tokens * a.group + (kRows - 1) * st->requests) / kRows;
+        const bool many = st->tokens * a.group > kFewRows * st->requests && row_blocks * cache->heads >= 256 && row_blocks <= 65535;
+        a.few_rows = many && st->requests > 1 ? kFewRows : 0;
+        if (many)
+            hipLaunchKernelGGL((k_kv_attend_rows<TYPE, DB>), dim3(static_cast<unsigned>(cache->heads), static_cast<unsigned>(row_blocks)),
+                               dim3(64 * kRowWaves), 0, s, a);
+        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 4>), dim3(kAttGroups), dim3(256), 0, s, a);
     };
     auto of_type = [&](auto type_c) {
         const int64_t db = (cache->dim + 63) / 64;

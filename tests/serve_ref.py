@@ -101,30 +101,31 @@ def attention(q, k, v, first, lens, table, scale, window, unit_bits, half_step):
         n, L = int(first[b + 1] - first[b]), int(lens[b])
         pages = table[b, :-(-L // PAGE)]
         ok = (pages >= 0) & (pages < len(k))
-        seen = np.repeat(ok, PAGE)[:L]
+        if n == 0 or L == 0:
+            continue
+        rows, j = slice(int(first[b]), int(first[b]) + n), np.arange(L)
+        place = (L - n + np.arange(n))[:, None]
+        m = np.repeat(ok, PAGE)[:L] & (j <= place) & ((j > place - window) if window else True)
+        some = m.any(1)
         for h in range(QH):
-            kk = np.concatenate([k[p if o else 0, h // G] for p, o in zip(pages, ok)] + [np.zeros((0, D))])[:L]
-            vv = np.concatenate([v[p if o else 0, h // G] for p, o in zip(pages, ok)] + [np.zeros((0, D))])[:L]
-            for i in range(n):
-                t, place = int(first[b]) + i, L - n + i
-                j = np.arange(L)
-                m = seen & (j <= place) & ((j > place - window) if window else True)
-                if not m.any():
-                    continue
-                x = q[t, h]
-                s = scale * (kk @ x)
-                w = np.where(m, np.exp(s - s[m].max()), 0.0)
-                l = w.sum()
-                out[t, h] = w @ vv / l
-                lse[t, h] = s[m].max() + math.log(l)
-                top = float(np.max(np.abs(x)))
-                u = 2.0 ** (exponent(np.array([top * (1 + 2.0 ** -6)])) - 126 - unit_bits)
-                d = float(np.max(np.where(m, scale * u / 2 * np.abs(kk).sum(1) + 8 * 2.0 ** -24 * (np.abs(s) + scale * np.abs(kk) @ np.abs(x) + 1), 0.0)))
-                mass = w @ np.abs(vv) / l
-                tops = np.array([w[p * PAGE:(p + 1) * PAGE].max() for p in range(len(pages))])
-                rounded = sum(tops[p] * np.abs(vv[p * PAGE:(p + 1) * PAGE][w[p * PAGE:(p + 1) * PAGE] > 0]).sum(0) for p in range(len(pages))) * 0.5 / most / l
-                inner = (math.expm1(2 * d) + 2.0 ** -24 * (2 * len(pages) + 80)) * mass + rounded * math.exp(2 * d) + 2.0 ** -126 * np.abs(vv).sum(0)
-                off[t, h] = half_step * (np.abs(out[t, h]) + inner) + inner
+            kk, vv = (np.concatenate([x[p if o else 0, h // G] for p, o in zip(pages, ok)])[:L] for x in (k, v))
+            x = q[rows, h]
+            s = scale * (x @ kk.T)
+            top_s = np.where(some, np.where(m, s, -np.inf).max(1), 0.0)[:, None]
+            w = np.where(m, np.exp(np.minimum(s - top_s, 0.0)), 0.0)
+            l = np.where(some, w.sum(1), 1.0)[:, None]
+            o = w @ vv / l
+            out[rows, h] = np.where(some[:, None], o, 0.0)
+            lse[rows, h] = np.where(some, top_s[:, 0] + np.log(l[:, 0]), -np.inf)
+            u = np.array([2.0 ** (exponent(r * (1 + 2.0 ** -6)) - 126 - unit_bits) for r in x])[:, None]
+            d = np.where(m, scale * u / 2 * np.abs(kk).sum(1) + 8 * 2.0 ** -24 * (np.abs(s) + scale * np.abs(x) @ np.abs(kk).T + 1), 0.0).max(1)[:, None]
+            mass = w @ np.abs(vv) / l
+            rounded = np.zeros_like(o)
+            for p in range(0, L, PAGE):
+                part = w[:, p:p + PAGE]
+                rounded += part.max(1, keepdims=True) * ((part > 0) @ np.abs(vv[p:p + PAGE])) * 0.5 / most / l
+            inner = (np.expm1(2 * d) + 2.0 ** -24 * (2 * len(pages) + 80)) * mass + rounded * np.exp(2 * d) + 2.0 ** -126 * np.abs(vv).sum(0)
+            off[rows, h] = np.where(some[:, None], half_step * (np.abs(o) + inner) + inner, 0.0)
     return out, lse, off
 
 

@@ -106,6 +106,22 @@ def test_attention(fxp, lens, news, QH, H, D, kind, window):
     assert (out[c.first[-1]:] == 9).all() and (lse[c.first[-1]:] == 9).all()      # rows behind the last request
 
 
+# requests whose rows fill 256 blocks of 64 together (heads x blocks): the kernel for many rows, short requests among them
+MANY = [([520, 3, 200, 0, 64], [300, 1, 200, 0, 40], 28, 14, 64), ([257], [257], 64, 16, 16), ([90, 700, 33], [80, 301, 33], 32, 32, 80),
+        ([300, 140], [150, 140], 48, 48, 128), ([130, 70], [65, 70], 130, 65, 192), ([150], [100], 128, 128, 256), ([10, 400], [100, 130], 66, 66, 112)]
+
+
+@pytest.mark.parametrize("lens,news,QH,H,D", MANY)
+@pytest.mark.parametrize("kind,window,bits", [("fp32", 0, 8), ("bf16", 90, 8), ("fp16", 0, 5)])
+def test_attention_of_prompts(fxp, lens, news, QH, H, D, kind, window, bits):
+    say("kv_attention of many rows", (lens, news, QH, H, D, kind, window, bits))
+    c = Case(fxp, lens, news, QH, H, D, kind, bits=bits, behind=3, missing=[(0, 1, -1)] if len(lens) > 2 else ())
+    out, lse = torch.full((c.T, QH, D), 9.0, dtype=c.dq.dtype, device="cuda"), torch.full((c.T, QH), 9.0, device="cuda")
+    fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, window=window, out=out, lse=lse)
+    c.check(out, lse, window)
+    assert (out[c.first[-1]:] == 9).all() and (lse[c.first[-1]:] == 9).all()
+
+
 @pytest.mark.parametrize("bits", [2, 4, 7])
 def test_attention_over_other_widths(fxp, bits):
     say("kv_attention, bits", bits)
