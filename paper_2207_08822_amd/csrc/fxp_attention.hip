@@ -198,13 +198,9 @@ __device__ inline int load_query(const AttArgs& a, const Extent& e, int tok, int
     m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16)));
     m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32)));
     const int unit = unit_of<ND>(m);
+    const bool finite = !__any(m >= 0x7f800000u);
 #pragma unroll
-    for (int i = 0; i < DB; ++i) {
-        int v[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[i][j], unit);
-        digits16<ND>(v, qd[i]);
-    }
+    for (int i = 0; i < DB; ++i) row_digits<ND>(x[i], unit, finite, qd[i]);
     return unit;
 }
 

@@ -129,6 +129,32 @@ template <int ND>
 __device__ inline int fixed_point(float x, int unit) {
     return min(max(static_cast<int>(rintf(ldexpf(x, -unit))), -Digits<ND>::kMost), Digits<ND>::kMost);
 }
+// Digits of 16 floats in units of 2^unit; `finite`: no Inf or NaN among the wave's.  Two digits: adding 1.5 * 2^23 rounds to a whole
+// number (to even) and leaves it in the low bits of the sum, so that scaling, rounding, conversion and the bias of digits16 are one
+// multiply-add (3 instructions an element in place of 9).
+template <int ND>
+__device__ inline void row_digits(const float (&x)[16], int unit, bool finite, v4i (&d)[ND]) {
+    if (ND == 2 && finite) {
+        // two factors: one alone passes the largest float for rows of sub-normal numbers
+        const float f0 = ldexpf(1.0f, -unit >> 1), f1 = ldexpf(1.0f, -unit - (-unit >> 1));
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(fmaf(x[4 * t + i] * f0, f1, 12582912.0f + 128.0f));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t by = bytes_of(w[0], w[1], w[2], w[3], 1 - j);
+                d[j][t] = static_cast<int>(j == 0 ? by : by ^ 0x80808080u);
+            }
+        }
+    } else {
+        int v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[j], unit);
+        digits16<ND>(v, d);
+    }
+}
 
 __device__ inline v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 

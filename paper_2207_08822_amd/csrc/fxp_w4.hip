@@ -15,6 +15,7 @@ struct W4Args {
     const void* x;
     int64_t ldx;
     int M, K, N, k_tiles, n_tiles, m_tiles;
+    int k_waves;         // waves that share a tile of outputs, 1 to 8 (k_w4_rows)
     const uint8_t* packed;
     const uint8_t* scales;
     void* y;
@@ -44,11 +45,8 @@ __global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
 #pragma unroll
     for (int d = 1; d < GROUP / 16; d <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), d)));
     const int unit = unit_of<ND>(m);
-    int v[16];
-#pragma unroll
-    for (int j = 0; j < 16; ++j) v[j] = fixed_point<ND>(x[j], unit);
     v4i d[ND];
-    digits16<ND>(v, d);
+    row_digits<ND>(x, unit, !__any(m >= 0x7f800000u), d);
     const int tile = k / 128, s = k % 128 / S, g = k % S / (S / 4), mt = row / 16, r = row % 16;
     uint8_t* base = a.digits + (static_cast<int64_t>(tile) * a.m_tiles + mt) * (ND * 2048);
 #pragma unroll
@@ -64,11 +62,15 @@ __global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
     if (k % GROUP == 0) a.units[static_cast<int64_t>(k / GROUP) * (16 * a.m_tiles) + row] = ldexpf(1.0f, unit - 6);
 }
 
-template <int TYPE, int GROUP, int NT, int MT>
-__global__ __launch_bounds__(kW4Threads) void k_w4_linear(W4Args a) {
-    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S;
+// Three rows or more: MT tiles of 16 rows, NT tiles of 16 outputs.  A wave has every eighth tile of 128 inputs, four of them on their way at a
+// time, and (up to two tiles of rows) the digits of the tile after the present one.
+template <int TYPE, int GROUP, int NT, int MT, int U>
+__global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT;
+    constexpr bool kAhead = MT <= 2;
+    using Digit = std::conditional_t<S == 64, v4i, long>;
     __shared__ float red[kW4Waves][NT * 16][17];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int nt0 = blockIdx.x * NT, mt0 = blockIdx.y * MT;
     float sum[MT][NT][4];
 #pragma unroll
@@ -78,70 +80,94 @@ __global__ __launch_bounds__(kW4Threads) void k_w4_linear(W4Args a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) sum[i][n][j] = 0.0f;
 
-    constexpr int GT = 128 / GROUP;                       // groups of a tile
-    for (int kt = wave; kt < a.k_tiles; kt += kW4Waves) {
-        v4i w[NT];
-        uint32_t e[NT][GT];
+    v4i w[U][NT];
+    uint32_t e[U][NT][GT];
+    Digit dig[MT][ND][STEPS];
+    float unit[MT][GT];
+    auto load_w = [&](int kt) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int nt = min(nt0 + n, a.n_tiles - 1);
-            w[n] = *reinterpret_cast<const v4i*>(a.packed + (static_cast<int64_t>(nt) * a.k_tiles + kt) * 1024 + lane * 16);
+        for (int i = 0; i < U; ++i) {
+            const int t = min(kt + kW4Waves * i, a.k_tiles - 1);
 #pragma unroll
-            for (int j = 0; j < GT; ++j)
-                e[n][j] = *reinterpret_cast<const uint32_t*>(a.scales + ((static_cast<int64_t>(nt) * a.k_tiles + kt) * GT + j) * 16 + 4 * g);
+            for (int n = 0; n < NT; ++n) {
+                const int64_t tile = static_cast<int64_t>(min(nt0 + n, a.n_tiles - 1)) * a.k_tiles + t;
+                w[i][n] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(a.packed + tile * 1024 + static_cast<uint32_t>(lane * 16)));
+#pragma unroll
+                for (int j = 0; j < GT; ++j)
+                    e[i][n][j] = *reinterpret_cast<const uint32_t*>(a.scales + (tile * GT + j) * 16 + static_cast<uint32_t>(4 * g));
+            }
         }
+    };
+    auto load_digits = [&](int kt) {
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int mt = min(mt0 + i, a.m_tiles - 1);
-            const uint8_t* dig = a.digits + (static_cast<int64_t>(kt) * a.m_tiles + mt) * (ND * 2048);
+            const uint8_t* const p = a.digits + (static_cast<int64_t>(kt) * a.m_tiles + mt) * (ND * 2048);
 #pragma unroll
-            for (int j = 0; j < GT; ++j) {
-                constexpr int SG = STEPS / GT;            // steps of a group
-                const float unit = a.units[(static_cast<int64_t>(kt) * GT + j) * (16 * a.m_tiles) + mt * 16 + col];
-                v4i acc[NT][ND];
+            for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                for (int s = 0; s < STEPS; ++s)
+                    dig[i][d][s] = *reinterpret_cast<const Digit*>(p + (d * STEPS + s) * (64 * sizeof(Digit)) + static_cast<uint32_t>(lane * sizeof(Digit)));
 #pragma unroll
-                    for (int d = 0; d < ND; ++d) acc[n][d] = v4i{0, 0, 0, 0};
+            for (int j = 0; j < GT; ++j) unit[i][j] = a.units[(static_cast<int64_t>(kt) * GT + j) * (16 * a.m_tiles) + mt * 16 + static_cast<uint32_t>(col)];
+        }
+    };
+    if (wave < a.k_tiles) {
+        load_w(wave);
+        if (kAhead) load_digits(wave);
+    }
+    for (int kt0 = wave; kt0 < a.k_tiles; kt0 += kW4Waves * U) {
 #pragma unroll
-                for (int t = 0; t < SG; ++t) {
-                    const int s = j * SG + t;
+        for (int u = 0; u < U; ++u) {
+            const int kt = kt0 + kW4Waves * u;
+            if (u && kt >= a.k_tiles) break;
+            if (!kAhead) load_digits(kt);
+            v4i acc[MT][GT][NT][ND];
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint32_t mask = 0xf0f0f0f0u;
+                    Digit q;
                     if constexpr (S == 64) {
-                        v4i b[ND];
-#pragma unroll
-                        for (int d = 0; d < ND; ++d) b[d] = *reinterpret_cast<const v4i*>(dig + ((d * STEPS + s) * 64 + lane) * 16);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const int w0 = w[n][2 * s], w1 = w[n][2 * s + 1];
-                            const int mask = static_cast<int>(0xf0f0f0f0u);
-                            const v4i q = {(w0 << 4) & mask, (w1 << 4) & mask, w0 & mask, w1 & mask};
-#pragma unroll
-                            for (int d = 0; d < ND; ++d) acc[n][d] = mfma_i8(q, b[d], acc[n][d]);
-                        }
+                        const uint32_t w0 = static_cast<uint32_t>(w[u][n][2 * s]), w1 = static_cast<uint32_t>(w[u][n][2 * s + 1]);
+                        q = v4i{static_cast<int>((w0 << 4) & mask), static_cast<int>((w1 << 4) & mask), static_cast<int>(w0 & mask),
+                                static_cast<int>(w1 & mask)};
                     } else {
-                        long b[ND];
-#pragma unroll
-                        for (int d = 0; d < ND; ++d) b[d] = *reinterpret_cast<const long*>(dig + ((d * STEPS + s) * 64 + lane) * 8);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            const uint32_t w0 = static_cast<uint32_t>(w[n][s]), mask = 0xf0f0f0f0u;
-                            const long q = static_cast<long>(static_cast<uint64_t>(w0 & mask) << 32 | ((w0 << 4) & mask));
-#pragma unroll
-                            for (int d = 0; d < ND; ++d) acc[n][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, b[d], acc[n][d], 0, 0, 0);
-                        }
+                        const uint32_t w0 = static_cast<uint32_t>(w[u][n][s]);
+                        q = static_cast<long>(static_cast<uint64_t>(w0 & mask) << 32 | ((w0 << 4) & mask));
                     }
-                }
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
+                    for (int i = 0; i < MT; ++i)
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) {
+                            const v4i before = s % SG ? acc[i][s / SG][n][d] : v4i{0, 0, 0, 0};
+                            if constexpr (S == 64) acc[i][s / SG][n][d] = mfma_i8(q, dig[i][d][s], before);
+                            else acc[i][s / SG][n][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, dig[i][d][s], before, 0, 0, 0);
+                        }
+                }
+            float scale_x[MT][GT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < GT; ++j) scale_x[i][j] = unit[i][j];
+            if (kAhead && kt + kW4Waves < a.k_tiles) load_digits(kt + kW4Waves);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int j = 0; j < GT; ++j)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        float v = static_cast<float>(acc[n][0][r] * 256 + acc[n][1][r]);
-                        if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[n][2][r]));
-                        const float scale = __uint_as_float(((e[n][j] >> (8 * r)) & 0xffu) << 23);
-                        sum[i][n][r] = fmaf(v * unit, scale, sum[i][n][r]);
+                        const float scale = __uint_as_float(((e[u][n][j] >> (8 * r)) & 0xffu) << 23);
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            float v = static_cast<float>((acc[i][j][n][0][r] << 8) + acc[i][j][n][1][r]);
+                            if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[i][j][n][2][r]));
+                            sum[i][n][r] = fmaf(v * scale_x[i][j], scale, sum[i][n][r]);
+                        }
                     }
-            }
         }
+        if (kt0 + kW4Waves * U < a.k_tiles) load_w(kt0 + kW4Waves * U);
     }
 
     // the waves' shares of the contraction
@@ -162,6 +188,146 @@ __global__ __launch_bounds__(kW4Threads) void k_w4_linear(W4Args a) {
             const int row = (mt0 + i) * 16 + m, out = nt0 * 16 + n;
             if (row < a.M && out < a.N) static_cast<T*>(a.y)[row * a.ldy + out] = static_cast<T>(v);
         }
+    }
+}
+
+// One or two rows, one launch.  a.k_waves waves share a tile of outputs; a wave has every k_waves-th tile of 128 inputs, eight on their
+// way at a time, and turns its own part of x into digits (a lane 16 inputs of a row, which is all of eight tiles at once).  With so few rows a matrix instruction
+// would leave 15 of 16 columns empty and its scaling (22 vector instructions a group) would be for nothing: here a lane sums the 16
+// mantissas it has loaded by byte dot products (one for four of them and a digit) and scales ONE sum a group.
+constexpr int kW4Ahead = 8;
+
+template <int TYPE, int GROUP, int ROWS>
+__global__ __launch_bounds__(kW4Threads, 4) void k_w4_rows(W4Args a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT, U = kW4Ahead;
+    __shared__ v4i s_digits[kW4Waves][U][ROWS][ND][8];          // pieces of 16 inputs
+    __shared__ float s_unit[kW4Waves][U][ROWS][GT];
+    __shared__ float red[kW4Waves][ROWS][16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int k_waves = a.k_waves, wave_n = wave / k_waves, first = wave - wave_n * k_waves;
+    const int nt = min(static_cast<int>(blockIdx.x) * (kW4Waves / k_waves) + wave_n, a.n_tiles - 1);      // a tile too many is done twice
+    const uint8_t* const packed = a.packed + static_cast<int64_t>(nt) * a.k_tiles * 1024;
+    const uint8_t* const scales = a.scales + static_cast<int64_t>(nt) * a.k_tiles * (GT * 16);
+    v4i w[U];
+    uint32_t e[U][GT];
+    // tile i of a turn is kt + k_waves i; tiles behind the last are the last again, and their x is zero
+    auto load_w = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int t = min(kt + k_waves * i, a.k_tiles - 1);
+            w[i] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(packed + t * 1024 + static_cast<uint32_t>(lane * 16)));
+#pragma unroll
+            for (int j = 0; j < GT; ++j) e[i][j] = scales[(t * GT + j) * 16 + static_cast<uint32_t>(r)];
+        }
+    };
+    float x[ROWS][16];
+    auto load_x = [&](int kt) {
+        const int t = kt + k_waves * (lane >> 3), k = t * 128 + (lane & 7) * 16;
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) {
+            const int row = min(m, a.M - 1);
+            if (t < a.k_tiles && k + 16 <= a.K) {
+                load_elems<TYPE, 16>(a.x, row * a.ldx + k, a.vec_x, x[m]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    x[m][j] = t < a.k_tiles && k + j < a.K ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(a.x)[row * a.ldx + k + j]) : 0.0f;
+            }
+        }
+    };
+    float sum[ROWS];
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) sum[m] = 0.0f;
+    // x before the weights: loads come back in order, and its digits are made while the weights are on their way
+    if (first < a.k_tiles) {
+        load_x(first);
+        load_w(first);
+    }
+    for (int kt = first; kt < a.k_tiles; kt += k_waves * U) {
+        // x's digits of this turn
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(x[m][j]) & 0x7fffffffu);
+#pragma unroll
+            for (int d = 1; d < GROUP / 16; d <<= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), d)));
+            const int unit = unit_of<ND>(top);
+            v4i d[ND];
+            row_digits<ND>(x[m], unit, !__any(top >= 0x7f800000u), d);
+#pragma unroll
+            for (int j = 0; j < ND; ++j) s_digits[wave][lane >> 3][m][j][lane & 7] = d[j];
+            if ((lane & 7) % (GROUP / 16) == 0) s_unit[wave][lane >> 3][m][(lane & 7) / (GROUP / 16)] = ldexpf(1.0f, unit - 6);
+        }
+        __builtin_amdgcn_wave_barrier();
+        const bool more = kt + k_waves * U < a.k_tiles;
+        if (more) load_x(kt + k_waves * U);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (i && kt + k_waves * i >= a.k_tiles) break;
+            const int mask = static_cast<int>(0xf0f0f0f0u);
+            int q[8];                                       // 16 times the mantissas, four to a word, in the order of the inputs of a step
+            if constexpr (S == 64) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    q[4 * s] = (w[i][2 * s] << 4) & mask;
+                    q[4 * s + 1] = (w[i][2 * s + 1] << 4) & mask;
+                    q[4 * s + 2] = w[i][2 * s] & mask;
+                    q[4 * s + 3] = w[i][2 * s + 1] & mask;
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    q[2 * s] = (w[i][s] << 4) & mask;
+                    q[2 * s + 1] = w[i][s] & mask;
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+                for (int j = 0; j < GT; ++j) {
+                    int acc[ND];
+#pragma unroll
+                    for (int d = 0; d < ND; ++d) acc[d] = 0;
+#pragma unroll
+                    for (int t = 0; t < SG; ++t) {
+                        const int s = j * SG + t;
+#pragma unroll
+                        for (int d = 0; d < ND; ++d) {
+                            if constexpr (S == 64) {
+                                const v4i b = s_digits[wave][i][m][d][4 * s + g];
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) acc[d] = __builtin_amdgcn_sdot4(q[4 * s + c], b[c], acc[d], false);
+                            } else {
+                                const int2 b = reinterpret_cast<const int2*>(s_digits[wave][i][m][d])[4 * s + g];
+                                acc[d] = __builtin_amdgcn_sdot4(q[2 * s], b.x, acc[d], false);
+                                acc[d] = __builtin_amdgcn_sdot4(q[2 * s + 1], b.y, acc[d], false);
+                            }
+                        }
+                    }
+                    float v = static_cast<float>((acc[0] << 8) + acc[1]);
+                    if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[2]));
+                    sum[m] = fmaf(v * s_unit[wave][i][m][j], __uint_as_float(e[i][j] << 23), sum[m]);
+                }
+        }
+        if (more) load_w(kt + k_waves * U);
+        __builtin_amdgcn_wave_barrier();
+    }
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) {
+        float v = sum[m];
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+        if (g == 0) red[wave][m][r] = v;
+    }
+    __syncthreads();
+    const int tiles = kW4Waves / k_waves;
+    for (int i = threadIdx.x; i < tiles * 16 * ROWS; i += kW4Threads) {
+        const int m = i / 16 % ROWS, t = i / (16 * ROWS), tile = blockIdx.x * tiles + t, n = tile * 16 + (i & 15);
+        float v = 0.0f;
+        for (int w = 0; w < k_waves; ++w) v += red[t * k_waves + w][m][i & 15];
+        using T = typename Elem<TYPE>::T;
+        if (m < a.M && n < a.N) static_cast<T*>(a.y)[m * a.ldy + n] = static_cast<T>(v);
     }
 }
 
@@ -276,18 +442,37 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
     a.ldy = ldy;
     a.digits = static_cast<uint8_t*>(ws);
     a.units = reinterpret_cast<float*>(a.digits + static_cast<size_t>(a.m_tiles) * 16 * a.k_tiles * 128 * (type == FXP_F32 ? 3 : 2));
-    a.vec_x = aligned(X, 16) && ldx * size % 16 == 0;
+    a.vec_x = aligned(X, 16) && (M == 1 || ldx * size % 16 == 0);
     const int64_t pieces = int64_t{16} * a.m_tiles * a.k_tiles * 8;
     if (pieces > (int64_t{1} << 30)) return FXP_ERR_DIMS;
     hipStream_t s = static_cast<hipStream_t>(stream);
     w4_of_type(type, [&](auto t) {
         w4_of_group(group, [&](auto g) {
             constexpr int TYPE = decltype(t)::value, GROUP = decltype(g)::value;
+            if (M <= 2) {
+                // Waves to a tile of outputs: two a SIMD in all, and no more than eight tiles of inputs to each (8192 x 8192, one row: 9.4 us; half
+                // as many waves 10.9, a quarter 15.7.  1024 x 16384: 6.0 us; with eight to each of the 1024 tiles 9.8).
+                a.k_waves = 1;
+                while (a.k_waves < kW4Waves && a.k_waves < a.k_tiles && (a.n_tiles * a.k_waves < 2048 || a.k_waves * kW4Ahead < a.k_tiles)) a.k_waves *= 2;
+                const int tiles = kW4Waves / a.k_waves;
+                const dim3 grid((a.n_tiles + tiles - 1) / tiles);
+                if (M == 1) hipLaunchKernelGGL((k_w4_rows<TYPE, GROUP, 1>), grid, dim3(kW4Threads), 0, s, a);
+                else hipLaunchKernelGGL((k_w4_rows<TYPE, GROUP, 2>), grid, dim3(kW4Threads), 0, s, a);
+                return;
+            }
             hipLaunchKernelGGL((k_w4_digits<TYPE, GROUP>), dim3(static_cast<unsigned>((pieces + 255) / 256)), dim3(256), 0, s, a);
-            if (a.m_tiles == 1)
-                hipLaunchKernelGGL((k_w4_linear<TYPE, GROUP, 1, 1>), dim3(a.n_tiles), dim3(kW4Threads), 0, s, a);
-            else
-                hipLaunchKernelGGL((k_w4_linear<TYPE, GROUP, 2, 4>), dim3((a.n_tiles + 1) / 2, (a.m_tiles + 3) / 4), dim3(kW4Threads), 0, s, a);
+            auto go = [&](auto nt_c, auto mt_c, auto u_c) {
+                constexpr int NT = decltype(nt_c)::value, MT = decltype(mt_c)::value;
+                hipLaunchKernelGGL((k_w4_linear<TYPE, GROUP, NT, MT, decltype(u_c)::value>), dim3((a.n_tiles + NT - 1) / NT, (a.m_tiles + MT - 1) / MT),
+                                   dim3(kW4Threads), 0, s, a);
+            };
+            using std::integral_constant;
+            constexpr integral_constant<int, 1> one{};
+            constexpr integral_constant<int, 2> two{};
+            constexpr integral_constant<int, 4> four{};
+            if (a.m_tiles > 2) go(two, four, one);
+            else if (a.n_tiles < 512) a.m_tiles == 1 ? go(one, one, two) : go(one, two, two);
+            else a.m_tiles == 1 ? go(two, one, two) : go(two, two, two);
         });
     });
     return launch_status();

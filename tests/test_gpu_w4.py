@@ -117,8 +117,8 @@ def test_linear4_strides_and_rows(fxp):
     fxp.linear4(x, w, out=out[:, 5:55])
     assert (out[:, :5] == 3).all() and (out[:, 55:] == 3).all()
     assert torch.equal(out[:, 5:55], fxp.linear4(x.contiguous(), w))
-    for m in (0, 19):                                                # a row does not depend on the rows beside it
-        assert torch.equal(out[m, 5:55], fxp.linear4(x[m:m + 1], w)[0])
+    for m in (0, 17):                                                # a row does not depend on the rows beside it
+        assert torch.equal(out[m, 5:55], fxp.linear4(x[m:m + 3], w)[0])
     assert fxp.linear4(x[:0], w).shape == (0, 50)
     with pytest.raises(fxp.FxpError):
         fxp.linear4(wide[:1, :333].expand(4, 333), w)
