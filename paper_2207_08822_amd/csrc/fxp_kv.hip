@@ -209,7 +209,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
 
 // ---- writer ----
 
-// four tokens x four elements of a [tokens, heads, dim] operand, rows behind `count` zero
+// four tokens x four elements of a [tokens, heads, dim] operand, rows before `from` and from `to` on zero
 template <int TYPE>
 __device__ inline void load_block(const void* x, int64_t at, int64_t token, int from, int to, bool vec, float (&v)[4][4]) {
 #pragma unroll
@@ -223,16 +223,58 @@ __device__ inline void load_block(const void* x, int64_t at, int64_t token, int 
     }
 }
 
+// The mapping of finite values under a scale in [25, 250].  Two bytes have 11 significant bits at most, so |x| in units plus 1/2 is exact and is cut
+// by the conversion; an fp32 value goes through its 24-bit mantissa as map_nearest has it (in units of its own, 0.5 - 2^-25 plus 1/2 rounds to 1).
+struct MapNearest {
+    float to;               // units (of the mantissa, for fp32) per 1
+    int cut, sat;
+};
+template <int TYPE>
+__device__ inline int map_finite(float x, const MapNearest& c) {
+    if constexpr (TYPE == FXP_F32) {
+        const uint32_t m = static_cast<uint32_t>(fabsf(x) * c.to);
+        const int q = min(static_cast<int>((m + (1u << (c.cut - 1))) >> c.cut), c.sat), sign = static_cast<int>(__float_as_uint(x)) >> 31;
+        return (q ^ sign) - sign;
+    } else {
+        const float y = x * c.to;
+        return min(max(static_cast<int>(y + copysignf(0.5f, y)), -c.sat), c.sat);
+    }
+}
+
+// Where a run's quads lie: the first, their number, the place behind the last token, quads of elements, ceil(2^32 / that).
+struct Quads {
+    int first, count, end, nd;
+    uint32_t inverse;
+    bool by_four;           // four quads of tokens beside each other in neighbouring threads: their values make 16 bytes
+    __device__ void at(int i, int& tq, int& d) const {
+        const int j = by_four ? i >> 2 : i, q = static_cast<int>(__umulhi(static_cast<uint32_t>(j), inverse));
+        d = (j - q * nd) * 4;
+        tq = first + (by_four ? 4 * q + (i & 3) : q);
+    }
+};
+__device__ inline Quads quads_of(const Run& run, int dim, uint32_t inverse, bool values) {
+    const int first = run.offset / 4, end = run.offset + run.count, count = (end + 3) / 4 - first;
+    return {first, count, end, dim / 4, inverse, values && count % 4 == 0};
+}
+// dword of a page that holds element d + j of a quad of tokens (values), or elements d .. d + 3 of token j of it (keys)
+__device__ inline int dword_of(bool values, int tq, int d, int j, int dim) {
+    return values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4;
+}
+
+// What bounds it: a step of single tokens the way of one token (run, then values, scale and old bytes together, then stores), a prompt
+// its reads and writes.
 template <int TYPE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const void* __restrict__ k, int64_t k_token, int64_t k_head,
                                                        const void* __restrict__ v, int64_t v_token, int64_t v_head, int64_t tokens,
-                                                       const int4* __restrict__ runs, int vec_k, int vec_v) {
+                                                       const int4* __restrict__ runs, int vec_k, int vec_v, uint32_t inverse) {
     __shared__ uint32_t lds[THREADS / 64];
     const int4 rr = runs[blockIdx.x];
     const Run run = {rr.x, rr.y, rr.z, rr.w};
     if (!run_ok(run, tokens, c.pages)) return;
     const bool values = blockIdx.z != 0;
-    const int head = blockIdx.y, dim = static_cast<int>(c.dim), nd = dim / 4;
+    const int head = blockIdx.y, dim = static_cast<int>(c.dim);
+    const Quads quads = quads_of(run, dim, inverse, values);
+    const int work = quads.count * quads.nd, nd = quads.nd;
     const void* x = values ? v : k;
     const int64_t token = values ? v_token : k_token;
     const bool vec = values ? vec_v : vec_k;
@@ -241,15 +283,23 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
     int32_t* const scale = (values ? c.ev : c.ek) + block;
     uint32_t* const page = reinterpret_cast<uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
 
-    // the new tokens as quads of places 4 tq .. 4 tq + 3 of the page, with those before the run and behind it left out
-    const int tq0 = run.offset / 4, end = run.offset + run.count, quads = (end + 3) / 4 - tq0, work = quads * nd;
     const int e_old = run.offset ? min(max(*scale, 1), 255) : 1;
     constexpr int kKept = 2;             // blocks of 16 values a thread keeps; others are read again, out of the cache
     float kept[kKept][4][4];
+    uint32_t old[kKept][4];              // of values: the dwords that the run's first tokens share with older ones
     uint32_t m = 0;
     auto fetch = [&](int i, float (&w)[4][4]) {
-        const int tq = tq0 + i / nd, d = i % nd * 4, place = 4 * tq;
-        load_block<TYPE>(x, row0 + (int64_t{place} - run.offset) * token + d, token, max(run.offset - place, 0), min(end - place, 4), vec, w);
+        int tq, d;
+        quads.at(i, tq, d);
+        const int place = 4 * tq;
+        load_block<TYPE>(x, row0 + (int64_t{place} - run.offset) * token + d, token, max(run.offset - place, 0), min(quads.end - place, 4), vec, w);
+    };
+    auto fetch_old = [&](int i, uint32_t (&b)[4]) {
+        int tq, d;
+        quads.at(i, tq, d);
+        if (values && 4 * tq < run.offset)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = page[dword_of(true, tq, d, j, dim)];
     };
     auto largest = [&](const float (&w)[4][4]) {
 #pragma unroll
@@ -261,8 +311,11 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
     for (int n = 0; n < kKept; ++n)
         if (static_cast<int>(threadIdx.x) + n * THREADS < work) {
             fetch(threadIdx.x + n * THREADS, kept[n]);
-            largest(kept[n]);
+            fetch_old(threadIdx.x + n * THREADS, old[n]);
         }
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) largest(kept[n]);
     for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
         float w[4][4];
         fetch(i, w);
@@ -271,37 +324,34 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
     m = THREADS == 64 ? wave_max(m) : block_max<THREADS / 64>(m, lds);
     const int e = max(e_old, min(max(static_cast<int>(m >> 23), 1), 255)), grown = e - e_old, cut = 25 - c.bits;
     if (threadIdx.x == 0) *scale = e;
+    const bool plain = e >= 25 && e <= 250;
+    const MapNearest how = {ldexpf(1.0f, TYPE == FXP_F32 ? 150 - e : 125 + c.bits - e), cut, (1 << (c.bits - 1)) - 1};
 
-    // address (in dwords) of a block of values' element j, or of keys' token j
-    auto place_of = [&](int tq, int d, int j) {
-        return values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4;
-    };
-    auto write = [&](int i, const float (&w)[4][4]) {
-        const int tq = tq0 + i / nd, d = i % nd * 4, from = max(run.offset - 4 * tq, 0), to = min(end - 4 * tq, 4);
+    auto write = [&](int i, const float (&w)[4][4], uint32_t (&was)[4]) {
+        int tq, d;
+        quads.at(i, tq, d);
+        const int from = max(run.offset - 4 * tq, 0), to = min(quads.end - 4 * tq, 4);
         uint32_t o[4];
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
-            o[a] = 0;
+            uint32_t b[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) o[a] |= (static_cast<uint32_t>(map_nearest(w[a][j], e, cut)) & 0xffu) << (8 * j);
+            for (int j = 0; j < 4; ++j) b[j] = static_cast<uint32_t>(plain ? map_finite<TYPE>(w[a][j], how) : map_nearest(w[a][j], e, cut));
+            o[a] = perm(perm(b[3], b[2], 0x0c0c0400u), perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
         }
         if (values) {
             uint32_t t[4];
             transpose4x4(o, t);
-            const uint32_t old = from ? (1u << (8 * from)) - 1u : 0u;        // bytes of the tokens before the run
+            const uint32_t keep = from ? (1u << (8 * from)) - 1u : 0u;       // bytes of the tokens before the run
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t* p = page + place_of(tq, d, j);
-                if (from) {
-                    const uint32_t b = *p;
-                    t[j] = (t[j] & ~old) | ((grown ? remap_nearest4(b, grown) : b) & old);
-                }
-                *p = t[j];
+                if (from) t[j] = (t[j] & ~keep) | ((grown ? remap_nearest4(was[j], grown) : was[j]) & keep);
+                page[dword_of(true, tq, d, j, dim)] = t[j];
             }
         } else {
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
-                uint32_t* p = page + place_of(tq, d, a);
+                uint32_t* const p = page + dword_of(false, tq, d, a, dim);
                 if (a >= from && a < to) *p = o[a];
                 else if (a < from && grown) *p = remap_nearest4(*p, grown);
             }
@@ -309,40 +359,48 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
     };
 #pragma unroll
     for (int n = 0; n < kKept; ++n)
-        if (static_cast<int>(threadIdx.x) + n * THREADS < work) write(threadIdx.x + n * THREADS, kept[n]);
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) write(threadIdx.x + n * THREADS, kept[n], old[n]);
     for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
         float w[4][4];
+        uint32_t was[4];
         fetch(i, w);
-        write(i, w);
+        fetch_old(i, was);
+        write(i, w, was);
     }
     // quads of old tokens alone
     if (run.offset && grown)
-        for (int i = threadIdx.x; i < tq0 * nd; i += THREADS)
+        for (int i = threadIdx.x; i < quads.first * nd; i += THREADS) {
+            const int q = static_cast<int>(__umulhi(static_cast<uint32_t>(i), inverse));
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                uint32_t* p = page + place_of(i / nd, i % nd * 4, j);
+                uint32_t* const p = page + dword_of(values, q, (i - q * nd) * 4, j, dim);
                 *p = remap_nearest4(*p, grown);
             }
+        }
 }
 
-// ---- inverse mapping: a wave has 4 tokens x 64 quads of elements at a time ----
+// ---- inverse mapping: a thread has blocks of 4 tokens x 4 elements ----
 template <int TYPE>
 __global__ __launch_bounds__(256) void k_kv_load(fxp_kv_cache c, void* __restrict__ k, void* __restrict__ v, int64_t tokens,
-                                                 const int4* __restrict__ runs) {
+                                                 const int4* __restrict__ runs, uint32_t inverse) {
     const int4 rr = runs[blockIdx.x];
     const Run run = {rr.x, rr.y, rr.z, rr.w};
     if (!run_ok(run, tokens, c.pages)) return;
     const bool values = blockIdx.z != 0;
-    const int head = blockIdx.y, dim = static_cast<int>(c.dim), nd = dim / 4;
+    const int head = blockIdx.y, dim = static_cast<int>(c.dim);
+    const Quads quads = quads_of(run, dim, inverse, values);
+    const int work = quads.count * quads.nd;
     const int64_t block = int64_t{run.page} * c.heads + head;
     const int unit = min(max((values ? c.ev : c.ek)[block], 1), 255) - 125 - c.bits;
-    const uint32_t* page = reinterpret_cast<const uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
-    const int tq0 = run.offset / 4, end = run.offset + run.count, work = ((end + 3) / 4 - tq0) * nd;
+    const bool plain = unit >= -126 && unit <= 120;                         // 2^unit and 127 of them are normal numbers
+    const float one = ldexpf(1.0f, plain ? unit : 0);
+    const uint32_t* const page = reinterpret_cast<const uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
     for (int i = threadIdx.x; i < work; i += 256) {
-        const int tq = tq0 + i / nd, d = i % nd * 4;
+        int tq, d;
+        quads.at(i, tq, d);
         uint32_t b[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) b[j] = page[values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4];
+        for (int j = 0; j < 4; ++j) b[j] = page[dword_of(values, tq, d, j, dim)];
         if (values) {
             uint32_t t[4];
             transpose4x4(b, t);
@@ -352,16 +410,21 @@ __global__ __launch_bounds__(256) void k_kv_load(fxp_kv_cache c, void* __restric
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
             const int place = 4 * tq + a;
-            if (place < run.offset || place >= end) continue;
+            if (place < run.offset || place >= quads.end) continue;
             float x[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = unmap_value(static_cast<int8_t>(b[a] >> (8 * j)), unit);
+            for (int j = 0; j < 4; ++j) {
+                const int q = static_cast<int8_t>(b[a] >> (8 * j));
+                x[j] = plain ? static_cast<float>(q) * one : unmap_value(q, unit);
+            }
             store4<TYPE>(values ? v : k, ((int64_t{run.first} + place - run.offset) * c.heads + head) * dim + d, true, x);
         }
     }
 }
 
 constexpr int64_t kMostRuns = (int64_t{1} << 24) - 1;      // 256 threads each, fewer than 2^32 in all
+
+static uint32_t inverse_of(int64_t n) { return static_cast<uint32_t>(((uint64_t{1} << 32) + n - 1) / n); }        // n > 1
 
 static bool multiple_of_4(const void* p, int64_t token, int64_t head, int type) {
     return aligned(p, 4 * elem_size(type)) && token % 4 == 0 && head % 4 == 0;
@@ -414,15 +477,16 @@ extern "C" int fxp_kv_append(const fxp_kv_cache* cache, int type, const void* k,
     if (!fxp::aligned(k, fxp::elem_size(type)) || !fxp::aligned(v, fxp::elem_size(type)) || !fxp::aligned(runs, 16)) return FXP_ERR_ALIGN;
     const int vk = fxp::multiple_of_4(k, k_token, k_head, type), vv = fxp::multiple_of_4(v, v_token, v_head, type);
     const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), 2);
+    const uint32_t inverse = fxp::inverse_of(cache->dim / 4);
     const bool few = tokens <= 4 * n_runs;
     auto go = [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
         if (few)
             hipLaunchKernelGGL((fxp::k_kv_append<TYPE, 64>), grid, dim3(64), 0, static_cast<hipStream_t>(stream), *cache, k, k_token, k_head, v,
-                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv);
+                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv, inverse);
         else
             hipLaunchKernelGGL((fxp::k_kv_append<TYPE, 256>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), *cache, k, k_token, k_head, v,
-                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv);
+                               v_token, v_head, tokens, reinterpret_cast<const int4*>(runs), vk, vv, inverse);
     };
     if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
     else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
@@ -442,7 +506,7 @@ extern "C" int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v
     const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), 2);
     auto go = [&](auto type_c) {
         hipLaunchKernelGGL((fxp::k_kv_load<decltype(type_c)::value>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), *cache, k, v, tokens,
-                           reinterpret_cast<const int4*>(runs));
+                           reinterpret_cast<const int4*>(runs), fxp::inverse_of(cache->dim / 4));
     };
     if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
     else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
