@@ -83,20 +83,6 @@ __device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
     return max(per, static_cast<uint32_t>(max(least, WAVES)));
 }
 
-// sum over the lanes up to this one, inside the vector ALU (rows of 16 first, then row to row)
-__device__ inline uint32_t wave_scan(uint32_t v) {
-    auto step = [](uint32_t x, auto ctrl, auto rows) {
-        return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
-    };
-    using std::integral_constant;
-    v = step(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});     // row_shr:1
-    v = step(v, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});     // row_shr:2
-    v = step(v, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});     // row_shr:4
-    v = step(v, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});     // row_shr:8
-    v = step(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});     // row_bcast:15 into rows 1 and 3
-    v = step(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});     // row_bcast:31 into rows 2 and 3
-    return v;
-}
 __device__ inline int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
 
 // Every wave by itself, 64 requests at a time; the loads of up to 64 requests are made once.

@@ -3,7 +3,7 @@
 // Tables.  Request b with l tokens that receives n more needs ceil((l + n) / 64) - ceil(l / 64) pages; an exclusive sum
 // over the requests gives each its first new token, its place in the stack of free pages and its first run (the new tokens
 // that share a page).  One launch: every workgroup sums over all requests (4 KB per thousand of them, out of the L2) and
-// fills 256 runs of its own, so nothing is exchanged between workgroups.
+// fills 64 or 256 runs of its own, so nothing is exchanged between workgroups.
 //
 // Writer.  q = floor(|x| 2^(125 + bits - e) + 1/2) with e the largest exponent of the block.  A workgroup has one run of one
 // head, keys or values; a thread has blocks of 4 tokens x 4 elements, which is one dword each way for keys (a token's four
@@ -13,7 +13,9 @@
 namespace fxp {
 
 constexpr int kTabThreads = 1024;
-constexpr int kTabRuns = 256;          // runs a workgroup fills
+// Runs a workgroup fills: up to 256 runs one workgroup, which may then write lengths in place as it goes (256 requests: 4.1 us), and 64 beyond
+// (999 requests, 100386 tokens in 2700 runs: 6.7 us; 128 a workgroup 7.4, 256 8.7).
+constexpr int kTabOne = 256, kTabMany = 64;
 
 struct Three {
     int tokens, need, runs;
@@ -23,12 +25,8 @@ __device__ inline Three add3(const Three& a, const Three& b) { return {a.tokens 
 // exclusive sums over the workgroup's threads; `total` receives the sum of all
 __device__ inline Three block_scan3(const Three& v, Three* lds, Three& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Three s = v;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const Three t = {__shfl_up(s.tokens, d), __shfl_up(s.need, d), __shfl_up(s.runs, d)};
-        if (lane >= d) s = add3(s, t);
-    }
+    auto scan = [](int x) { return static_cast<int>(wave_scan(static_cast<uint32_t>(x))); };
+    const Three s = {scan(v.tokens), scan(v.need), scan(v.runs)};
     if (lane == 63) lds[wave] = s;
     __syncthreads();
     Three before = {0, 0, 0};
@@ -64,7 +62,7 @@ __device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_
     return v;
 }
 
-// lengths, firsts, refusals and the rest of the stack, of all requests; `outputs`: firsts and refusals too
+// lengths of all requests and the stack's height, for the workgroup that is last to have read them
 __device__ inline void commit_lengths(const fxp_kv_step& st, const int32_t* n_new, Three* lds) {
     const int n_free = min(static_cast<int64_t>(max(st.n_free[0], 0)), st.pages);
     __shared__ int taken;
@@ -85,19 +83,23 @@ __device__ inline void commit_lengths(const fxp_kv_step& st, const int32_t* n_ne
     if (threadIdx.x == 0) st.n_free_after[0] = n_free - taken;
 }
 
+template <int RUNS>
 __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const int32_t* __restrict__ n_new, int64_t run_rows,
                                                            uint32_t* ticket) {
     __shared__ Three lds[kTabThreads / 64];
-    __shared__ Request req[kTabRuns];
-    __shared__ int mark[kTabRuns];          // position of the request that a run belongs to, at the request's first run here
-    __shared__ int64_t slot0[kTabRuns];
-    __shared__ int4 span[kTabRuns];         // first token, count, position of the first token
-    __shared__ int long_runs, last;
+    __shared__ Request req[RUNS];
+    __shared__ int mark[RUNS];          // position of the request that a run belongs to, at the request's first run here
+    __shared__ int64_t slot0[RUNS];
+    __shared__ int4 span[RUNS];         // first token, count, position of the first token
+    __shared__ int long_runs, last, taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r0 = blockIdx.x * kTabRuns;
+    const int r0 = blockIdx.x * RUNS;
     const int n_free = min(static_cast<int64_t>(max(st.n_free[0], 0)), st.pages);
-    if (tid < kTabRuns) mark[tid] = -1;
-    if (tid == 0) long_runs = 0;
+    if (tid < RUNS) mark[tid] = -1;
+    if (tid == 0) long_runs = taken = 0;
+    // A single workgroup has read what it replaces, and with outputs of their own nobody reads what is written: lengths and height are
+    // written along the way.  Otherwise the last workgroup to arrive writes them in the end.
+    const bool along = !ticket || gridDim.x == 1;
     __syncthreads();
 
     Three carry = {0, 0, 0}, total;
@@ -116,9 +118,11 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         if (b < st.requests && (base / kTabThreads) % gridDim.x == blockIdx.x) {
             st.first[b] = r.first;
             st.refused[b] = !r.served;
+            if (along) st.lens_after[b] = r.served ? r.after : st.lens[b];
         }
+        if (blockIdx.x == 0 && along && r.served && v.need) atomicMax(&taken, x.need + v.need);
         const int lo = max(x.runs, r0);
-        if (v.runs > 0 && lo < x.runs + v.runs && lo < r0 + kTabRuns && x.runs >= 0) {
+        if (v.runs > 0 && lo < x.runs + v.runs && lo < r0 + RUNS && x.runs >= 0) {
             req[lo - r0] = r;
             mark[lo - r0] = lo - r0;
         }
@@ -126,10 +130,11 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
     }
     if (blockIdx.x == 0 && tid == 0) st.first[st.requests] = carry.tokens;
     __syncthreads();
+    if (blockIdx.x == 0 && tid == 0 && along) st.n_free_after[0] = n_free - taken;
 
     // the request of each run: the nearest mark at or before it
     int owner = -1;
-    if (tid < kTabRuns) {
+    if (tid < RUNS) {
         owner = mark[tid];
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -139,7 +144,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         if (lane == 63) mark[tid] = owner;                  // the last of each wave: read below by the waves after it
     }
     __syncthreads();
-    if (tid < kTabRuns) {
+    if (tid < RUNS) {
         for (int w = 0; w < wave; ++w) owner = max(owner, mark[64 * w + 63]);
         const int run = r0 + tid;
         int4 s = make_int4(0, 0, 0, 0);
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
     }
     __syncthreads();
     if (long_runs)
-        for (int i = wave; i < kTabRuns; i += kTabThreads / 64) {
+        for (int i = wave; i < RUNS; i += kTabThreads / 64) {
             const int4 s = span[i];
             const int64_t t = int64_t{s.x} + lane;
             if (lane >= 1 && lane < s.y && t >= 0 && t < st.tokens) {
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         }
 
     // The lengths and the stack's height may be updated in place: by the workgroup that is last to have read them.
-    if (ticket) {
+    if (!along) {
         __syncthreads();
         if (tid == 0) {
             last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
@@ -202,8 +207,6 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         }
         __syncthreads();
         if (last) commit_lengths(st, n_new, lds);
-    } else if (blockIdx.x == gridDim.x - 1) {
-        commit_lengths(st, n_new, lds);
     }
 }
 
@@ -458,9 +461,13 @@ extern "C" int fxp_kv_tables(const fxp_kv_step* st, const int32_t* n_new, void* 
     if (in_place && (!ws || ws_bytes < 256)) return FXP_ERR_WORKSPACE;
     if (in_place && !fxp::aligned(ws, 4)) return FXP_ERR_ALIGN;
     const int64_t rows = fxp_kv_max_runs(st->requests, st->tokens);
-    const int64_t grid = rows > fxp::kTabRuns ? (rows + fxp::kTabRuns - 1) / fxp::kTabRuns : 1;
-    hipLaunchKernelGGL(fxp::k_kv_tables, dim3(static_cast<unsigned>(grid)), dim3(fxp::kTabThreads), 0, static_cast<hipStream_t>(stream), *st,
-                       n_new, rows, in_place ? static_cast<uint32_t*>(ws) : nullptr);
+    uint32_t* const ticket = in_place ? static_cast<uint32_t*>(ws) : nullptr;
+    if (rows <= fxp::kTabOne)
+        hipLaunchKernelGGL((fxp::k_kv_tables<fxp::kTabOne>), dim3(1), dim3(fxp::kTabThreads), 0, static_cast<hipStream_t>(stream), *st, n_new, rows,
+                           ticket);
+    else
+        hipLaunchKernelGGL((fxp::k_kv_tables<fxp::kTabMany>), dim3(static_cast<unsigned>((rows + fxp::kTabMany - 1) / fxp::kTabMany)),
+                           dim3(fxp::kTabThreads), 0, static_cast<hipStream_t>(stream), *st, n_new, rows, ticket);
     return fxp::launch_status();
 }
 
