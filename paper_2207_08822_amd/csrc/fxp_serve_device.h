@@ -173,6 +173,12 @@ __device__ inline uint32_t wave_scan(uint32_t v) {
     return v;
 }
 
+// Loads through a buffer descriptor: `bytes` from a uniform address, at a uniform and a lane's offset; 0 bytes: zeros, and no memory access.
+__device__ inline auto records(const void* base, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, bytes, 0x00027000);
+}
+constexpr int kNonTemporal = 2;
+
 struct Run {
     int first, count, page, offset;
 };

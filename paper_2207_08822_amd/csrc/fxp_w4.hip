@@ -30,14 +30,14 @@ template <int TYPE, int GROUP>
 __global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64;
     const int i = blockIdx.x * 256 + threadIdx.x, pieces = a.k_tiles * 8, row = i / pieces, piece = i % pieces, k = piece * 16;
-    if (row >= 16 * a.m_tiles) return;                     // whole groups of neighbours: pieces is a multiple of 8
+    if (row >= a.M) return;                                // whole groups of neighbours: pieces is a multiple of 8
     float x[16];
-    if (row < a.M && k + 16 <= a.K) {
+    if (k + 16 <= a.K) {
         load_elems<TYPE, 16>(a.x, row * a.ldx + k, a.vec_x, x);
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            x[j] = row < a.M && k + j < a.K ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(a.x)[row * a.ldx + k + j]) : 0.0f;
+            x[j] = k + j < a.K ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(a.x)[row * a.ldx + k + j]) : 0.0f;
     }
     uint32_t m = 0;
 #pragma unroll
@@ -62,12 +62,14 @@ __global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
     if (k % GROUP == 0) a.units[static_cast<int64_t>(k / GROUP) * (16 * a.m_tiles) + row] = ldexpf(1.0f, unit - 6);
 }
 
-// Three rows or more: MT tiles of 16 rows, NT tiles of 16 outputs.  A wave has every eighth tile of 128 inputs, four of them on their way at a
-// time, and (up to two tiles of rows) the digits of the tile after the present one.
+// Three rows or more: MT tiles of 16 rows, NT tiles of 16 outputs.  A wave has every eighth tile of 128 inputs.  U of its weight tiles and, up to
+// two tiles of rows, the next digits are on their way while one is worked on; loads are always issued, those of tiles that are none without records
+// (behind a branch the compiler would wait for all of them wherever it needs one).
 template <int TYPE, int GROUP, int NT, int MT, int U>
 __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT;
-    constexpr bool kAhead = MT <= 2;
+    constexpr int B = MT <= 2 ? 2 : 1;                      // buffers of digits
+    static_assert(U % B == 0, "a turn begins with the same buffer");
     using Digit = std::conditional_t<S == 64, v4i, long>;
     __shared__ float red[kW4Waves][NT * 16][17];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
@@ -82,51 +84,52 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
 
     v4i w[U][NT];
     uint32_t e[U][NT][GT];
-    Digit dig[MT][ND][STEPS];
-    float unit[MT][GT];
-    auto load_w = [&](int kt) {
+    Digit dig[B][MT][ND][STEPS];
+    float unit[B][MT][GT];
+    auto load_w = [&](int u, int kt) {
+        const bool there = kt < a.k_tiles;
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const int t = min(kt + kW4Waves * i, a.k_tiles - 1);
+        for (int n = 0; n < NT; ++n) {
+            const int64_t tile = static_cast<int64_t>(min(nt0 + n, a.n_tiles - 1)) * a.k_tiles + kt;
+            w[u][n] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(records(a.packed + tile * 1024, there ? 1024 : 0), lane * 16, 0, kNonTemporal));
+            const auto scales = records(a.scales + tile * (GT * 16), there ? GT * 16 : 0);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int64_t tile = static_cast<int64_t>(min(nt0 + n, a.n_tiles - 1)) * a.k_tiles + t;
-                w[i][n] = __builtin_nontemporal_load(reinterpret_cast<const v4i*>(a.packed + tile * 1024 + static_cast<uint32_t>(lane * 16)));
-#pragma unroll
-                for (int j = 0; j < GT; ++j)
-                    e[i][n][j] = *reinterpret_cast<const uint32_t*>(a.scales + (tile * GT + j) * 16 + static_cast<uint32_t>(4 * g));
-            }
+            for (int j = 0; j < GT; ++j) e[u][n][j] = __builtin_amdgcn_raw_buffer_load_b32(scales, 4 * g, 16 * j, 0);
         }
     };
-    auto load_digits = [&](int kt) {
+    auto load_digits = [&](int c, int kt) {
+        const bool there = kt < a.k_tiles;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int mt = min(mt0 + i, a.m_tiles - 1);
-            const uint8_t* const p = a.digits + (static_cast<int64_t>(kt) * a.m_tiles + mt) * (ND * 2048);
+            const int piece = mt * 16 + col < a.M ? lane * static_cast<int>(sizeof(Digit)) : 1 << 30;      // no digits were made of rows that are none
+            const auto digits = records(a.digits + (static_cast<int64_t>(kt) * a.m_tiles + mt) * (ND * 2048), there ? ND * 2048 : 0);
 #pragma unroll
             for (int d = 0; d < ND; ++d)
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-                    dig[i][d][s] = *reinterpret_cast<const Digit*>(p + (d * STEPS + s) * (64 * sizeof(Digit)) + static_cast<uint32_t>(lane * sizeof(Digit)));
+                for (int s = 0; s < STEPS; ++s) {
+                    const int off = (d * STEPS + s) * static_cast<int>(64 * sizeof(Digit));
+                    if constexpr (S == 64) dig[c][i][d][s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(digits, piece, off, 0));
+                    else dig[c][i][d][s] = __builtin_bit_cast(long, __builtin_amdgcn_raw_buffer_load_b64(digits, piece, off, 0));
+                }
+            const auto units = records(a.units + static_cast<int64_t>(kt) * GT * (16 * a.m_tiles) + mt * 16, there ? (GT - 1) * 64 * a.m_tiles + 64 : 0);
 #pragma unroll
-            for (int j = 0; j < GT; ++j) unit[i][j] = a.units[(static_cast<int64_t>(kt) * GT + j) * (16 * a.m_tiles) + mt * 16 + static_cast<uint32_t>(col)];
+            for (int j = 0; j < GT; ++j) unit[c][i][j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(units, 4 * col, 64 * a.m_tiles * j, 0));
         }
     };
-    if (wave < a.k_tiles) {
-        load_w(wave);
-        if (kAhead) load_digits(wave);
-    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_w(u, wave + kW4Waves * u);
+    if (B == 2) load_digits(0, wave);
     for (int kt0 = wave; kt0 < a.k_tiles; kt0 += kW4Waves * U) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int kt = kt0 + kW4Waves * u;
-            if (u && kt >= a.k_tiles) break;
-            if (!kAhead) load_digits(kt);
-            v4i acc[MT][GT][NT][ND];
+            const int kt = kt0 + kW4Waves * u, c = u % B;
+            load_digits(B == 2 ? 1 - c : 0, B == 2 ? kt + kW4Waves : kt);
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s)
+            for (int n = 0; n < NT; ++n) {
+                v4i acc[MT][GT][ND];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+                for (int s = 0; s < STEPS; ++s) {
                     const uint32_t mask = 0xf0f0f0f0u;
                     Digit q;
                     if constexpr (S == 64) {
@@ -141,33 +144,27 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
                     for (int i = 0; i < MT; ++i)
 #pragma unroll
                         for (int d = 0; d < ND; ++d) {
-                            const v4i before = s % SG ? acc[i][s / SG][n][d] : v4i{0, 0, 0, 0};
-                            if constexpr (S == 64) acc[i][s / SG][n][d] = mfma_i8(q, dig[i][d][s], before);
-                            else acc[i][s / SG][n][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, dig[i][d][s], before, 0, 0, 0);
+                            const v4i before = s % SG ? acc[i][s / SG][d] : v4i{0, 0, 0, 0};
+                            if constexpr (S == 64) acc[i][s / SG][d] = mfma_i8(q, dig[c][i][d][s], before);
+                            else acc[i][s / SG][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, dig[c][i][d][s], before, 0, 0, 0);
                         }
                 }
-            float scale_x[MT][GT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < GT; ++j) scale_x[i][j] = unit[i][j];
-            if (kAhead && kt + kW4Waves < a.k_tiles) load_digits(kt + kW4Waves);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int j = 0; j < GT; ++j)
+                for (int j = 0; j < GT; ++j)                // (of a tile that is none, all is zero)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const float scale = __uint_as_float(((e[u][n][j] >> (8 * r)) & 0xffu) << 23);
 #pragma unroll
                         for (int i = 0; i < MT; ++i) {
-                            float v = static_cast<float>((acc[i][j][n][0][r] << 8) + acc[i][j][n][1][r]);
-                            if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[i][j][n][2][r]));
-                            sum[i][n][r] = fmaf(v * scale_x[i][j], scale, sum[i][n][r]);
+                            float v = static_cast<float>((acc[i][j][0][r] << 8) + acc[i][j][1][r]);
+                            if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[i][j][2][r]));
+                            sum[i][n][r] = fmaf(v * unit[c][i][j], scale, sum[i][n][r]);
                         }
                     }
+                __builtin_amdgcn_sched_barrier(0);          // one tile of outputs after the other: interleaved, some of these spilled
+            }
+            load_w(u, kt + kW4Waves * U);
         }
-        if (kt0 + kW4Waves * U < a.k_tiles) load_w(kt0 + kW4Waves * U);
     }
 
     // the waves' shares of the contraction
@@ -425,8 +422,8 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
     if (!X || !packed || !scales || !Y) return FXP_ERR_NULL;
     const size_t size = elem_size(type);
     if (!aligned(X, size) || !aligned(Y, size) || !aligned(packed, 16) || !aligned(scales, 4)) return FXP_ERR_ALIGN;
-    if (!ws || ws_bytes < fxp_w4_workspace_bytes(type, M, K, group)) return FXP_ERR_WORKSPACE;
-    if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    if (M > 2 && (!ws || ws_bytes < fxp_w4_workspace_bytes(type, M, K, group))) return FXP_ERR_WORKSPACE;
+    if (M > 2 && !aligned(ws, 256)) return FXP_ERR_ALIGN;
     W4Args a;
     a.x = X;
     a.ldx = ldx;
@@ -443,7 +440,7 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
     a.digits = static_cast<uint8_t*>(ws);
     a.units = reinterpret_cast<float*>(a.digits + static_cast<size_t>(a.m_tiles) * 16 * a.k_tiles * 128 * (type == FXP_F32 ? 3 : 2));
     a.vec_x = aligned(X, 16) && (M == 1 || ldx * size % 16 == 0);
-    const int64_t pieces = int64_t{16} * a.m_tiles * a.k_tiles * 8;
+    const int64_t pieces = M * a.k_tiles * 8;
     if (pieces > (int64_t{1} << 30)) return FXP_ERR_DIMS;
     hipStream_t s = static_cast<hipStream_t>(stream);
     w4_of_type(type, [&](auto t) {
@@ -470,9 +467,20 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
             constexpr integral_constant<int, 1> one{};
             constexpr integral_constant<int, 2> two{};
             constexpr integral_constant<int, 4> four{};
+            constexpr integral_constant<int, 3> three{};
+            auto of_rows = [&](auto nt_c) {
+                if (a.m_tiles == 1) go(nt_c, one, two);
+                else go(nt_c, two, two);
+            };
+            // As many tiles of outputs to a workgroup as leave one for each CU: every wave reads its rows' digits (4 KB a tile of rows) for
+            // 1 KB of weights a tile of outputs, and that is what bounds it (23 rows, 4090 x 11007: three tiles 10.5 us, two 13.8; 8192 x 8192,
+            // two tiles 21.0 in all, one 25.8).
+            constexpr int kCus = 256;
             if (a.m_tiles > 2) go(two, four, one);
-            else if (a.n_tiles < 512) a.m_tiles == 1 ? go(one, one, two) : go(one, two, two);
-            else a.m_tiles == 1 ? go(two, one, two) : go(two, two, two);
+            else if (a.n_tiles <= kCus) of_rows(one);
+            else if (a.n_tiles <= 2 * kCus) of_rows(two);
+            else if (a.n_tiles <= 3 * kCus) of_rows(three);
+            else of_rows(four);
         });
     });
     return launch_status();

@@ -578,7 +578,7 @@ def _served(t, what, dims):
     if t.get_device() != torch._C._cuda_getDevice():
         raise FxpError(f"{what} is on another device than the current one")
     code = _TYPES.get(t.dtype)
-    if code is None or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+    if code is None or t.dim() != dims or not (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] == 1):
         raise FxpError(f"{what} must be a {dims}-dimensional float32, bfloat16 or float16 tensor with a contiguous last dimension")
     return code
 
@@ -715,7 +715,7 @@ def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=No
     if tokens != tab.tokens or dim != cache.dim:
         raise FxpError("q must be [tokens, q_heads, dim] of the tables and the cache")
     if out is None:
-        out = torch.empty((tokens, q_heads, dim), dtype=q.dtype, device=q.device)
+        out = q.new_empty((tokens, q_heads, dim))
     elif _served(out, "out", 3) != code or out.shape != q.shape or (tokens > 1 and out.stride(0) < dim) or (q_heads > 1 and out.stride(1) < dim):
         raise FxpError("out must have the shape and type of q, and rows that do not overlap")
     if lse is not None:
@@ -761,12 +761,12 @@ def linear4(x, w, out=None, ws=None):
     if K != w.K:
         raise FxpError("x must be [M, K] of the weights")
     if out is None:
-        out = torch.empty((M, w.N), dtype=x.dtype, device=x.device)
+        out = x.new_empty((M, w.N))
     elif _served(out, "out", 2) != code or tuple(out.shape) != (M, w.N):
         raise FxpError("out must be [M, N] of x's type")
-    if ws is None:
-        ws = torch.empty(max(256, int(lib().fxp_w4_workspace_bytes(code, M, K, w.group))), dtype=torch.uint8, device=x.device)
+    if ws is None and M > 2:
+        ws = x.new_empty(int(lib().fxp_w4_workspace_bytes(code, M, K, w.group)), dtype=torch.uint8)
     packed, scales = w.pointers
     _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), _row_stride(out, "out"),
-                               ws.data_ptr(), ws.numel(), _stream()), "fxp_w4_linear")
+                               _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
     return out
