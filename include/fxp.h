@@ -461,7 +461,11 @@ int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t t
  * Arithmetic: rows of q and the weights of 64 tokens are fixed-point numbers of two signed 8-bit digits (three for fp32: 23
  * bits) under a scale of their own, products are exact int32 sums over 64 terms, sums over more and the
  * softmax are fp32.  0 < scale < 2^64.  Scores are taken to lie below 2^89 in magnitude.
- * ws: fxp_kv_attention_workspace_bytes bytes, 256-byte aligned; 0 on bad arguments. */
+ * step->first must not decrease.
+ * ws: fxp_kv_attention_workspace_bytes bytes (0 on bad arguments), 256-byte aligned, of which the first FXP_KV_TICKET_BYTES are zero
+ * before the first call that uses them; every call leaves them zero.  Calls of any sizes may take turns with one workspace; two at
+ * once may not share it. */
+#define FXP_KV_TICKET_BYTES 2048
 size_t fxp_kv_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim);
 int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int type, const void* q, int64_t q_token, int64_t q_head,
                      int64_t q_heads, float scale, int64_t window, void* out, int64_t out_token, int64_t out_head, float* lse,
@@ -472,7 +476,7 @@ int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int typ
  * each group of `group` (32, 64 or 128) inputs of one output.  Packed layout, made once: tiles of 16 outputs x 128 inputs,
  * [ceil(N / 16), ceil(K / 128)] tiles of 1024 bytes.  With S = min(group, 64) and k counted in the tile, output r of
  * the tile and input k are in piece 16 * ((k % S) / (S / 4)) + r of 16 bytes, byte (k / S) * (S / 8) + k % (S / 8) of it, low
- * half if (k % (S / 4)) < S / 8, else the high half, in two's complement.  scales: uint8 biased exponents
+ * half if (k % (S / 4)) < S / 8, else the high half, in two's complement.  scales: uint8 biased exponents, 1 .. 254,
  * [ceil(N / 16), ceil(K / 128) * 128 / group, 16].  Inputs and outputs past K and N are zero.
  * K <= 2^20, N <= 2^24; K * ceil16(M) <= 2^34. */
 size_t fxp_w4_packed_bytes(int64_t K, int64_t N);

@@ -14,13 +14,16 @@
 // likewise under their own largest one.  Rounding a row to 15 bits is off by at most 2^-16 of its largest element's binade
 // - for bf16 and fp16 rows less than half a step of the type for elements within 2^-8 / 2^-5 of the largest - and weights
 // relative to the page's own largest, so a long tail of small weights behind one large one keeps its sum.  fp32 has 23 bits.
+#include <algorithm>
+
 #include "fxp_serve_device.h"
 
 namespace fxp {
 
 constexpr int kTile = 16;
 constexpr int kFewRows = 2 * kTile;
-constexpr int kAttGroups = 512;          // workgroups at most: two a CU
+constexpr int kAttWaves = 4;
+constexpr int kAttGroups = 512;          // workgroups: two a CU (768, which three a CU have room for, split more tiles: 57 -> 67 us for 64 requests)
 
 struct AttArgs {
     fxp_kv_cache c;
@@ -35,7 +38,7 @@ struct AttArgs {
     float* lse;
     float* part_o;          // [workgroup][2][16][dim]: parts of the tiles that the stretch ends in (0) and begins in (1)
     float2* part_ml;        // [workgroup][2][16]: largest score (log2), sum
-    uint32_t* tickets;      // [tiles][heads]: parts of a tile that are there; zero between calls
+    uint32_t* tickets;      // [workgroup]: parts that are there of the tile that begins in this stretch and ends in another; zero between calls
     int group;              // query heads per head of the cache
     uint32_t group_inverse; // ceil(2^32 / group): (x * it) >> 32 is x / group for x * group < 2^32
     int vec_q, vec_out;
@@ -63,69 +66,97 @@ __device__ inline Extent extent(const AttArgs& a, int64_t b) {
 
 // Cost of a tile in pages besides its own: its rows of q, the join of its parts, the first loads' way.  (Without it a workgroup
 // whose stretch is many short tiles takes as long as several others.)
-template <int WAVES>
-constexpr int kTileCost = 2 * WAVES;
-
-// The line, and where this workgroup's stretch of it begins.  Units are counted in 32 bits: the host sees to it.
-struct Stretch {
-    uint32_t units, per, u0;           // all units, those of a stretch, the first of this one
-    uint32_t unit_b;                   // units before request b
-    int b, tiles_before;               // request of unit u0, tiles before it
-    Extent e;
-};
+constexpr int kTileCost = 2 * kAttWaves;
 
 // Pages of a stretch: equal shares, but no fewer than one a wave, and so many that the parts of the longest tile are at
 // most some twice as many as the pages that a wave has of them (they are joined one after the other).
-template <int WAVES>
 __device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
     const uint32_t per = (units + gridDim.x - 1) / gridDim.x;
     const int least = static_cast<int>(0.7f * sqrtf(static_cast<float>(most_pages)));
-    return max(per, static_cast<uint32_t>(max(least, WAVES)));
+    return max(per, static_cast<uint32_t>(max(least, kAttWaves)));
 }
 
 __device__ inline int lane_of(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ inline Extent lane_of(const Extent& e, int lane) {
+    return {lane_of(e.n, lane), lane_of(e.len, lane), lane_of(e.tiles, lane), lane_of(e.page0, lane), lane_of(e.pages, lane), lane_of(e.tok0, lane)};
+}
 
-// Every wave by itself, 64 requests at a time; the loads of up to 64 requests are made once.
-template <int WAVES>
-__device__ inline Stretch survey(const AttArgs& a) {
-    const int lane = threadIdx.x & 63, requests = static_cast<int>(a.requests), heads = static_cast<int>(a.c.heads);
-    Stretch st = {};
-    auto units_of = [&](const Extent& e) { return static_cast<uint32_t>(e.tiles * heads) * static_cast<uint32_t>(e.pages + kTileCost<WAVES>); };
-    Extent e = {};
-    uint32_t v = 0;
-    int most = 0;
-    for (int base = 0; base < requests; base += 64) {
-        if (base + lane < requests) e = extent(a, base + lane);
-        else e.tiles = 0;
-        v = units_of(e);
-        most = max(most, e.tiles ? e.pages : 0);
-        st.units += static_cast<uint32_t>(lane_of(static_cast<int>(wave_scan(v)), 63));
+// Units of all requests (`units_of` each; 32 bits, the host sees to it), and the request that unit at_of(all units, most pages of one) belongs
+// to: its number (-1: behind the last), the units before it, its extent.  Every wave by itself: up to 64 requests are loaded once, a lane each;
+// of more, a lane sums up a row of neighbours, and the row with the unit in it is gone through again.
+struct Found {
+    uint32_t units, at, before;
+    int b;
+    Extent e;
+};
+template <typename U, typename A>
+__device__ inline Found find_request(const AttArgs& a, U units_of, A at_of) {
+    const int lane = threadIdx.x & 63, requests = static_cast<int>(a.requests);
+    Found found = {};
+    found.b = -1;
+    auto of_lane = [&](int b, int end, Extent& e) {
+        e = Extent{};
+        if (b < end) e = extent(a, b);
+        return b < end ? units_of(e) : 0u;
+    };
+    auto take = [&](uint32_t v, uint32_t carry, int base, const Extent& e) {
+        const uint32_t x = carry + wave_scan(v) - v;
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(found.at >= x && found.at < x + v);
+        if (!hit) return false;
+        const int w = __builtin_ctzll(hit);
+        found.b = base + w;
+        found.before = static_cast<uint32_t>(lane_of(static_cast<int>(x), w));
+        found.e = lane_of(e, w);
+        return true;
+    };
+    auto last = [](uint32_t v) { return static_cast<uint32_t>(lane_of(static_cast<int>(v), 63)); };
+    if (requests <= 64) {
+        Extent e;
+        const uint32_t v = of_lane(lane, requests, e);
+        found.units = last(wave_scan(v));
+        found.at = at_of(found.units, static_cast<int>(wave_max(static_cast<uint32_t>(v ? e.pages : 0))));
+        take(v, 0, 0, e);
+        return found;
     }
-    st.per = stretch_of<WAVES>(st.units, static_cast<int>(wave_max(static_cast<uint32_t>(most))));
-    st.u0 = st.per * blockIdx.x;
-    st.b = -1;
-    uint32_t carry = 0;
-    for (int base = 0; base < requests; base += 64) {
-        if (requests > 64) {
-            if (base + lane < requests) e = extent(a, base + lane);
-            else e.tiles = 0;
-            v = units_of(e);
-        }
-        const uint32_t sum = wave_scan(v), x = carry + sum - v;
-        const uint64_t hit = __builtin_amdgcn_ballot_w64(st.u0 >= x && st.u0 < x + v);
-        const int sum_t = static_cast<int>(wave_scan(static_cast<uint32_t>(e.tiles)));
+    const int row = (requests + 63) / 64;
+    uint32_t sum = 0;
+    int most = 0;
+#pragma unroll 4
+    for (int i = 0; i < row; ++i) {
+        Extent e;
+        const uint32_t v = of_lane(lane * row + i, requests, e);
+        sum += v;
+        most = max(most, v ? e.pages : 0);
+    }
+    const uint32_t scan = wave_scan(sum), x = scan - sum;
+    found.units = last(scan);
+    found.at = at_of(found.units, static_cast<int>(wave_max(static_cast<uint32_t>(most))));
+    const uint64_t hit = __builtin_amdgcn_ballot_w64(found.at >= x && found.at < x + sum);
+    if (!hit) return found;
+    const int w = __builtin_ctzll(hit), end = min((w + 1) * row, requests);
+    uint32_t carry = static_cast<uint32_t>(lane_of(static_cast<int>(x), w));
+    for (int base = w * row; base < end; base += 64) {
+        Extent e;
+        const uint32_t v = of_lane(base + lane, end, e);
+        if (take(v, carry, base, e)) break;
+        carry += last(wave_scan(v));
+    }
+    return found;
+}
+// the next request from b on that has tiles, or -1; 64 at a time: a padded batch has many that have none
+__device__ inline int next_request(const AttArgs& a, int b, Extent& e) {
+    const int lane = threadIdx.x & 63, requests = static_cast<int>(a.requests);
+    for (; b < requests; b += 64) {
+        Extent x = {};
+        if (b + lane < requests) x = extent(a, b + lane);
+        const uint64_t hit = __builtin_amdgcn_ballot_w64(x.tiles > 0);
         if (hit) {
             const int w = __builtin_ctzll(hit);
-            st.b = base + w;
-            st.unit_b = static_cast<uint32_t>(lane_of(static_cast<int>(x), w));
-            st.tiles_before += lane_of(sum_t - e.tiles, w);
-            st.e = {lane_of(e.n, w), lane_of(e.len, w), lane_of(e.tiles, w), lane_of(e.page0, w), lane_of(e.pages, w), lane_of(e.tok0, w)};
-            break;
+            e = lane_of(x, w);
+            return b + w;
         }
-        st.tiles_before += lane_of(sum_t, 63);
-        carry += static_cast<uint32_t>(lane_of(static_cast<int>(sum), 63));
     }
-    return st;
+    return -1;
 }
 
 // T tiles of sums of products of digits, as floats: acc = d1 * 256 + d0 fits 32 bits over 256 terms, a third digit is added in fp32.
@@ -155,13 +186,20 @@ __device__ inline void dot_digits(const v4i (&a)[T][N], const v4i (&b)[N][ND], f
         }
 }
 
-__device__ inline float swap_max(float v) {                  // over the four lanes that hold a row
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+// over the four lanes that hold a row, inside the vector ALU: exchanges of rows of 16 and of halves
+template <typename F>
+__device__ inline float over_row(float v, F f) {
+    const uint32_t a = __float_as_uint(v);
+    const auto x = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    const uint32_t b = __float_as_uint(f(__uint_as_float(x[0]), __uint_as_float(x[1])));
+    const auto y = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+    return f(__uint_as_float(y[0]), __uint_as_float(y[1]));
+}
+__device__ inline float swap_max(float v) {
+    return over_row(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ inline float swap_sum(float v) {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    return over_row(v, [](float a, float b) { return a + b; });
 }
 
 // This lane's row of Q (zeros where there is none); its digits, and the exponent of their unit
@@ -319,9 +357,9 @@ __device__ inline void finish(const AttArgs& a, const Extent& e, const TileRows&
     if (a.lse && d == 0) a.lse[t * (static_cast<int>(a.c.heads) * a.group) + h] = s.l > 0.0f ? (s.m + log2f(s.l)) * 0.693147180559945f : -INFINITY;
 }
 
-template <int TYPE, int DB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttArgs a) {
-    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, THREADS = 64 * WAVES, COST = kTileCost<WAVES>;
+template <int TYPE, int DB>
+__global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(AttArgs a) {
+    constexpr int ND = TYPE == FXP_F32 ? 3 : 2, WAVES = kAttWaves, THREADS = 64 * WAVES, COST = kTileCost;
     constexpr int DMAX = 64 * DB, ROW = DMAX + 4;
     __shared__ float s_m[WAVES][kTile], s_l[WAVES][kTile];
     __shared__ float4 s_o4[WAVES * kTile * ROW / 4];
@@ -329,15 +367,21 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
     float* const s_o = reinterpret_cast<float*>(s_o4);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), nd = dim / 4;
-    const Stretch st = survey<WAVES>(a);
-    const uint32_t per = st.per, u0 = st.u0, u1 = min(u0 + per, st.units);
+    uint32_t per = 0;
+    const Found st = find_request(
+        a, [&](const Extent& x) { return static_cast<uint32_t>(x.tiles * heads) * static_cast<uint32_t>(x.pages + COST); },
+        [&](uint32_t units, int most_pages) {
+            per = stretch_of(units, most_pages);
+            return per * blockIdx.x;
+        });
+    const uint32_t u0 = st.at, u1 = min(u0 + per, st.units);
     if (st.b < 0) return;                                               // behind the end of the line
-    int b = st.b, tiles_before = st.tiles_before;
+    int b = st.b;
     Extent e = st.e;
     // the tile of unit u0, and its first unit
-    const uint32_t first_seg = (u0 - st.unit_b) / static_cast<uint32_t>(e.pages + COST);
+    const uint32_t first_seg = (u0 - st.before) / static_cast<uint32_t>(e.pages + COST);
     int tile = static_cast<int>(first_seg / static_cast<uint32_t>(heads)), head = static_cast<int>(first_seg - static_cast<uint32_t>(tile * heads));
-    uint32_t s0 = st.unit_b + first_seg * static_cast<uint32_t>(e.pages + COST);
+    uint32_t s0 = st.before + first_seg * static_cast<uint32_t>(e.pages + COST);
 
     while (s0 < u1) {
         // this workgroup's pages of the tile
@@ -476,7 +520,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
             // the workgroups that have pages of this tile: w_first .. w_last; all but the first have it at the start of their stretch
             const int behind = static_cast<int>(s0 - u0) + COST + e.pages - 1;
             const int w_first = static_cast<int>(blockIdx.x) - (ahead > 0 ? static_cast<int>((static_cast<uint32_t>(ahead) + per - 1) / per) : 0);
-            const int w_last = static_cast<int>(blockIdx.x + static_cast<uint32_t>(behind) / per);
+            const int w_last = static_cast<int>(min(blockIdx.x + static_cast<uint32_t>(behind) / per, gridDim.x - 1));
             const bool whole = w_first == w_last;
             for (int i = threadIdx.x; i < rows * nd; i += THREADS) {
                 const int row = i / nd, d = i % nd * 4;
@@ -511,7 +555,7 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 if (threadIdx.x == 0) {
-                    uint32_t* ticket = a.tickets + (tiles_before + tile) * heads + head;
+                    uint32_t* ticket = a.tickets + w_first;             // no other tile begins there and ends elsewhere
                     const uint32_t others = static_cast<uint32_t>(w_last - w_first);
                     s_last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == others;
                     if (s_last) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -556,11 +600,8 @@ __global__ __launch_bounds__(64 * WAVES, DB <= 2 ? 2 : 1) void k_kv_attend(AttAr
             head = 0;
             if (++tile == e.tiles) {
                 tile = 0;
-                tiles_before += e.tiles;
-                do {
-                    if (++b == a.requests) return;
-                    e = extent(a, b);
-                } while (e.tiles == 0);
+                b = next_request(a, b + 1, e);
+                if (b < 0) return;
             }
         }
     }
@@ -583,32 +624,17 @@ __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_r
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, PAGE_BYTES = 64 * 64 * DB, THREADS = 64 * kRowWaves;
     __shared__ v4i lds[2][2][PAGE_BYTES / 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
-    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), head = blockIdx.x;
+    const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads);
     constexpr int ROWS = kRowWaves * kTile;
 
     // the request and the block of its rows; the last blocks come first, because they see the most pages
-    const int want = static_cast<int>(gridDim.y - 1 - blockIdx.y);
-    int b = -1, block = 0;
-    Extent e = {};
-    {
-        int carry = 0;
-        for (int base = 0; base < a.requests; base += 64) {
-            Extent x_e = {};
-            if (base + lane < a.requests) x_e = extent(a, base + lane);
-            const int v = x_e.n * a.group > a.few_rows ? (x_e.n * a.group + ROWS - 1) / ROWS : 0;
-            const int sum = static_cast<int>(wave_scan(static_cast<uint32_t>(v))), x = carry + sum - v;
-            const uint64_t hit = __builtin_amdgcn_ballot_w64(want >= x && want < x + v);
-            if (hit) {
-                const int w = __builtin_ctzll(hit);
-                b = base + w;
-                block = want - lane_of(x, w);
-                e = {lane_of(x_e.n, w), lane_of(x_e.len, w), lane_of(x_e.tiles, w), lane_of(x_e.page0, w), lane_of(x_e.pages, w), lane_of(x_e.tok0, w)};
-                break;
-            }
-            carry += lane_of(sum, 63);
-        }
-    }
-    if (b < 0) return;
+    const int line = static_cast<int>(gridDim.x - 1 - blockIdx.x), want = line / heads, head = line - want * heads;
+    const Found found = find_request(
+        a, [&](const Extent& x) { return static_cast<uint32_t>(x.n * a.group > a.few_rows ? (x.n * a.group + ROWS - 1) / ROWS : 0); },
+        [&](uint32_t, int) { return static_cast<uint32_t>(want); });
+    if (found.b < 0) return;
+    const int b = found.b, block = want - static_cast<int>(found.before);
+    const Extent e = found.e;
 
     // this lane's rows
     int tok, in_group;
@@ -693,15 +719,20 @@ __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_r
         if (j0 <= any_to && j0 + FXP_KV_PAGE - 1 >= (a.window > 0 ? shift + wave_of.tok - a.window + 1 : 0)) {
             const v4i* const kl = lds[buffer][0];
             const v4i* const vl = lds[buffer][1];
-            v4i kf[4][DB];
+            float s[16];
+            constexpr int QT = 2;                                       // tiles of tokens at a time: four take 32 registers more, and spill in fp32
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+            for (int h = 0; h < 4; h += QT) {
+                v4i kf[QT][DB];
 #pragma unroll
-                for (int i = 0; i < DB; ++i) kf[t][i] = kl[(4 * i + g) * 64 + ((16 * t + col) ^ ((2 * (4 * i + g)) & 15))];
-            float s4[4][4], s[16];
-            dot_digits<ND, DB, 4>(kf, qd, s4);
+                for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = s4[i / 4][i % 4];
+                    for (int i = 0; i < DB; ++i) kf[t][i] = kl[(4 * i + g) * 64 + ((16 * (h + t) + col) ^ ((2 * (4 * i + g)) & 15))];
+                float part[QT][4];
+                dot_digits<ND, DB, QT>(kf, qd, part);
+#pragma unroll
+                for (int i = 0; i < 4 * QT; ++i) s[4 * h + i] = part[i / 4][i % 4];
+            }
             if (dead || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) hide(s, dead, see_to - j0 - 16 * g, see_from - j0 - 16 * g);
             v4i pd[1][ND];
             const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd);
@@ -748,15 +779,11 @@ static bool attention_sizes_ok(int64_t requests, int64_t tokens, int64_t q_heads
            q_heads <= 16384 && q_heads % heads == 0 && dim > 0 && dim <= 256 && dim % 16 == 0 && tokens * q_heads < kMost;
 }
 
-// tiles of all requests, at most
-static int64_t most_tiles(int64_t requests, int64_t tokens, int64_t group) { return (tokens * group + (kTile - 1) * requests) / kTile; }
-
 }  // namespace fxp
 
 extern "C" size_t fxp_kv_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim) {
     if (!fxp::attention_sizes_ok(requests, tokens, q_heads, heads, dim)) return 0;
-    return static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float2)) +
-           fxp::round_up(fxp::most_tiles(requests, tokens, q_heads / heads) * heads * sizeof(uint32_t), 256);
+    return FXP_KV_TICKET_BYTES + static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float2));
 }
 
 extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st, int type, const void* q, int64_t q_token, int64_t q_head,
@@ -795,11 +822,9 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.out_head = out_head;
     a.lse = lse;
     a.window = static_cast<int>(window < (int64_t{1} << 30) ? window : (int64_t{1} << 30));
-    // the tickets stand first: what stands behind them may hold anything
-    const int64_t tiles = most_tiles(st->requests, st->tokens, a.group);
-    if (tiles >= int64_t{1} << 24) return FXP_ERR_DIMS;
     a.tickets = static_cast<uint32_t*>(ws);
-    a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + round_up(tiles * cache->heads * sizeof(uint32_t), 256));
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + FXP_KV_TICKET_BYTES);
+    static_assert(FXP_KV_TICKET_BYTES == kAttGroups * sizeof(uint32_t), "a ticket for each workgroup");
     a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<size_t>(kAttGroups) * 2 * kTile * cache->dim);
     a.group = static_cast<int>(q_heads / cache->heads);
     a.group_inverse = static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group);
@@ -807,31 +832,32 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.vec_out = aligned(out, 4 * size) && out_token % 4 == 0 && out_head % 4 == 0;
     a.scale_log2 = scale * 1.44269504088896f;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (tiles * cache->heads * (st->blocks + kTileCost<4>) >= int64_t{1} << 31) return FXP_ERR_DIMS;
-    auto go = [&](auto type_c, auto db_c) {
+    auto go = [&](auto type_c, auto db_c) -> int {
         constexpr int TYPE = decltype(type_c)::value, DB = decltype(db_c)::value;
         // Many rows a request, and enough blocks of 64 for every CU: the kernel that shares pages among rows (16 heads, 4 of the cache,
         // 128 elements, one request: 1024 rows of 0 earlier tokens 12 us against 13 of the other kernel, 2048 18 / 24, 8192 68 / 219).  It has no
         // way to split a context: with half as many blocks as CUs, 1024 rows behind 4000 tokens take 92 us against 53.  Requests of up to two
         // tiles stay with the other kernel (32 rows: 24 us against 30; 35 rows, three tiles: 36 / 28).
         constexpr int kRows = kRowWaves * kTile;
-        const int64_t row_blocks = (st->tokens * a.group + (kRows - 1) * st->requests) / kRows;
-        const bool many = st->tokens * a.group > kFewRows * st->requests && row_blocks * cache->heads >= 256 && row_blocks <= 65535;
+        const int64_t blocks = (st->tokens * a.group + (kRows - 1) * st->requests) / kRows * cache->heads;
+        const bool many = st->tokens * a.group > kFewRows * st->requests && blocks >= 256 && blocks < int64_t{1} << 24;
         a.few_rows = many && st->requests > 1 ? kFewRows : 0;
+        // units of the line, which are counted in 32 bits
+        const int64_t tiles = (st->tokens * a.group + (kTile - 1) * st->requests) / kTile, line_tiles = a.few_rows ? std::min(tiles, 2 * st->requests) : tiles;
+        if ((!many || a.few_rows) && line_tiles * cache->heads * (st->blocks + kTileCost) >= int64_t{1} << 31) return FXP_ERR_DIMS;
         if (many)
-            hipLaunchKernelGGL((k_kv_attend_rows<TYPE, DB>), dim3(static_cast<unsigned>(cache->heads), static_cast<unsigned>(row_blocks)),
-                               dim3(64 * kRowWaves), 0, s, a);
-        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB, 4>), dim3(kAttGroups), dim3(256), 0, s, a);
+            hipLaunchKernelGGL((k_kv_attend_rows<TYPE, DB>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kRowWaves), 0, s, a);
+        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroups), dim3(64 * kAttWaves), 0, s, a);
+        return launch_status();
     };
     auto of_type = [&](auto type_c) {
         const int64_t db = (cache->dim + 63) / 64;
-        if (db == 1) go(type_c, std::integral_constant<int, 1>{});
-        else if (db == 2) go(type_c, std::integral_constant<int, 2>{});
-        else if (db == 3) go(type_c, std::integral_constant<int, 3>{});
-        else go(type_c, std::integral_constant<int, 4>{});
+        if (db == 1) return go(type_c, std::integral_constant<int, 1>{});
+        if (db == 2) return go(type_c, std::integral_constant<int, 2>{});
+        if (db == 3) return go(type_c, std::integral_constant<int, 3>{});
+        return go(type_c, std::integral_constant<int, 4>{});
     };
-    if (type == FXP_F32) of_type(std::integral_constant<int, FXP_F32>{});
-    else if (type == FXP_BF16) of_type(std::integral_constant<int, FXP_BF16>{});
-    else of_type(std::integral_constant<int, FXP_F16>{});
-    return launch_status();
+    if (type == FXP_F32) return of_type(std::integral_constant<int, FXP_F32>{});
+    if (type == FXP_BF16) return of_type(std::integral_constant<int, FXP_BF16>{});
+    return of_type(std::integral_constant<int, FXP_F16>{});
 }

@@ -568,6 +568,7 @@ def sgd16_step_multi(buf, lr, momentum=0.0, weight_decay=0.0, seed=0, step=0, ro
 # ---- serving: a paged cache of mapped keys and values, attention over it, products with 4-bit weights ----
 
 KV_PAGE = 64            # tokens of a page (FXP_KV_PAGE)
+KV_TICKET_BYTES = 2048  # of the workspace of fxp_kv_attention, zero between calls (FXP_KV_TICKET_BYTES)
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
@@ -704,7 +705,8 @@ class AttentionBuffers:
         self.nbytes = int(lib().fxp_kv_attention_workspace_bytes(requests, tokens, q_heads, cache.heads, cache.dim))
         if self.nbytes == 0:
             raise FxpError("bad sizes: q_heads must be a multiple of the cache's heads")
-        self.ws = torch.zeros(self.nbytes, dtype=torch.uint8, device=cache.device)
+        self.ws = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.device)
+        self.ws[:KV_TICKET_BYTES].zero_()
 
 
 def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=None):

@@ -221,6 +221,31 @@ def test_attention_answers_alike_every_time(fxp):
         assert torch.equal(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale), want)
 
 
+def test_attention_calls_of_many_sizes_take_turns_with_one_workspace(fxp):
+    """What one call left behind the tickets is no ticket of the next: other numbers of tiles, other dims, other types."""
+    say("kv_attention, one workspace, many sizes")
+    cases = [Case(fxp, [3000], [1], 2, 1, 256, "fp32"), Case(fxp, [2000, 900, 640], [3, 1, 2], 32, 4, 64, "bf16"), Case(fxp, [4000], [2], 2, 2, 16, "fp16"),
+             Case(fxp, [700] * 20, [1] * 20, 16, 8, 128, "bf16"), Case(fxp, [1500], [40], 4, 4, 192, "fp32")]
+    buf = fxp.AttentionBuffers(20, 40, 16, cases[0].cache)
+    assert not buf.ws[:fxp.KV_TICKET_BYTES].any()
+    buf.ws[fxp.KV_TICKET_BYTES:].fill_(0xff)
+    for c in cases + cases[::-1]:
+        c.check(fxp.kv_attention(c.dq, c.cache, c.tab, buf, scale=c.scale))
+        assert not buf.ws[:fxp.KV_TICKET_BYTES].any()
+
+
+@pytest.mark.parametrize("requests", [65, 200, 4200])
+def test_attention_of_a_padded_batch(fxp, requests):
+    """Most requests have no new tokens, some of them cached ones; one long request in front, one behind them all."""
+    say("kv_attention, padded batch", requests)
+    lens, news = np.zeros(requests, int), np.zeros(requests, int)
+    lens[1], news[1], lens[-1], news[-1], lens[requests // 2], news[requests // 2], lens[3] = 2500, 2, 1300, 1, 64, 1, 200
+    c = Case(fxp, lens.tolist(), news.tolist(), 8, 2, 64, "bf16", behind=3)
+    out = torch.full((c.T, 8, 64), 9.0, dtype=c.dq.dtype, device="cuda")
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, out=out))
+    assert (out[c.first[-1]:] == 9).all()
+
+
 def test_attention_over_a_cache_past_32_bits(fxp):
     say("kv_attention behind 4 GiB of keys")
     c = Case(fxp, [130, 64], [1, 2], 16, 8, 256, "bf16", spare=33000)
