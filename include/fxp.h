@@ -427,9 +427,10 @@ int64_t fxp_kv_max_runs(int64_t requests, int64_t tokens);
 
 /* Makes room for n_new[b] (device, >= 0) more tokens of each request and fills the tables of the step.  Pages are
  * taken from the top of the stack in the order of the requests.  A request that would outgrow its row of
- * block_table is refused; so is, from the first one that the stack cannot serve on, every request that needs a page.
+ * block_table is refused; so is, from the first one that the stack cannot serve on, every request that needs a page, and from the first one
+ * whose tokens pass `tokens` on, every request that has any.
  * A refused request keeps its length and its row, its tokens get slot -1 and runs on page -1 (fxp_kv_append skips them).
- * Tokens and runs beyond `tokens` and the runs' capacity are not written.  Lengths that are negative count as 0.
+ * Tokens and runs beyond `tokens` and the runs' capacity are not written, but counted in first.  Lengths that are negative count as 0.
  * ws: NULL, or at least 256 bytes, zero before the first call that uses them, which every call leaves zero; required where
  * lens_after or n_free_after is the input itself. */
 int fxp_kv_tables(const fxp_kv_step* step, const int32_t* n_new, void* ws, size_t ws_bytes, void* stream);
@@ -478,14 +479,15 @@ int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int typ
  * the tile and input k are in piece 16 * ((k % S) / (S / 4)) + r of 16 bytes, byte (k / S) * (S / 8) + k % (S / 8) of it, low
  * half if (k % (S / 4)) < S / 8, else the high half, in two's complement.  scales: uint8 biased exponents, 1 .. 254,
  * [ceil(N / 16), ceil(K / 128) * 128 / group, 16].  Inputs and outputs past K and N are zero.
- * K <= 2^20, N <= 2^24; K * ceil16(M) <= 2^34. */
+ * K <= 2^20, N <= 2^24, M < 2^20; ceil128(K) * M <= 2^34. */
 size_t fxp_w4_packed_bytes(int64_t K, int64_t N);
 size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group);
 /* W: K rows of N elements of `type`, row stride ldw >= N.  packed 16-byte, scales 4-byte aligned. */
 int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales, void* stream);
 /* Y[M,N] = X[M,K] * W.  X, Y of `type`, row strides ldx >= K, ldy >= N.  Made for few rows (one pass over the weights for each 64 of
  * them); any M is right.  A group of a row of X is a fixed-point number of two signed 8-bit digits (three for fp32)
- * under its own scale: products are exact int32 sums over a group, sums over groups fp32.
+ * under its own scale: products are exact int32 sums over a group, sums over groups fp32.  (An fp32 group whose largest magnitude is below
+ * 2^-121 counts as zero.)  Y must not overlap X.
  * ws: fxp_w4_workspace_bytes bytes (0 on bad arguments), 256-byte aligned; not used, and may be NULL, for M <= 2. */
 size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group);
 int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, int64_t K, int64_t N, const uint8_t* packed, const uint8_t* scales,

@@ -51,8 +51,8 @@ __device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_
     fits = false;
     r.len = r.after = r.had = 0;
     if (b >= st.requests) return v;
-    const int64_t len = max(st.lens[b], 0), n = min(static_cast<int64_t>(max(n_new[b], 0)), st.tokens), after = len + n;
-    fits = after <= st.blocks * FXP_KV_PAGE;
+    const int64_t len = max(st.lens[b], 0), asked = max(n_new[b], 0), n = min(asked, st.tokens), after = len + n;
+    fits = asked == n && after <= st.blocks * FXP_KV_PAGE;
     r.len = static_cast<int>(len);
     r.after = static_cast<int>(min(after, (int64_t{1} << 31) - 1));
     r.had = static_cast<int>((len + FXP_KV_PAGE - 1) / FXP_KV_PAGE);
@@ -60,6 +60,12 @@ __device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_
     v.need = fits ? static_cast<int>((after + FXP_KV_PAGE - 1) / FXP_KV_PAGE) - r.had : 0;
     v.runs = n ? static_cast<int>((after - 1) / FXP_KV_PAGE - len / FXP_KV_PAGE) + 1 : 0;
     return v;
+}
+
+// Whether a request finds room: in its row, in the stack and among the step's tokens; `x` is the sum of those before it.  Both sums only
+// grow, so the requests that are served and take pages come before those that find too few.
+__device__ inline bool has_room(const fxp_kv_step& st, bool fits, const Three& v, const Three& x, int n_free) {
+    return fits && (v.need == 0 || x.need + v.need <= n_free) && (v.tokens == 0 || (x.tokens >= 0 && int64_t{x.tokens} + v.tokens <= st.tokens));
 }
 
 // lengths of all requests and the stack's height, for the workgroup that is last to have read them
@@ -74,7 +80,7 @@ __device__ inline void commit_lengths(const fxp_kv_step& st, const int32_t* n_ne
         bool fits;
         const Three v = asks(st, n_new, base + threadIdx.x, r, fits);
         const Three x = add3(carry, block_scan3(v, lds, total));
-        const bool served = fits && (v.need == 0 || x.need + v.need <= n_free);
+        const bool served = has_room(st, fits, v, x, n_free);
         if (base + threadIdx.x < st.requests) st.lens_after[base + threadIdx.x] = served ? r.after : st.lens[base + threadIdx.x];
         if (served && v.need) atomicMax(&taken, x.need + v.need);
         carry = add3(carry, total);
@@ -109,7 +115,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         bool fits;
         const Three v = asks(st, n_new, b, r, fits);
         const Three x = add3(carry, block_scan3(v, lds, total));
-        r.served = fits && (v.need == 0 || x.need + v.need <= n_free);
+        r.served = has_room(st, fits, v, x, n_free);
         r.first = x.tokens;
         r.need0 = x.need;
         r.run0 = x.runs;
@@ -446,7 +452,7 @@ extern "C" int fxp_kv_tables(const fxp_kv_step* st, const int32_t* n_new, void* 
     if (!st) return FXP_ERR_NULL;
     constexpr int64_t kMost = int64_t{1} << 31;
     if (st->requests <= 0 || st->blocks <= 0 || st->tokens < 0 || st->pages <= 0 || st->requests >= kMost || st->tokens >= kMost ||
-        st->pages >= kMost || st->blocks * FXP_KV_PAGE >= kMost || st->blocks >= kMost)
+        st->pages >= kMost || st->blocks >= kMost / FXP_KV_PAGE)
         return FXP_ERR_DIMS;
     if (!n_new || !st->lens || !st->free_pages || !st->n_free || !st->block_table || !st->lens_after || !st->n_free_after || !st->first ||
         !st->refused || (st->tokens && (!st->slots || !st->positions || !st->runs)))

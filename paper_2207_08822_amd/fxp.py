@@ -593,6 +593,12 @@ def _index(t, what, shape=None, dtype=torch.int32):
     return t
 
 
+def _here(owner, what):
+    """`owner` (a cache, tables, buffers, weights) is on the current device; .index is its device's."""
+    if owner.index != torch._C._cuda_getDevice():
+        raise FxpError(f"{what} is on another device than the current one")
+
+
 def _row_stride(t, what):
     """Elements from one row of a matrix to the next; rows may not overlap."""
     rows, cols = t.shape
@@ -629,7 +635,7 @@ class KvCache:
         if dim % 16 or dim > 256 or not 2 <= bits <= 8:
             raise FxpError("dim must be a multiple of 16, at most 256, and bits in 2..8")
         self.kq, self.vq, self.ek, self.ev, self.bits = kq, vq, ek, ev, bits
-        self.pages, self.heads, self.dim, self.device = pages, heads, dim, kq.device
+        self.pages, self.heads, self.dim, self.device, self.index = pages, heads, dim, kq.device, kq.get_device()
         self.c = _KvCache(_p(kq), _p(vq), _p(ek), _p(ev), pages, heads, dim, bits)
         self.ref = ctypes.byref(self.c)
 
@@ -656,14 +662,17 @@ class KvTables:
         self.runs[:, 2] = -1
         self.refused = torch.zeros(requests, **i32)
         self.ws = torch.zeros(256, dtype=torch.uint8, device=device)
+        self.index = self.ws.get_device()
         self.c = _KvStep(requests, blocks, tokens, pages, _p(self.lens), _p(self.free), _p(self.n_free), _p(self.block_table), _p(self.lens_after),
                          _p(self.n_free_after), _p(self.first), _p(self.slots), _p(self.positions), _p(self.runs), _p(self.refused))
         self.ref = ctypes.byref(self.c)
 
 
 def kv_tables(n_new, tab):
-    """Room for n_new[b] more tokens of each request, and the step's tables (tab.first, slots, positions, runs, refused); returns tab."""
+    """Room for n_new[b] more tokens of each request, and the step's tables (tab.first, slots, positions, runs, refused); returns tab.  A
+    request that finds no room in its row, on the stack or among tab.tokens rows is refused and keeps its length."""
     _index(n_new, "n_new", (tab.requests,))
+    _here(tab, "tab")
     _check(lib().fxp_kv_tables(tab.ref, n_new.data_ptr(), tab.ws.data_ptr(), 256, _stream()), "fxp_kv_tables")
     return tab
 
@@ -680,6 +689,7 @@ def kv_append(k, v, cache, runs):
     code = _served(k, "k", 3)
     if _served(v, "v", 3) != code or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.dim):
         raise FxpError("k and v must be [tokens, heads, dim] of the cache and of one type")
+    _here(cache, "cache")
     runs = _runs(runs)
     _check(lib().fxp_kv_append(cache.ref, code, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), k.shape[0],
                                runs.data_ptr(), runs.shape[0], _stream()), "fxp_kv_append")
@@ -688,6 +698,7 @@ def kv_append(k, v, cache, runs):
 def kv_load(cache, runs, tokens, dtype=torch.float32, out=None):
     """(k, v) [tokens, heads, dim]: the values that the cached tokens of `runs` stand for; out: the two tensors to fill."""
     runs = _runs(runs)
+    _here(cache, "cache")
     shape = (tokens, cache.heads, cache.dim)
     k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
     code = _served(k, "k", 3)
@@ -707,6 +718,7 @@ class AttentionBuffers:
             raise FxpError("bad sizes: q_heads must be a multiple of the cache's heads")
         self.ws = torch.empty(self.nbytes, dtype=torch.uint8, device=cache.device)
         self.ws[:KV_TICKET_BYTES].zero_()
+        self.index = self.ws.get_device()
 
 
 def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=None):
@@ -716,16 +728,17 @@ def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=No
     tokens, q_heads, dim = q.shape
     if tokens != tab.tokens or dim != cache.dim:
         raise FxpError("q must be [tokens, q_heads, dim] of the tables and the cache")
+    _here(cache, "cache")
+    _here(tab, "tab")
     if out is None:
         out = q.new_empty((tokens, q_heads, dim))
     elif _served(out, "out", 3) != code or out.shape != q.shape or (tokens > 1 and out.stride(0) < dim) or (q_heads > 1 and out.stride(1) < dim):
         raise FxpError("out must have the shape and type of q, and rows that do not overlap")
     if lse is not None:
-        _dev(lse, torch.float32, "lse")
-        if tuple(lse.shape) != (tokens, q_heads):
-            raise FxpError("lse must be [tokens, q_heads]")
+        _index(lse, "lse", (tokens, q_heads), torch.float32)
     if buf is None:
         buf = AttentionBuffers(tab.requests, tokens, q_heads, cache)
+    _here(buf, "buf")
     _check(lib().fxp_kv_attention(cache.ref, tab.ref, code, q.data_ptr(), q.stride(0), q.stride(1), q_heads, dim ** -0.5 if scale is None else scale,
                                   window, out.data_ptr(), out.stride(0), out.stride(1), _p(lse), buf.ws.data_ptr(), buf.nbytes, _stream()),
            "fxp_kv_attention")
@@ -743,7 +756,7 @@ class W4Weights:
         if packed.numel() != lib().fxp_w4_packed_bytes(K, N) or scales.numel() != lib().fxp_w4_scale_bytes(K, N, group):
             raise FxpError("packed or scales have another size than K, N and group ask for")
         self.packed, self.scales, self.K, self.N, self.group = packed, scales, K, N, group
-        self.pointers = packed.data_ptr(), scales.data_ptr()
+        self.pointers, self.index = (packed.data_ptr(), scales.data_ptr()), packed.get_device()
 
 
 def pack4(W, group=64):
@@ -762,11 +775,14 @@ def linear4(x, w, out=None, ws=None):
     M, K = x.shape
     if K != w.K:
         raise FxpError("x must be [M, K] of the weights")
+    _here(w, "w")
     if out is None:
         out = x.new_empty((M, w.N))
     elif _served(out, "out", 2) != code or tuple(out.shape) != (M, w.N):
         raise FxpError("out must be [M, N] of x's type")
-    if ws is None and M > 2:
+    if ws is not None:
+        _index(ws, "ws", dtype=torch.uint8)
+    elif M > 2:
         ws = x.new_empty(int(lib().fxp_w4_workspace_bytes(code, M, K, w.group)), dtype=torch.uint8)
     packed, scales = w.pointers
     _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), _row_stride(out, "out"),

@@ -13,12 +13,13 @@ def tables(lens, n_new, table, free, n_free, tokens, rows):
     slots, positions = np.full(tokens, -1, np.int64), np.full(tokens, -1, np.int64)
     runs = []
     for b in range(B):
-        n, at = int(n_new[b]), int(lens[b])
+        asked, at = int(n_new[b]), int(lens[b])
+        n = min(asked, tokens)
         need = -(-(at + n) // PAGE) - -(-at // PAGE)
-        fits = at + n <= blocks * PAGE
+        fits = at + n <= blocks * PAGE and asked == n
         if fits:
             sum_need += need
-        served = fits and (need == 0 or sum_need <= n_free)
+        served = fits and (need == 0 or sum_need <= n_free) and (n == 0 or first[-1] + n <= tokens)
         if served:
             for j in range(need):
                 table[b, -(-at // PAGE) + j] = free[n_free - 1 - taken - j]
@@ -28,14 +29,14 @@ def tables(lens, n_new, table, free, n_free, tokens, rows):
             k = min(end, (at // PAGE + 1) * PAGE) - at
             page = int(table[b, at // PAGE]) if served else -1
             runs.append((t, k, page, at % PAGE))
-            for i in range(k):
+            for i in range(max(min(k, tokens - t), 0)):
                 positions[t + i] = at + i
                 slots[t + i] = page * PAGE + at % PAGE + i if page >= 0 else -1
             t, at = t + k, at + k
         first.append(t)
         after.append(int(lens[b]) + n if served else int(lens[b]))
         refused.append(not served)
-    assert len(runs) <= rows
+    runs = runs[:rows]
     runs += [(0, 0, -1, 0)] * (rows - len(runs))
     return dict(block_table=table, first=np.array(first), lens_after=np.array(after), n_free_after=np.array([n_free - taken]), slots=slots,
                 positions=positions, runs=np.array(runs).reshape(rows, 4), refused=np.array(refused, dtype=np.int64))

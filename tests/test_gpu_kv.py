@@ -66,6 +66,23 @@ def test_tables(fxp, B, longest, most, blocks, short, behind, in_place):
         check_tables(tab, want)
 
 
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("B,most,tokens", [(4, 50, 0), (5, 90, 100), (900, 3, 700), (900, 40, 9000), (6, 500, 70), (1, 40, 39)])
+def test_tables_of_a_step_with_too_few_rows(fxp, B, most, tokens, in_place):
+    """From the first request whose tokens pass the step's on, those that have any are refused and keep their lengths; others are served."""
+    say("kv_tables, more new tokens than rows", (B, most, tokens, in_place))
+    rng = np.random.default_rng(B + most)
+    lens, n_new = rng.integers(0, 200, B), rng.integers(0, most + 1, B)
+    n_new[-1] = most
+    assert n_new.sum() > tokens
+    tab, table, free = make_tables(fxp, rng, lens, n_new, 12, 9 * B, tokens, in_place)
+    want = ref.tables(lens, n_new, table, free, 9 * B, tokens, len(tab.runs))
+    fxp.kv_tables(dev(n_new.astype(np.int32)), tab)
+    check_tables(tab, want)
+    refused = host(tab.refused).astype(bool)
+    assert refused.any() and (B < 900 or not refused.all()) and np.array_equal(host(tab.lens_after)[refused], lens[refused])
+
+
 def test_tables_step_by_step_from_a_graph(fxp):
     say("kv_tables, ten replays of one captured step in place")
     rng = np.random.default_rng(5)

@@ -133,3 +133,20 @@ def test_the_same_answer_in_one_prompt_and_token_by_token(fxp):
     k1, v1 = fxp.kv_load(at_once, torch.tensor([[0, 64, 0, 0], [64, 6, 1, 0]], dtype=torch.int32, device="cuda"), n)
     k2, v2 = fxp.kv_load(in_steps, torch.tensor([[0, 64, 0, 0], [64, 6, 1, 0]], dtype=torch.int32, device="cuda"), n)
     assert torch.equal(k1, k2) and torch.equal(v1, v2)
+
+
+def test_what_lies_on_another_device_is_refused(fxp):
+    """Pointers of another device than the current one, whose stream the calls use, must not reach a kernel."""
+    say("caches, tables, buffers and weights marked as another device's")
+    cache, tab, w = fxp.KvCache(4, H, D), fxp.KvTables(2, 2, 2, 4), fxp.pack4(torch.randn((D, 16), device="cuda"))
+    buf, q, n_new = fxp.AttentionBuffers(2, 2, QH, cache), torch.zeros((2, QH, D), device="cuda"), torch.ones(2, dtype=torch.int32, device="cuda")
+    calls = [(tab, lambda: fxp.kv_tables(n_new, tab)), (cache, lambda: fxp.kv_append(q[:, :H], q[:, :H], cache, tab.runs)),
+             (cache, lambda: fxp.kv_load(cache, tab.runs, 2)), (w, lambda: fxp.linear4(q[:, 0], w))]
+    calls += [(x, lambda: fxp.kv_attention(q, cache, tab, buf)) for x in (cache, tab, buf)]
+    for owner, call in calls:
+        call()
+        owner.index += 1
+        with pytest.raises(fxp.FxpError, match="another device"):
+            call()
+        owner.index -= 1
+    torch.cuda.synchronize()
