@@ -484,7 +484,7 @@ size_t fxp_w4_packed_bytes(int64_t K, int64_t N);
 size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group);
 /* W: K rows of N elements of `type`, row stride ldw >= N.  packed 16-byte, scales 4-byte aligned. */
 int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales, void* stream);
-/* Y[M,N] = X[M,K] * W.  X, Y of `type`, row strides ldx >= K, ldy >= N.  Made for few rows (one pass over the weights for each 64 of
+/* Y[M,N] = X[M,K] * W.  X, Y of `type`, row strides ldx >= K, ldy >= N.  Made for few rows (one pass over the weights for each 32 to 64 of
  * them); any M is right.  A group of a row of X is a fixed-point number of two signed 8-bit digits (three for fp32)
  * under its own scale: products are exact int32 sums over a group, sums over groups fp32.  (An fp32 group whose largest magnitude is below
  * 2^-121 counts as zero.)  Y must not overlap X.

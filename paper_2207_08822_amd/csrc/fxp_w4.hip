@@ -191,11 +191,12 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
 // One or two rows, one launch.  a.k_waves waves share a tile of outputs; a wave has every k_waves-th tile of 128 inputs, eight on their
 // way at a time, and turns its own part of x into digits (a lane 16 inputs of a row, which is all of eight tiles at once).  With so few rows a matrix instruction
 // would leave 15 of 16 columns empty and its scaling (22 vector instructions a group) would be for nothing: here a lane sums the 16
-// mantissas it has loaded by byte dot products (one for four of them and a digit) and scales ONE sum a group.
+// mantissas it has loaded by byte dot products (one for four of them and a digit) and scales ONE sum a group.  Two workgroups a CU but for two
+// rows in groups of 32: 128 registers are too few for their scales (4096 x 4096, bf16: 10.3 us with them, 7.8 with 256; fp32 12.4 / 8.9).
 constexpr int kW4Ahead = 8;
 
 template <int TYPE, int GROUP, int ROWS>
-__global__ __launch_bounds__(kW4Threads, 4) void k_w4_rows(W4Args a) {
+__global__ __launch_bounds__(kW4Threads, GROUP == 32 && ROWS == 2 ? 2 : 4) void k_w4_rows(W4Args a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT, U = kW4Ahead;
     __shared__ v4i s_digits[kW4Waves][U][ROWS][ND][8];          // pieces of 16 inputs
     __shared__ float s_unit[kW4Waves][U][ROWS][GT];
@@ -468,16 +469,22 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
             constexpr integral_constant<int, 2> two{};
             constexpr integral_constant<int, 4> four{};
             constexpr integral_constant<int, 3> three{};
+            // Three digits and four scales of two tiles of rows: registers for two tiles of outputs (23 rows, 4096 x 28672: two 65 us, three 88,
+            // four 112), and none for four tiles of rows (64 rows: 112 us as two passes, 162 as one).
+            constexpr bool kTight = TYPE == FXP_F32 && GROUP == 32;
             auto of_rows = [&](auto nt_c) {
                 if (a.m_tiles == 1) go(nt_c, one, two);
+                else if constexpr (kTight && decltype(nt_c)::value > 2) go(two, two, two);
                 else go(nt_c, two, two);
             };
             // As many tiles of outputs to a workgroup as leave one for each CU: every wave reads its rows' digits (4 KB a tile of rows) for
             // 1 KB of weights a tile of outputs, and that is what bounds it (23 rows, 4090 x 11007: three tiles 10.5 us, two 13.8; 8192 x 8192,
-            // two tiles 21.0 in all, one 25.8).
+            // two tiles 21.0 in all, one 25.8).  From 33 rows on, four tiles of rows read the weights half as often as two (64 rows, bf16, groups of
+            // 64: 8192 x 8192 28 us against 32, 1024 x 16384 14 / 18, 4090 x 11007 28 / 27).
             constexpr int kCus = 256;
-            if (a.m_tiles > 2) go(two, four, one);
-            else if (a.n_tiles <= kCus) of_rows(one);
+            if constexpr (!kTight)
+                if (a.m_tiles > 2) return go(two, four, one);
+            if (a.n_tiles <= kCus) of_rows(one);
             else if (a.n_tiles <= 2 * kCus) of_rows(two);
             else if (a.n_tiles <= 3 * kCus) of_rows(three);
             else of_rows(four);

@@ -74,7 +74,7 @@ def bound(x, W, y, group, unit_bits, half):
 
 
 SIZES = [(1, 1, 1), (1, 64, 16), (2, 130, 33), (16, 128, 48), (17, 1000, 100), (1, 4096, 20), (5, 768, 2304), (64, 300, 70), (65, 257, 17),
-         (130, 640, 40), (3, 20000, 5)]
+         (130, 640, 40), (3, 20000, 5), (4, 200, 4100), (20, 129, 8190), (6, 64, 8200), (18, 300, 12288), (3, 96, 12300), (31, 200, 12300), (35, 200, 12300)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
