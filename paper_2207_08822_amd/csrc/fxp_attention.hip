@@ -611,9 +611,9 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
 //
 // A workgroup has 64 consecutive rows of one request and head, each of its four waves a tile of 16.  The waves share the pages:
 // each page goes through LDS once (two buffers, the next page's loads in registers meanwhile).  Per page a wave issues 16 DB
-// matrix instructions of 16 cycles (two digits) and, at DB = 2, some 270 vector instructions of 4; they follow one another rather than
-// overlap (1650 cycles a page and SIMD measured, 1140 + 512), which is what bounds it.  32 rows a wave, which halves the LDS
-// reads, took 303 us in place of 249 for 4600 tokens behind up to 7000 (16 heads over 4 of 128): fewer, longer workgroups.
+// matrix instructions of 16 cycles (two digits) and, at DB = 2, some 290 vector instructions, which is what bounds it: the vector ALU is busy 84 % of
+// the time, the matrix cores 31 % (4600 rows behind up to 7000, 16 heads over 4 of 128: 245 us; 1, 2 and 3 workgroups a CU take
+// 480, 305 and 250).  32 rows a wave, which halves the LDS reads, took 303 us: fewer, longer workgroups.
 // In LDS the keys stand by pieces of 16 elements, [dim / 16][64 places][16], the places in the order that the A operand takes
 // them, turned by twice the piece's number: 16 lanes then read 256 consecutive bytes, and the 16 pieces that 16
 // lanes write (8 of a token, two tokens) fall on 16 different ones.

@@ -776,15 +776,18 @@ def linear4(x, w, out=None, ws=None):
     if K != w.K:
         raise FxpError("x must be [M, K] of the weights")
     _here(w, "w")
+    ldy = w.N
     if out is None:
-        out = x.new_empty((M, w.N))
-    elif _served(out, "out", 2) != code or tuple(out.shape) != (M, w.N):
+        out = x.new_empty((M, ldy))
+    elif _served(out, "out", 2) != code or tuple(out.shape) != (M, ldy):
         raise FxpError("out must be [M, N] of x's type")
+    else:
+        ldy = _row_stride(out, "out")
     if ws is not None:
         _index(ws, "ws", dtype=torch.uint8)
     elif M > 2:
         ws = x.new_empty(int(lib().fxp_w4_workspace_bytes(code, M, K, w.group)), dtype=torch.uint8)
     packed, scales = w.pointers
-    _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), _row_stride(out, "out"),
-                               _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
+    _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), ldy, _p(ws),
+                               ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
     return out
