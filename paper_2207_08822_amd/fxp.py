@@ -572,12 +572,18 @@ KV_TICKET_BYTES = 2048  # of the workspace of fxp_kv_attention, zero between cal
 _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
+def _on_current(t, what):
+    """t is a tensor on the current device, whose stream the calls use."""
+    at = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if at < 0:
+        raise FxpError(f"{what} must be a CUDA tensor: libfxp has no CPU path")
+    if at != torch._C._cuda_getDevice():
+        raise FxpError(f"{what} is on another device than the current one")
+
+
 def _served(t, what, dims):
     """The type code of a float tensor of `dims` dimensions on the current device whose last dimension is contiguous."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise FxpError(f"{what} must be a CUDA tensor: libfxp has no CPU path")
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise FxpError(f"{what} is on another device than the current one")
+    _on_current(t, what)
     code = _TYPES.get(t.dtype)
     if code is None or t.dim() != dims or not (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] == 1):
         raise FxpError(f"{what} must be a {dims}-dimensional float32, bfloat16 or float16 tensor with a contiguous last dimension")
@@ -585,10 +591,10 @@ def _served(t, what, dims):
 
 
 def _index(t, what, shape=None, dtype=torch.int32):
-    t = _dev(t, dtype, what)
-    if t.get_device() != torch._C._cuda_getDevice():
-        raise FxpError(f"{what} is on another device than the current one")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    _on_current(t, what)
+    if t.dtype != dtype or not t.is_contiguous():
+        raise FxpError(f"{what} must be a contiguous {dtype} tensor")
+    if shape is not None and t.shape != shape:
         raise FxpError(f"{what} must have the shape {tuple(shape)}")
     return t
 
@@ -687,7 +693,7 @@ def _runs(runs):
 def kv_append(k, v, cache, runs):
     """Maps the new tokens k, v [tokens, heads, dim] (any strides of the first two) into the cache; runs: KvTables.runs."""
     code = _served(k, "k", 3)
-    if _served(v, "v", 3) != code or k.shape != v.shape or tuple(k.shape[1:]) != (cache.heads, cache.dim):
+    if _served(v, "v", 3) != code or k.shape != v.shape or k.shape[1:] != (cache.heads, cache.dim):
         raise FxpError("k and v must be [tokens, heads, dim] of the cache and of one type")
     _here(cache, "cache")
     runs = _runs(runs)
@@ -700,11 +706,17 @@ def kv_load(cache, runs, tokens, dtype=torch.float32, out=None):
     runs = _runs(runs)
     _here(cache, "cache")
     shape = (tokens, cache.heads, cache.dim)
-    k, v = out if out is not None else (torch.empty(shape, dtype=dtype, device=cache.device), torch.empty(shape, dtype=dtype, device=cache.device))
-    code = _served(k, "k", 3)
-    for t, name in ((k, "k"), (v, "v")):
-        if tuple(t.shape) != shape or not t.is_contiguous() or _served(t, name, 3) != code:
-            raise FxpError("the outputs must be contiguous [tokens, heads, dim] tensors of one type")
+    if out is None:
+        code = _TYPES.get(dtype)
+        if code is None:
+            raise FxpError("dtype must be float32, bfloat16 or float16")
+        k, v = cache.kq.new_empty(shape, dtype=dtype), cache.kq.new_empty(shape, dtype=dtype)
+    else:
+        k, v = out
+        code = _served(k, "k", 3)
+        for t, name in ((k, "k"), (v, "v")):
+            if _served(t, name, 3) != code or t.shape != shape or not t.is_contiguous():
+                raise FxpError("the outputs must be contiguous [tokens, heads, dim] tensors of one type")
     _check(lib().fxp_kv_load(cache.ref, code, k.data_ptr(), v.data_ptr(), tokens, runs.data_ptr(), runs.shape[0], _stream()), "fxp_kv_load")
     return k, v
 
@@ -779,7 +791,7 @@ def linear4(x, w, out=None, ws=None):
     ldy = w.N
     if out is None:
         out = x.new_empty((M, ldy))
-    elif _served(out, "out", 2) != code or tuple(out.shape) != (M, ldy):
+    elif _served(out, "out", 2) != code or out.shape != (M, ldy):
         raise FxpError("out must be [M, N] of x's type")
     else:
         ldy = _row_stride(out, "out")

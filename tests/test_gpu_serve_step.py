@@ -149,4 +149,6 @@ def test_what_lies_on_another_device_is_refused(fxp):
         with pytest.raises(fxp.FxpError, match="another device"):
             call()
         owner.index -= 1
+    with pytest.raises(fxp.FxpError, match="dtype"):
+        fxp.kv_load(cache, tab.runs, 2, dtype=torch.int8)
     torch.cuda.synchronize()
