@@ -44,6 +44,7 @@ struct AttArgs {
     int vec_q, vec_out;
     float scale_log2;       // scale * log2(e)
     int window;             // 0: none
+    float join_turns;       // of a workgroup over the elements of a tile, four a thread, as the requests are on average
     int few_rows;           // requests of more rows are the other kernel's; 0: one kernel has all
 };
 
@@ -68,11 +69,13 @@ __device__ inline Extent extent(const AttArgs& a, int64_t b) {
 // whose stretch is many short tiles takes as long as several others.)
 constexpr int kTileCost = 2 * kAttWaves;
 
-// Pages of a stretch: equal shares, but no fewer than one a wave, and so many that the parts of the longest tile are at
-// most some twice as many as the pages that a wave has of them (they are joined one after the other).
-__device__ inline uint32_t stretch_of(uint32_t units, int most_pages) {
+// Pages of a stretch: equal shares, but no fewer than one a wave, nor than this.  A stretch of p pages takes p / kAttWaves turns and the longest tile,
+// of P pages, then has P / p parts, which one workgroup joins in `turns` turns over a tile's elements: the sum is least near p ~ sqrt(P turns).
+// Measured best factors: 0.5 to 0.7 at one turn (1 head of 16, 4 of 128: 131000 tokens 59 us, 66 with 1.0), 0.7 to 1 at two and three (16 x 128, 14 x 160), 1
+// at four (16 x 256, 2 x 32000 tokens: 52 us, 69 with 0.7, 62 with 2).
+__device__ inline uint32_t stretch_of(const AttArgs& a, uint32_t units, int most_pages) {
     const uint32_t per = (units + gridDim.x - 1) / gridDim.x;
-    const int least = static_cast<int>(0.7f * sqrtf(static_cast<float>(most_pages)));
+    const int least = static_cast<int>(0.55f * sqrtf(static_cast<float>(most_pages) * a.join_turns));
     return max(per, static_cast<uint32_t>(max(least, kAttWaves)));
 }
 
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
     const Found st = find_request(
         a, [&](const Extent& x) { return static_cast<uint32_t>(x.tiles * heads) * static_cast<uint32_t>(x.pages + COST); },
         [&](uint32_t units, int most_pages) {
-            per = stretch_of(units, most_pages);
+            per = stretch_of(a, units, most_pages);
             return per * blockIdx.x;
         });
     const uint32_t u0 = st.at, u1 = min(u0 + per, st.units);
@@ -563,6 +566,7 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                 __syncthreads();
                 if (s_last) {
                     // `ways` threads share four elements of a row
+                    constexpr int kBatch = 4;                           // (32000 tokens, 16 rows of one head of 128: 25 us; one by one 37, sixteen 28)
                     const int work = rows * nd, ways = max(THREADS / work, 1);
                     for (int i0 = 0; i0 < work; i0 += THREADS) {
                         const int i = i0 + static_cast<int>(threadIdx.x) % (work < THREADS ? work : THREADS);
@@ -570,12 +574,20 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                         Share s = {-INFINITY, 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
                         if (i < work && way < ways) {
                             const int row = i / nd, d = i % nd * 4;
-#pragma unroll 4
-                            for (int w = w_first + way; w <= w_last; w += ways) {
-                                const int64_t part = (int64_t{w} * 2 + (w == w_first)) * kTile + row;
-                                const float2 ml = load_part(&a.part_ml[part].x), x = load_part(a.part_o + part * dim + d),
-                                             y = load_part(a.part_o + part * dim + d + 2);
-                                join(s, ml.x, ml.y, make_float4(x.x, x.y, y.x, y.y));
+                            // kBatch parts on their way at a time; one behind the last is the last again, left out of the sum
+                            for (int w0 = w_first + way; w0 <= w_last; w0 += kBatch * ways) {
+                                float2 ml[kBatch], x[kBatch], y[kBatch];
+#pragma unroll
+                                for (int n = 0; n < kBatch; ++n) {
+                                    const int w = min(w0 + n * ways, w_last);
+                                    const int64_t part = (int64_t{w} * 2 + (w == w_first)) * kTile + row;
+                                    ml[n] = load_part(&a.part_ml[part].x);
+                                    x[n] = load_part(a.part_o + part * dim + d);
+                                    y[n] = load_part(a.part_o + part * dim + d + 2);
+                                }
+#pragma unroll
+                                for (int n = 0; n < kBatch; ++n)
+                                    if (w0 + n * ways <= w_last) join(s, ml[n].x, ml[n].y, make_float4(x[n].x, x[n].y, y[n].x, y[n].y));
                             }
                         }
                         if (ways > 1) {                                 // work < THREADS: one turn of the outer loop
@@ -831,6 +843,9 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.vec_q = aligned(q, 16) && q_token * size % 16 == 0 && q_head * size % 16 == 0;
     a.vec_out = aligned(out, 4 * size) && out_token % 4 == 0 && out_head % 4 == 0;
     a.scale_log2 = scale * 1.44269504088896f;
+    constexpr int64_t kTurn = 4 * 64 * kAttWaves;
+    const int64_t rows = std::min<int64_t>(std::max<int64_t>((st->tokens * a.group + st->requests - 1) / st->requests, a.group), kTile);
+    a.join_turns = static_cast<float>((rows * cache->dim + kTurn - 1) / kTurn);
     hipStream_t s = static_cast<hipStream_t>(stream);
     auto go = [&](auto type_c, auto db_c) -> int {
         constexpr int TYPE = decltype(type_c)::value, DB = decltype(db_c)::value;
