@@ -23,7 +23,12 @@ namespace fxp {
 constexpr int kTile = 16;
 constexpr int kFewRows = 2 * kTile;
 constexpr int kAttWaves = 4;
-constexpr int kAttGroups = 512;          // workgroups: two a CU (768, which three a CU have room for, split more tiles: 57 -> 67 us for 64 requests)
+// Workgroups: as many as are resident, one round of them.  Up to 128 elements two a CU (768, which three a CU have room for, split more tiles: 57 -> 67 us
+// for 64 requests); rows of more take the registers of one (64 requests of 200 to 4000 tokens, 4 heads of 192: 33 us, 39 with 512 workgroups, 35 with 512 and
+// two a CU; of 256, 43, 50 and 61 - spilled).
+constexpr int kAttGroups = 512;
+template <int DB>
+constexpr int kAttGroupsOf = DB <= 2 ? kAttGroups : kAttGroups / 2;
 
 struct AttArgs {
     fxp_kv_cache c;
@@ -862,7 +867,7 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
         if ((!many || a.few_rows) && line_tiles * cache->heads * (st->blocks + kTileCost) >= int64_t{1} << 31) return FXP_ERR_DIMS;
         if (many)
             hipLaunchKernelGGL((k_kv_attend_rows<TYPE, DB>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kRowWaves), 0, s, a);
-        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroups), dim3(64 * kAttWaves), 0, s, a);
+        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroupsOf<DB>), dim3(64 * kAttWaves), 0, s, a);
         return launch_status();
     };
     auto of_type = [&](auto type_c) {
