@@ -615,6 +615,17 @@ def _row_stride(t, what):
     return t.stride(0)
 
 
+def _rows_overlap(t):
+    """Whether rows of a [tokens, heads, dim] tensor share elements."""
+    reach = t.shape[2]                    # elements that the rows so far span
+    for stride, n in sorted((t.stride(i), t.shape[i]) for i in (0, 1)):
+        if n > 1:
+            if stride < reach:
+                return True
+            reach += stride * (n - 1)
+    return False
+
+
 class KvCache:
     """Caller-owned cache of one layer: int8 keys [pages, heads, 64, dim], values [pages, heads, 4, dim, 16], scales [pages, heads]."""
 
@@ -744,7 +755,7 @@ def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=No
     _here(tab, "tab")
     if out is None:
         out = q.new_empty((tokens, q_heads, dim))
-    elif _served(out, "out", 3) != code or out.shape != q.shape or (tokens > 1 and out.stride(0) < dim) or (q_heads > 1 and out.stride(1) < dim):
+    elif _served(out, "out", 3) != code or out.shape != q.shape or _rows_overlap(out):
         raise FxpError("out must have the shape and type of q, and rows that do not overlap")
     if lse is not None:
         _index(lse, "lse", (tokens, q_heads), torch.float32)

@@ -181,6 +181,27 @@ def test_attention_layouts_and_types_of_rows(fxp):
     assert torch.equal(fxp.kv_attention(first, c.cache, c.tab, scale=c.scale), fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
 
 
+def test_attention_refuses_rows_of_out_that_share_elements(fxp):
+    say("kv_attention, overlapping rows of out")
+    c = Case(fxp, [20], [3], 4, 2, 16, "fp32")
+    room = torch.zeros(400, device="cuda")
+    for strides in ((16, 16), (0, 16), (48, 16), (16, 40), (64, 8), (0, 0)):
+        with pytest.raises(fxp.FxpError, match="overlap"):
+            fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, out=room.as_strided((3, 4, 16), strides + (1,)))
+    want = c.want()
+    for strides in ((64, 16), (16, 48), (80, 20), (70, 17)):
+        c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, out=room.as_strided((3, 4, 16), strides + (1,))), want=want)
+
+
+def test_attention_in_place(fxp):
+    """out may be q: every row of q is read before its output is written, by whichever workgroups share it."""
+    say("kv_attention into q")
+    for lens, news, QH, H, D in (([4000, 70], [1, 2], 8, 2, 64), ([300, 140], [150, 140], 48, 48, 128)):
+        c = Case(fxp, lens, news, QH, H, D, "bf16")
+        want, q = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale), c.dq.clone()
+        assert torch.equal(fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=q), want)
+
+
 def test_attention_many_requests(fxp):
     say("kv_attention, 600 requests, most of them short")
     rng = np.random.default_rng(3)
