@@ -430,7 +430,8 @@ int64_t fxp_kv_max_runs(int64_t requests, int64_t tokens);
  * block_table is refused; so is, from the first one that the stack cannot serve on, every request that needs a page, and from the first one
  * whose tokens pass `tokens` on, every request that has any.
  * A refused request keeps its length and its row, its tokens get slot -1 and runs on page -1 (fxp_kv_append skips them).
- * Tokens and runs beyond `tokens` and the runs' capacity are not written, but counted in first.  Lengths that are negative count as 0.
+ * Tokens and runs beyond `tokens` and the runs' capacity are not written, but counted in first (up to 2^31 - 1, which also stands for all
+ * beyond).  Lengths that are negative count as 0.
  * ws: NULL, or at least 256 bytes, zero before the first call that uses them, which every call leaves zero; required where
  * lens_after or n_free_after is the input itself. */
 int fxp_kv_tables(const fxp_kv_step* step, const int32_t* n_new, void* ws, size_t ws_bytes, void* stream);

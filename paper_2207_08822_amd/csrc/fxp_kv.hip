@@ -17,16 +17,23 @@ constexpr int kTabThreads = 1024;
 // (999 requests, 100386 tokens in 2700 runs: 6.7 us; 128 a workgroup 7.4, 256 8.7).
 constexpr int kTabOne = 256, kTabMany = 64;
 
+// Sums over requests.  What requests ask for may pass 32 bits together (a thousand that ask for millions each): sums stay at 2^32 - 1 then, which
+// no count of tokens, pages or runs reaches, so that nobody behind such a sum is taken to fit.
 struct Three {
-    int tokens, need, runs;
+    uint32_t tokens, need, runs;
 };
-__device__ inline Three add3(const Three& a, const Three& b) { return {a.tokens + b.tokens, a.need + b.need, a.runs + b.runs}; }
+__device__ inline uint32_t add_up(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+__device__ inline Three add3(const Three& a, const Three& b) {
+    return {add_up(a.tokens, b.tokens), add_up(a.need, b.need), add_up(a.runs, b.runs)};
+}
+// a place that is written out: the largest int32 stands for all beyond
+__device__ inline int as_int(uint32_t x) { return static_cast<int>(min(x, 0x7fffffffu)); }
 
-// exclusive sums over the workgroup's threads; `total` receives the sum of all
+// Exclusive sums over the workgroup's threads; `total` receives the sum of all.  (Where the inclusive sum is 2^32 - 1, at least that
+// less a thread's own, which is below 2^31, is before the thread.)
 __device__ inline Three block_scan3(const Three& v, Three* lds, Three& total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    auto scan = [](int x) { return static_cast<int>(wave_scan(static_cast<uint32_t>(x))); };
-    const Three s = {scan(v.tokens), scan(v.need), scan(v.runs)};
+    const Three s = {wave_scan_up(v.tokens), wave_scan_up(v.need), wave_scan_up(v.runs)};
     if (lane == 63) lds[wave] = s;
     __syncthreads();
     Three before = {0, 0, 0};
@@ -37,14 +44,16 @@ __device__ inline Three block_scan3(const Three& v, Three* lds, Three& total) {
         total = add3(total, lds[w]);
     }
     __syncthreads();
-    return {before.tokens + s.tokens - v.tokens, before.need + s.need - v.need, before.runs + s.runs - v.runs};
+    return add3(before, {s.tokens - v.tokens, s.need - v.need, s.runs - v.runs});
 }
 
 struct Request {
-    int len, had, after, served, first, need0, run0, row;
+    int len, had, after, served;
+    uint32_t first, need0, run0;
+    int row;
 };
 
-// what request b asks for; lengths that no device program should hold (negative, sums past 32 bits) only have to stay harmless:
+// what request b asks for; lengths that no device program should hold (negative, past the table) only have to stay harmless:
 // every index that comes of them is compared with its array before it is used
 __device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_t b, Request& r, bool& fits) {
     Three v = {0, 0, 0};
@@ -56,16 +65,17 @@ __device__ inline Three asks(const fxp_kv_step& st, const int32_t* n_new, int64_
     r.len = static_cast<int>(len);
     r.after = static_cast<int>(min(after, (int64_t{1} << 31) - 1));
     r.had = static_cast<int>((len + FXP_KV_PAGE - 1) / FXP_KV_PAGE);
-    v.tokens = static_cast<int>(n);
-    v.need = fits ? static_cast<int>((after + FXP_KV_PAGE - 1) / FXP_KV_PAGE) - r.had : 0;
-    v.runs = n ? static_cast<int>((after - 1) / FXP_KV_PAGE - len / FXP_KV_PAGE) + 1 : 0;
+    v.tokens = static_cast<uint32_t>(n);
+    v.need = fits ? static_cast<uint32_t>((after + FXP_KV_PAGE - 1) / FXP_KV_PAGE - r.had) : 0u;
+    v.runs = n ? static_cast<uint32_t>((after - 1) / FXP_KV_PAGE - len / FXP_KV_PAGE + 1) : 0u;
     return v;
 }
 
 // Whether a request finds room: in its row, in the stack and among the step's tokens; `x` is the sum of those before it.  Both sums only
 // grow, so the requests that are served and take pages come before those that find too few.
 __device__ inline bool has_room(const fxp_kv_step& st, bool fits, const Three& v, const Three& x, int n_free) {
-    return fits && (v.need == 0 || x.need + v.need <= n_free) && (v.tokens == 0 || (x.tokens >= 0 && int64_t{x.tokens} + v.tokens <= st.tokens));
+    const Three upto = add3(x, v);
+    return fits && (v.need == 0 || upto.need <= static_cast<uint32_t>(n_free)) && (v.tokens == 0 || upto.tokens <= st.tokens);
 }
 
 // lengths of all requests and the stack's height, for the workgroup that is last to have read them
@@ -82,7 +92,7 @@ __device__ inline void commit_lengths(const fxp_kv_step& st, const int32_t* n_ne
         const Three x = add3(carry, block_scan3(v, lds, total));
         const bool served = has_room(st, fits, v, x, n_free);
         if (base + threadIdx.x < st.requests) st.lens_after[base + threadIdx.x] = served ? r.after : st.lens[base + threadIdx.x];
-        if (served && v.need) atomicMax(&taken, x.need + v.need);
+        if (served && v.need) atomicMax(&taken, static_cast<int>(x.need + v.need));
         carry = add3(carry, total);
     }
     __syncthreads();
@@ -99,7 +109,7 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
     __shared__ int4 span[RUNS];         // first token, count, position of the first token
     __shared__ int long_runs, last, taken;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r0 = blockIdx.x * RUNS;
+    const uint32_t r0 = blockIdx.x * RUNS;
     const int n_free = min(static_cast<int64_t>(max(st.n_free[0], 0)), st.pages);
     if (tid < RUNS) mark[tid] = -1;
     if (tid == 0) long_runs = taken = 0;
@@ -122,19 +132,19 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
         r.row = static_cast<int>(b);
         // each thousand of requests has a workgroup that writes what belongs to a request
         if (b < st.requests && (base / kTabThreads) % gridDim.x == blockIdx.x) {
-            st.first[b] = r.first;
+            st.first[b] = as_int(r.first);
             st.refused[b] = !r.served;
             if (along) st.lens_after[b] = r.served ? r.after : st.lens[b];
         }
-        if (blockIdx.x == 0 && along && r.served && v.need) atomicMax(&taken, x.need + v.need);
-        const int lo = max(x.runs, r0);
-        if (v.runs > 0 && lo < x.runs + v.runs && lo < r0 + RUNS && x.runs >= 0) {
+        if (blockIdx.x == 0 && along && r.served && v.need) atomicMax(&taken, static_cast<int>(x.need + v.need));
+        const uint32_t lo = max(x.runs, r0);
+        if (v.runs > 0 && lo < add_up(x.runs, v.runs) && lo < r0 + RUNS) {
             req[lo - r0] = r;
             mark[lo - r0] = lo - r0;
         }
         carry = add3(carry, total);
     }
-    if (blockIdx.x == 0 && tid == 0) st.first[st.requests] = carry.tokens;
+    if (blockIdx.x == 0 && tid == 0) st.first[st.requests] = as_int(carry.tokens);
     __syncthreads();
     if (blockIdx.x == 0 && tid == 0 && along) st.n_free_after[0] = n_free - taken;
 
@@ -152,20 +162,20 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
     __syncthreads();
     if (tid < RUNS) {
         for (int w = 0; w < wave; ++w) owner = max(owner, mark[64 * w + 63]);
-        const int run = r0 + tid;
+        const uint32_t run = r0 + tid;
         int4 s = make_int4(0, 0, 0, 0);
         if (run < run_rows) {
             int4 out = make_int4(0, 0, -1, 0);
             if (run < carry.runs && owner >= 0) {
                 const Request r = req[owner];
-                const int j = run - r.run0, block = r.len / FXP_KV_PAGE + j, off = j ? 0 : r.len % FXP_KV_PAGE;
-                const int t0 = r.first + (j ? j * FXP_KV_PAGE - r.len % FXP_KV_PAGE : 0);
+                const int j = static_cast<int>(run - r.run0), block = r.len / FXP_KV_PAGE + j, off = j ? 0 : r.len % FXP_KV_PAGE;
+                const int t0 = as_int(add_up(r.first, j ? j * FXP_KV_PAGE - r.len % FXP_KV_PAGE : 0));
                 const int count = min(FXP_KV_PAGE - off, r.after - (block * FXP_KV_PAGE + off));
                 int page = -1;
                 if (r.served && block < st.blocks) {
                     int32_t* entry = st.block_table + int64_t{r.row} * st.blocks + block;
                     if (block >= r.had) {
-                        const int at = n_free - 1 - (r.need0 + block - r.had);
+                        const int at = n_free - 1 - (static_cast<int>(r.need0) + block - r.had);
                         page = at >= 0 && at < n_free ? st.free_pages[at] : -1;
                         *entry = page;
                     } else {
@@ -198,11 +208,8 @@ __global__ __launch_bounds__(kTabThreads) void k_kv_tables(fxp_kv_step st, const
                 st.positions[t] = s.z + lane;
             }
         }
-    for (int64_t t = carry.tokens + int64_t{blockIdx.x} * kTabThreads + tid; t < st.tokens; t += int64_t{gridDim.x} * kTabThreads)
-        if (t >= 0) {
-            st.slots[t] = -1;
-            st.positions[t] = -1;
-        }
+    for (int64_t t = int64_t{carry.tokens} + int64_t{blockIdx.x} * kTabThreads + tid; t < st.tokens; t += int64_t{gridDim.x} * kTabThreads)
+        st.slots[t] = st.positions[t] = -1;
 
     // The lengths and the stack's height may be updated in place: by the workgroup that is last to have read them.
     if (!along) {

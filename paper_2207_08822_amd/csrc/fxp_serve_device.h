@@ -158,10 +158,11 @@ __device__ inline void row_digits(const float (&x)[16], int unit, bool finite, v
 
 __device__ inline v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
-// sum over the lanes up to this one, inside the vector ALU (rows of 16 first, then row to row)
-__device__ inline uint32_t wave_scan(uint32_t v) {
-    auto step = [](uint32_t x, auto ctrl, auto rows) {
-        return x + static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false));
+// sum over the lanes up to this one, inside the vector ALU (rows of 16 first, then row to row); `add` adds two of them
+template <typename F>
+__device__ inline uint32_t wave_scan(uint32_t v, F add) {
+    auto step = [&](uint32_t x, auto ctrl, auto rows) {
+        return add(x, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), decltype(ctrl)::value, decltype(rows)::value, 0xf, false)));
     };
     using std::integral_constant;
     v = step(v, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});     // row_shr:1
@@ -171,6 +172,12 @@ __device__ inline uint32_t wave_scan(uint32_t v) {
     v = step(v, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});     // row_bcast:15 into rows 1 and 3
     v = step(v, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});     // row_bcast:31 into rows 2 and 3
     return v;
+}
+__device__ inline uint32_t wave_scan(uint32_t v) {
+    return wave_scan(v, [](uint32_t a, uint32_t b) { return a + b; });
+}
+__device__ inline uint32_t wave_scan_up(uint32_t v) {               // stays at 2^32 - 1 where it would pass that
+    return wave_scan(v, [](uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); });
 }
 
 // Loads through a buffer descriptor: `bytes` from a uniform address, at a uniform and a lane's offset; 0 bytes: zeros, and no memory access.

@@ -241,3 +241,29 @@ def test_a_cache_past_32_bits(fxp):
     want = torch.tensor(np.concatenate([want.values()[0].transpose(1, 0, 2), want.values()[1][:, :6].transpose(1, 0, 2)])).float()
     assert torch.equal(k.cpu(), want) and torch.equal(v.cpu(), want)
     assert (cache.kq[0] == 3).all() and (cache.vq[0] == 3).all()
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("asked,many,tokens", [(1 << 20, 4096, 1 << 20), (1 << 16, 65536, 1 << 16), (2 ** 31 - 1, 4, 70)])
+def test_tables_of_requests_whose_sums_pass_32_bits(fxp, asked, many, tokens, in_place):
+    """`many` requests ask for more than their rows hold, 2^32 tokens together; those behind them, who ask for 5, must not be taken for the first."""
+    say("kv_tables, sums past 32 bits", (asked, many, tokens, in_place))
+    n_new = np.concatenate([np.full(many, asked, np.int64), np.full(5, 5), np.zeros(2, np.int64)])
+    B = len(n_new)
+    tab = fxp.KvTables(B, 3, tokens, 40, in_place=in_place)
+    lens = np.full(B, 7, np.int32)
+    lens[many:] = 62
+    tab.lens.copy_(torch.tensor(lens))
+    tab.refused.fill_(-1)
+    fxp.kv_tables(dev(n_new.astype(np.int32)), tab)
+    refused = np.ones(B)
+    refused[-2:] = 0                                          # these ask for nothing
+    assert np.array_equal(host(tab.refused), refused)
+    assert np.array_equal(host(tab.lens_after), lens) and int(tab.n_free_after) == 40 and (host(tab.block_table) == -1).all()
+    # of a request that asks for more than the step's rows, as many as those are counted
+    sums = np.concatenate([[0], np.cumsum(np.minimum(n_new, tokens))])
+    assert np.array_equal(host(tab.first), np.minimum(sums, 2 ** 31 - 1))
+    assert (host(tab.slots) == -1).all()
+    asked = min(asked, tokens)
+    assert np.array_equal(host(tab.positions), 7 + np.arange(tokens) % asked)
+    assert (host(tab.runs)[:, 2] == -1).all() and not host(tab.ws).any()
