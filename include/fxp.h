@@ -487,8 +487,7 @@ size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group);
 int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales, void* stream);
 /* Y[M,N] = X[M,K] * W.  X, Y of `type`, row strides ldx >= K, ldy >= N.  Made for few rows (one pass over the weights for each 32 to 64 of
  * them); any M is right.  A group of a row of X is a fixed-point number of two signed 8-bit digits (three for fp32)
- * under its own scale: products are exact int32 sums over a group, sums over groups fp32.  (An fp32 group whose largest magnitude is below
- * 2^-121 counts as zero.)  Y must not overlap X.
+ * under its own scale: products are exact int32 sums over a group, sums over groups fp32.  Y must not overlap X.
  * ws: fxp_w4_workspace_bytes bytes (0 on bad arguments), 256-byte aligned; not used, and may be NULL, for M <= 2. */
 size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group);
 int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, int64_t K, int64_t N, const uint8_t* packed, const uint8_t* scales,

@@ -3,13 +3,17 @@
 // A 16 x 16 x 64 int8 matrix instruction has 16 outputs' weights as A (the lane's 16 mantissas of one output: 8 bytes) and the digits
 // of up to 16 rows of x as B.  A mantissa is used in the upper half of its byte, 16 q, so that unpacking is a shift and two masks for
 // eight of them; the factor 16 is taken out with the scales.  The int32 sums of a group are exact; group by group
-// they are scaled into fp32 sums.
+// they are scaled into fp32 sums, by the exponents of x's unit and of the weights in one step (ldexp): scaled by one after the
+// other, large x would pass the largest float before small weights bring it back, and tiny x be lost before large ones do.
 #include "fxp_serve_device.h"
 
 namespace fxp {
 
 constexpr int kW4Waves = 8;
 constexpr int kW4Threads = 64 * kW4Waves;
+
+// x = digits * 2^unit and w = q 2^(e - 129), and q is used as 16 q: a sum counts 2^(unit + e - 133)
+constexpr int kUnitBias = 133;
 
 struct W4Args {
     const void* x;
@@ -21,7 +25,7 @@ struct W4Args {
     void* y;
     int64_t ldy;
     uint8_t* digits;     // [k_tiles][m_tiles][ND][128 / S][64][S / 4] bytes
-    float* units;        // [k_tiles * 128 / group][16 m_tiles]: 2^(exponent of one unit - 6)
+    int* units;          // [k_tiles * 128 / group][16 m_tiles]: exponent of one unit, less kUnitBias
     int vec_x;
 };
 
@@ -59,7 +63,7 @@ __global__ __launch_bounds__(256) void k_w4_digits(W4Args a) {
             *reinterpret_cast<int2*>(p + 16 * (S / 4)) = make_int2(d[j][2], d[j][3]);          // the next piece: 16 (g + 1) + r
         }
     }
-    if (k % GROUP == 0) a.units[static_cast<int64_t>(k / GROUP) * (16 * a.m_tiles) + row] = ldexpf(1.0f, unit - 6);
+    if (k % GROUP == 0) a.units[static_cast<int64_t>(k / GROUP) * (16 * a.m_tiles) + row] = unit - kUnitBias;
 }
 
 // Three rows or more: MT tiles of 16 rows, NT tiles of 16 outputs.  A wave has every eighth tile of 128 inputs.  U of its weight tiles and, up to
@@ -69,6 +73,9 @@ template <int TYPE, int GROUP, int NT, int MT, int U>
 __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT;
     constexpr int B = MT <= 2 ? 2 : 1;                      // buffers of digits
+    // groups whose sums are in registers together: with three digits and two tiles of rows, some of four spilled (23 rows, 4096 x 14336: 42 us, 35 by
+    // twos; with two digits, 64 rows, four 39.5, by twos 43.5)
+    constexpr int GROUPS = ND * GT * MT == 24 && MT == 2 ? 2 : GT;
     static_assert(U % B == 0, "a turn begins with the same buffer");
     using Digit = std::conditional_t<S == 64, v4i, long>;
     __shared__ float red[kW4Waves][NT * 16][17];
@@ -85,7 +92,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
     v4i w[U][NT];
     uint32_t e[U][NT][GT];
     Digit dig[B][MT][ND][STEPS];
-    float unit[B][MT][GT];
+    int unit[B][MT][GT];
     auto load_w = [&](int u, int kt) {
         const bool there = kt < a.k_tiles;
 #pragma unroll
@@ -114,7 +121,7 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
                 }
             const auto units = records(a.units + static_cast<int64_t>(kt) * GT * (16 * a.m_tiles) + mt * 16, there ? (GT - 1) * 64 * a.m_tiles + 64 : 0);
 #pragma unroll
-            for (int j = 0; j < GT; ++j) unit[c][i][j] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(units, 4 * col, 64 * a.m_tiles * j, 0));
+            for (int j = 0; j < GT; ++j) unit[c][i][j] = __builtin_amdgcn_raw_buffer_load_b32(units, 4 * col, 64 * a.m_tiles * j, 0);
         }
     };
 #pragma unroll
@@ -127,40 +134,44 @@ __global__ __launch_bounds__(kW4Threads, 2) void k_w4_linear(W4Args a) {
             load_digits(B == 2 ? 1 - c : 0, B == 2 ? kt + kW4Waves : kt);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                v4i acc[MT][GT][ND];
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s) {
-                    const uint32_t mask = 0xf0f0f0f0u;
-                    Digit q;
-                    if constexpr (S == 64) {
-                        const uint32_t w0 = static_cast<uint32_t>(w[u][n][2 * s]), w1 = static_cast<uint32_t>(w[u][n][2 * s + 1]);
-                        q = v4i{static_cast<int>((w0 << 4) & mask), static_cast<int>((w1 << 4) & mask), static_cast<int>(w0 & mask),
-                                static_cast<int>(w1 & mask)};
-                    } else {
-                        const uint32_t w0 = static_cast<uint32_t>(w[u][n][s]);
-                        q = static_cast<long>(static_cast<uint64_t>(w0 & mask) << 32 | ((w0 << 4) & mask));
+                for (int j0 = 0; j0 < GT; j0 += GROUPS) {
+                    v4i acc[MT][GROUPS][ND];
+#pragma unroll
+                    for (int s = j0 * SG; s < (j0 + GROUPS) * SG; ++s) {
+                        const uint32_t mask = 0xf0f0f0f0u;
+                        Digit q;
+                        if constexpr (S == 64) {
+                            const uint32_t w0 = static_cast<uint32_t>(w[u][n][2 * s]), w1 = static_cast<uint32_t>(w[u][n][2 * s + 1]);
+                            q = v4i{static_cast<int>((w0 << 4) & mask), static_cast<int>((w1 << 4) & mask), static_cast<int>(w0 & mask),
+                                    static_cast<int>(w1 & mask)};
+                        } else {
+                            const uint32_t w0 = static_cast<uint32_t>(w[u][n][s]);
+                            q = static_cast<long>(static_cast<uint64_t>(w0 & mask) << 32 | ((w0 << 4) & mask));
+                        }
+#pragma unroll
+                        for (int i = 0; i < MT; ++i)
+#pragma unroll
+                            for (int d = 0; d < ND; ++d) {
+                                const v4i before = s % SG ? acc[i][s / SG - j0][d] : v4i{0, 0, 0, 0};
+                                if constexpr (S == 64) acc[i][s / SG - j0][d] = mfma_i8(q, dig[c][i][d][s], before);
+                                else acc[i][s / SG - j0][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, dig[c][i][d][s], before, 0, 0, 0);
+                            }
                     }
 #pragma unroll
-                    for (int i = 0; i < MT; ++i)
+                    for (int j = 0; j < GROUPS; ++j)        // (of a tile that is none, all is zero)
 #pragma unroll
-                        for (int d = 0; d < ND; ++d) {
-                            const v4i before = s % SG ? acc[i][s / SG][d] : v4i{0, 0, 0, 0};
-                            if constexpr (S == 64) acc[i][s / SG][d] = mfma_i8(q, dig[c][i][d][s], before);
-                            else acc[i][s / SG][d] = __builtin_amdgcn_mfma_i32_16x16x32_i8(q, dig[c][i][d][s], before, 0, 0, 0);
+                        for (int r = 0; r < 4; ++r) {
+                            const int scale = static_cast<int>((e[u][n][j0 + j] >> (8 * r)) & 0xffu);
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) {
+                                float v = static_cast<float>((acc[i][j][0][r] << 8) + acc[i][j][1][r]);
+                                if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[i][j][2][r]));
+                                sum[i][n][r] += ldexpf(v, unit[c][i][j0 + j] + scale);
+                            }
                         }
+                    if constexpr (GROUPS < GT) __builtin_amdgcn_sched_barrier(0);
                 }
-#pragma unroll
-                for (int j = 0; j < GT; ++j)                // (of a tile that is none, all is zero)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float scale = __uint_as_float(((e[u][n][j] >> (8 * r)) & 0xffu) << 23);
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            float v = static_cast<float>((acc[i][j][0][r] << 8) + acc[i][j][1][r]);
-                            if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[i][j][2][r]));
-                            sum[i][n][r] = fmaf(v * unit[c][i][j], scale, sum[i][n][r]);
-                        }
-                    }
                 __builtin_amdgcn_sched_barrier(0);          // one tile of outputs after the other: interleaved, some of these spilled
             }
             load_w(u, kt + kW4Waves * U);
@@ -199,7 +210,7 @@ template <int TYPE, int GROUP, int ROWS>
 __global__ __launch_bounds__(kW4Threads, GROUP == 32 && ROWS == 2 ? 2 : 4) void k_w4_rows(W4Args a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, S = GROUP < 64 ? GROUP : 64, STEPS = 128 / S, GT = 128 / GROUP, SG = STEPS / GT, U = kW4Ahead;
     __shared__ v4i s_digits[kW4Waves][U][ROWS][ND][8];          // pieces of 16 inputs
-    __shared__ float s_unit[kW4Waves][U][ROWS][GT];
+    __shared__ int s_unit[kW4Waves][U][ROWS][GT];
     __shared__ float red[kW4Waves][ROWS][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int k_waves = a.k_waves, wave_n = wave / k_waves, first = wave - wave_n * k_waves;
@@ -255,7 +266,7 @@ __global__ __launch_bounds__(kW4Threads, GROUP == 32 && ROWS == 2 ? 2 : 4) void 
             row_digits<ND>(x[m], unit, !__any(top >= 0x7f800000u), d);
 #pragma unroll
             for (int j = 0; j < ND; ++j) s_digits[wave][lane >> 3][m][j][lane & 7] = d[j];
-            if ((lane & 7) % (GROUP / 16) == 0) s_unit[wave][lane >> 3][m][(lane & 7) / (GROUP / 16)] = ldexpf(1.0f, unit - 6);
+            if ((lane & 7) % (GROUP / 16) == 0) s_unit[wave][lane >> 3][m][(lane & 7) / (GROUP / 16)] = unit - kUnitBias;
         }
         __builtin_amdgcn_wave_barrier();
         const bool more = kt + k_waves * U < a.k_tiles;
@@ -305,7 +316,7 @@ __global__ __launch_bounds__(kW4Threads, GROUP == 32 && ROWS == 2 ? 2 : 4) void 
                     }
                     float v = static_cast<float>((acc[0] << 8) + acc[1]);
                     if constexpr (ND == 3) v = fmaf(v, 256.0f, static_cast<float>(acc[2]));
-                    sum[m] = fmaf(v * s_unit[wave][i][m][j], __uint_as_float(e[i][j] << 23), sum[m]);
+                    sum[m] += ldexpf(v, s_unit[wave][i][m][j] + static_cast<int>(e[i][j]));
                 }
         }
         if (more) load_w(kt + k_waves * U);
@@ -390,7 +401,7 @@ extern "C" size_t fxp_w4_scale_bytes(int64_t K, int64_t N, int group) {
 extern "C" size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group) {
     if (!fxp::known_type(type) || !fxp::w4_group_ok(group) || !fxp::w4_sizes_ok(K, 1) || M <= 0 || M >= (int64_t{1} << 20)) return 0;
     const size_t rows = (M + 15) / 16 * 16, tiles = (K + 127) / 128;
-    return rows * tiles * 128 * (type == FXP_F32 ? 3 : 2) + rows * tiles * (128 / group) * sizeof(float);
+    return rows * tiles * 128 * (type == FXP_F32 ? 3 : 2) + rows * tiles * (128 / group) * sizeof(int);
 }
 
 extern "C" int fxp_w4_pack(int type, const void* W, int64_t ldw, int64_t K, int64_t N, int group, uint8_t* packed, uint8_t* scales,
@@ -439,7 +450,7 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
     a.y = Y;
     a.ldy = ldy;
     a.digits = static_cast<uint8_t*>(ws);
-    a.units = reinterpret_cast<float*>(a.digits + static_cast<size_t>(a.m_tiles) * 16 * a.k_tiles * 128 * (type == FXP_F32 ? 3 : 2));
+    a.units = reinterpret_cast<int*>(a.digits + static_cast<size_t>(a.m_tiles) * 16 * a.k_tiles * 128 * (type == FXP_F32 ? 3 : 2));
     a.vec_x = aligned(X, 16) && (M == 1 || ldx * size % 16 == 0);
     const int64_t pieces = M * a.k_tiles * 8;
     if (pieces > (int64_t{1} << 30)) return FXP_ERR_DIMS;

@@ -153,3 +153,49 @@ def test_linear4_from_a_graph(fxp):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, fxp.linear4(x, w))
+
+
+@pytest.mark.parametrize("M", [1, 2, 5, 20, 40])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+def test_linear4_of_the_largest_and_smallest_numbers(fxp, M, group, kind):
+    """Results that the type holds come out whatever the sizes of x and of the weights are apart: nothing between passes the largest or the
+    smallest fp32 number.  2^-149 besides the bound: a sum among sub-normal numbers may be that far off for each group and part."""
+    say("w4_linear of the largest and smallest numbers", (M, group, kind))
+    rng = np.random.default_rng(M + group)
+    dtype, unit_bits, half = TYPES[kind]
+    for x_exp, w_exp in ((124, -20), (127, -100), (90, 20), (-118, 20), (-126, 120), (-120, 0)):
+        W = torch.tensor((rng.standard_normal((300, 33)) * 2.0 ** w_exp).astype(np.float32))
+        w = fxp.pack4(W.cuda(), group)
+        q, unit = ref.unpack4(host(w.packed), host(w.scales), 300, 33, group)
+        x = torch.tensor((rng.uniform(-1, 1, (M, 300)) * 2.0 ** x_exp).astype(np.float32)).to(dtype)
+        y = x.double().numpy() @ (q * unit)
+        assert np.abs(y).max() < 2.0 ** 127
+        got = fxp.linear4(x.cuda(), w).double().cpu().numpy()
+        off = bound(x.double().numpy(), q * unit, y, group, unit_bits, half) + 2.0 ** -149 * (300 // group + 12)
+        if dtype == torch.bfloat16:
+            off += 2.0 ** -134                                       # half a step of its own sub-normal numbers
+        assert (np.abs(got - y) <= off).all(), (x_exp, w_exp, np.max(np.abs(got - y) / off))
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 40])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_linear4_with_inf_in_several_groups(fxp, M, kind):
+    """Inf is mapped to the largest magnitude of its group, 2^129 and a little less, under a unit that leaves nothing of the others: with weights
+    below 2^-3 and of either sign the sums stay finite.  One step of the type and a few of fp32: 2^-10 of the magnitudes."""
+    say("w4_linear, Inf in three groups of a row", (M, kind))
+    rng = np.random.default_rng(9)
+    w = fxp.pack4(torch.tensor((rng.uniform(-1, 1, (256, 40)) / 8).astype(np.float32)).cuda(), 64)
+    q, unit = ref.unpack4(host(w.packed), host(w.scales), 256, 40, 64)
+    dtype, unit_bits, half = TYPES[kind]
+    x = torch.tensor(rng.standard_normal((M, 256)).astype(np.float32)).to(dtype)
+    x[0, 3], x[0, 70], x[0, 200] = float("inf"), float("inf"), float("-inf")
+    most = (32639 if unit_bits == 15 else 8355711) * 2.0 ** (129 - unit_bits)
+    as_mapped = np.zeros(256)
+    as_mapped[[3, 70, 200]] = most, most, -most
+    as_mapped[128:192] = x.double().numpy()[0, 128:192]
+    got = fxp.linear4(x.cuda(), w).double().cpu().numpy()
+    assert not np.isnan(got).any() and np.isfinite(got[1:]).all()
+    if kind != "fp16":                                               # 2^126 is Inf in fp16
+        want, mass = as_mapped @ (q * unit), np.abs(as_mapped) @ np.abs(q * unit)
+        assert (np.abs(got[0] - want) <= half * np.abs(want) + 2.0 ** -20 * mass).all()
