@@ -6,6 +6,7 @@ non-zero status.  All arithmetic runs in the HIP kernels; there is no CPU or PyT
 fallback: if libfxp.so cannot be loaded, or a tensor is not on the GPU, the call fails.
 """
 import ctypes
+import itertools
 import os
 
 import torch
@@ -626,6 +627,39 @@ def _rows_overlap(t):
     return False
 
 
+def _span(t):
+    """Addresses of a tensor's first byte and of the one behind its last."""
+    last = sum(stride * (n - 1) for stride, n in zip(t.stride(), t.shape)) + 1 if t.numel() else 0
+    return t.data_ptr(), t.data_ptr() + last * t.element_size()
+
+
+def _same_rows(a, b):
+    """Whether two tensors of one shape are the same elements in the same places."""
+    return a.data_ptr() == b.data_ptr() and all(n <= 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
+
+
+def _share(a, b):
+    """Whether rows (contiguous last dimensions) of two tensors of one type and of as many rows share elements.  Exact where their strides are
+    alike, as those of parts of one buffer are; otherwise whether the tensors' spans meet."""
+    (a0, a1), (b0, b1) = _span(a), _span(b)
+    if a1 <= b0 or b1 <= a0 or a0 == a1 or b0 == b1:
+        return False
+    lead = [(n, stride, other) for n, stride, other in zip(a.shape[:-1], a.stride(), b.stride()) if n > 1]
+    if any(stride != other for _, stride, other in lead):
+        return True
+    # rows of a lie at whole strides from each other: does one begin between `low` and `high` (both excluded), seen from its first row?
+    delta = (b0 - a0) // a.element_size()
+    low, high = delta - a.shape[-1], delta + b.shape[-1]
+    lead = sorted((n, stride) for n, stride, _ in lead)
+    n, stride = lead.pop() if lead else (1, 0)          # the longest dimension in one step, the others one by one
+    for at in itertools.product(*(range(1 - m, m) for m, _ in lead)):
+        c = sum(i * s for i, (_, s) in zip(at, lead))
+        i = min(max((low - c) // stride + 1, 1 - n), n - 1) if stride else 0
+        if low < c + i * stride < high:
+            return True
+    return False
+
+
 class KvCache:
     """Caller-owned cache of one layer: int8 keys [pages, heads, 64, dim], values [pages, heads, 4, dim, 16], scales [pages, heads]."""
 
@@ -793,7 +827,7 @@ def pack4(W, group=64):
 
 
 def linear4(x, w, out=None, ws=None):
-    """y [M, N] = x [M, K] W of x's type, W the 4-bit weights w; made for a few rows."""
+    """y [M, N] = x [M, K] W of x's type, W the 4-bit weights w; made for a few rows.  out: may not share elements with x."""
     code = _served(x, "x", 2)
     M, K = x.shape
     if K != w.K:
@@ -811,6 +845,8 @@ def linear4(x, w, out=None, ws=None):
     elif M > 2:
         ws = x.new_empty(int(lib().fxp_w4_workspace_bytes(code, M, K, w.group)), dtype=torch.uint8)
     packed, scales = w.pointers
+        if _share(x, out):
+            raise FxpError("out shares elements with x")
     _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), ldy, _p(ws),
                                ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
     return out

@@ -199,3 +199,19 @@ def test_linear4_with_inf_in_several_groups(fxp, M, kind):
     if kind != "fp16":                                               # 2^126 is Inf in fp16
         want, mass = as_mapped @ (q * unit), np.abs(as_mapped) @ np.abs(q * unit)
         assert (np.abs(got[0] - want) <= half * np.abs(want) + 2.0 ** -20 * mass).all()
+
+
+def test_linear4_refuses_an_output_that_shares_elements_with_its_input(fxp):
+    say("w4_linear, out over x")
+    rng = np.random.default_rng(10)
+    w, _ = weights(fxp, rng, 64, 64, 64)
+    room = torch.randn((41, 200), device="cuda")
+    for M in (1, 2, 4, 40):
+        x = room[:M, 10:74]
+        for out in (x, room[:M, 73:137], room[:M, :64], room[1:M + 1, 20:84] if M > 1 else x, room.view(-1)[5:5 + 64 * M].view(M, 64)):
+            before = room.clone()
+            with pytest.raises(fxp.FxpError, match="shares elements"):
+                fxp.linear4(x, w, out=out)
+            assert torch.equal(room, before)
+        want = fxp.linear4(x, w)
+        assert torch.equal(fxp.linear4(x, w, out=room[:M, 74:138]), want)            # beside x in the same rows

@@ -111,3 +111,34 @@ def test_the_binding_refuses_tensors_on_the_cpu():
         fxp.KvCache(2, 1, 64, device="cpu")
     with pytest.raises(fxp.FxpError):
         fxp.pack4(torch.zeros(64, 16))
+
+
+def test_whether_rows_share_elements():
+    """Against sets of addresses: exact for strides that are alike, never a no where elements are shared."""
+    import random
+
+    import torch
+    rng = random.Random(1)
+    room = torch.zeros(4000)
+
+    def elements(t):
+        return set((t.storage_offset() + sum(i * s for i, s in zip(at, t.stride()))) for at in torch.cartesian_prod(
+            *[torch.arange(n) for n in t.shape]).view(-1, t.dim()).tolist())
+
+    seen = {True: 0, False: 0}
+    for trial in range(600):
+        lead = [rng.choice([1, 2, 3, 5]) for _ in range(rng.choice([1, 2]))]
+        strides = [[rng.choice([0, 1, 4, 7, 8, 16, 33, 100]) for _ in lead] for _ in range(2)]
+        if rng.random() < 0.8:
+            strides[1] = [y if n == 1 else x for x, y, n in zip(*strides, lead)]
+        lasts = rng.choice([1, 3, 4, 8]), rng.choice([1, 3, 4, 8])
+        a, b = (room.as_strided(lead + [m], st + [1], rng.randrange(120)) for m, st in zip(lasts, strides))
+        want, got = bool(elements(a) & elements(b)), fxp._share(a, b)
+        alike = all(n == 1 or x == y for n, x, y in zip(lead, *strides))
+        assert got == want if alike else got or not want, (a.shape, a.stride(), a.storage_offset(), b.shape, b.stride(), b.storage_offset())
+        assert got == fxp._share(b, a)
+        seen[got] += 1
+        if lasts[0] == lasts[1]:
+            assert fxp._same_rows(a, b) == (alike and a.data_ptr() == b.data_ptr())
+    assert min(seen.values()) > 100
+    assert not fxp._share(room[:0], room) and not fxp._share(room.view(20, 200)[:, :0], room.view(20, 200))
