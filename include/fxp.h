@@ -447,7 +447,7 @@ int fxp_kv_append(const fxp_kv_cache* cache, int type, const void* k, int64_t k_
 
 /* The inverse mapping of cached tokens: row t of k, v [tokens, heads, dim] of `type` receives the values that the
  * token stands for, rounded once (exact in fp32 and bf16 but for overflow and underflow).  runs as above: the tokens
- * at places offset .. offset + count - 1 of a page go to rows first ..; rows of no run are left as they are. */
+ * at places offset .. offset + count - 1 of a page go to rows first ..; rows of no run are left as they are.  k and v share no elements. */
 int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t tokens, const int32_t* runs, int64_t n_runs,
                 void* stream);
 

@@ -762,6 +762,8 @@ def kv_load(cache, runs, tokens, dtype=torch.float32, out=None):
         for t, name in ((k, "k"), (v, "v")):
             if _served(t, name, 3) != code or t.shape != shape or not t.is_contiguous():
                 raise FxpError("the outputs must be contiguous [tokens, heads, dim] tensors of one type")
+        if _share(k, v):
+            raise FxpError("the outputs share elements")
     _check(lib().fxp_kv_load(cache.ref, code, k.data_ptr(), v.data_ptr(), tokens, runs.data_ptr(), runs.shape[0], _stream()), "fxp_kv_load")
     return k, v
 

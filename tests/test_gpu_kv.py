@@ -267,3 +267,18 @@ def test_tables_of_requests_whose_sums_pass_32_bits(fxp, asked, many, tokens, in
     asked = min(asked, tokens)
     assert np.array_equal(host(tab.positions), 7 + np.arange(tokens) % asked)
     assert (host(tab.runs)[:, 2] == -1).all() and not host(tab.ws).any()
+
+
+def test_load_refuses_outputs_that_share_elements(fxp):
+    say("kv_load into one tensor twice")
+    cache = fxp.KvCache(2, 3, 16)
+    cache.kq.fill_(1)
+    cache.vq.fill_(2)
+    runs = dev(np.array([[0, 4, 1, 0]], np.int32))
+    room = torch.zeros((9, 3, 16), device="cuda")
+    for k, v in ((room[:4], room[:4]), (room[:4], room[3:7]), (room[4:8], room[1:5])):
+        with pytest.raises(fxp.FxpError, match="share elements"):
+            fxp.kv_load(cache, runs, 4, out=(k, v))
+    assert not room.any()
+    k, v = fxp.kv_load(cache, runs, 4, out=(room[:4], room[4:8]))
+    assert (k * 2 == v).all() and k.any() and not room[8:].any()
