@@ -456,7 +456,8 @@ int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t t
  * lens_after[b] - n + i and sees the tokens at and before it; with window > 0 only the `window` last of them.
  * out = sum_j softmax_j(scale * q . k_j) v_j with k, v the values that the cache stands for.  Head h of q reads head
  * h / (q_heads / heads) of the cache; q_heads is a multiple of heads, at most 16384.  q and out: [tokens, q_heads, dim] of `type`, strides
- * as in fxp_kv_append; out may be q, and its rows may not overlap; rows behind the last request's are left as they are.  A row that sees nothing (no cached
+ * as in fxp_kv_append; out may be q (with q's strides) and shares no elements with it otherwise, and its rows may not overlap; rows behind
+ * the last request's are left as they are.  A row that sees nothing (no cached
  * token; all of its pages missing) gives zeros and lse -Inf.  Of *step only requests, blocks, tokens, first,
  * lens_after and block_table are used; firsts beyond `tokens` count as `tokens`, tokens on a page outside [0, pages) are not seen.
  * lse: NULL, or [tokens, q_heads] fp32 receiving log sum_j exp(scale * q . k_j).

@@ -782,7 +782,8 @@ class AttentionBuffers:
 
 def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=None):
     """Attention of the step's rows q [tokens, q_heads, dim] over the cache: causal, over the last `window` tokens where it is > 0.
-    scale: dim ** -0.5 by default; lse: [tokens, q_heads] fp32 to fill with the logarithms of the softmax's sums."""
+    scale: dim ** -0.5 by default; out: may be q itself, and shares no elements with it otherwise; lse: [tokens, q_heads] fp32 to fill with
+    the logarithms of the softmax's sums."""
     code = _served(q, "q", 3)
     tokens, q_heads, dim = q.shape
     if tokens != tab.tokens or dim != cache.dim:
@@ -793,6 +794,8 @@ def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=No
         out = q.new_empty((tokens, q_heads, dim))
     elif _served(out, "out", 3) != code or out.shape != q.shape or _rows_overlap(out):
         raise FxpError("out must have the shape and type of q, and rows that do not overlap")
+    elif not _same_rows(out, q) and _share(q, out):
+        raise FxpError("out shares elements with q, and is not q")
     if lse is not None:
         _index(lse, "lse", (tokens, q_heads), torch.float32)
     if buf is None:
@@ -842,13 +845,13 @@ def linear4(x, w, out=None, ws=None):
         raise FxpError("out must be [M, N] of x's type")
     else:
         ldy = _row_stride(out, "out")
+        if _share(x, out):
+            raise FxpError("out shares elements with x")
     if ws is not None:
         _index(ws, "ws", dtype=torch.uint8)
     elif M > 2:
         ws = x.new_empty(int(lib().fxp_w4_workspace_bytes(code, M, K, w.group)), dtype=torch.uint8)
     packed, scales = w.pointers
-        if _share(x, out):
-            raise FxpError("out shares elements with x")
     _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), ldy, _p(ws),
                                ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
     return out

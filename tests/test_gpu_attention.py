@@ -284,3 +284,57 @@ def test_attention_of_rows_that_are_not_finite(fxp):
     assert torch.equal(out[1], want[1]) and torch.isfinite(out).all()
     c.cache.ek.fill_(255)
     assert torch.isfinite(fxp.kv_attention(c.dq * 1e30, c.cache, c.tab, scale=c.scale)).all()
+
+
+def one_large_weight(fxp, c, above):
+    """Every row of c scores `above` at the first token of each request and 0 at the others; all values are 1."""
+    c.cache.kq.zero_()
+    c.cache.ek.fill_(127)                                     # 64 * 2^(127 - 133) = 1
+    c.cache.kq[torch.tensor(c.table[:, 0]).long(), :, 0, 0] = 64
+    c.cache.vq.fill_(64)
+    c.cache.ev.fill_(127)
+    c.dq.zero_()
+    c.dq[:, :, 0] = 1
+    return float(torch.tensor(above, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("lens,news,QH,H,D", [([64], [1], 2, 1, 64), ([1500, 3], [1, 1], 4, 2, 64), ([900], [2], 4, 1, 160), ([257], [257], 64, 16, 16),
+                                              ([300, 140], [150, 140], 48, 48, 128)])
+def test_attention_to_values_of_one_is_one(fxp, kind, lens, news, QH, H, D):
+    """Outputs are divided by the sum of the weights they were made with, as rounded.  An output and that sum then differ by the fp32 roundings
+    of either: a page's product (three with a third digit) and its place in the sum, for up to 24 pages, the joins of eight parts and the quotient:
+    fewer than 2 * (24 * 4 + 40) of 2^-24, below 2^-15.  Rounded to 8 or 11 bits, 1 less 2^-15 is 1.  `above`: 63 weights of 1.5e-5, under half
+    a unit of 1/32639, so that none of them reaches the output, and of 4.6e-5, which are rounded up."""
+    say("kv_attention over values of one", kind, (lens, news, QH, H, D))
+    c = Case(fxp, lens, news, QH, H, D, kind)
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale))
+    for above in (11.1, 10.0, 0.5):
+        scale = one_large_weight(fxp, c, above)
+        lse = torch.empty((c.T, QH), device="cuda")
+        out = fxp.kv_attention(c.dq, c.cache, c.tab, scale=scale, lse=lse).double()
+        if kind == "fp32":
+            assert float((out - 1).abs().max()) <= 2.0 ** -15
+        else:
+            assert (out == 1).all(), float((out - 1).abs().max())
+        # the logarithm's sum has the weights as they are: fp32 roundings of as many terms
+        seen = np.concatenate([n_all - n + 1 + np.arange(n) for n_all, n in zip(lens, news)])
+        want = above + np.log1p((seen - 1) * np.exp(-above))
+        assert np.abs(lse.double().cpu().numpy() - want[:, None]).max() <= 2.0 ** -15 + 2.0 ** -21 * above
+
+
+def test_attention_refuses_an_output_that_is_q_in_part(fxp):
+    say("kv_attention, out over a part of q")
+    c = Case(fxp, [700, 20], [2, 1], 4, 2, 64, "bf16")
+    room = torch.zeros((4, 4, 200), dtype=torch.bfloat16, device="cuda")
+    q = room[:3, :, :64]
+    q.copy_(c.dq)
+    flat = room.view(-1)
+    for out in (room[1:, :, :64], room[:3, :, 1:65], room[:3, :, 63:127], flat[64:64 + 3 * 256].view(3, 4, 64), flat.as_strided((3, 4, 64), (64, 192, 1)),
+                q.transpose(0, 1)[:3].as_strided((3, 4, 64), (200, 800, 1))):
+        with pytest.raises(fxp.FxpError):
+            fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=out)
+    assert torch.equal(q, c.dq)
+    want = fxp.kv_attention(q, c.cache, c.tab, scale=c.scale)
+    assert torch.equal(fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=room[:3, :, 64:128]), want)
+    assert torch.equal(fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=q), want)
