@@ -11,9 +11,8 @@
 // softmax's weights never leave their lane.
 //
 // Digits.  A row of Q is v * 2^u with |v| < 2^15 (2^23) and v = 256 d1 + d0 (65536 d2 + ...), d signed bytes; a page's weights
-// likewise under their own largest one.  Rounding a row to 15 bits is off by at most 2^-16 of its largest element's binade
-// - for bf16 and fp16 rows less than half a step of the type for elements within 2^-8 / 2^-5 of the largest - and weights
-// relative to the page's own largest, so a long tail of small weights behind one large one keeps its sum.  fp32 has 23 bits.
+// likewise under their own largest one.  Outputs are divided by the sum of the weights as rounded, so that they stay weighted means of the
+// values (constant values come out as they are, whatever the scores); the sum of the weights as they are serves lse alone.
 #include <algorithm>
 
 #include "fxp_serve_device.h"
@@ -42,7 +41,7 @@ struct AttArgs {
     int64_t out_token, out_head;
     float* lse;
     float* part_o;          // [workgroup][2][16][dim]: parts of the tiles that the stretch ends in (0) and begins in (1)
-    float2* part_ml;        // [workgroup][2][16]: largest score (log2), sum
+    float4* part_ml;        // [workgroup][2][16]: reference score (log2), sum of the weights as rounded, sum of the weights
     uint32_t* tickets;      // [workgroup]: parts that are there of the tile that begins in this stretch and ends in another; zero between calls
     int group;              // query heads per head of the cache
     uint32_t group_inverse; // ceil(2^32 / group): (x * it) >> 32 is x / group for x * group < 2^32
@@ -240,11 +239,13 @@ __device__ inline int query_digits(const float (&x)[DB][16], v4i (&qd)[DB][ND]) 
     return unit;
 }
 
-// Weights 2^(f s - top) of 16 scores as digits, and their sum; `top` becomes the score that weighs 1 (32767 / 32639 for two digits: the
-// packing conversion multiplies by 32767, and the largest weight has to stay at 127 in each digit).
+// Weights 2^(f s - top) of 16 scores as digits, and their sum before the rounding; `top` becomes the score that weighs 1 (32767 / 32639 for two digits: the
+// packing conversion multiplies by 32767, and the largest weight has to stay at 127 in each digit).  rounded: of three digits, the sum
+// of the weights in their units.
 template <int ND>
-__device__ inline float weigh(const float (&s)[16], float f, float& top, v4i (&pd)[1][ND]) {
+__device__ inline float weigh(const float (&s)[16], float f, float& top, v4i (&pd)[1][ND], int& rounded) {
     float l = 0.0f;
+    rounded = 0;
     if constexpr (ND == 2) {
         top += 0.00564698f;                    // log2(32767 / 32639), rounded up
 #pragma unroll
@@ -268,6 +269,7 @@ __device__ inline float weigh(const float (&s)[16], float f, float& top, v4i (&p
             const float w = __builtin_amdgcn_exp2f(fmaf(s[i], f, -top));
             l += w;
             v[i] = static_cast<int>(rintf(w * Digits<ND>::kMost));
+            rounded += v[i];
         }
         digits16<ND>(v, pd[0]);
     }
@@ -299,20 +301,56 @@ __device__ inline void hide(float (&s)[16], bool all, int to, int from) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = ((i > last) | (i < from)) ? -INFINITY : s[i];
 }
-// One page of a row: the weights of this lane's 16 scores f * s as digits, the row's reference and sum (of this lane's tokens) moved on.
+// One page of a row: the weights of this lane's 16 scores f * s as digits, the row's reference and sum (of this lane's tokens, for lse) moved on.
 template <int ND>
-__device__ inline Turn softmax_page(const float (&s)[16], float f, float& ref, float& l, v4i (&pd)[1][ND]) {
+__device__ inline Turn softmax_page(const float (&s)[16], float f, float& ref, float& l, v4i (&pd)[1][ND], int& rounded) {
     float m = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) m = fmaxf(m, s[i]);
     m = swap_max(m) * f;
     // a little above the largest score: f s - top rounds once, and must not come out above 0
     float top = m == -INFINITY ? 0.0f : fmaf(fabsf(m), 0x1p-22f, m);
-    const float sum = weigh<ND>(s, f, top, pd);
+    const float sum = weigh<ND>(s, f, top, pd, rounded);
     const Turn turn = next_reference(ref, m == -INFINITY ? m : top);
     l = l * turn.keep + sum * turn.gain;
     ref = turn.ref;
     return turn;
+}
+
+// One page's values, weighted by `pd`, added to a row's outputs in units of `fv`, and the sum of these weights to `r` in units of `fr`: two
+// digits by one more tile of the products, whose values are ones, for all 64 tokens (the matrix cores have the time); three, which have no
+// registers for its sums (12 spilled), by `rounded`, that of this lane's 16 tokens.
+// value_of(i): this lane's bytes of the i-th 16 elements of the page's values.
+template <int ND, int DB, typename F>
+__device__ inline void add_values(F value_of, const v4i (&pd)[1][ND], int rounded, float fv, float fr, float (&o)[4 * DB][4], float& r) {
+    auto add = [&](int i, const float(&y)[4]) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[i][j] = fmaf(y[j], fv, o[i][j]);
+    };
+    if constexpr (ND == 3) r = fmaf(static_cast<float>(rounded), fr, r);
+#pragma unroll
+    for (int i = 0; i < 4 * DB; i += 4) {
+        if (ND == 2 && i == 0) {
+            constexpr int kOnes = 0x01010101;
+            const v4i five[5][1] = {{value_of(0)}, {value_of(1)}, {value_of(2)}, {value_of(3)}, {v4i{kOnes, kOnes, kOnes, kOnes}}};
+            float y[5][4];
+            dot_digits<ND, 1, 5>(five, pd, y);
+            r = fmaf(y[4][0], fr, r);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) add(t, y[t]);
+        } else {
+            const v4i four[4][1] = {{value_of(i)}, {value_of(i + 1)}, {value_of(i + 2)}, {value_of(i + 3)}};
+            float y[4][4];
+            dot_digits<ND, 1, 4>(four, pd, y);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) add(i + t, y[t]);
+        }
+    }
+}
+// the sum over a row's lanes, where add_values left each its own part
+template <int ND>
+__device__ inline float whole_sum(float r) {
+    return ND == 3 ? swap_sum(r) : r;
 }
 
 // Rows of a tile: row i is token tok + (rest + i) / group of the request, head (rest + i) % group of its group.
@@ -331,13 +369,13 @@ __device__ inline TileRows tile_rows(const AttArgs& a, int tile) {
 
 // one row's share of four elements, and the join of two shares
 struct Share {
-    float m, l, x[4];
+    float m, r, x[4];           // reference, sum of the weights as rounded, elements
 };
-__device__ inline void join(Share& s, float m, float l, const float4 y) {
+__device__ inline void join(Share& s, float m, float r, const float4 y) {
     const float top = fmaxf(s.m, m), ref = top == -INFINITY ? 0.0f : top;
     const float keep = __builtin_amdgcn_exp2f(s.m - ref), gain = __builtin_amdgcn_exp2f(m - ref);
     s.m = top;
-    s.l = s.l * keep + l * gain;
+    s.r = s.r * keep + r * gain;
     s.x[0] = s.x[0] * keep + y.x * gain;
     s.x[1] = s.x[1] * keep + y.y * gain;
     s.x[2] = s.x[2] * keep + y.z * gain;
@@ -356,20 +394,23 @@ template <int TYPE>
 __device__ inline void finish(const AttArgs& a, const Extent& e, const TileRows& rows_of, int head, int row, int d, Share s) {
     int tok, in_group;
     rows_of.at(a, row, tok, in_group);
-    const int64_t t = int64_t{e.tok0} + tok;
-    const int h = head * a.group + in_group;
-    const float inv = s.l > 0.0f ? 1.0f / s.l : 0.0f;
+    const float inv = s.r > 0.0f ? 1.0f / s.r : 0.0f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) s.x[j] *= inv;
-    store4<TYPE>(a.out, t * a.out_token + h * a.out_head + d, a.vec_out, s.x);
-    if (a.lse && d == 0) a.lse[t * (static_cast<int>(a.c.heads) * a.group) + h] = s.l > 0.0f ? (s.m + log2f(s.l)) * 0.693147180559945f : -INFINITY;
+    store4<TYPE>(a.out, (int64_t{e.tok0} + tok) * a.out_token + (head * a.group + in_group) * a.out_head + d, a.vec_out, s.x);
+}
+__device__ inline void finish_lse(const AttArgs& a, const Extent& e, const TileRows& rows_of, int head, int row, float m, float l) {
+    int tok, in_group;
+    rows_of.at(a, row, tok, in_group);
+    a.lse[(int64_t{e.tok0} + tok) * (static_cast<int>(a.c.heads) * a.group) + head * a.group + in_group] =
+        l > 0.0f ? (m + log2f(l)) * 0.693147180559945f : -INFINITY;
 }
 
 template <int TYPE, int DB>
 __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(AttArgs a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, WAVES = kAttWaves, THREADS = 64 * WAVES, COST = kTileCost;
     constexpr int DMAX = 64 * DB, ROW = DMAX + 4;
-    __shared__ float s_m[WAVES][kTile], s_l[WAVES][kTile];
+    __shared__ float s_m[WAVES][kTile], s_r[WAVES][kTile], s_l[WAVES][kTile];
     __shared__ float4 s_o4[WAVES * kTile * ROW / 4];
     __shared__ int s_last;
     float* const s_o = reinterpret_cast<float*>(s_o4);
@@ -461,7 +502,7 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
             if (kAhead) load_v(at_next, dead_next);
 
             float o[4 * DB][4];
-            float m_run = -INFINITY, l_run = 0.0f;                     // l_run: of this lane's 16 tokens of each page
+            float m_run = -INFINITY, r_run = 0.0f, l_run = 0.0f;       // l_run: of this lane's 16 tokens of each page
 #pragma unroll
             for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
@@ -486,24 +527,17 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                     const int j0 = (e.page0 + from + WAVES * n) * FXP_KV_PAGE;
                     if (dead || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) hide(s, dead, see_to - j0 - 16 * g, see_from - j0 - 16 * g);
                     v4i pd[1][ND];
-                    const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd);
-                    const float fv = ldexpf(turn.gain * kWeightUnit<ND>, ev);
+                    int rounded;
+                    const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd, rounded);
+                    const float fr = turn.gain * kWeightUnit<ND>, fv = ldexpf(fr, ev);
                     if (__any(turn.keep != 1.0f)) {
+                        r_run *= turn.keep;
 #pragma unroll
                         for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
                             for (int j = 0; j < 4; ++j) o[i][j] *= turn.keep;
                     }
-#pragma unroll
-                    for (int i = 0; i < 4 * DB; i += 4) {
-                        float y[4][4];
-                        const v4i four[4][1] = {{vf[i]}, {vf[i + 1]}, {vf[i + 2]}, {vf[i + 3]}};
-                        dot_digits<ND, 1, 4>(four, pd, y);
-#pragma unroll
-                        for (int t = 0; t < 4; ++t)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) o[i + t][j] = fmaf(y[t][j], fv, o[i + t][j]);
-                    }
+                    add_values<ND, DB>([&](int i) { return vf[i]; }, pd, rounded, fv, fr, o, r_run);
                     if (kAhead) load_v(at_next, none);
                 }
                 from += 64 * WAVES;
@@ -517,8 +551,10 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
 
             // the waves' parts
             l_run = swap_sum(l_run);
+            r_run = whole_sum<ND>(r_run);
             if (g == 0) {
                 s_m[wave][col] = m_run;
+                s_r[wave][col] = r_run;
                 s_l[wave][col] = l_run;
             }
 #pragma unroll
@@ -533,6 +569,7 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
             for (int i = threadIdx.x; i < rows * nd; i += THREADS) {
                 const int row = i / nd, d = i % nd * 4;
                 Share s = {s_m[0][row], 0.0f, {0.0f, 0.0f, 0.0f, 0.0f}};
+                float l = 0.0f;
 #pragma unroll
                 for (int w = 1; w < WAVES; ++w) s.m = fmaxf(s.m, s_m[w][row]);
                 const float ref = s.m == -INFINITY ? 0.0f : s.m;
@@ -540,7 +577,8 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                 for (int w = 0; w < WAVES; ++w) {
                     const float f = __builtin_amdgcn_exp2f(s_m[w][row] - ref);
                     const float4 y = *reinterpret_cast<const float4*>(s_o + (w * kTile + row) * ROW + d);
-                    s.l = fmaf(s_l[w][row], f, s.l);
+                    s.r = fmaf(s_r[w][row], f, s.r);
+                    l = fmaf(s_l[w][row], f, l);
                     s.x[0] = fmaf(y.x, f, s.x[0]);
                     s.x[1] = fmaf(y.y, f, s.x[1]);
                     s.x[2] = fmaf(y.z, f, s.x[2]);
@@ -548,11 +586,15 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                 }
                 if (whole) {
                     finish<TYPE>(a, e, rows_of, head, row, d, s);
+                    if (a.lse && d == 0) finish_lse(a, e, rows_of, head, row, s.m, l);
                 } else {
                     const int64_t part = (int64_t{blockIdx.x} * 2 + (static_cast<int>(blockIdx.x) == w_first)) * kTile + row;
                     store_part(a.part_o + part * dim + d, s.x[0], s.x[1]);
                     store_part(a.part_o + part * dim + d + 2, s.x[2], s.x[3]);
-                    if (d == 0) store_part(&a.part_ml[part].x, s.m, s.l);
+                    if (d == 0) {
+                        store_part(&a.part_ml[part].x, s.m, s.r);
+                        store_part(&a.part_ml[part].z, l, 0.0f);
+                    }
                 }
             }
             if (!whole) {
@@ -581,31 +623,43 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
                             const int row = i / nd, d = i % nd * 4;
                             // kBatch parts on their way at a time; one behind the last is the last again, left out of the sum
                             for (int w0 = w_first + way; w0 <= w_last; w0 += kBatch * ways) {
-                                float2 ml[kBatch], x[kBatch], y[kBatch];
+                                float2 mr[kBatch], x[kBatch], y[kBatch];
 #pragma unroll
                                 for (int n = 0; n < kBatch; ++n) {
                                     const int w = min(w0 + n * ways, w_last);
                                     const int64_t part = (int64_t{w} * 2 + (w == w_first)) * kTile + row;
-                                    ml[n] = load_part(&a.part_ml[part].x);
+                                    mr[n] = load_part(&a.part_ml[part].x);
                                     x[n] = load_part(a.part_o + part * dim + d);
                                     y[n] = load_part(a.part_o + part * dim + d + 2);
                                 }
 #pragma unroll
                                 for (int n = 0; n < kBatch; ++n)
-                                    if (w0 + n * ways <= w_last) join(s, ml[n].x, ml[n].y, make_float4(x[n].x, x[n].y, y[n].x, y[n].y));
+                                    if (w0 + n * ways <= w_last) join(s, mr[n].x, mr[n].y, make_float4(x[n].x, x[n].y, y[n].x, y[n].y));
                             }
                         }
                         if (ways > 1) {                                 // work < THREADS: one turn of the outer loop
                             s_o4[threadIdx.x] = make_float4(s.x[0], s.x[1], s.x[2], s.x[3]);
-                            s_o4[THREADS + threadIdx.x] = make_float4(s.m, s.l, 0.0f, 0.0f);
+                            s_o4[THREADS + threadIdx.x] = make_float4(s.m, s.r, 0.0f, 0.0f);
                             __syncthreads();
                             if (way == 0)
                                 for (int w = 1; w < ways; ++w) {
-                                    const float4 ml = s_o4[THREADS + i + w * work];
-                                    join(s, ml.x, ml.y, s_o4[i + w * work]);
+                                    const float4 mr = s_o4[THREADS + i + w * work];
+                                    join(s, mr.x, mr.y, s_o4[i + w * work]);
                                 }
                         }
                         if (i < work && way == 0) finish<TYPE>(a, e, rows_of, head, i / nd, i % nd * 4, s);
+                    }
+                    // apart from the rest: in the loop above these loads cost calls without lse as much (52000 tokens, 2 heads of 128: 31 us, 23 so)
+                    if (a.lse && static_cast<int>(threadIdx.x) < rows) {
+                        float m = -INFINITY, l = 0.0f;
+                        for (int w = w_first; w <= w_last; ++w) {
+                            const float* const part = &a.part_ml[(int64_t{w} * 2 + (w == w_first)) * kTile + threadIdx.x].x;
+                            const float m_part = load_part(part).x, l_part = load_part(part + 2).x, top = fmaxf(m, m_part);
+                            const float ref = top == -INFINITY ? 0.0f : top;
+                            l = l * __builtin_amdgcn_exp2f(m - ref) + l_part * __builtin_amdgcn_exp2f(m_part - ref);
+                            m = top;
+                        }
+                        finish_lse(a, e, rows_of, head, threadIdx.x, m, l);
                     }
                 }
             }
@@ -717,7 +771,7 @@ __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_r
         }
     };
 
-    float o[4 * DB][4], m_run = -INFINITY, l_run = 0.0f;
+    float o[4 * DB][4], m_run = -INFINITY, r_run = 0.0f, l_run = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
@@ -752,30 +806,22 @@ __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_r
             }
             if (dead || j0 + FXP_KV_PAGE - 1 > all_to || j0 < all_from) hide(s, dead, see_to - j0 - 16 * g, see_from - j0 - 16 * g);
             v4i pd[1][ND];
-            const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd);
-            const float fv = ldexpf(turn.gain * kWeightUnit<ND>, ev);
+            int rounded;
+            const Turn turn = softmax_page<ND>(s, score_unit<ND>(a, qe + ek), m_run, l_run, pd, rounded);
+            const float fr = turn.gain * kWeightUnit<ND>, fv = ldexpf(fr, ev);
             if (__any(turn.keep != 1.0f)) {
+                r_run *= turn.keep;
 #pragma unroll
                 for (int i = 0; i < 4 * DB; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[i][j] *= turn.keep;
             }
-#pragma unroll
-            for (int i = 0; i < 4 * DB; i += 4) {
-                const v4i* const vt = vl + g * dim + 16 * i + col;
-                const v4i vf[4][1] = {{vt[0]}, {vt[16]}, {vt[32]}, {vt[48]}};
-                float x[4][4];
-                dot_digits<ND, 1, 4>(vf, pd, x);
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[i + t][j] = fmaf(x[t][j], fv, o[i + t][j]);
-            }
+            add_values<ND, DB>([&](int i) { return vl[g * dim + 16 * i + col]; }, pd, rounded, fv, fr, o, r_run);
         }
         if (p + 1 < p_end) put(buffer ^ 1);
         __syncthreads();
     }
-    const float l = swap_sum(l_run), inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float l = swap_sum(l_run), r = whole_sum<ND>(r_run), inv = r > 0.0f ? 1.0f / r : 0.0f;
     if (!row_ok) return;
     const int64_t t = int64_t{e.tok0} + tok;
     const int h = head * a.group + in_group;
@@ -800,7 +846,7 @@ static bool attention_sizes_ok(int64_t requests, int64_t tokens, int64_t q_heads
 
 extern "C" size_t fxp_kv_attention_workspace_bytes(int64_t requests, int64_t tokens, int64_t q_heads, int64_t heads, int64_t dim) {
     if (!fxp::attention_sizes_ok(requests, tokens, q_heads, heads, dim)) return 0;
-    return FXP_KV_TICKET_BYTES + static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float2));
+    return FXP_KV_TICKET_BYTES + static_cast<size_t>(fxp::kAttGroups) * 2 * fxp::kTile * (dim * sizeof(float) + sizeof(float4));
 }
 
 extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st, int type, const void* q, int64_t q_token, int64_t q_head,
@@ -842,7 +888,7 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
     a.tickets = static_cast<uint32_t*>(ws);
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(ws) + FXP_KV_TICKET_BYTES);
     static_assert(FXP_KV_TICKET_BYTES == kAttGroups * sizeof(uint32_t), "a ticket for each workgroup");
-    a.part_ml = reinterpret_cast<float2*>(a.part_o + static_cast<size_t>(kAttGroups) * 2 * kTile * cache->dim);
+    a.part_ml = reinterpret_cast<float4*>(a.part_o + static_cast<size_t>(kAttGroups) * 2 * kTile * cache->dim);
     a.group = static_cast<int>(q_heads / cache->heads);
     a.group_inverse = static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group);
     a.vec_q = aligned(q, 16) && q_token * size % 16 == 0 && q_head * size % 16 == 0;
