@@ -14,6 +14,7 @@
 // likewise under their own largest one.  Outputs are divided by the sum of the weights as rounded, so that they stay weighted means of the
 // values (constant values come out as they are, whatever the scores); the sum of the weights as they are serves lse alone.
 #include <algorithm>
+#include <limits>
 
 #include "fxp_serve_device.h"
 
@@ -21,6 +22,7 @@ namespace fxp {
 
 constexpr int kTile = 16;
 constexpr int kFewRows = 2 * kTile;
+constexpr int kShortTable = 32;      // pages
 constexpr int kAttWaves = 4;
 // Workgroups: as many as are resident, one round of them.  Up to 128 elements two a CU (768, which three a CU have room for, split more tiles: 57 -> 67 us
 // for 64 requests); rows of more take the registers of one (64 requests of 200 to 4000 tokens, 4 heads of 192: 33 us, 39 with 512 workgroups, 35 with 512 and
@@ -49,24 +51,57 @@ struct AttArgs {
     float scale_log2;       // scale * log2(e)
     int window;             // 0: none
     float join_turns;       // of a workgroup over the elements of a tile, four a thread, as the requests are on average
-    int few_rows;           // requests of more rows are the other kernel's; 0: one kernel has all
+    int rows_from;          // requests of more rows are k_kv_attend_rows's, unless they are too long for it
+    int walk;               // window > 0: pages that 64 rows see, at most
+    bool balance;           // both kernels are launched, and requests that are too long for k_kv_attend_rows left to the other
+    int longest;            // walk from which on they are (longest_walk)
 };
 
+constexpr int kCus = 256, kShortWalk = 16, kRowWaves = 4, kBlock = kRowWaves * kTile;
+
+// n, len: rows (tokens) and cached tokens of a request; tiles: of kTile rows, 0 where the request is k_kv_attend_rows's
 struct Extent {
     int n, len, tiles, page0, pages, tok0;
 };
+// blocks of kBlock rows of a request of many rows
+__device__ inline int blocks_of(const AttArgs& a, const Extent& e) {
+    const int rows = e.n * a.group;
+    return rows > a.rows_from ? (rows + kBlock - 1) / kBlock : 0;
+}
+// pages that a workgroup of k_kv_attend_rows goes through one after the other, at most
+__device__ inline int walk_of(const AttArgs& a, const Extent& e) { return a.window > 0 ? min(e.pages, a.walk) : e.pages; }
 __device__ inline Extent extent(const AttArgs& a, int64_t b) {
     Extent e;
     const int most = static_cast<int>(a.tokens);
     e.tok0 = min(max(a.first[b], 0), most);
     e.n = max(min(max(a.first[b + 1], 0), most) - e.tok0, 0);
     e.len = static_cast<int>(min(static_cast<int64_t>(max(a.lens[b], 0)), a.blocks * FXP_KV_PAGE));
-    e.tiles = (e.n * a.group + kTile - 1) / kTile;
-    if (a.few_rows > 0 && e.n * a.group > a.few_rows) e.tiles = 0;
     const int from = a.window > 0 ? max(e.len - e.n + 1 - a.window, 0) : 0;
     e.page0 = from / FXP_KV_PAGE;
     e.pages = max((e.len + FXP_KV_PAGE - 1) / FXP_KV_PAGE - e.page0, 1);       // an empty request still has its zeros to write
+    e.tiles = blocks_of(a, e) && walk_of(a, e) <= a.longest ? 0 : (e.n * a.group + kTile - 1) / kTile;
     return e;
+}
+
+// The longest walk that k_kv_attend_rows takes on: a CU's share of the pages that all requests of many rows go through there.  It cannot split a
+// context, and one that is longer than that would be walked by a few workgroups while the others have nothing left to do; k_kv_attend
+// spreads it over all.  (22 requests of 40 rows, 8 heads of 64, one of them of 131000 tokens among 500s: 70 us, 1830 without this rule; all of 8000: 75
+// / 127.)  Of one request it is whether it has 256 blocks.  Up to kShortWalk pages it is the better one all the same (22 requests of 500
+// tokens: 16 us, 22 of the other).  In whole numbers: both kernels have to come to the same.
+__device__ inline int longest_walk(const AttArgs& a) {
+    static_assert(kAttWaves == kRowWaves, "workgroups of 256 threads, all of which come here");
+    __shared__ unsigned long long s_sum[kAttWaves];
+    unsigned long long sum = 0;
+    for (int64_t b = threadIdx.x; b < a.requests; b += 64 * kAttWaves) {
+        const Extent e = extent(a, b);
+        sum += static_cast<unsigned long long>(blocks_of(a, e) * static_cast<int>(a.c.heads)) * static_cast<uint32_t>(walk_of(a, e));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = s_sum[0] + s_sum[1] + s_sum[2] + s_sum[3];
+    return __builtin_amdgcn_readfirstlane(static_cast<int>(min(max(sum / kCus, uint64_t{kShortWalk}), uint64_t{0x7fffffff})));
 }
 
 // Cost of a tile in pages besides its own: its rows of q, the join of its parts, the first loads' way.  (Without it a workgroup
@@ -417,6 +452,7 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads), nd = dim / 4;
     uint32_t per = 0;
+    if (a.balance) a.longest = longest_walk(a);
     const Found st = find_request(
         a, [&](const Extent& x) { return static_cast<uint32_t>(x.tiles * heads) * static_cast<uint32_t>(x.pages + COST); },
         [&](uint32_t units, int most_pages) {
@@ -688,22 +724,21 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
 // In LDS the keys stand by pieces of 16 elements, [dim / 16][64 places][16], the places in the order that the A operand takes
 // them, turned by twice the piece's number: 16 lanes then read 256 consecutive bytes, and the 16 pieces that 16
 // lanes write (8 of a token, two tokens) fall on 16 different ones.
-constexpr int kRowWaves = 4;
-
 template <int TYPE, int DB>
 __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_rows(AttArgs a) {
     constexpr int ND = TYPE == FXP_F32 ? 3 : 2, PAGE_BYTES = 64 * 64 * DB, THREADS = 64 * kRowWaves;
     __shared__ v4i lds[2][2][PAGE_BYTES / 16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, g = lane >> 4;
     const int dim = static_cast<int>(a.c.dim), heads = static_cast<int>(a.c.heads);
-    constexpr int ROWS = kRowWaves * kTile;
 
-    // the request and the block of its rows; the last blocks come first, because they see the most pages
+    // the request and the block of its rows, too long ones among them; the last blocks come first, because they see the most pages
     const int line = static_cast<int>(gridDim.x - 1 - blockIdx.x), want = line / heads, head = line - want * heads;
     const Found found = find_request(
-        a, [&](const Extent& x) { return static_cast<uint32_t>(x.n * a.group > a.few_rows ? (x.n * a.group + ROWS - 1) / ROWS : 0); },
-        [&](uint32_t, int) { return static_cast<uint32_t>(want); });
+        a, [&](const Extent& x) { return static_cast<uint32_t>(blocks_of(a, x)); }, [&](uint32_t, int) { return static_cast<uint32_t>(want); });
     if (found.b < 0) return;
+    // (a request's own pages are its walk for each of its blocks: of 256 blocks and more it is within the share, whatever the others are)
+    const int walk = walk_of(a, found.e);
+    if (a.balance && walk > kShortWalk && blocks_of(a, found.e) * heads < kCus && walk > longest_walk(a)) return;
     const int b = found.b, block = want - static_cast<int>(found.before);
     const Extent e = found.e;
 
@@ -722,7 +757,7 @@ __global__ __launch_bounds__(64 * kRowWaves, DB <= 2 ? 3 : 2) void k_kv_attend_r
     // pages that any row of the workgroup sees, places that every and any row of the wave does
     const TileRows first_of = tile_rows(a, block * kRowWaves);
     int last_tok, wave_last, unused;
-    first_of.at(a, ROWS - 1, last_tok, unused);
+    first_of.at(a, kBlock - 1, last_tok, unused);
     wave_of.at(a, kTile - 1, wave_last, unused);
     last_tok = min(last_tok, e.n - 1);
     wave_last = min(wave_last, e.n - 1);
@@ -903,17 +938,25 @@ extern "C" int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* st
         // Many rows a request, and enough blocks of 64 for every CU: the kernel that shares pages among rows (16 heads, 4 of the cache,
         // 128 elements, one request: 1024 rows of 0 earlier tokens 12 us against 13 of the other kernel, 2048 18 / 24, 8192 68 / 219).  It has no
         // way to split a context: with half as many blocks as CUs, 1024 rows behind 4000 tokens take 92 us against 53.  Requests of up to two
-        // tiles stay with the other kernel (32 rows: 24 us against 30; 35 rows, three tiles: 36 / 28).
-        constexpr int kRows = kRowWaves * kTile;
-        const int64_t blocks = (st->tokens * a.group + (kRows - 1) * st->requests) / kRows * cache->heads;
-        const bool many = st->tokens * a.group > kFewRows * st->requests && blocks >= 256 && blocks < int64_t{1} << 24;
-        a.few_rows = many && st->requests > 1 ? kFewRows : 0;
+        // tiles stay with the other kernel (32 rows: 24 us against 30; 35 rows, three tiles: 36 / 28), and so do, found on the device, those
+        // too long for their number of rows (longest_walk).  One request whose table holds few pages needs the one launch only: its walk is short
+        // whatever its rows are.
+        const int64_t blocks = (st->tokens * a.group + (kBlock - 1) * st->requests) / kBlock * cache->heads;
+        const bool many = st->tokens * a.group > kFewRows * st->requests && blocks >= kCus && blocks < int64_t{1} << 24;
         // units of the line, which are counted in 32 bits
-        const int64_t tiles = (st->tokens * a.group + (kTile - 1) * st->requests) / kTile, line_tiles = a.few_rows ? std::min(tiles, 2 * st->requests) : tiles;
-        if ((!many || a.few_rows) && line_tiles * cache->heads * (st->blocks + kTileCost) >= int64_t{1} << 31) return FXP_ERR_DIMS;
+        auto fit = [&](int64_t tiles) { return tiles * (st->blocks + kTileCost) < int64_t{1} << 31; };
+        const int64_t tiles = (st->tokens * a.group + (kTile - 1) * st->requests) / kTile * cache->heads;
+        const int64_t short_tiles = std::min(tiles, 2 * st->requests * cache->heads);
+        const bool both = many && (st->requests > 1 || (st->blocks > kShortTable && fit(short_tiles)));
+        if ((!many && !fit(tiles)) || (both && !fit(short_tiles))) return FXP_ERR_DIMS;
+        // walks that are longer than a CU's share have fewer blocks together than there are CUs
+        a.balance = both && fit(short_tiles + std::min<int64_t>(tiles, kCus * kRowWaves));
+        a.rows_from = !many ? std::numeric_limits<int>::max() : both ? kFewRows : 0;
+        a.longest = std::numeric_limits<int>::max();
+        a.walk = a.window / FXP_KV_PAGE + (kBlock / a.group + 1) / FXP_KV_PAGE + 3;
         if (many)
             hipLaunchKernelGGL((k_kv_attend_rows<TYPE, DB>), dim3(static_cast<unsigned>(blocks)), dim3(64 * kRowWaves), 0, s, a);
-        if (!many || a.few_rows) hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroupsOf<DB>), dim3(64 * kAttWaves), 0, s, a);
+        if (!many || both) hipLaunchKernelGGL((k_kv_attend<TYPE, DB>), dim3(kAttGroupsOf<DB>), dim3(64 * kAttWaves), 0, s, a);
         return launch_status();
     };
     auto of_type = [&](auto type_c) {

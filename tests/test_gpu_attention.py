@@ -338,3 +338,53 @@ def test_attention_refuses_an_output_that_is_q_in_part(fxp):
     want = fxp.kv_attention(q, c.cache, c.tab, scale=c.scale)
     assert torch.equal(fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=room[:3, :, 64:128]), want)
     assert torch.equal(fxp.kv_attention(q, c.cache, c.tab, scale=c.scale, out=q), want)
+
+
+# requests of many rows, some of them too long for their number of rows beside the others; lengths, new tokens, query heads, heads, dim, rows behind, window
+LONG = [([6000, 3, 200, 300, 64], [40, 1, 200, 200, 40], 28, 14, 64, 0, 0), ([5000], [40], 16, 8, 64, 1001, 0), ([2500, 2600, 300], [50, 1, 300], 64, 16, 16, 0, 0),
+        ([4000, 4000, 1100], [60, 33, 600], 16, 16, 80, 5, 3000), ([200, 5000, 40], [200, 40, 40], 96, 24, 128, 0, 0), ([3000, 90], [70, 90], 66, 66, 160, 0, 0)]
+
+
+@pytest.mark.parametrize("lens,news,QH,H,D,behind,window", LONG)
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_attention_of_prompts_beside_long_contexts(fxp, lens, news, QH, H, D, behind, window, kind):
+    say("kv_attention of many rows, long contexts among them", (lens, news, QH, H, D, behind, window, kind))
+    c = Case(fxp, lens, news, QH, H, D, kind, behind=behind)
+    out, lse = torch.full((c.T, QH, D), 9.0, dtype=c.dq.dtype, device="cuda"), torch.full((c.T, QH), 9.0, device="cuda")
+    buf = fxp.AttentionBuffers(len(lens), c.T, QH, c.cache)
+    for _ in range(2):
+        fxp.kv_attention(c.dq, c.cache, c.tab, buf, scale=c.scale, window=window, out=out, lse=lse)
+    c.check(out, lse, window)
+    assert (out[c.first[-1]:] == 9).all() and (lse[c.first[-1]:] == 9).all() and not buf.ws[:fxp.KV_TICKET_BYTES].any()
+
+
+def test_attention_to_one_long_context_is_spread_out_whatever_else_is_in_the_step(fxp):
+    """22 requests of 40 rows, 131000 tokens in one of them: one page after the other, eight workgroups take 25 times as long as all for it and for the
+    rest apart; 4 times is the limit here."""
+    say("kv_attention, a long context among short ones, timed")
+    H, QH, D, long_, short = 8, 64, 64, 131000, 500
+    rng = np.random.default_rng(0)
+    i8 = lambda *shape: dev(rng.integers(-100, 101, shape).astype(np.int8))  # noqa: E731
+    ones = lambda: torch.full((100, H), 127, dtype=torch.int32, device="cuda")  # noqa: E731
+    cache = fxp.KvCache.of(i8(100, H, 64, D), i8(100, H, 4, D, 16), ones(), ones())
+
+    def time_of(lens):
+        tab = fxp.KvTables(len(lens), -(-max(lens) // 64), 5 * len(lens), 100, in_place=False)
+        tab.block_table.copy_(torch.tensor(rng.integers(0, 100, tab.block_table.shape)))
+        tab.lens_after.copy_(torch.tensor(lens))
+        tab.first.copy_(torch.arange(0, 5 * len(lens) + 1, 5))
+        q = torch.randn((tab.tokens, QH, D), device="cuda").bfloat16()
+        buf, out, best = fxp.AttentionBuffers(len(lens), tab.tokens, QH, cache), torch.empty_like(q), float("inf")
+        for _ in range(6):
+            begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            begin.record()
+            for _ in range(3):
+                fxp.kv_attention(q, cache, tab, buf, out=out)
+            end.record()
+            end.synchronize()
+            best = min(best, begin.elapsed_time(end))
+        return best
+
+    apart = time_of([long_]) + time_of([short] * 21)
+    together = time_of([short] * 9 + [long_] + [short] * 12)
+    assert together < 4 * apart, (together, apart)
