@@ -464,7 +464,8 @@ int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t t
  * Arithmetic: rows of q and the weights of 64 tokens are fixed-point numbers of two signed 8-bit digits (three for fp32: 23
  * bits) under a scale of their own, products are exact int32 sums over 64 terms, sums over more and the
  * softmax are fp32.  Outputs are divided by the sum of the weights as rounded, so that they are weighted means of the values; lse has that of
- * the weights as they are.  0 < scale < 2^64.  Scores are taken to lie below 2^89 in magnitude.
+ * the weights as they are.  0 < scale < 2^64.  Scores are taken to lie below 2^89 in magnitude, and
+ * values times the number of tokens that a row sees below 2^119 (beyond that outputs may be Inf or NaN).
  * step->first must not decrease.  Sizes whose tiles of 16 rows times their pages (all requests as long as blocks allows) pass 2^31 a call are refused.
  * ws: fxp_kv_attention_workspace_bytes bytes (0 on bad arguments), 256-byte aligned, of which the first FXP_KV_TICKET_BYTES are zero
  * before the first call that uses them; every call leaves them zero.  Calls of any sizes may take turns with one workspace; two at

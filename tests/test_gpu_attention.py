@@ -388,3 +388,30 @@ def test_attention_to_one_long_context_is_spread_out_whatever_else_is_in_the_ste
     apart = time_of([long_]) + time_of([short] * 21)
     together = time_of([short] * 9 + [long_] + [short] * 12)
     assert together < 4 * apart, (together, apart)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+def test_attention_of_more_than_64_pages_a_wave(fxp, kind):
+    """32 heads of 5000 pages: a workgroup's share is 313 pages, 79 of them one wave's, whose numbers it loads 64 at a time."""
+    say("kv_attention over 320000 tokens", kind)
+    c, rng = Case(fxp, [640], [1], 32, 32, 16, kind), np.random.default_rng(2)
+    c.lens, c.table = np.array([5000 * 64 - 5]), rng.integers(0, 10, (1, 5000)).astype(np.int32)
+    c.table[0, rng.integers(0, 5000, 40)] = -1
+    c.tab = fxp.KvTables(1, 5000, 1, 4, in_place=False)
+    for mine, theirs in ((c.tab.block_table, c.table), (c.tab.lens_after, c.lens), (c.tab.first, c.first)):
+        mine.copy_(torch.tensor(theirs.astype(np.int32)))
+    lse = torch.empty((1, 32), device="cuda")
+    c.check(fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale, lse=lse), lse)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "fp32"])
+@pytest.mark.parametrize("lens,news,QH,H,D", [([1500], [1], 4, 2, 64), ([257], [257], 64, 16, 16)])
+def test_attention_to_the_largest_values(fxp, kind, lens, news, QH, H, D):
+    """Values times the tokens seen up to 2^119: outputs before the division hold up to 2^8 of them, the lag of the scores' reference."""
+    say("kv_attention to values near 2^108", kind, (lens, news, QH, H, D))
+    c = Case(fxp, lens, news, QH, H, D, kind, sharp=20.0)
+    ev = np.full(c.v.e.shape, 108 + 126)                      # below 2^108, times 1500
+    c.v.e, c.cache.ev[:] = ev, 108 + 126
+    out = fxp.kv_attention(c.dq, c.cache, c.tab, scale=c.scale)
+    assert torch.isfinite(out).all()
+    c.check(out)
