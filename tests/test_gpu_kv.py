@@ -282,3 +282,23 @@ def test_load_refuses_outputs_that_share_elements(fxp):
     assert not room.any()
     k, v = fxp.kv_load(cache, runs, 4, out=(room[:4], room[4:8]))
     assert (k * 2 == v).all() and k.any() and not room[8:].any()
+
+
+@pytest.mark.parametrize("bits", [2, 8])
+def test_load_under_every_scale(fxp, bits):
+    """The smallest and the largest scales, and what is none: counted as 1 and 255."""
+    say("kv_load under all scales", bits)
+    H, D, top = 2, 16, 2 ** (bits - 1) - 1
+    scales = np.array(list(range(1, 256)) + [0, -7, 256, 2 ** 31 - 1, -(2 ** 31)])
+    rng = np.random.default_rng(3)
+    q = rng.integers(-top, top + 1, (len(scales), H, 64, D)).astype(np.int8)
+    cache = fxp.KvCache(len(scales), H, D, bits)
+    cache.kq.copy_(torch.tensor(q))
+    cache.vq.copy_(torch.tensor(q.reshape(len(scales), H, 4, 16, D).transpose(0, 1, 2, 4, 3).copy()))
+    cache.ek.copy_(torch.tensor(scales.astype(np.int32))[:, None])
+    cache.ev.copy_(torch.tensor(scales.astype(np.int32))[:, None])
+    runs = np.array([[i * 6, 6, i, 3] for i in range(len(scales))], np.int32)
+    want = q[:, :, 3:9].transpose(0, 2, 1, 3).reshape(-1, H, D) * np.repeat(2.0 ** (np.clip(scales, 1, 255) - 125.0 - bits), 6)[:, None, None]
+    for dtype in TYPES.values():
+        for got in fxp.kv_load(cache, dev(runs), len(want), dtype):
+            assert torch.equal(got.cpu(), torch.tensor(want).float().to(dtype))
