@@ -430,6 +430,7 @@ int64_t fxp_kv_max_runs(int64_t requests, int64_t tokens);
  * block_table is refused; so is, from the first one that the stack cannot serve on, every request that needs a page, and from the first one
  * whose tokens pass `tokens` on, every request that has any.
  * A refused request keeps its length and its row, its tokens get slot -1 and runs on page -1 (fxp_kv_append skips them).
+ * Pages are counted by lengths: a caller that lowers one pushes the pages behind the first ceil(length / 64) of the row on the stack itself.
  * Tokens and runs beyond `tokens` and the runs' capacity are not written, but counted in first (up to 2^31 - 1, which also stands for all
  * beyond).  Lengths that are negative count as 0.
  * ws: NULL, or at least 256 bytes, zero before the first call that uses them, which every call leaves zero; required where
@@ -452,8 +453,9 @@ int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v, int64_t t
                 void* stream);
 
 /* Attention of new tokens over the cache (the paper's int8 attention products with the softmax in floating point,
- * Sec. 5).  Request b has step->first[b+1] - step->first[b] rows of q, which are its last ones: row i of n stands at place
- * lens_after[b] - n + i and sees the tokens at and before it; with window > 0 only the `window` last of them.
+ * Sec. 5).  Request b has step->first[b+1] - step->first[b] rows of q, which are its last ones (rows of a refused request, whose tokens
+ * are not in the cache, are to be dropped): row i of n stands at place lens_after[b] - n + i and sees the tokens at and before it;
+ * with window > 0 only the `window` last of them.
  * out = sum_j softmax_j(scale * q . k_j) v_j with k, v the values that the cache stands for.  Head h of q reads head
  * h / (q_heads / heads) of the cache; q_heads is a multiple of heads, at most 16384.  q and out: [tokens, q_heads, dim] of `type`, strides
  * as in fxp_kv_append; out may be q (with q's strides) and shares no elements with it otherwise, and its rows may not overlap; rows behind

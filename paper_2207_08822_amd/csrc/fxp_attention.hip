@@ -11,8 +11,13 @@
 // softmax's weights never leave their lane.
 //
 // Digits.  A row of Q is v * 2^u with |v| < 2^15 (2^23) and v = 256 d1 + d0 (65536 d2 + ...), d signed bytes; a page's weights
-// likewise under their own largest one.  Outputs are divided by the sum of the weights as rounded, so that they stay weighted means of the
-// values (constant values come out as they are, whatever the scores); the sum of the weights as they are serves lse alone.
+// likewise under their own largest one (below half a unit of it, 2^-16, they add nothing).  Rounding a row to 15 bits is off by up to
+// 2^-15 of the lower end of its largest element's binade, or 2^-14 where that element is within 2^-7 of the next: no more than half a
+// step of the type for bf16 elements down to 2^-7 (2^-6) of it and fp16 ones down to 2^-4 (2^-3).  Rows with single elements far above
+// the rest lose bits of the rest; fp32 rows have 23.  Two digits, because a third of q alone costs 5 % over 70 shapes (4600 rows of
+// prompts 250 us against 230, 64 requests of one row 63.6 against 62.3).  Outputs are divided by the sum of the weights as rounded, so
+// that they stay weighted means of the values (constant values come out as they are, whatever the scores); the sum of the weights as they
+// are serves lse alone.
 #include <algorithm>
 #include <limits>
 
@@ -635,9 +640,10 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
             }
             if (!whole) {
                 // The last to arrive joins the parts.  Parts are stored past the L2 of this XCD (store_part) and loaded past that of the
-                // reader's, so it is enough that every wave's stores are there before the ticket is drawn.  Release and acquire
-                // fences instead write back and drop whole L2 caches, in every workgroup: 97 us in place of 65 for 64 requests of 200
-                // to 8000 tokens.
+                // reader's, so it is enough that every wave's stores are there before the ticket is drawn.  That is no happens-before of the
+                // memory model: it rests on what this chip does with relaxed atomics of device scope, whose stores write through to memory and
+                // whose loads do not end in an L2, and on the wait, which lasts until the stores have arrived.  Release and acquire fences
+                // instead write back and drop whole L2 caches, in every workgroup: 97 us in place of 65 for 64 requests of 200 to 8000 tokens.
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 if (threadIdx.x == 0) {
@@ -717,10 +723,10 @@ __global__ __launch_bounds__(64 * kAttWaves, DB <= 2 ? 2 : 1) void k_kv_attend(A
 // ---- many rows of one request (prompts) ----
 //
 // A workgroup has 64 consecutive rows of one request and head, each of its four waves a tile of 16.  The waves share the pages:
-// each page goes through LDS once (two buffers, the next page's loads in registers meanwhile).  Per page a wave issues 16 DB
-// matrix instructions of 16 cycles (two digits) and, at DB = 2, some 290 vector instructions, which is what bounds it: the vector ALU is busy 84 % of
-// the time, the matrix cores 31 % (4600 rows behind up to 7000, 16 heads over 4 of 128: 245 us; 1, 2 and 3 workgroups a CU take
-// 480, 305 and 250).  32 rows a wave, which halves the LDS reads, took 303 us: fewer, longer workgroups.
+// each page goes through LDS once (two buffers, the next page's loads in registers meanwhile).  Per page a wave issues 16 DB + 2
+// matrix instructions of 16 cycles (two digits) and, at DB = 2, some 295 vector instructions, which is what bounds it: the vector ALU is busy 83 % of
+// the time, the matrix cores 32 % (4600 rows behind up to 7000, 16 heads over 4 of 128: 221 us, 255 in the first calls of a process; in such
+// calls 1, 2 and 3 workgroups a CU took 480, 305 and 250, and 32 rows a wave, which halves the LDS reads, 303: fewer, longer workgroups).
 // In LDS the keys stand by pieces of 16 elements, [dim / 16][64 places][16], the places in the order that the A operand takes
 // them, turned by twice the piece's number: 16 lanes then read 256 consecutive bytes, and the 16 pieces that 16
 // lanes write (8 of a token, two tokens) fall on 16 different ones.

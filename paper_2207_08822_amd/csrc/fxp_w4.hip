@@ -481,7 +481,7 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
             constexpr integral_constant<int, 4> four{};
             constexpr integral_constant<int, 3> three{};
             // Three digits and four scales of two tiles of rows: registers for two tiles of outputs (23 rows, 4096 x 28672: two 65 us, three 88,
-            // four 112), and none for four tiles of rows (64 rows: 112 us as two passes, 162 as one).
+            // four 112), and none for four tiles of rows (64 rows: 107 us as two passes, 162 as one).
             constexpr bool kTight = TYPE == FXP_F32 && GROUP == 32;
             auto of_rows = [&](auto nt_c) {
                 if (a.m_tiles == 1) go(nt_c, one, two);
@@ -491,7 +491,7 @@ extern "C" int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, in
             // As many tiles of outputs to a workgroup as leave one for each CU: every wave reads its rows' digits (4 KB a tile of rows) for
             // 1 KB of weights a tile of outputs, and that is what bounds it (23 rows, 4090 x 11007: three tiles 10.5 us, two 13.8; 8192 x 8192,
             // two tiles 21.0 in all, one 25.8).  From 33 rows on, four tiles of rows read the weights half as often as two (64 rows, bf16, groups of
-            // 64: 8192 x 8192 28 us against 32, 1024 x 16384 14 / 18, 4090 x 11007 28 / 27).
+            // 64: 8192 x 8192 29 us against 32, 1024 x 16384 14 / 18, 4090 x 11007 30 / 27).
             constexpr int kCus = 256;
             if constexpr (!kTight)
                 if (a.m_tiles > 2) return go(two, four, one);

@@ -567,6 +567,7 @@ def sgd16_step_multi(buf, lr, momentum=0.0, weight_decay=0.0, seed=0, step=0, ro
 
 
 # ---- serving: a paged cache of mapped keys and values, attention over it, products with 4-bit weights ----
+# None of these calls records gradients.
 
 KV_PAGE = 64            # tokens of a page (FXP_KV_PAGE)
 KV_TICKET_BYTES = 2048  # of the workspace of fxp_kv_attention, zero between calls (FXP_KV_TICKET_BYTES)
@@ -694,7 +695,10 @@ class KvCache:
 class KvTables:
     """Caller-owned tables of up to `requests` requests of `blocks` pages and of a step of up to `tokens` new tokens; all layers of
     a model share them.  The caller frees a finished request by pushing its pages on `free` (free[n_free] and up), raising
-    n_free and setting its length to 0.  in_place: a step moves lens and n_free on (lens_after is lens); otherwise it leaves them and
+    n_free and setting its length to 0; tokens that are taken back (guesses that were rejected) likewise: the pages behind the first
+    ceil(length / 64) of its row are pushed and the length lowered - a page that is left in the row is not found again, because a request's
+    pages are counted by its length.  Rows of a step's q that belong to a refused request have no tokens of their own in the cache; what
+    kv_attention makes of them is to be dropped.  in_place: a step moves lens and n_free on (lens_after is lens); otherwise it leaves them and
     writes lens_after and n_free_after."""
 
     def __init__(self, requests, blocks, tokens, pages, in_place=True, device="cuda"):
@@ -783,7 +787,8 @@ class AttentionBuffers:
 def kv_attention(q, cache, tab, buf=None, scale=None, window=0, out=None, lse=None):
     """Attention of the step's rows q [tokens, q_heads, dim] over the cache: causal, over the last `window` tokens where it is > 0.
     scale: dim ** -0.5 by default; out: may be q itself, and shares no elements with it otherwise; lse: [tokens, q_heads] fp32 to fill with
-    the logarithms of the softmax's sums."""
+    the logarithms of the softmax's sums.  Rows of bfloat16 and float16 are held in 15 bits under their largest element, and so are the
+    softmax's weights of 64 tokens; of float32 in 23: for rows with single elements far above the rest, whose rest matters, pass float32."""
     code = _served(q, "q", 3)
     tokens, q_heads, dim = q.shape
     if tokens != tab.tokens or dim != cache.dim:
@@ -832,7 +837,8 @@ def pack4(W, group=64):
 
 
 def linear4(x, w, out=None, ws=None):
-    """y [M, N] = x [M, K] W of x's type, W the 4-bit weights w; made for a few rows.  out: may not share elements with x."""
+    """y [M, N] = x [M, K] W of x's type, W the 4-bit weights w; made for a few rows.  out: may not share elements with x.  bfloat16 and
+    float16 x is held in 15 bits under the largest of its `group` elements, float32 in 23."""
     code = _served(x, "x", 2)
     M, K = x.shape
     if K != w.K:
