@@ -6,7 +6,6 @@ non-zero status.  All arithmetic runs in the HIP kernels; there is no CPU or PyT
 fallback: if libfxp.so cannot be loaded, or a tensor is not on the GPU, the call fails.
 """
 import ctypes
-import itertools
 import os
 
 import torch
@@ -630,8 +629,10 @@ def _rows_overlap(t):
 
 def _span(t):
     """Addresses of a tensor's first byte and of the one behind its last."""
-    last = sum(stride * (n - 1) for stride, n in zip(t.stride(), t.shape)) + 1 if t.numel() else 0
-    return t.data_ptr(), t.data_ptr() + last * t.element_size()
+    at, reach = t.data_ptr(), 1
+    for stride, n in zip(t.stride(), t.shape):
+        reach += stride * (n - 1)
+    return at, at + reach * t.element_size()
 
 
 def _same_rows(a, b):
@@ -639,26 +640,32 @@ def _same_rows(a, b):
     return a.data_ptr() == b.data_ptr() and all(n <= 1 or x == y for n, x, y in zip(a.shape, a.stride(), b.stride()))
 
 
+def _between(lead, low, high):
+    """Whether a sum of i * stride with -n < i < n, one for each (stride, n) of `lead`, smallest strides first, lies between `low` and `high` (both
+    excluded)."""
+    if not lead:
+        return low < 0 < high
+    *rest, (stride, n) = lead
+    reach = sum(s * (m - 1) for s, m in rest)
+    if stride == 0:
+        return _between(rest, low, high)
+    # where rows do not overlap, the others together reach no further than one stride: few i are left
+    first, last = max((low - reach) // stride + 1, 1 - n), min((high + reach - 1) // stride, n - 1)
+    return any(_between(rest, low - i * stride, high - i * stride) for i in range(first, last + 1))
+
+
 def _share(a, b):
     """Whether rows (contiguous last dimensions) of two tensors of one type and of as many rows share elements.  Exact where their strides are
     alike, as those of parts of one buffer are; otherwise whether the tensors' spans meet."""
     (a0, a1), (b0, b1) = _span(a), _span(b)
-    if a1 <= b0 or b1 <= a0 or a0 == a1 or b0 == b1:
+    if a1 <= b0 or b1 <= a0 or not a.numel() or not b.numel():
         return False
     lead = [(n, stride, other) for n, stride, other in zip(a.shape[:-1], a.stride(), b.stride()) if n > 1]
     if any(stride != other for _, stride, other in lead):
         return True
-    # rows of a lie at whole strides from each other: does one begin between `low` and `high` (both excluded), seen from its first row?
+    # rows of a and of b lie at the same strides: does the distance of two of them leave them short of each other's ends?
     delta = (b0 - a0) // a.element_size()
-    low, high = delta - a.shape[-1], delta + b.shape[-1]
-    lead = sorted((n, stride) for n, stride, _ in lead)
-    n, stride = lead.pop() if lead else (1, 0)          # the longest dimension in one step, the others one by one
-    for at in itertools.product(*(range(1 - m, m) for m, _ in lead)):
-        c = sum(i * s for i, (_, s) in zip(at, lead))
-        i = min(max((low - c) // stride + 1, 1 - n), n - 1) if stride else 0
-        if low < c + i * stride < high:
-            return True
-    return False
+    return _between(sorted((stride, n) for n, stride, _ in lead), delta - a.shape[-1], delta + b.shape[-1])
 
 
 class KvCache:
