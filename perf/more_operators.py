@@ -1,5 +1,5 @@
 """What is measured of the operators of a decoder block with rotary positions whose products run in microscaled 4-bit floating point: the
-rotation and its gradient (fxp.rotary), the cache's writer with the rotation on the way (fxp.kv_append_rotary), the mapping to 4 bits and its
+rotation and its gradient (fxp.rotary, fxp.rotary_bwd), the cache's writer with the rotation on the way (fxp.kv_append_rotary), the mapping to 4 bits and its
 inverse (fxp.mx4_map, fxp.mx4_unmap), the product of floating rows with mapped weights (fxp.mx4_linear) and a layer's training step
 (fxp.mx4_linear_fwd, fxp.mx4_linear_bwd).
 
@@ -290,7 +290,7 @@ def run(s):
 def _own(s):
     fxp, case = s["fxp"], s["case"]
     if s["kind"] == "rotary":
-        return dict(y=fxp.rotary(s["x"], s["positions"], s["rope"], inverse=bool(case["back"])))
+        return dict(y=(fxp.rotary_bwd if case["back"] else fxp.rotary)(s["x"], s["positions"], s["rope"]))
     if s["kind"] == "append":
         q = fxp.kv_append_rotary(s["k"], s["v"], s["cache"], s["tab"], s["rope"], q=s["q"] if case["q_heads"] else None)
         k, v = fxp.kv_load(s["cache"], s["read"], s["T_read"])
