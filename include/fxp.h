@@ -478,6 +478,37 @@ int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int typ
                      int64_t q_heads, float scale, int64_t window, void* out, int64_t out_token, int64_t out_head, float* lse,
                      void* ws, size_t ws_bytes, void* stream);
 
+/* ---- rotary positions ----
+ * Pair i < rot / 2 of a head's elements stands for a point of the plane that is turned by position * f_i and stretched by `amplitude`:
+ * (u, w) -> amplitude * (u cos - w sin, u sin + w cos).  Pairs are elements 2 i and 2 i + 1 (interleaved) or i and i + rot / 2; elements from rot
+ * on stay as they are.  turns[i] is f_i as a fraction of a turn in units of 2^-64, modulo one turn: the angle of every 31-bit position is
+ * exact to 2^-34 turns.  Host struct; rot even, 2 .. min(dim, FXP_ROTARY_MOST), 0 < amplitude < 1e30; turns [rot / 2] on the device, 8-byte aligned. */
+#define FXP_ROTARY_MOST 1024
+typedef struct fxp_rotation {
+    const uint64_t* turns;
+    int64_t rot;
+    int interleaved;
+    double amplitude;
+} fxp_rotation;
+
+/* y = x turned by its positions, or with `backward` by the opposite angles (and stretched alike): the gradient of that.  x and y: [batch, tokens,
+ * heads, dim] of `type` at any strides >= 0 of the first three (fastest where bases, strides, rot / 2 and dim - rot are multiples of 16 bytes);
+ * positions: int32, sequence b's at p_batch * b (0: the same for all).  Rows at negative positions are left as they are in y.  y may be x (with
+ * x's strides) and shares no elements with it otherwise; y's rows may not overlap.  Cosines and sums are fp32, rounded once to `type`.
+ * batch * ceil(tokens / 64) < 2^31, heads <= 65535, dim <= 65536. */
+int fxp_rotary(const fxp_rotation* rotation, int backward, int type, int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
+               const void* x, int64_t x_batch, int64_t x_token, int64_t x_head, const int32_t* positions, int64_t p_batch, void* y,
+               int64_t y_batch, int64_t y_token, int64_t y_head, void* stream);
+
+/* fxp_kv_append of keys that are turned on the way, and in the same launch the step's queries (q NULL: none): of *step only requests, tokens, runs
+ * and positions are used (a run's token t stands at positions[t]).  A turned key is not rounded before it is mapped: rotation and rounding are
+ * done in 64 bits.  Values are mapped as fxp_kv_append does.  q, out: [tokens, q_heads, dim] of `type`, q_heads a multiple of the cache's heads, at
+ * most 16384; out receives the turned queries of every token of a run that is written (rows of others are left as they are), may be
+ * q (with q's strides) and shares no elements with q otherwise, or with k or v; its rows may not overlap.  Inf and NaN spread to their pair. */
+int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step* step, const fxp_rotation* rotation, int type, const void* k,
+                         int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head, const void* q, int64_t q_token,
+                         int64_t q_head, int64_t q_heads, void* out, int64_t out_token, int64_t out_head, void* stream);
+
 /* ---- products of a few rows with 4-bit weights ----
  * A weight matrix W [K, N] as mantissas -7..7 (the mapping with bits = 4, rounded to nearest) with one scale for
  * each group of `group` (32, 64 or 128) inputs of one output.  Packed layout, made once: tiles of 16 outputs x 128 inputs,

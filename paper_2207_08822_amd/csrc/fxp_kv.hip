@@ -8,6 +8,7 @@
 // Writer.  q = floor(|x| 2^(125 + bits - e) + 1/2) with e the largest exponent of the block.  A workgroup has one run of one
 // head, keys or values; a thread has blocks of 4 tokens x 4 elements, which is one dword each way for keys (a token's four
 // elements) and, transposed in registers, for values (an element's four tokens).
+#include "fxp_rotary_device.h"
 #include "fxp_serve_device.h"
 
 namespace fxp {
@@ -277,24 +278,14 @@ __device__ inline int dword_of(bool values, int tq, int d, int j, int dim) {
     return values ? (tq >> 2) * (dim * 4) + (d + j) * 4 + (tq & 3) : ((4 * tq + j) * dim + d) / 4;
 }
 
-// What bounds it: a step of single tokens the way of one token (run, then values, scale and old bytes together, then stores), a prompt
-// its reads and writes.
+// A run of one head's keys or values.
 template <int TYPE, int THREADS>
-__global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const void* __restrict__ k, int64_t k_token, int64_t k_head,
-                                                       const void* __restrict__ v, int64_t v_token, int64_t v_head, int64_t tokens,
-                                                       const int4* __restrict__ runs, int vec_k, int vec_v, uint32_t inverse) {
-    __shared__ uint32_t lds[THREADS / 64];
-    const int4 rr = runs[blockIdx.x];
-    const Run run = {rr.x, rr.y, rr.z, rr.w};
-    if (!run_ok(run, tokens, c.pages)) return;
-    const bool values = blockIdx.z != 0;
-    const int head = blockIdx.y, dim = static_cast<int>(c.dim);
+__device__ inline void append_run(const fxp_kv_cache& c, const void* __restrict__ x, int64_t token, int64_t head_step, const Run& run, int head,
+                                  bool values, bool vec, uint32_t inverse, uint32_t* lds) {
+    const int dim = static_cast<int>(c.dim);
     const Quads quads = quads_of(run, dim, inverse, values);
     const int work = quads.count * quads.nd, nd = quads.nd;
-    const void* x = values ? v : k;
-    const int64_t token = values ? v_token : k_token;
-    const bool vec = values ? vec_v : vec_k;
-    const int64_t row0 = int64_t{run.first} * token + head * (values ? v_head : k_head);
+    const int64_t row0 = int64_t{run.first} * token + head * head_step;
     const int64_t block = int64_t{run.page} * c.heads + head;
     int32_t* const scale = (values ? c.ev : c.ek) + block;
     uint32_t* const page = reinterpret_cast<uint32_t*>((values ? c.vq : c.kq) + block * (FXP_KV_PAGE * dim));
@@ -393,6 +384,190 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
                 *p = remap_nearest4(*p, grown);
             }
         }
+}
+
+// What bounds it: a step of single tokens the way of one token (run, then values, scale and old bytes together, then stores), a prompt
+// its reads and writes.
+template <int TYPE, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const void* __restrict__ k, int64_t k_token, int64_t k_head,
+                                                       const void* __restrict__ v, int64_t v_token, int64_t v_head, int64_t tokens,
+                                                       const int4* __restrict__ runs, int vec_k, int vec_v, uint32_t inverse) {
+    __shared__ uint32_t lds[THREADS / 64];
+    const int4 rr = runs[blockIdx.x];
+    const Run run = {rr.x, rr.y, rr.z, rr.w};
+    if (!run_ok(run, tokens, c.pages)) return;
+    const bool values = blockIdx.z != 0;
+    append_run<TYPE, THREADS>(c, values ? v : k, values ? v_token : k_token, values ? v_head : k_head, run, blockIdx.y, values, values ? vec_v : vec_k,
+                              inverse, lds);
+}
+
+// ---- writer that turns keys and queries ----
+//
+// Keys: a thread has items of eight elements of a token, two runs of four that hold their pairs together; they are turned in 64 bits and mapped
+// from there, so that what the cache holds is the formula's rounding, not that of a cosine in 32 bits (an element near a half would go the other way
+// once in some 10^4).  The vector ALU does a 64-bit multiply-add in the time of a 32-bit one; angles are found in registers, item by item.
+struct RotaryWriter {
+    const uint64_t* turns;
+    const int32_t* positions;
+    double amplitude;
+    int rot, pairs, dim;
+    int turned, pieces;     // items of a head: those that hold pairs, all
+    int whole;              // every item has its eight elements, in two runs that begin at multiples of four
+    const void* q;
+    void* out;
+    int64_t q_token, q_head, out_token, out_head;
+    int group, vec_q;       // query heads of a head of the cache; 0: no queries
+};
+
+// Item i of a head: eight elements, four pairs of them or eight that stay.  Element j is `first` + j, or `second` + j - 4 from the fourth on.
+struct Piece {
+    int first, second, pairs, elements;     // of the last items there may be fewer: pairs (0: none are turned), elements that stay
+};
+template <bool NEAR>
+__device__ inline Piece piece_of(const RotaryWriter& r, int i) {
+    if (i < r.turned) return {NEAR ? 8 * i : 4 * i, NEAR ? 8 * i + 4 : r.pairs + 4 * i, min(4, r.pairs - 4 * i), 0};
+    const int first = r.rot + 8 * (i - r.turned);
+    return {first, first + 4, 0, min(8, r.dim - first)};
+}
+// whether element j of the item exists
+template <bool NEAR>
+__device__ inline bool has_element(const Piece& p, int j) {
+    return p.pairs ? (NEAR ? j / 2 : j % 4) < p.pairs : j < p.elements;
+}
+
+// the elements of an item, turned; at: of the head's first element
+template <int TYPE, typename F, bool NEAR>
+__device__ inline void turned_piece(const RotaryWriter& r, const void* x, int64_t at, int position, bool vec, F amplitude, int i, const Piece& p, F (&y)[8]) {
+    if (r.whole) {
+        float a[4], b[4];
+        load_elems<TYPE, 4>(x, at + p.first, vec, a);
+        load_elems<TYPE, 4>(x, at + p.second, vec, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            y[j] = a[j];
+            y[4 + j] = b[j];
+        }
+    } else {
+        const typename Elem<TYPE>::T* const row = static_cast<const typename Elem<TYPE>::T*>(x) + at;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = has_element<NEAR>(p, j) ? static_cast<F>(static_cast<float>(row[j < 4 ? p.first + j : p.second + j - 4])) : F(0);
+    }
+    if (p.pairs == 0) return;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        F c, s;
+        cos_sin(angle_of(r.turns[min(4 * i + j, r.pairs - 1)], position), c, s);
+        if constexpr (NEAR) turn_pair(y[2 * j], y[2 * j + 1], c * amplitude, s * amplitude);
+        else turn_pair(y[j], y[4 + j], c * amplitude, s * amplitude);
+    }
+}
+
+__device__ inline uint32_t high_word(double x) { return static_cast<uint32_t>(__builtin_bit_cast(uint64_t, x) >> 32) & 0x7fffffffu; }
+
+template <int TYPE, int THREADS, bool NEAR>
+__device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& r, const void* __restrict__ x, int64_t token, int64_t head_step, const Run& run,
+                                     int head, bool vec, uint32_t by_pieces, uint32_t* lds) {
+    const int dim = static_cast<int>(c.dim), pieces = r.pieces, work = run.count * pieces;
+    const int64_t row0 = int64_t{run.first} * token + head * head_step;
+    const int64_t block = int64_t{run.page} * c.heads + head;
+    int32_t* const scale = c.ek + block;
+    uint32_t* const page = reinterpret_cast<uint32_t*>(c.kq + block * (FXP_KV_PAGE * dim));
+    const int e_old = run.offset ? min(max(*scale, 1), 255) : 1;
+    constexpr int kKept = THREADS == 64 ? 2 : 4;         // items that a thread keeps; others are turned again
+    double kept[kKept][8];
+    uint32_t m = 0;
+    auto fetch = [&](int n, double (&y)[8]) {
+        const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces)), i = n - t * pieces;
+        turned_piece<TYPE, double, NEAR>(r, x, row0 + t * token, r.positions[run.first + t], vec, r.amplitude, i, piece_of<NEAR>(r, i), y);
+    };
+    auto largest = [&](const double (&y)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = max(m, high_word(y[j]));
+    };
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) {
+            fetch(threadIdx.x + n * THREADS, kept[n]);
+            largest(kept[n]);
+        }
+    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+        double y[8];
+        fetch(i, y);
+        largest(y);
+    }
+    m = THREADS == 64 ? wave_max(m) : block_max<THREADS / 64>(m, lds);
+    // a double's exponent is biased by 1023, a scale by 127
+    const int e = max(e_old, min(max(static_cast<int>(m >> 20) - 896, 1), 255)), grown = e - e_old;
+    if (threadIdx.x == 0) *scale = e;
+    const double unit = ldexp(1.0, 125 + c.bits - e), most = static_cast<double>((1 << (c.bits - 1)) - 1);
+    auto write = [&](int n, const double (&y)[8]) {
+        const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces));
+        const Piece p = piece_of<NEAR>(r, n - t * pieces);
+        uint32_t b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const double z = fabs(y[j]) * unit + 0.5;
+            const int v = static_cast<int>(z > most ? most : z);         // NaN: 0
+            b[j] = static_cast<uint32_t>(y[j] < 0 ? -v : v);
+        }
+        uint32_t* const row = page + (run.offset + t) * (dim / 4);
+        if (r.whole) {
+            row[p.first / 4] = perm(perm(b[3], b[2], 0x0c0c0400u), perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+            row[p.second / 4] = perm(perm(b[7], b[6], 0x0c0c0400u), perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (has_element<NEAR>(p, j)) reinterpret_cast<int8_t*>(row)[j < 4 ? p.first + j : p.second + j - 4] = static_cast<int8_t>(b[j]);
+        }
+    };
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) write(threadIdx.x + n * THREADS, kept[n]);
+    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+        double y[8];
+        fetch(i, y);
+        write(i, y);
+    }
+    if (grown && run.offset)
+        for (int i = threadIdx.x; i < run.offset * (dim / 4); i += THREADS) page[i] = remap_nearest4(page[i], grown);
+}
+
+// the queries of a run's tokens, of the heads that read one head of the cache
+template <int TYPE, int THREADS, bool NEAR>
+__device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int head, uint32_t by_pieces) {
+    const int rows = run.count * r.group, work = rows * r.pieces;
+    for (int n = threadIdx.x; n < work; n += THREADS) {
+        // heads inside tokens: a step of one token has its heads beside each other
+        const int row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces)), i = n - row * r.pieces;
+        const int t = row / r.group, h = head * r.group + row - t * r.group;
+        const Piece p = piece_of<NEAR>(r, i);
+        float y[8];
+        turned_piece<TYPE, float, NEAR>(r, r.q, (int64_t{run.first} + t) * r.q_token + h * r.q_head, r.positions[run.first + t], r.vec_q,
+                                        static_cast<float>(r.amplitude), i, p, y);
+        const int64_t to = (int64_t{run.first} + t) * r.out_token + h * r.out_head;
+        if (r.whole) {
+            store4<TYPE>(r.out, to + p.first, r.vec_q, {y[0], y[1], y[2], y[3]});
+            store4<TYPE>(r.out, to + p.second, r.vec_q, {y[4], y[5], y[6], y[7]});
+        } else {
+            typename Elem<TYPE>::T* const out = static_cast<typename Elem<TYPE>::T*>(r.out) + to;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (has_element<NEAR>(p, j)) out[j < 4 ? p.first + j : p.second + j - 4] = static_cast<typename Elem<TYPE>::T>(y[j]);
+        }
+    }
+}
+
+template <int TYPE, int THREADS, bool NEAR>
+__global__ __launch_bounds__(THREADS) void k_kv_append_rotary(fxp_kv_cache c, RotaryWriter r, const void* __restrict__ k, int64_t k_token, int64_t k_head,
+                                                              const void* __restrict__ v, int64_t v_token, int64_t v_head, int64_t tokens,
+                                                              const int4* __restrict__ runs, int vec_k, int vec_v, uint32_t inverse, uint32_t by_pieces) {
+    __shared__ uint32_t lds[THREADS / 64];
+    const int4 rr = runs[blockIdx.x];
+    const Run run = {rr.x, rr.y, rr.z, rr.w};
+    if (!run_ok(run, tokens, c.pages)) return;
+    if (blockIdx.z == 0) append_turned<TYPE, THREADS, NEAR>(c, r, k, k_token, k_head, run, blockIdx.y, vec_k, by_pieces, lds);
+    else if (blockIdx.z == 1) append_run<TYPE, THREADS>(c, v, v_token, v_head, run, blockIdx.y, true, vec_v, inverse, lds);
+    else turn_queries<TYPE, THREADS, NEAR>(r, run, blockIdx.y, by_pieces);
 }
 
 // ---- inverse mapping: a thread has blocks of 4 tokens x 4 elements ----
@@ -530,6 +705,67 @@ extern "C" int fxp_kv_load(const fxp_kv_cache* cache, int type, void* k, void* v
     auto go = [&](auto type_c) {
         hipLaunchKernelGGL((fxp::k_kv_load<decltype(type_c)::value>), grid, dim3(256), 0, static_cast<hipStream_t>(stream), *cache, k, v, tokens,
                            reinterpret_cast<const int4*>(runs), fxp::inverse_of(cache->dim / 4));
+    };
+    if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
+    else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
+    else go(std::integral_constant<int, FXP_F16>{});
+    return fxp::launch_status();
+}
+
+extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step* step, const fxp_rotation* rotation, int type, const void* k,
+                                    int64_t k_token, int64_t k_head, const void* v, int64_t v_token, int64_t v_head, const void* q, int64_t q_token,
+                                    int64_t q_head, int64_t q_heads, void* out, int64_t out_token, int64_t out_head, void* stream) {
+    int rc = fxp::check_cache(cache);
+    if (rc) return rc;
+    rc = fxp::check_rotation(rotation, cache->dim);
+    if (rc) return rc;
+    if (!step) return FXP_ERR_NULL;
+    if (!fxp::known_type(type)) return FXP_ERR_TYPE;
+    const int64_t tokens = step->tokens, n_runs = fxp_kv_max_runs(step->requests, tokens);
+    if (step->requests <= 0 || tokens < 0 || step->requests >= (int64_t{1} << 31) || tokens >= (int64_t{1} << 31) || n_runs > fxp::kMostRuns ||
+        !fxp::strides_ok(k_token, k_head) || !fxp::strides_ok(v_token, v_head) || !fxp::strides_ok(q_token, q_head) || !fxp::strides_ok(out_token, out_head))
+        return FXP_ERR_DIMS;
+    if (q && (q_heads <= 0 || q_heads > 16384 || q_heads % cache->heads)) return FXP_ERR_DIMS;
+    if (tokens == 0) return FXP_OK;
+    if (!k || !v || !step->runs || !step->positions || (q && !out)) return FXP_ERR_NULL;
+    const size_t size = static_cast<size_t>(fxp::elem_size(type));
+    if (!fxp::aligned(k, size) || !fxp::aligned(v, size) || !fxp::aligned(q, size) || !fxp::aligned(out, size) || !fxp::aligned(step->runs, 16) ||
+        !fxp::aligned(step->positions, 4))
+        return FXP_ERR_ALIGN;
+    fxp::RotaryWriter r{};
+    r.turns = rotation->turns;
+    r.positions = step->positions;
+    r.amplitude = rotation->amplitude;
+    r.rot = static_cast<int>(rotation->rot);
+    r.pairs = r.rot / 2;
+    r.dim = static_cast<int>(cache->dim);
+    r.turned = (r.pairs + 3) / 4;
+    r.pieces = r.turned + (r.dim - r.rot + 7) / 8;
+    r.whole = r.rot % 8 == 0;                       // and so is the rest of a head
+    if (q) {
+        r.q = q;
+        r.out = out;
+        r.q_token = q_token; r.q_head = q_head;
+        r.out_token = out_token; r.out_head = out_head;
+        r.group = static_cast<int>(q_heads / cache->heads);
+        r.vec_q = fxp::multiple_of_4(q, q_token, q_head, type) && fxp::multiple_of_4(out, out_token, out_head, type);
+    }
+    const int vk = fxp::multiple_of_4(k, k_token, k_head, type), vv = fxp::multiple_of_4(v, v_token, v_head, type);
+    const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), q ? 3 : 2);
+    const uint32_t inverse = fxp::inverse_of(cache->dim / 4), by_pieces = fxp::inverse_of(r.pieces);
+    const bool few = tokens <= 4 * n_runs;          // the rule of fxp_kv_append
+    auto launch = [&](auto type_c, auto threads_c, auto near_c) {
+        constexpr int TYPE = decltype(type_c)::value, THREADS = decltype(threads_c)::value;
+        hipLaunchKernelGGL((fxp::k_kv_append_rotary<TYPE, THREADS, decltype(near_c)::value>), grid, dim3(THREADS), 0, static_cast<hipStream_t>(stream), *cache,
+                           r, k, k_token, k_head, v, v_token, v_head, tokens, reinterpret_cast<const int4*>(step->runs), vk, vv, inverse, by_pieces);
+    };
+    auto go = [&](auto type_c) {
+        auto with = [&](auto threads_c) {
+            if (rotation->interleaved) launch(type_c, threads_c, std::true_type{});
+            else launch(type_c, threads_c, std::false_type{});
+        };
+        if (few) with(std::integral_constant<int, 64>{});
+        else with(std::integral_constant<int, 256>{});
     };
     if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
     else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});

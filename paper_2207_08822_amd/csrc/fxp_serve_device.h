@@ -62,6 +62,22 @@ __device__ inline void store4(void* base, int64_t at, bool vec, const float (&x)
     }
 }
 
+// N floats rounded to nearest, to an address that is a multiple of N elements or, from 16 bytes on, of 16 bytes
+template <int TYPE, int N>
+__device__ inline void store_elems(void* base, int64_t at, const float (&x)[N]) {
+    using T = typename Elem<TYPE>::T;
+    T* p = static_cast<T*>(base) + at;
+    constexpr int kPiece = N * sizeof(T) < 16 ? N : 16 / static_cast<int>(sizeof(T));
+    typedef T Vec __attribute__((ext_vector_type(kPiece)));
+#pragma unroll
+    for (int i = 0; i < N; i += kPiece) {
+        Vec v;
+#pragma unroll
+        for (int j = 0; j < kPiece; ++j) v[j] = static_cast<T>(x[i + j]);
+        *reinterpret_cast<Vec*>(p + i) = v;
+    }
+}
+
 // The mapping of one value under scale e with `cut` = 25 - bits low bits dropped, half up on the magnitude (what
 // fxp_map does with FXP_ROUND_NEAREST), as a signed byte.
 __device__ inline int map_nearest(float x, int e, int cut) {

@@ -6,7 +6,9 @@ non-zero status.  All arithmetic runs in the HIP kernels; there is no CPU or PyT
 fallback: if libfxp.so cannot be loaded, or a tensor is not on the GPU, the call fails.
 """
 import ctypes
+import math
 import os
+from fractions import Fraction
 
 import torch
 
@@ -55,6 +57,10 @@ class _KvStep(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int64) for n in ("requests", "blocks", "tokens", "pages")] +
                 [(n, ctypes.c_void_p) for n in ("lens", "free_pages", "n_free", "block_table", "lens_after", "n_free_after", "first",
                                                 "slots", "positions", "runs", "refused")])
+
+
+class _Rotation(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("rot", ctypes.c_int64), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_double)]
 
 
 _lib = None
@@ -148,6 +154,11 @@ def lib():
     L.fxp_w4_workspace_bytes.restype = sz
     L.fxp_w4_pack.argtypes = [ci, vp, i64, i64, i64, ci, vp, vp, vp]
     L.fxp_w4_linear.argtypes = [ci, vp, i64, i64, i64, i64, vp, vp, ci, vp, i64, vp, sz, vp]
+    turn = c.POINTER(_Rotation)
+    L.fxp_rotary.argtypes = [turn, ci, ci, i64, i64, i64, i64, vp, i64, i64, i64, vp, i64, vp, i64, i64, i64, vp]
+    L.fxp_rotary.restype = ci
+    L.fxp_kv_append_rotary.argtypes = [cache, step, turn, ci, vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp]
+    L.fxp_kv_append_rotary.restype = ci
     for name in ("fxp_kv_tables", "fxp_kv_append", "fxp_kv_load", "fxp_kv_attention", "fxp_w4_pack", "fxp_w4_linear"):
         getattr(L, name).restype = ci
     for name in ("fxp_scale", "fxp_map", "fxp_scale_map", "fxp_gemm", "fxp_unmap", "fxp_unmap_i8", "fxp_gemm_unmap",
@@ -617,9 +628,9 @@ def _row_stride(t, what):
 
 
 def _rows_overlap(t):
-    """Whether rows of a [tokens, heads, dim] tensor share elements."""
-    reach = t.shape[2]                    # elements that the rows so far span
-    for stride, n in sorted((t.stride(i), t.shape[i]) for i in (0, 1)):
+    """Whether rows (the last dimension) of a tensor share elements."""
+    reach = t.shape[-1]                   # elements that the rows so far span
+    for stride, n in sorted((t.stride(i), t.shape[i]) for i in range(t.dim() - 1)):
         if n > 1:
             if stride < reach:
                 return True
@@ -867,4 +878,133 @@ def linear4(x, w, out=None, ws=None):
     packed, scales = w.pointers
     _check(lib().fxp_w4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, K, w.N, packed, scales, w.group, out.data_ptr(), ldy, _p(ws),
                                ws.numel() if ws is not None else 0, _stream()), "fxp_w4_linear")
+    return out
+
+
+# ---- rotary positions ----
+# None of these calls records gradients: rotary_bwd is the gradient of rotary.
+
+# 1 / (2 pi) to 190 bits and more
+_TURN = Fraction("0.1591549430918953357688837633725143620344596457404564487476673440588967976")
+
+
+class Rotary:
+    """How heads are turned: pair i of dim / 2 by position * f_i radians, f_i = base ** (-2 i / dim).  Pairs are neighbouring elements (interleaved)
+    or elements dim / 2 apart; a head's elements from `dim` on stay.  scaling, for contexts longer than a model was trained with: "linear" (f / factor), "base"
+    (base * factor ** (dim / (dim - 2)): the slowest pair becomes `factor` times slower) or "parts" (f where a pair makes `high` turns or more over the
+    `original` tokens, f / factor where it makes `low` or fewer, in between in proportion).  amplitude: what turned elements are multiplied by.
+    frequencies: f itself, in place of all that."""
+
+    def __init__(self, dim, base=10000.0, interleaved=False, scaling=None, factor=1.0, original=0, low=1.0, high=32.0, amplitude=1.0, frequencies=None,
+                 device="cuda"):
+        if dim < 2 or dim % 2 or dim > 1024:
+            raise FxpError("dim must be even, 2 to 1024")
+        if not base > 0 or not factor > 0 or not 0 < amplitude < 1e30:
+            raise FxpError("base, factor and amplitude must be positive")
+        if frequencies is None:
+            if scaling == "base" and dim > 2:
+                base = base * factor ** (dim / (dim - 2))
+            frequencies = [base ** (-2 * i / dim) for i in range(dim // 2)]
+            if scaling == "linear":
+                frequencies = [f / factor for f in frequencies]
+            elif scaling == "parts":
+                if not original > 0 or not low < high:
+                    raise FxpError("parts need original > 0 and low < high")
+                share = [min(1.0, max(0.0, (original * f / (2 * math.pi) - low) / (high - low))) for f in frequencies]
+                frequencies = [f * (s + (1 - s) / factor) for f, s in zip(frequencies, share)]
+            elif scaling not in (None, "base"):
+                raise FxpError("scaling must be None, 'linear', 'base' or 'parts'")
+        frequencies = [float(f) for f in frequencies]
+        if len(frequencies) != dim // 2 or not all(math.isfinite(f) for f in frequencies):
+            raise FxpError("frequencies must be dim / 2 finite numbers")
+        turns = [round(Fraction(f) * _TURN * 2 ** 64) % 2 ** 64 for f in frequencies]
+        self.dim, self.interleaved, self.amplitude, self.frequencies = dim, bool(interleaved), float(amplitude), frequencies
+        self.turns = torch.tensor([t - 2 ** 64 if t >= 2 ** 63 else t for t in turns], dtype=torch.int64).to(device)
+        if not self.turns.is_cuda:
+            raise FxpError("the table must be on a GPU: libfxp has no CPU path")
+        self.index = self.turns.get_device()
+        self.c = _Rotation(_p(self.turns), dim, int(self.interleaved), self.amplitude)
+        self.ref = ctypes.byref(self.c)
+
+
+def _rotary(x, positions, rope, out, backward):
+    if not isinstance(x, torch.Tensor) or x.dim() not in (3, 4):
+        raise FxpError("x must be [tokens, heads, dim] or [batch, tokens, heads, dim]")
+    code = _served(x, "x", x.dim())
+    *batch, tokens, heads, dim = x.shape
+    _here(rope, "rope")
+    _index(positions, "positions")
+    if positions.shape != (tokens,) and positions.shape != (*batch, tokens):
+        raise FxpError("positions must be [tokens] or [batch, tokens]")
+    if rope.dim > dim:
+        raise FxpError("the rotated part is larger than a head")
+    if out is None:
+        out = x.new_empty(x.shape)
+    elif _served(out, "out", x.dim()) != code or out.shape != x.shape or _rows_overlap(out):
+        raise FxpError("out must have the shape and type of x, and rows that do not overlap")
+    elif not _same_rows(out, x) and _share(x, out):
+        raise FxpError("out shares elements with x, and is not x")
+    xs, ys = x.stride(), out.stride()
+    xb, yb = (xs[0], ys[0]) if batch else (0, 0)
+    _check(lib().fxp_rotary(rope.ref, backward, code, batch[0] if batch else 1, tokens, heads, dim, x.data_ptr(), xb, xs[-3], xs[-2], positions.data_ptr(),
+                            tokens if positions.dim() == 2 else 0, out.data_ptr(), yb, ys[-3], ys[-2], _stream()), "fxp_rotary")
+    return out
+
+
+def rotary(x, positions, rope, out=None):
+    """x [tokens, heads, dim] or [batch, tokens, heads, dim] (any strides but the last) turned by rope's angles at `positions`, int32 [tokens] or
+    [batch, tokens]; rows at negative positions are left as they are in out.  out: may be x itself, and shares no elements with it otherwise."""
+    return _rotary(x, positions, rope, out, 0)
+
+
+def rotary_bwd(dy, positions, rope, out=None):
+    """The gradient of rotary for its x, from the upstream gradient dy; arguments as there."""
+    return _rotary(dy, positions, rope, out, 1)
+
+
+def _meet(a, b):
+    """Whether tensors [tokens, heads, dim] of one type share elements; exact where a token's heads lie together and tokens are as far apart in both."""
+    (a0, a1), (b0, b1) = _span(a), _span(b)
+    if a1 <= b0 or b1 <= a0 or not a.numel() or not b.numel():
+        return False
+    step = a.stride(0)
+    reach = [(t.shape[1] - 1) * t.stride(1) + t.shape[2] for t in (a, b)]
+    if a.shape[0] <= 1 or b.shape[0] <= 1 or step != b.stride(0) or max(reach) > step:
+        return True
+    at = (b0 - a0) // a.element_size() % step           # of a token of b behind one of a
+    return at < reach[0] or at + reach[1] > step
+
+
+def kv_append_rotary(k, v, cache, tab, rope, q=None, out=None):
+    """kv_append of the step's tokens with the keys turned by `rope` on the way (tab.runs, tab.positions); keys are mapped as they come out of the
+    rotation, without a rounding between.  q [tokens, q_heads, dim]: the step's queries, which the same launch turns into out (q itself, or a tensor
+    that shares no elements with q, k and v); returns out, or None without q.  Rows of out whose tokens are not written to the cache - of refused
+    requests, behind the last one - are left as they are."""
+    code = _served(k, "k", 3)
+    if _served(v, "v", 3) != code or k.shape != v.shape or k.shape != (tab.tokens, cache.heads, cache.dim):
+        raise FxpError("k and v must be [tokens, heads, dim] of the tables and the cache, and of one type")
+    _here(cache, "cache")
+    _here(tab, "tab")
+    _here(rope, "rope")
+    if rope.dim > cache.dim:
+        raise FxpError("the rotated part is larger than a head")
+    if q is None:
+        if out is not None:
+            raise FxpError("out goes with q")
+        queries = (None, 0, 0, 0, None, 0, 0)
+    else:
+        if _served(q, "q", 3) != code or q.shape[0] != tab.tokens or q.shape[2] != cache.dim or q.shape[1] < 1 or q.shape[1] % cache.heads:
+            raise FxpError("q must be [tokens, q_heads, dim] of k's type, q_heads a multiple of the cache's heads")
+        if out is None:
+            out = q.new_empty(q.shape)
+        else:
+            if _served(out, "out", 3) != code or out.shape != q.shape or _rows_overlap(out):
+                raise FxpError("out must have the shape and type of q, and rows that do not overlap")
+            if not _same_rows(out, q) and _share(q, out):
+                raise FxpError("out shares elements with q, and is not q")
+            if _meet(out, k) or _meet(out, v):
+                raise FxpError("out shares elements with k or v")
+        queries = (q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], out.data_ptr(), out.stride(0), out.stride(1))
+    _check(lib().fxp_kv_append_rotary(cache.ref, tab.ref, rope.ref, code, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
+                                      *queries, _stream()), "fxp_kv_append_rotary")
     return out

@@ -1,0 +1,175 @@
+"""Rotary positions and their gradient against 64 bits: layouts, part of a head, strides, positions from zero to the last, types, refusals."""
+import numpy as np
+import pytest
+
+from tests import rotary_ref as ref
+from tests.gpu_util import host, say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+@pytest.fixture(scope="module")
+def fxp():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU path in libfxp")
+    from paper_2207_08822_amd import fxp as binding
+    binding.lib()
+    return binding
+
+
+def normal(shape, dtype, seed=0):
+    g = torch.Generator("cuda").manual_seed(seed)
+    return torch.randn(shape, device="cuda", generator=g).to(dtype)
+
+
+def check(fxp, x, positions, rope, backward=False, out=None):
+    want = ref.turn(host(x.float()), np.broadcast_to(host(positions), x.shape[:-2]), rope, backward)
+    before = x.clone()
+    y = (fxp.rotary_bwd if backward else fxp.rotary)(x, positions, rope, out=out)
+    torch.cuda.synchronize()
+    assert y.dtype == x.dtype and y.shape == x.shape
+    assert ref.within(host(y.double()), want, host(before.double()), rope, torch.finfo(x.dtype).eps)
+    if out is None or out.data_ptr() != x.data_ptr():
+        assert torch.equal(x, before)
+    # elements behind the rotated ones are the input's
+    assert torch.equal(y[..., rope.dim:], before[..., rope.dim:])
+    return y
+
+
+@pytest.mark.parametrize("near", [False, True])
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("tokens, heads, dim, rot", [(1, 1, 2, 2), (1, 12, 64, 64), (3, 2, 16, 6), (5, 3, 80, 40), (17, 1, 128, 128), (130, 4, 128, 32),
+                                                     (67, 7, 97, 96), (33, 5, 258, 192), (9, 1, 1030, 1024), (1, 300, 20, 12), (2, 1, 4000, 10)])
+def test_sizes(fxp, near, kind, tokens, heads, dim, rot):
+    say("rotary", near, kind, tokens, heads, dim, rot)
+    rope = fxp.Rotary(rot, interleaved=near, amplitude=1.25)
+    x = normal((tokens, heads, dim), TYPES[kind])
+    positions = torch.randint(0, 5000, (tokens,), dtype=torch.int32, device="cuda")
+    for backward in (False, True):
+        check(fxp, x, positions, rope, backward)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("shared", [False, True])
+def test_batches_with_heads_outside(fxp, kind, shared):
+    """[batch, heads, tokens, dim] memory seen as [batch, tokens, heads, dim], slices of wider rows, offsets that break the alignment."""
+    rope = fxp.Rotary(32, interleaved=shared)
+    g = torch.Generator("cuda").manual_seed(1)
+    wide = torch.randn((3, 4, 21, 56), device="cuda", generator=g).to(TYPES[kind])
+    positions = torch.randint(0, 9000, (21,) if shared else (3, 21), dtype=torch.int32, device="cuda", generator=g)
+    for lo in (0, 8, 1, 2, 4):
+        say("heads outside", kind, shared, lo)
+        x = wide[..., lo:lo + 48].transpose(1, 2)
+        check(fxp, x, positions, rope, out=torch.empty_like(wide)[..., :48].transpose(1, 2))
+        check(fxp, x, positions, rope, backward=True)
+    # rows that are one row seen many times
+    check(fxp, wide[:1, :, :1, :48].expand(3, 4, 21, 48).transpose(1, 2), positions, rope)
+
+
+def test_in_place_leaves_the_rest_alone(fxp):
+    rope = fxp.Rotary(40, interleaved=False)
+    buffer = normal((19, 5 * 64), torch.bfloat16, 3)
+    before = buffer.clone()
+    x = buffer[:, 64:64 + 3 * 64].unflatten(1, (3, 64))
+    positions = torch.arange(7, 26, dtype=torch.int32, device="cuda")
+    check(fxp, x, positions, rope, out=x)
+    assert torch.equal(buffer[:, :64], before[:, :64]) and torch.equal(buffer[:, 256:], before[:, 256:])
+    # parts of rows next to each other: what is read is not what is written
+    a, b = before[:, :64].unflatten(1, (1, 64)), before[:, 64:128].unflatten(1, (1, 64))
+    check(fxp, a, positions, rope, out=b)
+
+
+def test_rows_without_a_token_stay(fxp):
+    rope = fxp.Rotary(64)
+    x, out = normal((6, 2, 64), torch.float32), torch.full((6, 2, 64), 7.0, device="cuda")
+    positions = torch.tensor([0, -1, 5, -7, 9, -1], dtype=torch.int32, device="cuda")
+    fxp.rotary(x, positions, rope, out=out)
+    want = ref.turn(host(x), host(positions), rope)
+    there = host(positions) >= 0
+    assert np.all(host(out)[~there] == 7.0) and ref.within(host(out)[there], want[there], host(x)[there], rope, 2.0 ** -23)
+
+
+@pytest.mark.parametrize("scaling", [None, "linear", "base", "parts"])
+def test_far_positions(fxp, scaling):
+    """Angles of the farthest positions are as exact as those of near ones."""
+    more = dict(factor=8.0, original=4096, low=1.0, high=32.0) if scaling else {}
+    rope = fxp.Rotary(128, base=500000.0, scaling=scaling, **more)
+    positions = torch.tensor([0, 1, 2, 1000, 65535, 1 << 20, (1 << 24) + 1, (1 << 30) + 12345, (1 << 31) - 1], dtype=torch.int32, device="cuda")
+    check(fxp, normal((9, 2, 128), torch.float32), positions, rope)
+
+
+def test_frequencies_are_what_they_are_said_to_be(fxp):
+    f = fxp.Rotary(8, base=10000.0).frequencies
+    assert np.allclose(f, [1, 0.1, 0.01, 0.001], rtol=1e-15)
+    assert np.allclose(fxp.Rotary(8, scaling="linear", factor=4.0).frequencies, np.array(f) / 4, rtol=1e-15)
+    # the first pair keeps its frequency, the last one turns `factor` times more slowly
+    b = fxp.Rotary(8, scaling="base", factor=4.0).frequencies
+    assert b[0] == 1 and np.isclose(b[3], f[3] / 4, rtol=1e-12)
+    # over 1000 tokens the pairs make 159, 15.9, 1.59 and 0.159 turns
+    p = fxp.Rotary(8, scaling="parts", factor=4.0, original=1000, low=1.0, high=32.0).frequencies
+    share = (100 / (2 * np.pi) - 1) / 31
+    assert np.allclose(p[:2], [1, 0.1 * (share + (1 - share) / 4)], rtol=1e-12) and np.isclose(p[3], f[3] / 4, rtol=1e-12)
+    mine = fxp.Rotary(8, frequencies=[2 * np.pi, np.pi, 3.5, -1.0])
+    turns = [t % 2 ** 64 for t in mine.turns.tolist()]
+    # 2 pi of 64 bits is a turn but for 2.4e-16 of one's radians
+    assert min(turns[0], 2 ** 64 - turns[0]) < 2 ** 64 * 1e-16 and abs(turns[1] - 2 ** 63) < 2 ** 64 * 1e-16
+    assert abs(turns[2] / 2 ** 64 - 3.5 / (2 * np.pi)) < 1e-15 and abs(turns[3] / 2 ** 64 - (1 - 1 / (2 * np.pi))) < 1e-15
+    x, positions = normal((3, 1, 8), torch.float32), torch.tensor([0, 1, 77], dtype=torch.int32, device="cuda")
+    check(fxp, x, positions, mine)
+
+
+def test_gradient_against_differences(fxp):
+    """The rotation is linear: the difference over a step is the derivative, for any step; of size 1 with sums of fp32."""
+    rope = fxp.Rotary(12, interleaved=True, amplitude=0.75)
+    x, dy = normal((4, 2, 16), torch.float32, 1), normal((4, 2, 16), torch.float32, 2)
+    positions = torch.tensor([0, 3, 900, 70000], dtype=torch.int32, device="cuda")
+    dx = fxp.rotary_bwd(dy, positions, rope).double()
+    base = (fxp.rotary(x, positions, rope).double() * dy.double()).sum()
+    for at in [(0, 0, 0), (1, 1, 3), (2, 0, 11), (3, 1, 6), (3, 1, 15)]:
+        step = x.clone()
+        step[at] += 1.0
+        d = (fxp.rotary(step, positions, rope).double() * dy.double()).sum() - base
+        # two elements of y change; each of the two sides is off by 2^-20.9 (|u| + |w|) and a rounding, times |dy|: far below 2^-15 for these sizes
+        assert abs(d - dx[at] * (step.double() - x.double())[at]) < 2.0 ** -15
+
+
+def test_empty_and_refused(fxp):
+    rope = fxp.Rotary(32)
+    p = torch.zeros(4, dtype=torch.int32, device="cuda")
+    x = torch.zeros((4, 2, 64), device="cuda")
+    assert fxp.rotary(x[:0], p[:0], rope).shape == (0, 2, 64)
+    assert fxp.rotary(x[:, :0], p, rope).shape == (4, 0, 64)
+    assert fxp.rotary(x[None][:0], p, rope).shape == (0, 4, 2, 64)
+    bad = [lambda: fxp.rotary(x.cpu(), p, rope), lambda: fxp.rotary(x, p.long(), rope), lambda: fxp.rotary(x, p[:3], rope), lambda: fxp.rotary(x[0], p, rope),
+           lambda: fxp.rotary(x[..., :16], p, rope), lambda: fxp.rotary(x.double(), p, rope), lambda: fxp.rotary(x.transpose(1, 2), p, rope),
+           lambda: fxp.rotary(x, p, rope, out=x.half()), lambda: fxp.rotary(x, p, rope, out=x[:1].expand(4, 2, 64)),
+           lambda: fxp.rotary(x[:3], p[:3], rope, out=x[1:]), lambda: fxp.Rotary(7), lambda: fxp.Rotary(2000), lambda: fxp.Rotary(8, base=0.0),
+           lambda: fxp.Rotary(8, scaling="else"), lambda: fxp.Rotary(8, scaling="parts"), lambda: fxp.Rotary(8, frequencies=[1.0]),
+           lambda: fxp.Rotary(8, frequencies=[1.0, 2.0, float("nan"), 0.0]), lambda: fxp.Rotary(8, amplitude=0.0), lambda: fxp.Rotary(8, device="cpu")]
+    for i, call in enumerate(bad):
+        with pytest.raises(fxp.FxpError):
+            call()
+            pytest.fail(str(i))
+
+
+def test_replayed_and_on_another_stream(fxp):
+    rope = fxp.Rotary(64, interleaved=True)
+    x, positions, out = normal((40, 3, 64), torch.bfloat16), torch.arange(40, dtype=torch.int32, device="cuda"), torch.empty((40, 3, 64), dtype=torch.bfloat16, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        fxp.rotary(x, positions, rope, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, fxp.rotary(x, positions, rope))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fxp.rotary(x, positions, rope, out=out)
+    for i in range(3):
+        x.copy_(normal(x.shape, x.dtype, 10 + i))
+        positions += 1000
+        graph.replay()
+        assert torch.equal(out, fxp.rotary(x, positions, rope))
+        torch.cuda.synchronize()

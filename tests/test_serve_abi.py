@@ -142,3 +142,37 @@ def test_whether_rows_share_elements():
             assert fxp._same_rows(a, b) == (alike and a.data_ptr() == b.data_ptr())
     assert min(seen.values()) > 100
     assert not fxp._share(room[:0], room) and not fxp._share(room.view(20, 200)[:, :0], room.view(20, 200))
+
+
+def rotation(**over):
+    a = dict(turns=BIG, rot=32, interleaved=0, amplitude=1.0) | over
+    return c.byref(fxp._Rotation(*[a[n] for n, _ in fxp._Rotation._fields_]))
+
+
+def test_rotary(L):
+    def f(rot=rotation(), back=0, type=1, batch=2, tokens=4, heads=2, dim=64, x=BIG, xb=512, xt=128, xh=64, p=BIG, pb=0, y=BIG, yb=512, yt=128, yh=64):
+        return L.fxp_rotary(rot, back, type, batch, tokens, heads, dim, x, xb, xt, xh, p, pb, y, yb, yt, yh, None)
+
+    assert f(rot=None) == -1 and f(rot=rotation(turns=None)) == -1 and f(rot=rotation(turns=BIG + 4)) == -3
+    for rot in (0, 1, 3, 66, -2):
+        assert f(rot=rotation(rot=rot)) == -2
+    assert f(rot=rotation(rot=1026), dim=2000) == -2
+    for amplitude in (0.0, -1.0, float("nan"), float("inf")):
+        assert f(rot=rotation(amplitude=amplitude)) == -10
+    assert f(type=3) == -9 and f(batch=-1) == -2 and f(tokens=-1) == -2 and f(tokens=1 << 31) == -2 and f(heads=65536) == -2 and f(dim=65537) == -2
+    assert f(xt=-1) == -2 and f(yh=-1) == -2 and f(xb=-1) == -2 and f(pb=-1) == -2 and f(yb=1 << 40) == -2 and f(batch=1 << 30, tokens=1 << 12) == -2
+    assert f(x=None) == -1 and f(y=None) == -1 and f(p=None) == -1 and f(x=BIG + 1) == -3 and f(y=BIG + 1) == -3 and f(p=BIG + 2) == -3
+    assert f(batch=0) == 0 and f(tokens=0) == 0 and f(heads=0) == 0
+
+
+def test_append_rotary(L):
+    def f(ca=cache(), st=step(), rot=rotation(), type=1, k=BIG, kt=128, kh=64, v=BIG, q=BIG, qt=256, qh=64, heads=4, out=BIG, ot=256, oh=64):
+        return L.fxp_kv_append_rotary(ca, st, rot, type, k, kt, kh, v, 128, 64, q, qt, qh, heads, out, ot, oh, None)
+
+    assert f(ca=None) == -1 and f(ca=cache(dim=24)) == -2 and f(ca=cache(bits=9)) == -6 and f(st=None) == -1 and f(rot=None) == -1
+    assert f(rot=rotation(rot=66)) == -2 and f(rot=rotation(rot=33)) == -2 and f(rot=rotation(amplitude=0.0)) == -10 and f(type=4) == -9
+    assert f(st=step(requests=0)) == -2 and f(st=step(tokens=-1)) == -2 and f(st=step(requests=1 << 31)) == -2 and f(st=step(tokens=1 << 30)) == -2
+    assert f(heads=3) == -2 and f(heads=0) == -2 and f(heads=16386) == -2 and f(kt=-1) == -2 and f(qt=-1) == -2 and f(oh=-1) == -2
+    assert f(st=step(runs=None)) == -1 and f(st=step(positions=None)) == -1 and f(k=None) == -1 and f(v=None) == -1 and f(out=None) == -1
+    assert f(st=step(runs=BIG + 4)) == -3 and f(st=step(positions=BIG + 2)) == -3 and f(k=BIG + 1) == -3 and f(q=BIG + 1) == -3 and f(out=BIG + 1) == -3
+    assert f(st=step(tokens=0)) == 0 and f(st=step(tokens=0), q=None, heads=0) == 0
