@@ -529,6 +529,30 @@ size_t fxp_w4_workspace_bytes(int type, int64_t M, int64_t K, int group);
 int fxp_w4_linear(int type, const void* X, int64_t ldx, int64_t M, int64_t K, int64_t N, const uint8_t* packed, const uint8_t* scales,
                   int group, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- products in microscaled 4-bit floating point ----
+ * A mapped matrix [rows, cols] for products that contract over its columns: 32 elements of a row (a block) are 4-bit floats under one power of two,
+ * the smallest under which the largest of them is at most 6 - the method's shared exponent, for 32 elements in place of a tensor.  A code is a sign (8)
+ * and the place of a magnitude in 0, 0.5, 1, 1.5, 2, 3, 4, 6; a scale byte s stands for 2^(s - 127), 0 <= s <= 253.  A block with Inf or NaN has s = 255 and
+ * is NaN, every element of it, in products too.  Panels of 256 columns, [ceil(cols / 256), rows, 128] bytes, even elements in the low halves; scales
+ * [ceil(cols / 256), rows, 8], of the panel's blocks 0, 2, 4, 6, 1, 3, 5, 7.  Codes and scales behind the last column are zeros.
+ * Host struct of device pointers; data 16-byte, scales 8-byte aligned; rows, cols <= 2^24 - 2^16. */
+typedef struct fxp_mx4 {
+    uint8_t* data;
+    uint8_t* scales;
+    int64_t rows, cols;
+} fxp_mx4;
+size_t fxp_mx4_data_bytes(int64_t rows, int64_t cols);  /* 0 on bad arguments */
+size_t fxp_mx4_scale_bytes(int64_t rows, int64_t cols);
+
+/* Maps x [rows, cols] of `type`, row stride ldx >= cols: q [rows, cols] with blocks along the rows and / or qT [cols, rows], x transposed, with blocks
+ * along x's columns (either may be NULL), in one pass.  rounding: FXP_ROUND_NEAREST is to nearest, ties to even; FXP_ROUND_STOCHASTIC up with the
+ * probability of what is cut off, in units of 2^-22: where the top 22 bits of the element's random word are less than the top 22 bits behind the code.
+ * Words as in fxp_map: element i of x (row-major, without gaps) has word i % 4 of Philox block i / 4, in both copies. */
+int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT, uint64_t seed,
+                uint64_t stream_id, int rounding, void* stream);
+/* The values [rows, cols] that q stands for, rounded once to `type` (exact in fp32; in bf16 but for underflow). */
+int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream);
+
 /* ---- measurement helper (not a step of the method) ----
  * Core clock while other work runs: enqueues one wave on `stream` (use a stream of its own, next to the kernels
  * under test) that stays alive for `microseconds` (1 .. 1000000) of the constant 100 MHz counter and then writes

@@ -14,6 +14,21 @@ using IC = std::integral_constant<int, V>;
 
 constexpr int kNumXcd = 8;
 
+// Workgroup b runs on XCD b % 8.  Give XCD x the contiguous range of tile numbers
+// [start(x), start(x+1)), then walk tiles in column-major groups of `group_m` tile rows
+// so that concurrently resident tiles share A and B panels in that XCD's L2.
+__device__ inline void tile_of_block(int b, int tiles_m, int tiles_n, int group_m, int* tm, int* tn) {
+    const int total = tiles_m * tiles_n;
+    const int q = total / kNumXcd, r = total % kNumXcd;
+    const int xcd = b % kNumXcd, local = b / kNumXcd;
+    const int t = (xcd < r) ? xcd * (q + 1) + local : r * (q + 1) + (xcd - r) * q + local;
+    const int per_group = group_m * tiles_n;
+    const int g = t / per_group, in_g = t % per_group;
+    const int rows_here = min(group_m, tiles_m - g * group_m);
+    *tm = g * group_m + in_g % rows_here;
+    *tn = in_g / rows_here;
+}
+
 template <int BK>
 __device__ inline int swizzle_of_row(int row) {
     constexpr int CPR = BK / 16;            // 16-byte pieces per LDS row

@@ -1,0 +1,290 @@
+// Mapping to microscaled 4-bit numbers and back, and a linear layer's step in them.
+//
+// A mapped matrix serves products that contract over its columns; a training step contracts every operand along both of its axes and therefore maps it twice,
+// with blocks of 32 along the rows and of 32 along the columns.  Both copies come out of one pass: 32 x 32 elements hold whole blocks of both.
+#include <algorithm>
+
+#include "fxp_mx4_device.h"
+
+namespace fxp {
+
+constexpr int kMxThreads = 256;
+
+struct Mx4Job {
+    Mx4Map m;
+    int tiles_c;            // tiles of a row of tiles
+    unsigned first;         // workgroup of the job's first tile
+    int vec;                // rows are multiples of four elements and so is the base
+};
+struct Mx4Jobs {
+    Mx4Job job[2];
+    int count;
+};
+
+// largest of eight neighbouring lanes, in all of them
+__device__ inline uint32_t max_of_8(uint32_t m) {
+    auto step = [&](auto ctrl) { m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), decltype(ctrl)::value, 0xf, 0xf, false))); };
+    step(std::integral_constant<int, 0xb1>{});      // neighbours
+    step(std::integral_constant<int, 0x4e>{});      // pairs
+    step(std::integral_constant<int, 0x141>{});     // the eight mirrored
+    return m;
+}
+// largest of the lanes eight apart
+__device__ inline uint32_t max_over_8(uint32_t m) {
+    typedef unsigned v2u __attribute__((ext_vector_type(2)));
+    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x128, 0xf, 0xf, false)));      // row_ror:8
+    v2u p = __builtin_amdgcn_permlane16_swap(m, m, false, false);
+    m = max(p[0], p[1]);
+    p = __builtin_amdgcn_permlane32_swap(m, m, false, false);
+    return max(p[0], p[1]);
+}
+
+// A workgroup maps BR x BC blocks of 32 x 32; a lane has 4 x 4 elements of each of its wave's blocks: four quads of consecutive elements, one Philox block each.
+// Codes are put together in LDS and leave in 16-byte pieces.
+// Bound by memory for nearest, by the vector ALU for stochastic rounding (10 rounds of Philox a quad and 14 operations an element and copy).
+template <int TYPE, bool STOCH, int BR, int BC>
+__global__ __launch_bounds__(kMxThreads) void k_mx4_map(Mx4Jobs jobs, uint32_t key0, uint32_t key1) {
+    constexpr int TR = 32 * BR, TC = 32 * BC, kPad = 16, SQ = TC / 2 + kPad, ST = TR / 2 + kPad;
+    static_assert(BR * BC % 4 == 0 && kMxPanel % TR == 0 && kMxPanel % TC == 0, "tiles lie in one panel, waves have as many blocks");
+    __shared__ __attribute__((aligned(16))) uint8_t lq[TR * SQ], lt[TC * ST];
+    __shared__ uint8_t eq[TR * BC], et[TC * BR];
+    const Mx4Job& J = jobs.job[jobs.count > 1 && blockIdx.x >= jobs.job[1].first ? 1 : 0];
+    const int tile = static_cast<int>(blockIdx.x - J.first);
+    const int64_t r0 = int64_t{tile / J.tiles_c} * TR, c0 = int64_t{tile % J.tiles_c} * TC;
+    const int64_t rows = J.m.rows, cols = J.m.cols;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rb = lane >> 3, cb = lane & 7;
+    const bool want_q = J.m.q != nullptr, want_t = J.m.t != nullptr, vec = J.vec;
+    const uint32_t sid0 = static_cast<uint32_t>(J.m.stream_id), sid1 = static_cast<uint32_t>(J.m.stream_id >> 32);
+    constexpr int kMine = BR * BC / 4;
+
+    auto load = [&](int n, float (&x)[4][4]) {
+        const int block = wave + 4 * n;
+        const int64_t r = r0 + (block / BC) * 32 + 4 * rb, c = c0 + (block % BC) * 32 + 4 * cb;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t at = (r + i) * J.m.ld + c;
+            if (r + i < rows && c + 3 < cols) {
+                load_elems<TYPE, 4>(J.m.x, at, vec, x[i]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[i][j] = r + i < rows && c + j < cols ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(J.m.x)[at + j]) : 0.0f;
+            }
+        }
+    };
+    float x[4][4];
+    load(0, x);
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+        float next[4][4];
+        if (n + 1 < kMine) load(n + 1, next);
+        const int block = wave + 4 * n, br = block / BC, bc = block % BC;
+        uint32_t word[4][4];
+        if constexpr (STOCH) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t at = static_cast<uint64_t>(r0 + br * 32 + 4 * rb + i) * static_cast<uint64_t>(cols) + static_cast<uint64_t>(c0 + bc * 32 + 4 * cb);
+                const uint64_t quad = at >> 2;
+                const uint4 w = philox4x32_10(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32), sid0, sid1, key0, key1);
+                word[i][0] = w.x; word[i][1] = w.y; word[i][2] = w.z; word[i][3] = w.w;
+                if (cols & 3) {                             // the lane's four elements lie in two quads
+                    const uint4 v = philox4x32_10(static_cast<uint32_t>(quad + 1), static_cast<uint32_t>((quad + 1) >> 32), sid0, sid1, key0, key1);
+                    const uint32_t all[7] = {w.x, w.y, w.z, w.w, v.x, v.y, v.z};
+                    const int shift = static_cast<int>(at & 3);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint32_t u = all[j];
+#pragma unroll
+                        for (int k = 1; k < 4; ++k) u = shift == k ? all[j + k] : u;
+                        word[i][j] = u;
+                    }
+                }
+            }
+        }
+        auto four = [&](float a, float b, float c, float d, uint32_t wa, uint32_t wb, uint32_t wc, uint32_t wd) {
+            if constexpr (STOCH)
+                return mx_stochastic(a, wa) | mx_stochastic(b, wb) << 4 | mx_stochastic(c, wc) << 8 | mx_stochastic(d, wd) << 12;
+            else
+                return mx_nearest4(a, b, c, d);
+        };
+        auto bits = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
+        if (want_q) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int s = mx_scale_of(max_of_8(max(max(bits(x[i][0]), bits(x[i][1])), max(bits(x[i][2]), bits(x[i][3])))));
+                const float f = mx_inverse(s);
+                const int row = br * 32 + 4 * rb + i;
+                const uint32_t o = four(x[i][0] * f, x[i][1] * f, x[i][2] * f, x[i][3] * f, word[i][0], word[i][1], word[i][2], word[i][3]);
+                *reinterpret_cast<uint16_t*>(&lq[row * SQ + bc * 16 + 2 * cb]) = static_cast<uint16_t>(o);
+                if (cb == 0) eq[row * BC + bc] = static_cast<uint8_t>(s);
+            }
+        }
+        if (want_t) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int s = mx_scale_of(max_over_8(max(max(bits(x[0][j]), bits(x[1][j])), max(bits(x[2][j]), bits(x[3][j])))));
+                const float f = mx_inverse(s);
+                const int col = bc * 32 + 4 * cb + j;
+                const uint32_t o = four(x[0][j] * f, x[1][j] * f, x[2][j] * f, x[3][j] * f, word[0][j], word[1][j], word[2][j], word[3][j]);
+                *reinterpret_cast<uint16_t*>(&lt[col * ST + br * 16 + 2 * rb]) = static_cast<uint16_t>(o);
+                if (rb == 0) et[col * BR + br] = static_cast<uint8_t>(s);
+            }
+        }
+        if (n + 1 < kMine) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[i][j] = next[i][j];
+        }
+    }
+    __syncthreads();
+    // `height` lines of `width` blocks: line l of the copy is row l0 + l of `lines`, its blocks begin at b0 of the contraction
+    auto leave = [&](const uint8_t* codes, const uint8_t* scales, int stride, int height, int width, int64_t l0, int64_t lines, int64_t b0, uint8_t* data,
+                     uint8_t* out_scales) {
+        const int64_t panel = b0 / kMxPanel * lines + l0;
+        const int at = static_cast<int>(b0 % kMxPanel) / kMxBlock, here = static_cast<int>(min(int64_t{height}, lines - l0));
+        for (int i = threadIdx.x; i < here * width; i += kMxThreads) {
+            const int l = i / width, p = i % width;
+            *reinterpret_cast<uint4*>(data + (panel + l) * kMxRowBytes + (at + p) * 16) = *reinterpret_cast<const uint4*>(&codes[l * stride + p * 16]);
+            out_scales[(panel + l) * kMxRowScales + mx_scale_place(at + p)] = scales[i];
+        }
+    };
+    if (want_q) leave(lq, eq, SQ, TR, BC, r0, rows, c0, J.m.q, J.m.q_scales);
+    if (want_t) leave(lt, et, ST, TC, BR, c0, cols, r0, J.m.t, J.m.t_scales);
+}
+
+int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int rounding, hipStream_t s) {
+    auto launch = [&](auto type_c, auto stoch_c, auto br_c, auto bc_c) {
+        constexpr int BR = decltype(br_c)::value, BC = decltype(bc_c)::value;
+        Mx4Jobs jobs{};
+        int64_t tiles = 0;
+        for (int i = 0; i < count; ++i) {
+            const Mx4Map& m = maps[i];
+            if (m.rows == 0 || m.cols == 0) continue;
+            Mx4Job& j = jobs.job[jobs.count++];
+            j.m = m;
+            // a copy is written up to the end of its last panel
+            const int64_t R = m.t ? mx_panels(m.rows) * kMxPanel : m.rows, C = m.q ? mx_panels(m.cols) * kMxPanel : m.cols;
+            j.tiles_c = static_cast<int>((C + 32 * BC - 1) / (32 * BC));
+            j.first = static_cast<unsigned>(tiles);
+            j.vec = aligned(m.x, 4 * static_cast<size_t>(elem_size(type))) && m.ld % 4 == 0;
+            tiles += j.tiles_c * ((R + 32 * BR - 1) / (32 * BR));
+        }
+        if (tiles >= int64_t{1} << 31) return static_cast<int>(FXP_ERR_DIMS);
+        if (tiles == 0) return static_cast<int>(FXP_OK);
+        hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value, BR, BC>), dim3(static_cast<unsigned>(tiles)), dim3(kMxThreads), 0, s, jobs,
+                           static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
+        return launch_status();
+    };
+    int64_t elements = 0;
+    for (int i = 0; i < count; ++i) elements += maps[i].rows * maps[i].cols;
+    auto sized = [&](auto type_c, auto stoch_c) {
+        using std::integral_constant;
+        if (elements >= int64_t{1} << 22) return launch(type_c, stoch_c, integral_constant<int, 4>{}, integral_constant<int, 4>{});
+        return launch(type_c, stoch_c, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+    };
+    auto typed = [&](auto type_c) {
+        return rounding == FXP_ROUND_STOCHASTIC ? sized(type_c, std::true_type{}) : sized(type_c, std::false_type{});
+    };
+    if (type == FXP_F32) return typed(std::integral_constant<int, FXP_F32>{});
+    if (type == FXP_BF16) return typed(std::integral_constant<int, FXP_BF16>{});
+    return typed(std::integral_constant<int, FXP_F16>{});
+}
+
+// ---- inverse mapping: a thread has eight elements of a row ----
+template <int TYPE>
+__global__ __launch_bounds__(kMxThreads) void k_mx4_unmap(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, int64_t rows, int64_t cols, void* y, int64_t ld,
+                                                          int vec) {
+    const int64_t piece = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) % (kMxRowBytes / 4), row = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) / (kMxRowBytes / 4);
+    const int64_t c = int64_t{blockIdx.y} * kMxPanel + piece * 8;
+    if (row >= rows || c >= cols) return;
+    const int64_t line = blockIdx.y * rows + row;
+    const uint32_t codes = *reinterpret_cast<const uint32_t*>(data + line * kMxRowBytes + piece * 4);
+    const int s = scales[line * kMxRowScales + mx_scale_place(static_cast<int>(piece) / 4)];
+    // 2^-127 is a sub-normal number, and there is no number for 255
+    const float unit = s == 255 ? __uint_as_float(0x7fc00000u) : s == 0 ? __uint_as_float(0x400000u) : __uint_as_float(static_cast<uint32_t>(s) << 23);
+    float v[8];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const float2 two = mx_values(codes, b);
+        v[2 * b] = two.x * unit;
+        v[2 * b + 1] = two.y * unit;
+    }
+    const int64_t at = row * ld + c;
+    if (vec && c + 8 <= cols) {
+        store_elems<TYPE, 8>(y, at, v);
+    } else {
+        typename Elem<TYPE>::T* const p = static_cast<typename Elem<TYPE>::T*>(y) + at;
+        for (int j = 0; j < 8; ++j)
+            if (c + j < cols) p[j] = static_cast<typename Elem<TYPE>::T>(v[j]);
+    }
+}
+
+static Mx4Map map_of(const void* x, int64_t ld, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* t, uint64_t stream_id) {
+    Mx4Map m{x, ld, rows, cols, nullptr, nullptr, nullptr, nullptr, stream_id};
+    if (q) m.q = q->data, m.q_scales = q->scales;
+    if (t) m.t = t->data, m.t_scales = t->scales;
+    return m;
+}
+
+static int check_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT) {
+    if (!known_type(type)) return FXP_ERR_TYPE;
+    if (rows < 0 || cols < 0 || rows > kMxMost || cols > kMxMost || ldx < cols || ldx >= int64_t{1} << 40) return FXP_ERR_DIMS;
+    if (q) {
+        const int rc = check_mx4(q);
+        if (rc) return rc;
+        if (q->rows != rows || q->cols != cols) return FXP_ERR_DIMS;
+    }
+    if (qT) {
+        const int rc = check_mx4(qT);
+        if (rc) return rc;
+        if (qT->rows != cols || qT->cols != rows) return FXP_ERR_DIMS;
+    }
+    if (rows && cols) {
+        if (!x) return FXP_ERR_NULL;
+        if (!aligned(x, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    }
+    return FXP_OK;
+}
+
+static bool known_rounding(int r) { return r == FXP_ROUND_STOCHASTIC || r == FXP_ROUND_NEAREST; }
+
+}  // namespace fxp
+
+extern "C" size_t fxp_mx4_data_bytes(int64_t rows, int64_t cols) {
+    if (rows < 0 || cols < 0 || rows > fxp::kMxMost || cols > fxp::kMxMost) return 0;
+    return static_cast<size_t>(fxp::mx_panels(cols) * rows * fxp::kMxRowBytes);
+}
+
+extern "C" size_t fxp_mx4_scale_bytes(int64_t rows, int64_t cols) { return fxp_mx4_data_bytes(rows, cols) / 16; }
+
+extern "C" int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT, uint64_t seed, uint64_t stream_id,
+                           int rounding, void* stream) {
+    if (!q && !qT) return FXP_ERR_NULL;
+    const int rc = fxp::check_map(type, x, ldx, rows, cols, q, qT);
+    if (rc) return rc;
+    if (!fxp::known_rounding(rounding)) return FXP_ERR_ROUNDING;
+    const fxp::Mx4Map m = fxp::map_of(x, ldx, rows, cols, q, qT, stream_id);
+    return fxp::mx4_map_launch(type, &m, 1, seed, rounding, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream) {
+    using namespace fxp;
+    const int rc = check_mx4(q);
+    if (rc) return rc;
+    if (!known_type(type)) return FXP_ERR_TYPE;
+    if (ldy < q->cols || ldy >= int64_t{1} << 40) return FXP_ERR_DIMS;
+    if (q->rows == 0 || q->cols == 0) return FXP_OK;
+    if (!y) return FXP_ERR_NULL;
+    if (!aligned(y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    constexpr int kRows = kMxThreads / (kMxRowBytes / 4);
+    const dim3 grid(static_cast<unsigned>((q->rows + kRows - 1) / kRows), static_cast<unsigned>(mx_panels(q->cols)));
+    const int vec = aligned(y, 16) && ldy * elem_size(type) % 16 == 0;
+    auto go = [&](auto type_c) {
+        hipLaunchKernelGGL((k_mx4_unmap<decltype(type_c)::value>), grid, dim3(kMxThreads), 0, static_cast<hipStream_t>(stream), q->data, q->scales, q->rows, q->cols, y, ldy, vec);
+    };
+    if (type == FXP_F32) go(std::integral_constant<int, FXP_F32>{});
+    else if (type == FXP_BF16) go(std::integral_constant<int, FXP_BF16>{});
+    else go(std::integral_constant<int, FXP_F16>{});
+    return launch_status();
+}

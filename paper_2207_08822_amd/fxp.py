@@ -63,6 +63,10 @@ class _Rotation(ctypes.Structure):
     _fields_ = [("turns", ctypes.c_void_p), ("rot", ctypes.c_int64), ("interleaved", ctypes.c_int), ("amplitude", ctypes.c_double)]
 
 
+class _Mx4(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -159,6 +163,15 @@ def lib():
     L.fxp_rotary.restype = ci
     L.fxp_kv_append_rotary.argtypes = [cache, step, turn, ci, vp, i64, i64, vp, i64, i64, vp, i64, i64, i64, vp, i64, i64, vp]
     L.fxp_kv_append_rotary.restype = ci
+    mx = c.POINTER(_Mx4)
+    L.fxp_mx4_data_bytes.argtypes = [i64, i64]
+    L.fxp_mx4_data_bytes.restype = sz
+    L.fxp_mx4_scale_bytes.argtypes = [i64, i64]
+    L.fxp_mx4_scale_bytes.restype = sz
+    L.fxp_mx4_map.argtypes = [ci, vp, i64, i64, i64, mx, mx, u64, u64, ci, vp]
+    L.fxp_mx4_map.restype = ci
+    L.fxp_mx4_unmap.argtypes = [mx, ci, vp, i64, vp]
+    L.fxp_mx4_unmap.restype = ci
     for name in ("fxp_kv_tables", "fxp_kv_append", "fxp_kv_load", "fxp_kv_attention", "fxp_w4_pack", "fxp_w4_linear"):
         getattr(L, name).restype = ci
     for name in ("fxp_scale", "fxp_map", "fxp_scale_map", "fxp_gemm", "fxp_unmap", "fxp_unmap_i8", "fxp_gemm_unmap",
@@ -1007,4 +1020,72 @@ def kv_append_rotary(k, v, cache, tab, rope, q=None, out=None):
         queries = (q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], out.data_ptr(), out.stride(0), out.stride(1))
     _check(lib().fxp_kv_append_rotary(cache.ref, tab.ref, rope.ref, code, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1),
                                       *queries, _stream()), "fxp_kv_append_rotary")
+    return out
+
+
+# ---- products in microscaled 4-bit floating point ----
+# None of these calls records gradients: mx4_linear_bwd is the gradient of mx4_linear_fwd.
+
+MX4_PANEL = 256         # columns of a panel of a mapped matrix
+
+
+class Mx4:
+    """A matrix [rows, cols] in 4-bit floats with a scale for each 32 elements of a row (the layout of include/fxp.h), for products that contract over cols:
+    data uint8 [panels, rows, 128], scales uint8 [panels, rows, 8]."""
+
+    def __init__(self, rows, cols, device="cuda"):
+        if min(rows, cols) < 0 or max(rows, cols) > 2 ** 24 - 2 ** 16:
+            raise FxpError("rows and cols must be between 0 and 2^24 - 2^16")
+        panels = -(-cols // MX4_PANEL)
+        self._set(torch.empty((panels, rows, 128), dtype=torch.uint8, device=device), torch.empty((panels, rows, 8), dtype=torch.uint8, device=device), rows, cols)
+
+    @classmethod
+    def of(cls, data, scales, rows, cols):
+        """The matrix that two tensors of these shapes are; codes and scales behind the last column have to be zeros."""
+        self = cls.__new__(cls)
+        self._set(data, scales, rows, cols)
+        return self
+
+    def _set(self, data, scales, rows, cols):
+        panels = -(-cols // MX4_PANEL)
+        _index(data, "data", (panels, rows, 128), torch.uint8)
+        _index(scales, "scales", (panels, rows, 8), torch.uint8)
+        self.data, self.scales, self.rows, self.cols, self.index = data, scales, rows, cols, data.get_device()
+        self.c = _Mx4(data.data_ptr(), scales.data_ptr(), rows, cols)
+        self.ref = ctypes.byref(self.c)
+
+
+def mx4_map(x, rounding=STOCHASTIC, seed=0, stream_id=0, want_q=True, want_qT=False, out=None):
+    """(q, qT): x [rows, cols] mapped with blocks along its rows, for products that contract over cols, and x transposed with blocks along its columns, for
+    products that contract over rows; None where not wanted.  rounding: NEAREST (ties to even) or STOCHASTIC (Philox words as in map).  out: the pair of
+    Mx4 to fill, None where not wanted."""
+    code = _served(x, "x", 2)
+    rows, cols = x.shape
+    if out is None:
+        q, qT = Mx4(rows, cols, x.device) if want_q else None, Mx4(cols, rows, x.device) if want_qT else None
+    else:
+        q, qT = out
+        for t, shape in ((q, (rows, cols)), (qT, (cols, rows))):
+            if t is not None:
+                _here(t, "out")
+                if (t.rows, t.cols) != shape:
+                    raise FxpError("out must be the mapped matrix of x's shape, and of the transposed one")
+    if q is None and qT is None:
+        raise FxpError("neither copy is wanted")
+    _check(lib().fxp_mx4_map(code, x.data_ptr(), _row_stride(x, "x"), rows, cols, q.ref if q else None, qT.ref if qT else None, seed, stream_id, rounding, _stream()),
+           "fxp_mx4_map")
+    return q, qT
+
+
+def mx4_unmap(q, dtype=torch.float32, out=None):
+    """The values [rows, cols] that q stands for, in `dtype` or out's type."""
+    _here(q, "q")
+    if out is None:
+        if dtype not in _TYPES:
+            raise FxpError("dtype must be float32, bfloat16 or float16")
+        out = q.data.new_empty((q.rows, q.cols), dtype=dtype)
+    code = _served(out, "out", 2)
+    if out.shape != (q.rows, q.cols):
+        raise FxpError("out must be [rows, cols] of q")
+    _check(lib().fxp_mx4_unmap(q.ref, code, out.data_ptr(), _row_stride(out, "out"), _stream()), "fxp_mx4_unmap")
     return out

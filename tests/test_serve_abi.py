@@ -176,3 +176,27 @@ def test_append_rotary(L):
     assert f(st=step(runs=None)) == -1 and f(st=step(positions=None)) == -1 and f(k=None) == -1 and f(v=None) == -1 and f(out=None) == -1
     assert f(st=step(runs=BIG + 4)) == -3 and f(st=step(positions=BIG + 2)) == -3 and f(k=BIG + 1) == -3 and f(q=BIG + 1) == -3 and f(out=BIG + 1) == -3
     assert f(st=step(tokens=0)) == 0 and f(st=step(tokens=0), q=None, heads=0) == 0
+
+
+def mx4(**over):
+    a = dict(data=BIG, scales=BIG, rows=5, cols=70) | over
+    return c.byref(fxp._Mx4(*[a[n] for n, _ in fxp._Mx4._fields_]))
+
+
+def test_mx4_sizes(L):
+    assert L.fxp_mx4_data_bytes(5, 70) == 5 * 128 and L.fxp_mx4_scale_bytes(5, 70) == 5 * 8 and L.fxp_mx4_data_bytes(3, 257) == 2 * 3 * 128
+    assert L.fxp_mx4_data_bytes(0, 9) == 0 and L.fxp_mx4_data_bytes(-1, 9) == 0 and L.fxp_mx4_data_bytes(9, 1 << 24) == 0
+
+
+def test_mx4_map_and_unmap(L):
+    def f(type=0, x=BIG, ld=70, rows=5, cols=70, q=mx4(), t=mx4(rows=70, cols=5), rounding=0):
+        return L.fxp_mx4_map(type, x, ld, rows, cols, q, t, 0, 0, rounding, None)
+
+    assert f(q=None, t=None) == -1 and f(type=5) == -9 and f(rounding=2) == -5 and f(x=None) == -1 and f(x=BIG + 2) == -3 and f(ld=69) == -2
+    assert f(rows=-1) == -2 and f(cols=1 << 24, ld=1 << 24) == -2 and f(q=mx4(rows=6)) == -2 and f(t=mx4()) == -2
+    for bad, rc in ((dict(data=None), -1), (dict(scales=None), -1), (dict(data=BIG + 8), -3), (dict(scales=BIG + 4), -3), (dict(rows=-1), -2)):
+        assert f(q=mx4(**bad)) == rc and f(t=mx4(**(dict(rows=70, cols=5) | bad))) == rc
+        assert L.fxp_mx4_unmap(mx4(**bad), 0, BIG, 70, None) == rc
+    assert L.fxp_mx4_unmap(None, 0, BIG, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 3, BIG, 70, None) == -9 and L.fxp_mx4_unmap(mx4(), 0, BIG, 69, None) == -2
+    assert L.fxp_mx4_unmap(mx4(), 0, None, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 0, BIG + 2, 70, None) == -3
+    assert f(x=None, rows=0, q=mx4(rows=0), t=mx4(rows=70, cols=0)) == 0 and L.fxp_mx4_unmap(mx4(rows=0, data=None), 0, None, 70, None) == 0
