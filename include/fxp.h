@@ -553,6 +553,30 @@ int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols
 /* The values [rows, cols] that q stands for, rounded once to `type` (exact in fp32; in bf16 but for underflow). */
 int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream);
 
+/* C[M,N] of `type` = A B^T for mapped A [M,K] and B [N,K], row stride ldc >= N: products are exact, sums fp32 in no stated order (the same order on every call
+ * of a size), rounded once to `type`.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
+size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream);
+
+/* Y[M,N] = X[M,K] W of `type`, W = [N,K] mapped (W^T with blocks along the contraction: fxp_mx4_map's qT of W[K,N]); X is mapped to nearest on the way.  Row strides
+ * ldx >= K, ldy >= N.  Any M, one row to many.  Y must not overlap X.  ws: fxp_mx4_linear_workspace_bytes bytes, 256-byte aligned. */
+size_t fxp_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx4* W, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+
+/* A layer's training step, as fxp_linear_fwd / _bwd with blocks of 4-bit floats in place of int8 tensors: Y = X W, dX = dY W^T, dW = X^T dY, dense
+ * row-major of one `type`, every operand mapped along the contraction that it is used in (the same random words in both copies).  The mapped operands belong to the
+ * caller: fwd fills X [M,K], WT [N,K], XT [K,M] and W [K,N] (the last two may have data NULL where no backward call follows), bwd reads XT for dW and W for dX, and
+ * fills dY [M,N] for dX and dYT [N,M] for dW.  dX or dW may be NULL.  Streams: (step << 8) | 0, 1, 2 for X, W, dY; step < 2^56.
+ * ws: fxp_mx4_layer_workspace_bytes bytes (at least 256), 256-byte aligned. */
+typedef struct fxp_mx4_layer {
+    fxp_mx4 X, XT, W, WT, dY, dYT;
+} fxp_mx4_layer;
+size_t fxp_mx4_layer_workspace_bytes(int64_t M, int64_t K, int64_t N);
+int fxp_mx4_linear_fwd(int type, const void* X, const void* W, int64_t M, int64_t K, int64_t N, void* Y, const fxp_mx4_layer* layer, uint64_t seed, uint64_t step,
+                       int rounding, void* ws, size_t ws_bytes, void* stream);
+int fxp_mx4_linear_bwd(int type, const void* dY, const fxp_mx4_layer* layer, int64_t M, int64_t K, int64_t N, void* dX, void* dW, uint64_t seed, uint64_t step,
+                       int rounding, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- measurement helper (not a step of the method) ----
  * Core clock while other work runs: enqueues one wave on `stream` (use a stream of its own, next to the kernels
  * under test) that stays alive for `microseconds` (1 .. 1000000) of the constant 100 MHz counter and then writes

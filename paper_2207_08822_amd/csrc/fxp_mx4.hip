@@ -288,3 +288,136 @@ extern "C" int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, v
     else go(std::integral_constant<int, FXP_F16>{});
     return launch_status();
 }
+
+// ---- products ----
+
+extern "C" size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    for (int64_t n : {M, N, K})
+        if (n < 0 || n > fxp::kMxMost) return 0;
+    return fxp::mx4_gemm_bytes(M, N, K);
+}
+
+extern "C" int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream) {
+    using namespace fxp;
+    for (const fxp_mx4* q : {A, B}) {
+        const int rc = check_mx4(q);
+        if (rc) return rc;
+    }
+    if (!known_type(type)) return FXP_ERR_TYPE;
+    if (A->cols != B->cols || ldc < B->rows || ldc >= int64_t{1} << 40) return FXP_ERR_DIMS;
+    if (A->rows == 0 || B->rows == 0) return FXP_OK;
+    if (!C) return FXP_ERR_NULL;
+    if (!aligned(C, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    const size_t need = mx4_gemm_bytes(A->rows, B->rows, A->cols);
+    if (need && (!ws || ws_bytes < need)) return FXP_ERR_WORKSPACE;
+    if (need && !aligned(ws, 256)) return FXP_ERR_ALIGN;
+    return mx4_gemm_launch(*A, *B, type, C, ldc, ws, static_cast<hipStream_t>(stream));
+}
+
+// the mapped rows of x in a workspace: codes, scales, then the product's own
+namespace fxp {
+static size_t mapped_bytes(int64_t M, int64_t K) {
+    return round_up(static_cast<size_t>(mx_panels(K) * M * kMxRowBytes), 256) + round_up(static_cast<size_t>(mx_panels(K) * M * kMxRowScales), 256);
+}
+}  // namespace fxp
+
+extern "C" size_t fxp_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+    for (int64_t n : {M, N, K})
+        if (n < 0 || n > fxp::kMxMost) return 0;
+    return fxp::mapped_bytes(M, K) + fxp::mx4_gemm_bytes(M, N, K);
+}
+
+extern "C" int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx4* W, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
+    using namespace fxp;
+    int rc = check_mx4(W);
+    if (rc) return rc;
+    const int64_t K = W->cols, N = W->rows;
+    rc = check_map(type, X, ldx, M, K, nullptr, nullptr);
+    if (rc) return rc;
+    if (ldy < N || ldy >= int64_t{1} << 40) return FXP_ERR_DIMS;
+    if (M == 0 || N == 0) return FXP_OK;
+    if (!Y) return FXP_ERR_NULL;
+    if (!aligned(Y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    const size_t codes = round_up(static_cast<size_t>(mx_panels(K) * M * kMxRowBytes), 256), mapped = mapped_bytes(M, K);
+    const size_t need = fxp_mx4_linear_workspace_bytes(M, N, K);               // 0: a contraction of nothing
+    if (need && (!ws || ws_bytes < need)) return FXP_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    uint8_t* const at = static_cast<uint8_t*>(ws);
+    const fxp_mx4 q{at, at + codes, M, K};
+    const Mx4Map m = map_of(X, ldx, M, K, &q, nullptr, 0);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = mx4_map_launch(type, &m, 1, 0, FXP_ROUND_NEAREST, s);
+    return rc ? rc : mx4_gemm_launch(q, *W, type, Y, ldy, at + mapped, s);
+}
+
+// ---- a layer's training step ----
+
+namespace fxp {
+static int check_layer(const fxp_mx4_layer* l, int64_t M, int64_t K, int64_t N, bool backward, bool need_x, bool need_w) {
+    if (!l) return FXP_ERR_NULL;
+    for (int64_t n : {M, K, N})
+        if (n < 0 || n > kMxMost) return FXP_ERR_DIMS;
+    struct Want {
+        const fxp_mx4* q;
+        int64_t rows, cols;
+        bool needed;
+    };
+    const Want forward[] = {{&l->X, M, K, true}, {&l->WT, N, K, true}, {&l->XT, K, M, false}, {&l->W, K, N, false}};
+    const Want back[] = {{&l->dY, M, N, need_x}, {&l->W, K, N, need_x}, {&l->dYT, N, M, need_w}, {&l->XT, K, M, need_w}};
+    for (const Want& w : backward ? back : forward) {
+        if (!w.q->data && !w.needed) continue;
+        if (w.q->rows != w.rows || w.q->cols != w.cols) return FXP_ERR_DIMS;
+        const int rc = check_mx4(w.q);
+        if (rc) return rc;
+    }
+    return FXP_OK;
+}
+static const fxp_mx4* if_there(const fxp_mx4& q) { return q.data ? &q : nullptr; }
+}  // namespace fxp
+
+extern "C" size_t fxp_mx4_layer_workspace_bytes(int64_t M, int64_t K, int64_t N) {
+    for (int64_t n : {M, N, K})
+        if (n < 0 || n > fxp::kMxMost) return 0;
+    return std::max({fxp::mx4_gemm_bytes(M, N, K), fxp::mx4_gemm_bytes(M, K, N), fxp::mx4_gemm_bytes(K, N, M), size_t{256}});
+}
+
+extern "C" int fxp_mx4_linear_fwd(int type, const void* X, const void* W, int64_t M, int64_t K, int64_t N, void* Y, const fxp_mx4_layer* layer, uint64_t seed,
+                                  uint64_t step, int rounding, void* ws, size_t ws_bytes, void* stream) {
+    using namespace fxp;
+    int rc = check_layer(layer, M, K, N, false, true, true);
+    if (rc) return rc;
+    rc = check_map(type, X, K, M, K, nullptr, nullptr);
+    if (!rc) rc = check_map(type, W, N, K, N, nullptr, nullptr);
+    if (rc) return rc;
+    if (!known_rounding(rounding)) return FXP_ERR_ROUNDING;
+    if (M && N && !Y) return FXP_ERR_NULL;
+    if (!aligned(Y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    if (!ws || ws_bytes < fxp_mx4_layer_workspace_bytes(M, K, N)) return FXP_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    const Mx4Map maps[2] = {map_of(X, K, M, K, &layer->X, if_there(layer->XT), step << 8), map_of(W, N, K, N, if_there(layer->W), &layer->WT, (step << 8) | 1)};
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = mx4_map_launch(type, maps, 2, seed, rounding, s);
+    if (rc || M == 0 || N == 0) return rc;
+    return mx4_gemm_launch(layer->X, layer->WT, type, Y, N, ws, s);
+}
+
+extern "C" int fxp_mx4_linear_bwd(int type, const void* dY, const fxp_mx4_layer* layer, int64_t M, int64_t K, int64_t N, void* dX, void* dW, uint64_t seed,
+                                  uint64_t step, int rounding, void* ws, size_t ws_bytes, void* stream) {
+    using namespace fxp;
+    int rc = check_layer(layer, M, K, N, true, dX != nullptr, dW != nullptr);
+    if (rc) return rc;
+    rc = check_map(type, dY, N, M, N, nullptr, nullptr);
+    if (rc) return rc;
+    if (!known_rounding(rounding)) return FXP_ERR_ROUNDING;
+    for (const void* p : {dX, dW})
+        if (!aligned(p, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    if (!ws || ws_bytes < fxp_mx4_layer_workspace_bytes(M, K, N)) return FXP_ERR_WORKSPACE;
+    if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    if (!dX && !dW) return FXP_OK;
+    const Mx4Map m = map_of(dY, N, M, N, dX ? &layer->dY : nullptr, dW ? &layer->dYT : nullptr, (step << 8) | 2);
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    rc = mx4_map_launch(type, &m, 1, seed, rounding, s);
+    if (!rc && dW && K && N) rc = mx4_gemm_launch(layer->XT, layer->dYT, type, dW, N, ws, s);
+    if (!rc && dX && M && K) rc = mx4_gemm_launch(layer->dY, layer->W, type, dX, K, ws, s);
+    return rc;
+}

@@ -1,0 +1,337 @@
+// Products of matrices in microscaled 4-bit floats: C[M,N] = A[M,K] * B[N,K]^T on v_mfma_scale_f32_32x32x64_f8f6f4 (16x16x128 for a few rows).
+//
+// A lane of the instruction holds one block of one row - 32 codes in four registers - and its scale byte, so blocks need no work of their own: a panel of 256 columns is
+// four instructions along the contraction, whose scales are the four bytes of one register.  Sums are fp32.
+#include <algorithm>
+
+#include "fxp_gemm_device.h"
+#include "fxp_mx4_device.h"
+
+namespace fxp {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+constexpr int kFp4 = 4;                 // both operands' format in the instruction
+
+// 4-bit operands are the low half of the operand registers
+__device__ inline v8i wide(v4i x) { return __builtin_shufflevector(x, x, 0, 1, 2, 3, -1, -1, -1, -1); }
+
+template <int BYTE_A, int BYTE_B>
+__device__ inline v16f mfma32(v4i a, v4i b, v16f c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wide(a), wide(b), c, kFp4, kFp4, BYTE_A, sa, BYTE_B, sb);
+}
+template <int BYTE_A, int BYTE_B>
+__device__ inline v4f mfma16(v4i a, v4i b, v4f c, int sa, int sb) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wide(a), wide(b), c, kFp4, kFp4, BYTE_A, sa, BYTE_B, sb);
+}
+
+// BYTES a lane from `at` of the `bytes` at a uniform address to LDS, lane after lane; zeros past the end
+template <int BYTES>
+__device__ inline void load_to_lds(const uint8_t* from, int bytes, int at, uint8_t* to) {
+    static_assert(BYTES == 16 || BYTES == 4, "sizes of the load");
+    const auto lds = (__attribute__((address_space(3))) void*)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(records(from, bytes), lds, 16, at, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(records(from, bytes), lds, 4, at, 0, 0, 0);
+}
+// memory operations are not moved across it by the compiler
+__device__ inline void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+struct Mx4Operand {
+    const uint8_t *data, *scales;
+    int rows;
+};
+struct Mx4Product {
+    Mx4Operand a, b;
+    int M, N, panels, per_split;        // panels of a workgroup's part of the contraction
+    void* c;
+    int64_t ldc, split_stride;          // of partial sums, in elements: 0 where there is one part
+    int tiles_m, tiles_n, group_m;
+};
+
+template <int TYPE>
+__device__ inline void store_one(void* c, int64_t at, float v) {
+    static_cast<typename Elem<TYPE>::T*>(c)[at] = static_cast<typename Elem<TYPE>::T>(v);
+}
+
+// ---- tiles ----
+//
+// BM x BN outputs a workgroup, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's bound).  16-byte pieces of a row
+// of 128 bytes are exchanged by the row, so that a fragment's reads spread over all banks.
+template <int BM, int BN, int WM, int WN, int STAGES, int TYPE>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Product p) {
+    constexpr int NW = (BM / WM) * (BN / WN), FM = WM / 32, FN = WN / 32;
+    constexpr int kCodes = (BM + BN) * kMxRowBytes, kScales = (BM + BN) * kMxRowScales, kStage = kCodes + kScales;
+    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LS = (BM + BN) / 32 / NW, kLoads = LA + LB + LS;       // loads of a wave a panel
+    static_assert(LA * 8 * NW == BM && LB * 8 * NW == BN && LS * 32 * NW == BM + BN, "waves load as much");
+    static_assert(kLoads * (STAGES - 1) < 64, "loads in flight");
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage];
+
+    int tm, tn;
+    tile_of_block(static_cast<int>(blockIdx.x), p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+    const int m0 = tm * BM, n0 = tn * BN;
+    const int first = static_cast<int>(blockIdx.y) * p.per_split, panels = min(p.per_split, p.panels - first);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm0 = (wave / (BN / WN)) * WM, wn0 = (wave % (BN / WN)) * WN;
+
+    int off_a[LA], off_b[LB];
+#pragma unroll
+    for (int j = 0; j < LA; ++j) {
+        const int row = (wave + j * NW) * 8 + lane / 8;
+        off_a[j] = (m0 + row) * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < LB; ++j) {
+        const int row = (wave + j * NW) * 8 + lane / 8;
+        off_b[j] = (n0 + row) * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
+    }
+    auto issue = [&](int t) {
+        const int64_t panel = first + t;
+        const bool there = t < panels;                              // past the last: no memory access, zeros
+        uint8_t* const stage = lds + (t % STAGES) * kStage;
+        const int size_a = there ? p.a.rows * kMxRowBytes : 0, size_b = there ? p.b.rows * kMxRowBytes : 0;
+        const uint8_t* const a = p.a.data + panel * p.a.rows * kMxRowBytes;
+        const uint8_t* const b = p.b.data + panel * p.b.rows * kMxRowBytes;
+#pragma unroll
+        for (int j = 0; j < LA; ++j) load_to_lds<16>(a, size_a, off_a[j], stage + (wave + j * NW) * 1024);
+#pragma unroll
+        for (int j = 0; j < LB; ++j) load_to_lds<16>(b, size_b, off_b[j], stage + BM * kMxRowBytes + (wave + j * NW) * 1024);
+#pragma unroll
+        for (int j = 0; j < LS; ++j) {
+            const int i = wave + j * NW;                            // 256 bytes: 32 rows
+            const bool of_a = i < BM / 32;
+            const Mx4Operand& o = of_a ? p.a : p.b;
+            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, there ? o.rows * kMxRowScales : 0,
+                           (of_a ? m0 + 32 * i : n0 + 32 * (i - BM / 32)) * kMxRowScales + 4 * lane, stage + kCodes + 256 * i);
+        }
+    };
+
+    v16f acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = {};
+    const int frow = lane & 31, fhalf = lane >> 5, fswz = swizzle_of_row<kMxRowBytes>(frow);
+#pragma unroll
+    for (int t = 0; t < STAGES - 1; ++t) issue(t);
+    for (int t = 0; t < panels; ++t) {
+        wait_loads_and_lds<(STAGES - 2) * kLoads>();
+        barrier();
+        issue(t + STAGES - 1);
+        const uint8_t* const stage = lds + (t % STAGES) * kStage;
+        const uint8_t* const sa = stage + (wm0 + frow) * kMxRowBytes;
+        const uint8_t* const sb = stage + (BM + wn0 + frow) * kMxRowBytes;
+        const uint8_t* const se = stage + kCodes + 4 * fhalf;
+        int ea[FM], eb[FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i) ea[i] = *reinterpret_cast<const int*>(se + (wm0 + 32 * i + frow) * kMxRowScales);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) eb[j] = *reinterpret_cast<const int*>(se + (BM + wn0 + 32 * j + frow) * kMxRowScales);
+        auto quarter = [&](auto ks_c) {
+            constexpr int KS = decltype(ks_c)::value;
+            const int piece = ((2 * KS + fhalf) ^ fswz) * 16;
+            v4i fa[FM], fb[FN];
+#pragma unroll
+            for (int i = 0; i < FM; ++i) fa[i] = *reinterpret_cast<const v4i*>(sa + i * 32 * kMxRowBytes + piece);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) fb[j] = *reinterpret_cast<const v4i*>(sb + j * 32 * kMxRowBytes + piece);
+#pragma unroll
+            for (int i = 0; i < FM; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) acc[i][j] = mfma32<KS, KS>(fa[i], fb[j], acc[i][j], ea[i], eb[j]);
+        };
+        quarter(IC<0>{});
+        quarter(IC<1>{});
+        quarter(IC<2>{});
+        quarter(IC<3>{});
+    }
+    wait_loads_and_lds<0>();                                        // none into LDS may outlive the workgroup
+
+    const int64_t base = static_cast<int64_t>(blockIdx.y) * p.split_stride;
+    const int col0 = n0 + wn0 + frow;
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = m0 + wm0 + 32 * i + 8 * (r >> 2) + 4 * fhalf + (r & 3);
+            if (row >= p.M) continue;
+            const int64_t at = base + row * p.ldc + col0;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                if (col0 + 32 * j < p.N) store_one<TYPE>(p.c, at + 32 * j, acc[i][j][r]);
+        }
+}
+
+// partial sums [parts][M * N] added in order
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts, int count, int64_t stride, int M, int N, void* c, int64_t ldc) {
+    const int64_t i = int64_t{blockIdx.x} * 256 + threadIdx.x;
+    if (i >= int64_t{M} * N) return;
+    float s = 0.0f;
+    for (int n = 0; n < count; ++n) s += parts[n * stride + i];
+    store_one<TYPE>(c, i / N * ldc + i % N, s);
+}
+
+// ---- a few rows ----
+//
+// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up in LDS.  B is read once, straight into the instruction's registers.
+template <int MT, int NT, int WAVES, int TYPE>
+__global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
+    __shared__ v4f sums[WAVES > 1 ? WAVES : 1][MT * NT][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = static_cast<int>(blockIdx.x) * NT * 16, r = lane & 15, kb = lane >> 4;
+    v4f acc[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = {};
+    // block 4 h + kb of a panel: 16 bytes at 64 h + 16 kb, its scale in byte kb / 2 + 2 h of word kb % 2
+    const int code_at = r * kMxRowBytes + kb * 16, scale_at = r * kMxRowScales + 4 * (kb & 1), shift = 8 * (kb >> 1);
+    for (int t = wave; t < p.panels; t += WAVES) {
+        const auto rb = records(p.b.data + int64_t{t} * p.b.rows * kMxRowBytes, p.b.rows * kMxRowBytes);
+        const auto re = records(p.b.scales + int64_t{t} * p.b.rows * kMxRowScales, p.b.rows * kMxRowScales);
+        const auto ra = records(p.a.data + int64_t{t} * p.a.rows * kMxRowBytes, p.a.rows * kMxRowBytes);
+        const auto rs = records(p.a.scales + int64_t{t} * p.a.rows * kMxRowScales, p.a.rows * kMxRowScales);
+        v4i b[NT][2], a[MT][2];
+        int eb[NT], ea[MT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int at = (n0 + 16 * n) * kMxRowBytes + code_at;
+            b[n][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at, 0, kNonTemporal));
+            b[n][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at + 64, 0, kNonTemporal));
+            eb[n] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, (n0 + 16 * n) * kMxRowScales + scale_at, 0, 0) >> shift);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const int at = 16 * m * kMxRowBytes + code_at;
+            a[m][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at, 0, 0));
+            a[m][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at + 64, 0, 0));
+            ea[m] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rs, 16 * m * kMxRowScales + scale_at, 0, 0) >> shift);
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                acc[m][n] = mfma16<0, 0>(b[n][0], a[m][0], acc[m][n], eb[n], ea[m]);
+                acc[m][n] = mfma16<2, 2>(b[n][1], a[m][1], acc[m][n], eb[n], ea[m]);
+            }
+    }
+    if constexpr (WAVES > 1) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) sums[wave][m * NT + n][lane] = acc[m][n];
+        __syncthreads();
+    }
+    // outputs 4 kb .. 4 kb + 3 of a tile of B's rows, row r of A's
+    for (int tile = wave; tile < MT * NT; tile += WAVES) {
+        v4f s;
+        if constexpr (WAVES > 1) {
+            s = sums[0][tile][lane];
+            for (int w = 1; w < WAVES; ++w) s += sums[w][tile][lane];
+        } else {
+            s = acc[0][0];
+#pragma unroll
+            for (int i = 1; i < MT * NT; ++i)
+                if (i == tile) s = acc[i / NT][i % NT];
+        }
+        const int row = 16 * (tile / NT) + r, col = n0 + 16 * (tile % NT) + 4 * kb;
+        if (row >= p.M) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (col + j < p.N) store_one<TYPE>(p.c, row * p.ldc + col + j, s[j]);
+    }
+}
+
+constexpr int kRowsMost = 64;
+
+// How a product is cut: tiles, and parts of the contraction where the tiles alone leave CUs idle.
+struct Mx4Plan {
+    bool rows;
+    int tile, splits, per_split;
+};
+static Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K) {
+    const int64_t panels = mx_panels(K);
+    Mx4Plan p{M <= kRowsMost, 128, 1, static_cast<int>(panels)};
+    if (p.rows) return p;
+    auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+    if (tiles(128) < 256) p.tile = 64;
+    const int64_t count = tiles(p.tile);
+    if (count < 256 && panels >= 8) {
+        const int64_t want = std::min<int64_t>(panels / 4, (512 + count - 1) / count);
+        p.per_split = static_cast<int>((panels + want - 1) / want);
+        p.splits = static_cast<int>((panels + p.per_split - 1) / p.per_split);
+    }
+    return p;
+}
+
+size_t mx4_gemm_bytes(int64_t M, int64_t N, int64_t K) {
+    const Mx4Plan p = mx4_plan(M, N, K);
+    return p.splits > 1 ? round_up(static_cast<size_t>(p.splits) * M * N * sizeof(float), 256) : 0;
+}
+
+int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s) {
+    const int64_t M = A.rows, N = B.rows, K = A.cols;
+    const Mx4Plan plan = mx4_plan(M, N, K);
+    Mx4Product p{};
+    p.a = {A.data, A.scales, static_cast<int>(M)};
+    p.b = {B.data, B.scales, static_cast<int>(N)};
+    p.M = static_cast<int>(M);
+    p.N = static_cast<int>(N);
+    p.panels = static_cast<int>(mx_panels(K));
+    p.per_split = plan.per_split;
+    p.c = C;
+    p.ldc = ldc;
+    auto typed = [&](int t, auto go) {
+        if (t == FXP_F32) go(IC<FXP_F32>{});
+        else if (t == FXP_BF16) go(IC<FXP_BF16>{});
+        else go(IC<FXP_F16>{});
+    };
+    if (plan.rows) {
+        typed(type, [&](auto type_c) {
+            constexpr int TYPE = decltype(type_c)::value;
+            auto go = [&](auto mt_c, auto nt_c, auto w_c) {
+                constexpr int NT = decltype(nt_c)::value, W = decltype(w_c)::value;
+                hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, NT, W, TYPE>), dim3(static_cast<unsigned>((N + 16 * NT - 1) / (16 * NT))), dim3(64 * W), 0, s, p);
+            };
+            auto waves = [&](auto mt_c, auto nt_c) {
+                if (p.panels >= 8) go(mt_c, nt_c, IC<8>{});
+                else if (p.panels >= 3) go(mt_c, nt_c, IC<4>{});
+                else go(mt_c, nt_c, IC<1>{});
+            };
+            if (M <= 16) waves(IC<1>{}, IC<1>{});
+            else if (M <= 32) waves(IC<2>{}, IC<1>{});
+            else waves(IC<4>{}, IC<1>{});
+        });
+        return launch_status();
+    }
+    const bool parts = plan.splits > 1;
+    if (parts) {
+        p.c = ws;
+        p.ldc = N;
+        p.split_stride = M * N;
+    }
+    const int t = plan.tile;
+    p.tiles_m = static_cast<int>((M + t - 1) / t);
+    p.tiles_n = static_cast<int>((N + t - 1) / t);
+    p.group_m = 8;
+    const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
+    typed(parts ? FXP_F32 : type, [&](auto type_c) {
+        constexpr int TYPE = decltype(type_c)::value;
+        if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
+        else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
+    });
+    if (parts)
+        typed(type, [&](auto type_c) {
+            hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(static_cast<unsigned>((M * N + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(ws), plan.splits,
+                               p.split_stride, p.M, p.N, C, ldc);
+        });
+    return launch_status();
+}
+
+}  // namespace fxp

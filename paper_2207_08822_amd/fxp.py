@@ -67,6 +67,10 @@ class _Mx4(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64)]
 
 
+class _Mx4Layer(ctypes.Structure):
+    _fields_ = [(n, _Mx4) for n in ("X", "XT", "W", "WT", "dY", "dYT")]
+
+
 _lib = None
 
 
@@ -172,6 +176,15 @@ def lib():
     L.fxp_mx4_map.restype = ci
     L.fxp_mx4_unmap.argtypes = [mx, ci, vp, i64, vp]
     L.fxp_mx4_unmap.restype = ci
+    L.fxp_mx4_gemm.argtypes = [mx, mx, ci, vp, i64, vp, sz, vp]
+    L.fxp_mx4_linear.argtypes = [ci, vp, i64, i64, mx, vp, i64, vp, sz, vp]
+    L.fxp_mx4_linear_fwd.argtypes = [ci, vp, vp, i64, i64, i64, vp, c.POINTER(_Mx4Layer), u64, u64, ci, vp, sz, vp]
+    L.fxp_mx4_linear_bwd.argtypes = [ci, vp, c.POINTER(_Mx4Layer), i64, i64, i64, vp, vp, u64, u64, ci, vp, sz, vp]
+    for name in ("fxp_mx4_gemm", "fxp_mx4_linear", "fxp_mx4_linear_fwd", "fxp_mx4_linear_bwd"):
+        getattr(L, name).restype = ci
+    for name in ("fxp_mx4_gemm_workspace_bytes", "fxp_mx4_linear_workspace_bytes", "fxp_mx4_layer_workspace_bytes"):
+        getattr(L, name).argtypes = [i64, i64, i64]
+        getattr(L, name).restype = sz
     for name in ("fxp_kv_tables", "fxp_kv_append", "fxp_kv_load", "fxp_kv_attention", "fxp_w4_pack", "fxp_w4_linear"):
         getattr(L, name).restype = ci
     for name in ("fxp_scale", "fxp_map", "fxp_scale_map", "fxp_gemm", "fxp_unmap", "fxp_unmap_i8", "fxp_gemm_unmap",
@@ -1089,3 +1102,94 @@ def mx4_unmap(q, dtype=torch.float32, out=None):
         raise FxpError("out must be [rows, cols] of q")
     _check(lib().fxp_mx4_unmap(q.ref, code, out.data_ptr(), _row_stride(out, "out"), _stream()), "fxp_mx4_unmap")
     return out
+
+
+def mx4_gemm(A, B, dtype=torch.float32, out=None, ws=None):
+    """C [A.rows, B.rows] = A B^T of two mapped matrices, in `dtype` or out's type."""
+    _here(A, "A")
+    _here(B, "B")
+    if A.cols != B.cols:
+        raise FxpError("contraction lengths differ")
+    if out is None:
+        if dtype not in _TYPES:
+            raise FxpError("dtype must be float32, bfloat16 or float16")
+        out = A.data.new_empty((A.rows, B.rows), dtype=dtype)
+    code = _served(out, "out", 2)
+    if out.shape != (A.rows, B.rows):
+        raise FxpError("out must be [A.rows, B.rows]")
+    if ws is not None:
+        _index(ws, "ws", dtype=torch.uint8)
+    else:
+        nbytes = int(lib().fxp_mx4_gemm_workspace_bytes(A.rows, B.rows, A.cols))
+        ws = A.data.new_empty(nbytes) if nbytes else None
+    _check(lib().fxp_mx4_gemm(A.ref, B.ref, code, out.data_ptr(), _row_stride(out, "out"), _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_mx4_gemm")
+    return out
+
+
+def mx4_linear(x, w, out=None, ws=None):
+    """y [M, N] = x [M, K] W of x's type; w: W transposed and mapped, [N, K] (mx4_map(W, want_q=False, want_qT=True)[1] of W [K, N]).  x is mapped to nearest on the way.  Any M,
+    one token to many.  out: may not share elements with x."""
+    code = _served(x, "x", 2)
+    M, K = x.shape
+    if K != w.cols:
+        raise FxpError("x must be [M, K] of the weights")
+    _here(w, "w")
+    ldy = w.rows
+    if out is None:
+        out = x.new_empty((M, ldy))
+    elif _served(out, "out", 2) != code or out.shape != (M, ldy):
+        raise FxpError("out must be [M, N] of x's type")
+    else:
+        ldy = _row_stride(out, "out")
+        if _share(x, out):
+            raise FxpError("out shares elements with x")
+    if ws is not None:
+        _index(ws, "ws", dtype=torch.uint8)
+    else:
+        ws = x.new_empty(int(lib().fxp_mx4_linear_workspace_bytes(M, w.rows, K)), dtype=torch.uint8)
+    _check(lib().fxp_mx4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, w.ref, out.data_ptr(), ldy, ws.data_ptr(), ws.numel(), _stream()), "fxp_mx4_linear")
+    return out
+
+
+class Mx4LayerBuffers:
+    """Caller-owned device buffers of one layer in 4-bit floats, allocated once and reused."""
+
+    def __init__(self, M, K, N, dtype=torch.float32, device="cuda"):
+        if dtype not in _TYPES:
+            raise FxpError("dtype must be float32, bfloat16 or float16")
+        self.M, self.K, self.N, self.dtype = M, K, N, dtype
+        shapes = dict(X=(M, K), XT=(K, M), W=(K, N), WT=(N, K), dY=(M, N), dYT=(N, M))
+        for name, shape in shapes.items():
+            setattr(self, name, Mx4(*shape, device=device))
+        like = dict(dtype=dtype, device=device)
+        self.y, self.dx, self.dw = torch.empty((M, N), **like), torch.empty((M, K), **like), torch.empty((K, N), **like)
+        self.ws = torch.empty(int(lib().fxp_mx4_layer_workspace_bytes(M, K, N)), dtype=torch.uint8, device=device)
+        self.index = self.ws.get_device()
+        self.c = _Mx4Layer(*[getattr(self, name).c for name in shapes])
+        self.ref = ctypes.byref(self.c)
+
+
+def _layer_operand(t, shape, buf, what):
+    _on_current(t, what)
+    if t.dtype != buf.dtype or t.shape != shape or not t.is_contiguous():
+        raise FxpError(f"{what} must be a contiguous {buf.dtype} tensor of the layer's shape")
+
+
+def mx4_linear_fwd(X, W, buf, seed=0, step=0, rounding=STOCHASTIC):
+    """Y = X W in 4-bit floats, X [M, K], W [K, N] of the buffers' type; fills buf.X, XT, W, WT and returns buf.y."""
+    _here(buf, "buf")
+    _layer_operand(X, (buf.M, buf.K), buf, "X")
+    _layer_operand(W, (buf.K, buf.N), buf, "W")
+    _check(lib().fxp_mx4_linear_fwd(_TYPES[buf.dtype], X.data_ptr(), W.data_ptr(), buf.M, buf.K, buf.N, buf.y.data_ptr(), buf.ref, seed, step, rounding,
+                                    buf.ws.data_ptr(), buf.ws.numel(), _stream()), "fxp_mx4_linear_fwd")
+    return buf.y
+
+
+def mx4_linear_bwd(dY, buf, seed=0, step=0, rounding=STOCHASTIC, need_dX=True, need_dW=True):
+    """(dX, dW) from the upstream gradient and the operands the forward call left in buf."""
+    _here(buf, "buf")
+    _layer_operand(dY, (buf.M, buf.N), buf, "dY")
+    dX, dW = buf.dx if need_dX else None, buf.dw if need_dW else None
+    _check(lib().fxp_mx4_linear_bwd(_TYPES[buf.dtype], dY.data_ptr(), buf.ref, buf.M, buf.K, buf.N, _p(dX), _p(dW), seed, step, rounding, buf.ws.data_ptr(),
+                                    buf.ws.numel(), _stream()), "fxp_mx4_linear_bwd")
+    return dX, dW

@@ -200,3 +200,45 @@ def test_mx4_map_and_unmap(L):
     assert L.fxp_mx4_unmap(None, 0, BIG, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 3, BIG, 70, None) == -9 and L.fxp_mx4_unmap(mx4(), 0, BIG, 69, None) == -2
     assert L.fxp_mx4_unmap(mx4(), 0, None, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 0, BIG + 2, 70, None) == -3
     assert f(x=None, rows=0, q=mx4(rows=0), t=mx4(rows=70, cols=0)) == 0 and L.fxp_mx4_unmap(mx4(rows=0, data=None), 0, None, 70, None) == 0
+
+
+def test_mx4_products(L):
+    def f(A=mx4(rows=4), B=mx4(rows=9), type=0, C=BIG, ldc=9, ws=None, n=0):
+        return L.fxp_mx4_gemm(A, B, type, C, ldc, ws, n, None)
+
+    assert f(A=None) == -1 and f(B=None) == -1 and f(A=mx4(data=None)) == -1 and f(type=3) == -9 and f(ldc=8) == -2 and f(A=mx4(cols=71)) == -2
+    assert f(C=None) == -1 and f(C=BIG + 2) == -3 and f(A=mx4(rows=0), C=None) == 0 and f(B=mx4(rows=0), C=None) == 0
+    need = L.fxp_mx4_gemm_workspace_bytes(100, 100, 10000)
+    big = dict(A=mx4(rows=100, cols=10000), B=mx4(rows=100, cols=10000), ldc=100)
+    assert need > 0 and f(**big) == -4 and f(**big, ws=BIG, n=need - 1) == -4 and f(**big, ws=BIG + 8, n=need) == -3
+    assert L.fxp_mx4_gemm_workspace_bytes(-1, 4, 4) == 0 and L.fxp_mx4_linear_workspace_bytes(4, 4, 1 << 24) == 0 and L.fxp_mx4_layer_workspace_bytes(1, -1, 1) == 0
+
+    def g(type=0, X=BIG, ldx=70, M=4, W=mx4(rows=9), Y=BIG, ldy=9, ws=BIG, n=1 << 20):
+        return L.fxp_mx4_linear(type, X, ldx, M, W, Y, ldy, ws, n, None)
+
+    assert g(W=None) == -1 and g(type=3) == -9 and g(X=None) == -1 and g(Y=None) == -1 and g(ldx=69) == -2 and g(ldy=8) == -2 and g(M=-1) == -2
+    assert g(X=BIG + 2) == -3 and g(Y=BIG + 1) == -3 and g(ws=None) == -4 and g(n=100) == -4 and g(ws=BIG + 128) == -3 and g(M=0, X=None, Y=None, ws=None) == 0
+
+
+def test_mx4_layers(L):
+    M, K, N = 4, 70, 9
+    shapes = dict(X=(M, K), XT=(K, M), W=(K, N), WT=(N, K), dY=(M, N), dYT=(N, M))
+
+    def layer(**over):
+        make = lambda n, s: fxp._Mx4(*(over.get(n) or (BIG, BIG, *s)))  # noqa: E731
+        return c.byref(fxp._Mx4Layer(*[make(n, s) for n, s in shapes.items()]))
+
+    def fwd(type=0, X=BIG, W=BIG, M=M, K=K, N=N, Y=BIG, l=layer(), rounding=0, ws=BIG, n=1 << 20):
+        return L.fxp_mx4_linear_fwd(type, X, W, M, K, N, Y, l, 0, 0, rounding, ws, n, None)
+
+    def bwd(type=0, dY=BIG, l=layer(), M=M, K=K, N=N, dX=BIG, dW=BIG, rounding=0, ws=BIG, n=1 << 20):
+        return L.fxp_mx4_linear_bwd(type, dY, l, M, K, N, dX, dW, 0, 0, rounding, ws, n, None)
+
+    for f, first in ((fwd, "X"), (bwd, "dY")):
+        assert f(l=None) == -1 and f(type=3) == -9 and f(rounding=2) == -5 and f(ws=None) == -4 and f(n=255) == -4 and f(ws=BIG + 16) == -3 and f(M=-1) == -2 and f(N=1 << 24) == -2
+        assert f(M=M + 1) == -2 and f(**{first: None}) == -1 and f(**{first: BIG + 2}) == -3
+    assert fwd(W=None) == -1 and fwd(Y=None) == -1 and fwd(Y=BIG + 2) == -3 and bwd(dX=BIG + 2) == -3 and bwd(dW=BIG + 1) == -3 and bwd(dX=None, dW=None) == 0
+    for name in ("X", "WT"):
+        assert fwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and fwd(l=layer(**{name: (BIG + 8, BIG, *shapes[name])})) == -3
+    for name in ("dY", "W", "dYT", "XT"):
+        assert bwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and bwd(l=layer(**{name: (BIG, BIG + 4, *shapes[name])})) == -3
