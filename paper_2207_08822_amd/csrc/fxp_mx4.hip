@@ -14,119 +14,136 @@ struct Mx4Job {
     Mx4Map m;
     int tiles_c;            // tiles of a row of tiles
     unsigned first;         // workgroup of the job's first tile
-    int vec;                // rows are multiples of four elements and so is the base
+    int vec;                // rows and the base are multiples of 16 bytes
 };
 struct Mx4Jobs {
     Mx4Job job[2];
     int count;
 };
 
-// largest of eight neighbouring lanes, in all of them
-__device__ inline uint32_t max_of_8(uint32_t m) {
-    auto step = [&](auto ctrl) { m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), decltype(ctrl)::value, 0xf, 0xf, false))); };
-    step(std::integral_constant<int, 0xb1>{});      // neighbours
-    step(std::integral_constant<int, 0x4e>{});      // pairs
-    step(std::integral_constant<int, 0x141>{});     // the eight mirrored
-    return m;
+// largest of eight neighbouring lanes, or of four, in all of them
+template <int CTRL>
+__device__ inline uint32_t max_dpp(uint32_t m) {
+    return max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), CTRL, 0xf, 0xf, false)));
 }
+__device__ inline uint32_t max_of_4(uint32_t m) { return max_dpp<0x4e>(max_dpp<0xb1>(m)); }       // neighbours, then pairs
 // largest of the lanes eight apart
 __device__ inline uint32_t max_over_8(uint32_t m) {
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
-    m = max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), 0x128, 0xf, 0xf, false)));      // row_ror:8
+    m = max_dpp<0x128>(m);                                                                         // row_ror:8
     v2u p = __builtin_amdgcn_permlane16_swap(m, m, false, false);
     m = max(p[0], p[1]);
     p = __builtin_amdgcn_permlane32_swap(m, m, false, false);
     return max(p[0], p[1]);
 }
+__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-// A workgroup maps BR x BC blocks of 32 x 32; a lane has 4 x 4 elements of each of its wave's blocks: four quads of consecutive elements, one Philox block each.
-// Codes are put together in LDS and leave in 16-byte pieces.
-// Bound by memory for nearest, by the vector ALU for stochastic rounding (10 rounds of Philox a quad and 14 operations an element and copy).
-template <int TYPE, bool STOCH, int BR, int BC>
-__global__ __launch_bounds__(kMxThreads) void k_mx4_map(Mx4Jobs jobs, uint32_t key0, uint32_t key1) {
-    constexpr int TR = 32 * BR, TC = 32 * BC, kPad = 16, SQ = TC / 2 + kPad, ST = TR / 2 + kPad;
-    static_assert(BR * BC % 4 == 0 && kMxPanel % TR == 0 && kMxPanel % TC == 0, "tiles lie in one panel, waves have as many blocks");
+// What stochastic rounding adds to eight elements from element `at` of the matrix on: 2^22 - 1 less the top 22 bits of their words.
+__device__ inline void adds_of_8(uint64_t at, bool whole_quads, uint32_t sid0, uint32_t sid1, uint32_t key0, uint32_t key1, uint32_t (&add)[8]) {
+    const uint64_t quad = at >> 2;
+    auto words = [&](uint64_t q) { return philox4x32_10(static_cast<uint32_t>(q), static_cast<uint32_t>(q >> 32), sid0, sid1, key0, key1); };
+    const uint4 a = words(quad), b = words(quad + 1);
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    if (!whole_quads) {                                    // they lie in three quads
+        const uint4 c = words(quad + 2);
+        const uint32_t all[11] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w, c.x, c.y, c.z};
+        const int shift = static_cast<int>(at & 3);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = shift == 0 ? all[j] : shift == 1 ? all[j + 1] : shift == 2 ? all[j + 2] : all[j + 3];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) add[j] = ~w[j] >> 10;
+}
+
+// Codes of N elements under the factor f; sign[j]: 8 for a negative element.
+template <bool STOCH, int N>
+__device__ inline uint32_t codes_of(const float (&x)[N], float f, const uint32_t (&add)[N], const uint32_t (&sign)[N]) {
+    if constexpr (STOCH) {
+        uint32_t r = 0;
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) r = r << 4 | mx_stochastic(fabsf(x[j]) * f, add[j]) | sign[j];
+        return r;
+    } else {
+        float y[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) y[j] = x[j] * f;
+        return mx_nearest(y);
+    }
+}
+
+// A wave's step is 32 rows x 64 columns, whole blocks of both copies; a lane has 4 x 8 elements of it.  A workgroup maps STEPS_R x STEPS_C steps; codes are put
+// together in LDS and leave in 16-byte pieces.
+// Bound by memory for nearest, by the vector ALU for stochastic rounding (14 operations an element for Philox, 10 for each copy).
+template <int TYPE, bool STOCH, int STEPS_R, int STEPS_C>
+__global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4)) void k_mx4_map(Mx4Jobs jobs, uint32_t key0, uint32_t key1) {
+    constexpr int BR = STEPS_R, BC = 2 * STEPS_C, TR = 32 * BR, TC = 32 * BC, kPad = 16, SQ = TC / 2 + kPad, ST = TR / 2 + kPad;
+    constexpr int kWaves = STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4, kMine = STEPS_R * STEPS_C / kWaves, kAll = 64 * kWaves;
+    static_assert(kMine * kWaves == STEPS_R * STEPS_C && kMxPanel % TR == 0 && kMxPanel % TC == 0, "tiles lie in one panel, waves have as many steps");
     __shared__ __attribute__((aligned(16))) uint8_t lq[TR * SQ], lt[TC * ST];
     __shared__ uint8_t eq[TR * BC], et[TC * BR];
     const Mx4Job& J = jobs.job[jobs.count > 1 && blockIdx.x >= jobs.job[1].first ? 1 : 0];
     const int tile = static_cast<int>(blockIdx.x - J.first);
-    const int64_t r0 = int64_t{tile / J.tiles_c} * TR, c0 = int64_t{tile % J.tiles_c} * TC;
-    const int64_t rows = J.m.rows, cols = J.m.cols;
+    const int r0 = tile / J.tiles_c * TR, c0 = tile % J.tiles_c * TC;
+    const int rows = static_cast<int>(J.m.rows), cols = static_cast<int>(J.m.cols);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rb = lane >> 3, cb = lane & 7;
-    const bool want_q = J.m.q != nullptr, want_t = J.m.t != nullptr, vec = J.vec;
+    const bool want_q = J.m.q != nullptr, want_t = J.m.t != nullptr, inside = J.vec && r0 + TR <= rows && c0 + TC <= cols;
     const uint32_t sid0 = static_cast<uint32_t>(J.m.stream_id), sid1 = static_cast<uint32_t>(J.m.stream_id >> 32);
-    constexpr int kMine = BR * BC / 4;
+    using T = typename Elem<TYPE>::T;
+    const T* const corner = static_cast<const T*>(J.m.x) + r0 * J.m.ld + c0;
 
-    auto load = [&](int n, float (&x)[4][4]) {
-        const int block = wave + 4 * n;
-        const int64_t r = r0 + (block / BC) * 32 + 4 * rb, c = c0 + (block % BC) * 32 + 4 * cb;
+    auto load = [&](int n, float (&x)[4][8]) {
+        const int step = wave + kWaves * n, r = step / STEPS_C * 32 + 4 * rb, c = step % STEPS_C * 64 + 8 * cb;
+        const T* const p = corner + r * J.m.ld + c;
+        if (inside) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t at = (r + i) * J.m.ld + c;
-            if (r + i < rows && c + 3 < cols) {
-                load_elems<TYPE, 4>(J.m.x, at, vec, x[i]);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    x[i][j] = r + i < rows && c + j < cols ? static_cast<float>(static_cast<const typename Elem<TYPE>::T*>(J.m.x)[at + j]) : 0.0f;
-            }
-        }
-    };
-    float x[4][4];
-    load(0, x);
-#pragma unroll
-    for (int n = 0; n < kMine; ++n) {
-        float next[4][4];
-        if (n + 1 < kMine) load(n + 1, next);
-        const int block = wave + 4 * n, br = block / BC, bc = block % BC;
-        uint32_t word[4][4];
-        if constexpr (STOCH) {
+            for (int i = 0; i < 4; ++i) load_elems<TYPE, 8>(p, i * J.m.ld, true, x[i]);
+        } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint64_t at = static_cast<uint64_t>(r0 + br * 32 + 4 * rb + i) * static_cast<uint64_t>(cols) + static_cast<uint64_t>(c0 + bc * 32 + 4 * cb);
-                const uint64_t quad = at >> 2;
-                const uint4 w = philox4x32_10(static_cast<uint32_t>(quad), static_cast<uint32_t>(quad >> 32), sid0, sid1, key0, key1);
-                word[i][0] = w.x; word[i][1] = w.y; word[i][2] = w.z; word[i][3] = w.w;
-                if (cols & 3) {                             // the lane's four elements lie in two quads
-                    const uint4 v = philox4x32_10(static_cast<uint32_t>(quad + 1), static_cast<uint32_t>((quad + 1) >> 32), sid0, sid1, key0, key1);
-                    const uint32_t all[7] = {w.x, w.y, w.z, w.w, v.x, v.y, v.z};
-                    const int shift = static_cast<int>(at & 3);
+                if (J.vec && r0 + r + i < rows && c0 + c + 8 <= cols) {
+                    load_elems<TYPE, 8>(p, i * J.m.ld, true, x[i]);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t u = all[j];
-#pragma unroll
-                        for (int k = 1; k < 4; ++k) u = shift == k ? all[j + k] : u;
-                        word[i][j] = u;
-                    }
+                    for (int j = 0; j < 8; ++j) x[i][j] = r0 + r + i < rows && c0 + c + j < cols ? static_cast<float>(p[i * J.m.ld + j]) : 0.0f;
                 }
             }
         }
-        auto four = [&](float a, float b, float c, float d, uint32_t wa, uint32_t wb, uint32_t wc, uint32_t wd) {
-            if constexpr (STOCH)
-                return mx_stochastic(a, wa) | mx_stochastic(b, wb) << 4 | mx_stochastic(c, wc) << 8 | mx_stochastic(d, wd) << 12;
-            else
-                return mx_nearest4(a, b, c, d);
-        };
-        auto bits = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
+    };
+    float x[4][8];
+    load(0, x);
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+        float next[4][8];
+        if (n + 1 < kMine) load(n + 1, next);
+        const int step = wave + kWaves * n, br = step / STEPS_C, sc = step % STEPS_C;
+        uint32_t add[4][8], sign[4][8];
+        if constexpr (STOCH) {
+            const uint64_t at = static_cast<uint64_t>(r0 + br * 32 + 4 * rb) * static_cast<uint32_t>(cols) + static_cast<uint32_t>(c0 + sc * 64 + 8 * cb);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                adds_of_8(at + static_cast<uint64_t>(i) * static_cast<uint32_t>(cols), (cols & 3) == 0, sid0, sid1, key0, key1, add[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sign[i][j] = __float_as_uint(x[i][j]) >> 28 & 8u;
+            }
+        }
         if (want_q) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int s = mx_scale_of(max_of_8(max(max(bits(x[i][0]), bits(x[i][1])), max(bits(x[i][2]), bits(x[i][3])))));
-                const float f = mx_inverse(s);
-                const int row = br * 32 + 4 * rb + i;
-                const uint32_t o = four(x[i][0] * f, x[i][1] * f, x[i][2] * f, x[i][3] * f, word[i][0], word[i][1], word[i][2], word[i][3]);
-                *reinterpret_cast<uint16_t*>(&lq[row * SQ + bc * 16 + 2 * cb]) = static_cast<uint16_t>(o);
-                if (cb == 0) eq[row * BC + bc] = static_cast<uint8_t>(s);
+                uint32_t m = 0;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) m = max(m, magnitude(x[i][j]));
+                const int s = mx_scale_of(max_of_4(m)), row = br * 32 + 4 * rb + i;
+                *reinterpret_cast<uint32_t*>(&lq[row * SQ + sc * 32 + 4 * cb]) = codes_of<STOCH>(x[i], mx_inverse(s), add[i], sign[i]);
+                if ((cb & 3) == 0) eq[row * BC + 2 * sc + (cb >> 2)] = static_cast<uint8_t>(s);
             }
         }
         if (want_t) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int s = mx_scale_of(max_over_8(max(max(bits(x[0][j]), bits(x[1][j])), max(bits(x[2][j]), bits(x[3][j])))));
-                const float f = mx_inverse(s);
-                const int col = bc * 32 + 4 * cb + j;
-                const uint32_t o = four(x[0][j] * f, x[1][j] * f, x[2][j] * f, x[3][j] * f, word[0][j], word[1][j], word[2][j], word[3][j]);
-                *reinterpret_cast<uint16_t*>(&lt[col * ST + br * 16 + 2 * rb]) = static_cast<uint16_t>(o);
+            for (int j = 0; j < 8; ++j) {
+                const float y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
+                const uint32_t a[4] = {add[0][j], add[1][j], add[2][j], add[3][j]}, g[4] = {sign[0][j], sign[1][j], sign[2][j], sign[3][j]};
+                const int s = mx_scale_of(max_over_8(max(max(magnitude(y[0]), magnitude(y[1])), max(magnitude(y[2]), magnitude(y[3]))))), col = sc * 64 + 8 * cb + j;
+                *reinterpret_cast<uint16_t*>(&lt[col * ST + br * 16 + 2 * rb]) = static_cast<uint16_t>(codes_of<STOCH>(y, mx_inverse(s), a, g));
                 if (rb == 0) et[col * BR + br] = static_cast<uint8_t>(s);
             }
         }
@@ -134,28 +151,66 @@ __global__ __launch_bounds__(kMxThreads) void k_mx4_map(Mx4Jobs jobs, uint32_t k
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[i][j] = next[i][j];
+                for (int j = 0; j < 8; ++j) x[i][j] = next[i][j];
         }
     }
     __syncthreads();
-    // `height` lines of `width` blocks: line l of the copy is row l0 + l of `lines`, its blocks begin at b0 of the contraction
-    auto leave = [&](const uint8_t* codes, const uint8_t* scales, int stride, int height, int width, int64_t l0, int64_t lines, int64_t b0, uint8_t* data,
-                     uint8_t* out_scales) {
-        const int64_t panel = b0 / kMxPanel * lines + l0;
-        const int at = static_cast<int>(b0 % kMxPanel) / kMxBlock, here = static_cast<int>(min(int64_t{height}, lines - l0));
-        for (int i = threadIdx.x; i < here * width; i += kMxThreads) {
-            const int l = i / width, p = i % width;
-            *reinterpret_cast<uint4*>(data + (panel + l) * kMxRowBytes + (at + p) * 16) = *reinterpret_cast<const uint4*>(&codes[l * stride + p * 16]);
-            out_scales[(panel + l) * kMxRowScales + mx_scale_place(at + p)] = scales[i];
+    // `height` lines of `width` blocks: line l of the copy is row l0 + l of `lines`, its blocks begin at element b0 of the contraction
+    auto leave = [&](const uint8_t* codes, const uint8_t* scales, int stride, auto height_c, auto width_c, int l0, int lines, int b0, uint8_t* data, uint8_t* out_scales) {
+        constexpr int height = decltype(height_c)::value, width = decltype(width_c)::value;
+        const int64_t line = static_cast<int64_t>(b0 / kMxPanel) * lines + l0;
+        data += line * kMxRowBytes;
+        out_scales += line * kMxRowScales;
+        const int at = b0 % kMxPanel / kMxBlock, here = min(height, lines - l0) * width;
+#pragma unroll
+        for (int i0 = 0; i0 < height * width; i0 += kAll) {
+            const int i = i0 + static_cast<int>(threadIdx.x), l = i / width, p = i % width;
+            if (i >= here) break;
+            *reinterpret_cast<uint4*>(data + l * kMxRowBytes + (at + p) * 16) = *reinterpret_cast<const uint4*>(&codes[l * stride + p * 16]);
+            out_scales[l * kMxRowScales + mx_scale_place(at + p)] = scales[i];
         }
     };
-    if (want_q) leave(lq, eq, SQ, TR, BC, r0, rows, c0, J.m.q, J.m.q_scales);
-    if (want_t) leave(lt, et, ST, TC, BR, c0, cols, r0, J.m.t, J.m.t_scales);
+    using std::integral_constant;
+    if (want_q) leave(lq, eq, SQ, integral_constant<int, TR>{}, integral_constant<int, BC>{}, r0, rows, c0, J.m.q, J.m.q_scales);
+    if (want_t) leave(lt, et, ST, integral_constant<int, TC>{}, integral_constant<int, BR>{}, c0, cols, r0, J.m.t, J.m.t_scales);
+}
+
+// Rows alone: a lane has eight elements of a row, a block is four lanes, a panel of a row half a wave; nothing goes through LDS.
+template <int TYPE, bool STOCH>
+__global__ __launch_bounds__(kMxThreads) void k_mx4_map_rows(Mx4Map m, int panels, int vec, uint32_t key0, uint32_t key1) {
+    const int64_t piece = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) >> 5;        // a panel of a row, panel after panel of a row
+    const int64_t row = piece / panels;
+    if (row >= m.rows) return;                                                          // whole blocks leave together
+    const int panel = static_cast<int>(piece - row * panels), lane = threadIdx.x & 31, c = panel * kMxPanel + 8 * lane, cols = static_cast<int>(m.cols);
+    using T = typename Elem<TYPE>::T;
+    const T* const p = static_cast<const T*>(m.x) + row * m.ld + c;
+    float x[8];
+    if (vec && c + 8 <= cols) {
+        load_elems<TYPE, 8>(p, 0, true, x);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = c + j < cols ? static_cast<float>(p[j]) : 0.0f;
+    }
+    uint32_t add[8], sign[8], top = 0;
+    if constexpr (STOCH) {
+        adds_of_8(static_cast<uint64_t>(row) * static_cast<uint32_t>(cols) + static_cast<uint32_t>(c), (cols & 3) == 0, static_cast<uint32_t>(m.stream_id),
+                  static_cast<uint32_t>(m.stream_id >> 32), key0, key1, add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sign[j] = __float_as_uint(x[j]) >> 28 & 8u;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = max(top, magnitude(x[j]));
+    const int s = mx_scale_of(max_of_4(top));
+    const int64_t line = panel * m.rows + row;
+    *reinterpret_cast<uint32_t*>(m.q + line * kMxRowBytes + 4 * lane) = codes_of<STOCH>(x, mx_inverse(s), add, sign);
+    if ((lane & 3) == 0) m.q_scales[line * kMxRowScales + mx_scale_place(lane >> 2)] = static_cast<uint8_t>(s);
 }
 
 int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int rounding, hipStream_t s) {
-    auto launch = [&](auto type_c, auto stoch_c, auto br_c, auto bc_c) {
-        constexpr int BR = decltype(br_c)::value, BC = decltype(bc_c)::value;
+    const uint32_t key0 = static_cast<uint32_t>(seed), key1 = static_cast<uint32_t>(seed >> 32);
+    auto vec_of = [&](const Mx4Map& m) { return aligned(m.x, 16) && m.ld * elem_size(type) % 16 == 0; };
+    auto launch = [&](auto type_c, auto stoch_c, auto r_c, auto c_c) {
+        constexpr int SR = decltype(r_c)::value, SC = decltype(c_c)::value, TR = 32 * SR, TC = 64 * SC;
         Mx4Jobs jobs{};
         int64_t tiles = 0;
         for (int i = 0; i < count; ++i) {
@@ -165,23 +220,31 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
             j.m = m;
             // a copy is written up to the end of its last panel
             const int64_t R = m.t ? mx_panels(m.rows) * kMxPanel : m.rows, C = m.q ? mx_panels(m.cols) * kMxPanel : m.cols;
-            j.tiles_c = static_cast<int>((C + 32 * BC - 1) / (32 * BC));
+            j.tiles_c = static_cast<int>((C + TC - 1) / TC);
             j.first = static_cast<unsigned>(tiles);
-            j.vec = aligned(m.x, 4 * static_cast<size_t>(elem_size(type))) && m.ld % 4 == 0;
-            tiles += j.tiles_c * ((R + 32 * BR - 1) / (32 * BR));
+            j.vec = vec_of(m);
+            tiles += j.tiles_c * ((R + TR - 1) / TR);
         }
         if (tiles >= int64_t{1} << 31) return static_cast<int>(FXP_ERR_DIMS);
         if (tiles == 0) return static_cast<int>(FXP_OK);
-        hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value, BR, BC>), dim3(static_cast<unsigned>(tiles)), dim3(kMxThreads), 0, s, jobs,
-                           static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32));
+        hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value, SR, SC>), dim3(static_cast<unsigned>(tiles)), dim3(64 * std::min(SR * SC, 4)), 0, s,
+                           jobs, key0, key1);
         return launch_status();
     };
     int64_t elements = 0;
     for (int i = 0; i < count; ++i) elements += maps[i].rows * maps[i].cols;
     auto sized = [&](auto type_c, auto stoch_c) {
         using std::integral_constant;
-        if (elements >= int64_t{1} << 22) return launch(type_c, stoch_c, integral_constant<int, 4>{}, integral_constant<int, 4>{});
-        return launch(type_c, stoch_c, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+        if (count == 1 && !maps[0].t) {
+            const int64_t pieces = maps[0].rows * mx_panels(maps[0].cols), blocks = (pieces * 32 + kMxThreads - 1) / kMxThreads;
+            if (blocks >= int64_t{1} << 31) return static_cast<int>(FXP_ERR_DIMS);
+            if (blocks == 0) return static_cast<int>(FXP_OK);
+            hipLaunchKernelGGL((k_mx4_map_rows<decltype(type_c)::value, decltype(stoch_c)::value>), dim3(static_cast<unsigned>(blocks)), dim3(kMxThreads), 0, s, maps[0],
+                               static_cast<int>(mx_panels(maps[0].cols)), vec_of(maps[0]), key0, key1);
+            return launch_status();
+        }
+        if (elements >= int64_t{1} << 22) return launch(type_c, stoch_c, integral_constant<int, 4>{}, integral_constant<int, 2>{});
+        return launch(type_c, stoch_c, integral_constant<int, 2>{}, integral_constant<int, 1>{});
     };
     auto typed = [&](auto type_c) {
         return rounding == FXP_ROUND_STOCHASTIC ? sized(type_c, std::true_type{}) : sized(type_c, std::false_type{});

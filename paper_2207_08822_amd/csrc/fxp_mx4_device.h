@@ -12,28 +12,37 @@ __host__ __device__ inline int64_t mx_panels(int64_t cols) { return (cols + kMxP
 // (l / 16 of each 128), so that the scales it needs for a panel lie in four bytes of one word.
 __host__ __device__ constexpr int mx_scale_place(int block) { return (block & 1) * 4 + (block >> 1); }
 
-// The scale byte of a block whose largest magnitude has the bits m: the smallest power of two 2^(s - 127) under which it is at most 6 = 1.5 * 2^2; 255
-// for one with Inf or NaN.
+// The scale byte of a block whose largest magnitude has the bits m: the smallest power of two 2^(s - 127) under which it is at most 6 = 1.5 * 2^2 (a mantissa above
+// 1.5 carries into the exponent); 255 for one with Inf or NaN.
 __device__ inline int mx_scale_of(uint32_t m) {
-    const int e = static_cast<int>(m >> 23);
-    return e == 255 ? 255 : max(e - 2 + ((m & 0x7fffffu) > 0x400000u ? 1 : 0), 0);
+    const int s = max(static_cast<int>((m + 0x3fffffu) >> 23) - 2, 0);
+    return m >= 0x7f800000u ? 255 : s;
 }
 // 2^(127 - s); 0 for the scale that is none
 __device__ inline float mx_inverse(int s) { return __uint_as_float(static_cast<uint32_t>(max(254 - s, 0)) << 23); }
 
-// Four elements in units of their scale as four codes, the first in the lowest bits: a sign, then the magnitude's place in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
-// To nearest, ties to even: what the conversion instruction does.
-__device__ inline uint32_t mx_nearest4(float a, float b, float c, float d) {
-    uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, a, b, 1.0f, 0);
-    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, c, d, 1.0f, 1);
-    return r & 0xffffu;
+// Elements in units of their scale as codes, the first in the lowest bits: a sign, then the magnitude's place in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+// To nearest, ties to even: what the conversion instruction does.  |x| with its sign put aside serves both roundings: y = x * f.
+template <int N>
+__device__ inline uint32_t mx_nearest(const float (&y)[N]) {
+    static_assert(N == 4 || N == 8, "two or four bytes");
+    uint32_t r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], 1.0f, 0);
+    r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[2], y[3], 1.0f, 1);
+    if constexpr (N == 8) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[4], y[5], 1.0f, 2);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(r, y[6], y[7], 1.0f, 3);
+    }
+    return r;
 }
-// Stochastic: the magnitude as a fixed-point number whose upper part is the code, 22 bits behind the point.  From 1 on that is a float's bits less those of
-// 2^-126 (the code counts binades and one mantissa bit); below it is |y| * 2^23.  A carry out of low + 2^22 - 1 - r is r < low.
-__device__ inline uint32_t mx_stochastic(float y, uint32_t word) {
-    const float m = fabsf(y);
-    const uint32_t t = m < 1.0f ? static_cast<uint32_t>(m * 8388608.0f) : __float_as_uint(m) - (252u << 22);
-    return min((t + ((word >> 10) ^ 0x3fffffu)) >> 22, 7u) | ((__float_as_uint(y) >> 28) & 8u);
+// Stochastic: a magnitude m as a fixed-point number whose upper part is the code, 22 bits behind the point.  From 1 on that is a float's bits less those of
+// 2^-1 (the code counts binades and one mantissa bit), below it is m * 2^23: of the two and 2^23 the median, because from 1 on
+// it is 2^23 <= the first <= the second, and below the first <= the second < 2^23.  A carry out of low + 2^22 - 1 - r (`add`) is r < low.  NaN, in a block that is none, gives
+// some code.
+__device__ inline uint32_t mx_stochastic(float m, uint32_t add) {
+    const int line = static_cast<int>(m * 8388608.0f), bits = static_cast<int>(__float_as_uint(m)) - (252 << 22);
+    int t;
+    asm("v_med3_i32 %0, %1, %2, %3" : "=v"(t) : "v"(line), "v"(bits), "s"(1 << 23));
+    return (static_cast<uint32_t>(t) + add) >> 22 & 7u;
 }
 
 // two values of a byte of codes

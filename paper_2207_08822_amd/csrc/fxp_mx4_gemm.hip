@@ -260,7 +260,8 @@ static Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K) {
     Mx4Plan p{M <= kRowsMost, 128, 1, static_cast<int>(panels)};
     if (p.rows) return p;
     auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-    if (tiles(128) < 256) p.tile = 64;
+    if (tiles(256) >= 512) p.tile = 256;
+    else if (tiles(128) < 256) p.tile = 64;
     const int64_t count = tiles(p.tile);
     if (count < 256 && panels >= 8) {
         const int64_t want = std::min<int64_t>(panels / 4, (512 + count - 1) / count);
@@ -323,7 +324,8 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
     typed(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
-        if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
+        if (t == 256) hipLaunchKernelGGL((k_mx4_tiles<256, 256, 64, 128, 2, TYPE>), grid, dim3(512), 0, s, p);
+        else if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
         else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
     });
     if (parts)
