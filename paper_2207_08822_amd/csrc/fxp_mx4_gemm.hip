@@ -59,6 +59,24 @@ __device__ inline void store_one(void* c, int64_t at, float v) {
     static_cast<typename Elem<TYPE>::T*>(c)[at] = static_cast<typename Elem<TYPE>::T>(v);
 }
 
+// The fragments of a wave to C from row row0, column col0 on: register r of a lane is row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32 of its fragment.
+template <int TYPE, int FM, int FN>
+__device__ inline void store_tile(const Mx4Product& p, const v16f (&acc)[FM][FN], int row0, int col0, int fhalf, int frow) {
+    const int64_t base = static_cast<int64_t>(blockIdx.y) * p.split_stride + (row0 + 4 * fhalf) * p.ldc + col0 + frow;
+    const bool inside = row0 + 32 * FM <= p.M && col0 + 32 * FN <= p.N;              // uniform
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int dr = 32 * i + 8 * (r >> 2) + (r & 3);
+            if (!inside && row0 + 4 * fhalf + dr >= p.M) continue;
+            const int64_t at = base + dr * p.ldc;
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                if (inside || col0 + 32 * j + frow < p.N) store_one<TYPE>(p.c, at + 32 * j, acc[i][j][r]);
+        }
+}
+
 // ---- tiles ----
 //
 // BM x BN outputs a workgroup, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's bound).  16-byte pieces of a row
@@ -152,19 +170,135 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
     }
     wait_loads_and_lds<0>();                                        // none into LDS may outlive the workgroup
 
-    const int64_t base = static_cast<int64_t>(blockIdx.y) * p.split_stride;
-    const int col0 = n0 + wn0 + frow;
+    store_tile<TYPE, FM, FN>(p, acc, m0 + wm0, n0 + wn0, fhalf, frow);
+}
+
+// ---- large tiles ----
+//
+// 256 x 256 outputs, eight waves of 64 x 128, two panels in LDS.  A wave holds the fragments of two quarters of a panel: those of the next quarter are read while
+// one is multiplied, across the barrier too, which stands before a panel's last quarter.  Behind it the panel after next goes where this one was: its loads are spread
+// over the multiplications of that quarter and the next and have most of a panel's time.
+template <int WM, int WN, int TYPE>
+__global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4Product p) {
+    constexpr int B = 256, NW = (B / WM) * (B / WN), FM = WM / 32, FN = WN / 32;
+    constexpr int kCodes = 2 * B * kMxRowBytes, kStage = kCodes + 2 * B * kMxRowScales, L = B / 8 / NW, LS = B / 32 / NW;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
+
+    int tm, tn;
+    tile_of_block(static_cast<int>(blockIdx.x), p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
+    const int m0 = tm * B, n0 = tn * B;
+    const int first = static_cast<int>(blockIdx.y) * p.per_split, panels = min(p.per_split, p.panels - first);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm0 = (wave / (B / WN)) * WM, wn0 = (wave % (B / WN)) * WN;
+
+    int off_a[L], off_b[L];
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+        const int row = (wave + j * NW) * 8 + lane / 8, piece = ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
+        off_a[j] = (m0 + row) * kMxRowBytes + piece;
+        off_b[j] = (n0 + row) * kMxRowBytes + piece;
+    }
+    const int off_sa = (m0 + 32 * wave) * kMxRowScales + 4 * lane, off_sb = (n0 + 32 * wave) * kMxRowScales + 4 * lane;       // 32 rows of scales a load
+    auto issue = [&](const Mx4Operand& o, int t, const int (&off)[L], int off_s, int at, int at_s) {
+        const int64_t panel = first + t;
+        const bool there = t < panels;                              // past the last: no memory access, zeros
+        uint8_t* const stage = lds + (t & 1) * kStage;
+        const uint8_t* const codes = o.data + panel * o.rows * kMxRowBytes;
+#pragma unroll
+        for (int j = 0; j < L; ++j) load_to_lds<16>(codes, there ? o.rows * kMxRowBytes : 0, off[j], stage + at + (wave + j * NW) * 1024);
+#pragma unroll
+        for (int j = 0; j < LS; ++j)
+            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, there ? o.rows * kMxRowScales : 0, off_s + j * NW * 256, stage + at_s + (wave + j * NW) * 256);
+    };
+    auto issue_a = [&](int t) { issue(p.a, t, off_a, off_sa, 0, kCodes); };
+    auto issue_b = [&](int t) { issue(p.b, t, off_b, off_sb, B * kMxRowBytes, kCodes + B * kMxRowScales); };
+
+    v16f acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = m0 + wm0 + 32 * i + 8 * (r >> 2) + 4 * fhalf + (r & 3);
-            if (row >= p.M) continue;
-            const int64_t at = base + row * p.ldc + col0;
+        for (int j = 0; j < FN; ++j) acc[i][j] = {};
+    const int frow = lane & 31, fhalf = lane >> 5, fswz = swizzle_of_row<kMxRowBytes>(frow);
+    v4i fa[2][FM], fb[2][FN];
+    int ea[FM], eb[FN], next_a[FM], next_b[FN];
+    auto read = [&](auto buf_c, int t, auto ks_c) {
+        constexpr int BUF = decltype(buf_c)::value, KS = decltype(ks_c)::value;
+        const uint8_t* const stage = lds + (t & 1) * kStage;
+        const int piece = ((2 * KS + fhalf) ^ fswz) * 16;
 #pragma unroll
-            for (int j = 0; j < FN; ++j)
-                if (col0 + 32 * j < p.N) store_one<TYPE>(p.c, at + 32 * j, acc[i][j][r]);
+        for (int i = 0; i < FM; ++i) fa[BUF][i] = *reinterpret_cast<const v4i*>(stage + (wm0 + 32 * i + frow) * kMxRowBytes + piece);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[BUF][j] = *reinterpret_cast<const v4i*>(stage + (B + wn0 + 32 * j + frow) * kMxRowBytes + piece);
+    };
+    auto read_scales = [&](int t) {
+        const uint8_t* const at = lds + (t & 1) * kStage + kCodes + 4 * fhalf;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) next_a[i] = *reinterpret_cast<const int*>(at + (wm0 + 32 * i + frow) * kMxRowScales);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) next_b[j] = *reinterpret_cast<const int*>(at + (B + wn0 + 32 * j + frow) * kMxRowScales);
+    };
+    auto take_scales = [&] {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) ea[i] = next_a[i];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) eb[j] = next_b[j];
+    };
+    auto multiply = [&](auto buf_c, auto ks_c, auto reads_c, auto loads_c) {
+        constexpr int BUF = decltype(buf_c)::value, KS = decltype(ks_c)::value, reads = decltype(reads_c)::value, loads = decltype(loads_c)::value;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = mfma32<KS, KS>(fa[BUF][i], fb[BUF][j], acc[i][j], ea[i], eb[j]);
+        // one multiplication, then two reads of LDS or a load, and so on
+#pragma unroll
+        for (int n = 0; n < reads / 2; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
         }
+#pragma unroll
+        for (int n = 0; n < loads; ++n) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - reads / 2 - loads, 0);
+    };
+
+    issue_a(0);
+    issue_b(0);
+    issue_a(1);
+    wait_loads_and_lds<L + LS>();
+    barrier();
+    if (panels > 0) {
+        read_scales(0);
+        take_scales();
+        read(IC<0>{}, 0, IC<0>{});
+        int t = 0;
+        for (; t + 1 < panels; ++t) {
+            read(IC<1>{}, t, IC<1>{});
+            issue_b(t + 1);
+            multiply(IC<0>{}, IC<0>{}, IC<FM + FN>{}, IC<L + LS>{});
+            read(IC<0>{}, t, IC<2>{});
+            multiply(IC<1>{}, IC<1>{}, IC<FM + FN>{}, IC<0>{});
+            read(IC<1>{}, t, IC<3>{});
+            multiply(IC<0>{}, IC<2>{}, IC<FM + FN>{}, IC<0>{});
+            wait_loads_and_lds<0>();
+            barrier();
+            read_scales(t + 1);
+            read(IC<0>{}, t + 1, IC<0>{});
+            issue_a(t + 2);
+            multiply(IC<1>{}, IC<3>{}, IC<FM + FN>{}, IC<L + LS>{});
+            take_scales();
+        }
+        read(IC<1>{}, t, IC<1>{});
+        multiply(IC<0>{}, IC<0>{}, IC<FM + FN>{}, IC<0>{});
+        read(IC<0>{}, t, IC<2>{});
+        multiply(IC<1>{}, IC<1>{}, IC<FM + FN>{}, IC<0>{});
+        read(IC<1>{}, t, IC<3>{});
+        multiply(IC<0>{}, IC<2>{}, IC<FM + FN>{}, IC<0>{});
+        multiply(IC<1>{}, IC<3>{}, IC<0>{}, IC<0>{});
+    }
+    wait_loads_and_lds<0>();                                        // none into LDS may outlive the workgroup
+    store_tile<TYPE, FM, FN>(p, acc, m0 + wm0, n0 + wn0, fhalf, frow);
 }
 
 // partial sums [parts][M * N] added in order
@@ -324,7 +458,7 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
     typed(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
-        if (t == 256) hipLaunchKernelGGL((k_mx4_tiles<256, 256, 64, 128, 2, TYPE>), grid, dim3(512), 0, s, p);
+        if (t == 256) hipLaunchKernelGGL((k_mx4_large<64, 128, TYPE>), grid, dim3(512), 0, s, p);
         else if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
         else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
     });
