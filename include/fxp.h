@@ -559,7 +559,7 @@ size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream);
 
 /* Y[M,N] = X[M,K] W of `type`, W = [N,K] mapped (W^T with blocks along the contraction: fxp_mx4_map's qT of W[K,N]); X is mapped to nearest on the way.  Row strides
- * ldx >= K, ldy >= N.  Any M, one row to many.  Y must not overlap X.  ws: fxp_mx4_linear_workspace_bytes bytes, 256-byte aligned. */
+ * ldx >= K, ldy >= N.  Any M, one row to many.  Y must not overlap X.  ws: fxp_mx4_linear_workspace_bytes bytes (0, and NULL allowed, for M <= 4), 256-byte aligned. */
 size_t fxp_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx4* W, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
 

@@ -21,12 +21,6 @@ struct Mx4Jobs {
     int count;
 };
 
-// largest of eight neighbouring lanes, or of four, in all of them
-template <int CTRL>
-__device__ inline uint32_t max_dpp(uint32_t m) {
-    return max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), CTRL, 0xf, 0xf, false)));
-}
-__device__ inline uint32_t max_of_4(uint32_t m) { return max_dpp<0x4e>(max_dpp<0xb1>(m)); }       // neighbours, then pairs
 // largest of the lanes eight apart
 __device__ inline uint32_t max_over_8(uint32_t m) {
     typedef unsigned v2u __attribute__((ext_vector_type(2)));
@@ -36,8 +30,6 @@ __device__ inline uint32_t max_over_8(uint32_t m) {
     p = __builtin_amdgcn_permlane32_swap(m, m, false, false);
     return max(p[0], p[1]);
 }
-__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
 // What stochastic rounding adds to eight elements from element `at` of the matrix on: 2^22 - 1 less the top 22 bits of their words.
 __device__ inline void adds_of_8(uint64_t at, bool whole_quads, uint32_t sid0, uint32_t sid1, uint32_t key0, uint32_t key1, uint32_t (&add)[8]) {
     const uint64_t quad = at >> 2;
@@ -387,7 +379,7 @@ static size_t mapped_bytes(int64_t M, int64_t K) {
 extern "C" size_t fxp_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
     for (int64_t n : {M, N, K})
         if (n < 0 || n > fxp::kMxMost) return 0;
-    return fxp::mapped_bytes(M, K) + fxp::mx4_gemm_bytes(M, N, K);
+    return fxp::mx4_is_fused(M) ? 0 : fxp::mapped_bytes(M, K) + fxp::mx4_gemm_bytes(M, N, K);
 }
 
 extern "C" int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx4* W, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream) {
@@ -401,8 +393,9 @@ extern "C" int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, c
     if (M == 0 || N == 0) return FXP_OK;
     if (!Y) return FXP_ERR_NULL;
     if (!aligned(Y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    if (mx4_is_fused(M)) return mx4_fused_launch(type, X, ldx, M, *W, Y, ldy, static_cast<hipStream_t>(stream));
     const size_t codes = round_up(static_cast<size_t>(mx_panels(K) * M * kMxRowBytes), 256), mapped = mapped_bytes(M, K);
-    const size_t need = fxp_mx4_linear_workspace_bytes(M, N, K);               // 0: a contraction of nothing
+    const size_t need = fxp_mx4_linear_workspace_bytes(M, N, K);               // 0: a few rows, or a contraction of nothing
     if (need && (!ws || ws_bytes < need)) return FXP_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
     uint8_t* const at = static_cast<uint8_t*>(ws);

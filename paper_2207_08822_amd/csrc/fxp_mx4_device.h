@@ -45,6 +45,18 @@ __device__ inline uint32_t mx_stochastic(float m, uint32_t add) {
     return (static_cast<uint32_t>(t) + add) >> 22 & 7u;
 }
 
+// largest of four neighbouring lanes, in all of them
+template <int CTRL>
+__device__ inline uint32_t max_dpp(uint32_t m) {
+    return max(m, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(m), CTRL, 0xf, 0xf, false)));
+}
+__device__ inline uint32_t max_of_4(uint32_t m) { return max_dpp<0x4e>(max_dpp<0xb1>(m)); }       // neighbours, then pairs
+__device__ inline uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// bits of the largest magnitude of a block of which each of eight neighbouring lanes has four elements
+__device__ inline uint32_t mx_max_of_8(const float (&x)[4]) {
+    return max_dpp<0x141>(max_of_4(max(max(magnitude(x[0]), magnitude(x[1])), max(magnitude(x[2]), magnitude(x[3])))));      // row_half_mirror
+}
+
 // two values of a byte of codes
 __device__ inline float2 mx_values(uint32_t codes, int byte) {
     typedef float v2f __attribute__((ext_vector_type(2)));
@@ -80,6 +92,8 @@ struct Mx4Map {
 int mx4_map_launch(int type, const Mx4Map* jobs, int count, uint64_t seed, int rounding, hipStream_t s);
 // C [A.rows, B.rows] = A B^T; ws: mx4_gemm_bytes
 size_t mx4_gemm_bytes(int64_t M, int64_t N, int64_t K);
+bool mx4_is_fused(int64_t M);
+int mx4_fused_launch(int type, const void* x, int64_t ldx, int64_t M, const fxp_mx4& B, void* y, int64_t ldy, hipStream_t s);
 int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s);
 
 }  // namespace fxp

@@ -42,6 +42,13 @@ __device__ inline void barrier() {
     asm volatile("" ::: "memory");
 }
 
+// a wave's stores to LDS are done, and seen by its other lanes
+__device__ inline void wave_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 struct Mx4Operand {
     const uint8_t *data, *scales;
     int rows;
@@ -313,8 +320,9 @@ __global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts
 
 // ---- a few rows ----
 //
-// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up in LDS.  B is read once, straight into the instruction's registers.
-template <int MT, int NT, int WAVES, int TYPE>
+// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up in LDS.  B is read once, straight into the instruction's registers, U panels
+// of a wave at a time.
+template <int MT, int NT, int U, int WAVES, int TYPE>
 __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
     __shared__ v4f sums[WAVES > 1 ? WAVES : 1][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -326,34 +334,42 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
         for (int n = 0; n < NT; ++n) acc[m][n] = {};
     // block 4 h + kb of a panel: 16 bytes at 64 h + 16 kb, its scale in byte kb / 2 + 2 h of word kb % 2
     const int code_at = r * kMxRowBytes + kb * 16, scale_at = r * kMxRowScales + 4 * (kb & 1), shift = 8 * (kb >> 1);
-    for (int t = wave; t < p.panels; t += WAVES) {
-        const auto rb = records(p.b.data + int64_t{t} * p.b.rows * kMxRowBytes, p.b.rows * kMxRowBytes);
-        const auto re = records(p.b.scales + int64_t{t} * p.b.rows * kMxRowScales, p.b.rows * kMxRowScales);
-        const auto ra = records(p.a.data + int64_t{t} * p.a.rows * kMxRowBytes, p.a.rows * kMxRowBytes);
-        const auto rs = records(p.a.scales + int64_t{t} * p.a.rows * kMxRowScales, p.a.rows * kMxRowScales);
-        v4i b[NT][2], a[MT][2];
-        int eb[NT], ea[MT];
+    for (int t0 = wave; t0 < p.panels; t0 += WAVES * U) {
+        v4i b[U][NT][2], a[U][MT][2];
+        int eb[U][NT], ea[U][MT];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int at = (n0 + 16 * n) * kMxRowBytes + code_at;
-            b[n][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at, 0, kNonTemporal));
-            b[n][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at + 64, 0, kNonTemporal));
-            eb[n] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, (n0 + 16 * n) * kMxRowScales + scale_at, 0, 0) >> shift);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const int at = 16 * m * kMxRowBytes + code_at;
-            a[m][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at, 0, 0));
-            a[m][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at + 64, 0, 0));
-            ea[m] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rs, 16 * m * kMxRowScales + scale_at, 0, 0) >> shift);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * WAVES;
+            const bool there = t < p.panels;                        // past the last: no memory access, zeros
+            const auto rb = records(p.b.data + int64_t{t} * p.b.rows * kMxRowBytes, there ? p.b.rows * kMxRowBytes : 0);
+            const auto re = records(p.b.scales + int64_t{t} * p.b.rows * kMxRowScales, there ? p.b.rows * kMxRowScales : 0);
+            const auto ra = records(p.a.data + int64_t{t} * p.a.rows * kMxRowBytes, there ? p.a.rows * kMxRowBytes : 0);
+            const auto rs = records(p.a.scales + int64_t{t} * p.a.rows * kMxRowScales, there ? p.a.rows * kMxRowScales : 0);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                acc[m][n] = mfma16<0, 0>(b[n][0], a[m][0], acc[m][n], eb[n], ea[m]);
-                acc[m][n] = mfma16<2, 2>(b[n][1], a[m][1], acc[m][n], eb[n], ea[m]);
+                const int at = (n0 + 16 * n) * kMxRowBytes + code_at;
+                b[u][n][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at, 0, kNonTemporal));
+                b[u][n][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at + 64, 0, kNonTemporal));
+                eb[u][n] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, (n0 + 16 * n) * kMxRowScales + scale_at, 0, 0));
             }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const int at = 16 * m * kMxRowBytes + code_at;
+                a[u][m][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at, 0, 0));
+                a[u][m][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at + 64, 0, 0));
+                ea[u][m] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rs, 16 * m * kMxRowScales + scale_at, 0, 0));
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);                          // all loads first: the compiler would hold few registers and wait more often
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    acc[m][n] = mfma16<0, 0>(b[u][n][0], a[u][m][0], acc[m][n], eb[u][n] >> shift, ea[u][m] >> shift);
+                    acc[m][n] = mfma16<2, 2>(b[u][n][1], a[u][m][1], acc[m][n], eb[u][n] >> shift, ea[u][m] >> shift);
+                }
     }
     if constexpr (WAVES > 1) {
 #pragma unroll
@@ -379,6 +395,99 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < p.N) store_one<TYPE>(p.c, row * p.ldc + col + j, s[j]);
+    }
+}
+
+// ---- single tokens ----
+//
+// Up to four rows that are not mapped yet.  A wave maps the panels that it takes, a row at a time, four elements a lane, and passes the codes on in LDS: less than a launch of
+// its own.  16 rows of B a workgroup, a panel of eight of them a load, so that every load is 1024 bytes in a row: lane (r, kb) of the instruction (r < 16, kb < 4) has
+// block 2 kb + r / 8 of row r % 8 - rows 8 to 15 of the product are the odd blocks - and of X alike, so that the sum of an output's even blocks is at (n, m)
+// and that of its odd ones at (n + 8, m + 8); the other half of the product is not used.
+// Bound by B's bytes, in flight all at once.
+constexpr int kTokens = 4;
+
+struct Mx4Vector {
+    Mx4Operand b;
+    int M, N, K, panels, vec;
+    const void* x;
+    int64_t ldx;
+    void* y;
+    int64_t ldy;
+};
+
+template <int MR, int U, int WAVES, int TYPE>
+__global__ __launch_bounds__(WAVES * 64) void k_mx4_vector(Mx4Vector g) {
+    __shared__ v4f sums[WAVES][2][64];
+    __shared__ __attribute__((aligned(16))) uint8_t codes[WAVES * U * MR][kMxRowBytes], scales[WAVES * U * MR][kMxRowScales];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = static_cast<int>(blockIdx.x) * 16, r = lane & 15, kb = lane >> 4, half = r >> 3, m_of = r & 7;
+    const int code_at = (n0 + m_of) * kMxRowBytes + (2 * kb + half) * 16, scale_at = (n0 + m_of) * kMxRowScales + 4 * half, shift = 8 * kb;
+    using T = typename Elem<TYPE>::T;
+    v4f acc[2] = {{}, {}};
+    for (int t0 = wave; t0 < g.panels; t0 += WAVES * U) {
+        v4i b[U][2];
+        int e[U][2];
+        float x[U][MR][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = t0 + u * WAVES;
+            const bool there = t < g.panels;                        // past the last: no memory access, zeros
+            const auto rb = records(g.b.data + int64_t{t} * g.b.rows * kMxRowBytes, there ? g.b.rows * kMxRowBytes : 0);
+            const auto re = records(g.b.scales + int64_t{t} * g.b.rows * kMxRowScales, there ? g.b.rows * kMxRowScales : 0);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                b[u][i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, code_at + i * 8 * kMxRowBytes, 0, kNonTemporal));
+                e[u][i] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, scale_at + i * 8 * kMxRowScales, 0, 0));
+            }
+            const int c = t * kMxPanel + 4 * lane;
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                const T* const row = static_cast<const T*>(g.x) + m * g.ldx + c;
+                if (g.vec && c + 4 <= g.K && m < g.M) {
+                    load_elems<TYPE, 4>(row, 0, true, x[u][m]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[u][m][j] = c + j < g.K && m < g.M ? static_cast<float>(row[j]) : 0.0f;
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);                          // all loads first
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < MR; ++m) {
+                const int slot = (wave * U + u) * MR + m, s = mx_scale_of(mx_max_of_8(x[u][m]));
+                const float f = mx_inverse(s);
+                const float y[4] = {x[u][m][0] * f, x[u][m][1] * f, x[u][m][2] * f, x[u][m][3] * f};
+                *reinterpret_cast<uint16_t*>(&codes[slot][2 * lane]) = static_cast<uint16_t>(mx_nearest(y));
+                if ((lane & 7) == 0) scales[slot][mx_scale_place(lane >> 3)] = static_cast<uint8_t>(s);
+            }
+        wave_barrier();                                             // a wave's own slots
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int slot = (wave * U + u) * MR + min(m_of, MR - 1);
+            const v4i code = *reinterpret_cast<const v4i*>(&codes[slot][(2 * kb + half) * 16]);
+            const int scale = *reinterpret_cast<const int*>(&scales[slot][4 * half]) >> shift;
+            const v4i a = m_of < MR ? code : v4i{};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[i] = mfma16<0, 0>(b[u][i], a, acc[i], e[u][i] >> shift, scale);
+        }
+        wave_barrier();
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    // lane (m, q, i): outputs 8 i + 4 q + j of row m
+    if (threadIdx.x >= 32) return;
+    const int m = lane & 7, q = lane >> 3 & 1, i = lane >> 4;
+    if (m >= g.M) return;
+    v4f s = {};
+    for (int w = 0; w < WAVES; ++w) s += sums[w][i][16 * q + m] + sums[w][i][16 * (q + 2) + m + 8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + 8 * i + 4 * q + j;
+        if (n < g.N) store_one<TYPE>(g.y, m * g.ldy + n, s[j]);
     }
 }
 
@@ -410,6 +519,58 @@ size_t mx4_gemm_bytes(int64_t M, int64_t N, int64_t K) {
     return p.splits > 1 ? round_up(static_cast<size_t>(p.splits) * M * N * sizeof(float), 256) : 0;
 }
 
+template <typename F>
+static void by_type(int type, F go) {
+    if (type == FXP_F32) go(IC<FXP_F32>{});
+    else if (type == FXP_BF16) go(IC<FXP_BF16>{});
+    else go(IC<FXP_F16>{});
+}
+
+static int rows_launch(const Mx4Product& p, int type, hipStream_t s) {
+    by_type(type, [&](auto type_c) {
+        constexpr int TYPE = decltype(type_c)::value;
+        auto go = [&](auto mt_c, auto u_c, auto w_c) {
+            constexpr int W = decltype(w_c)::value;
+            hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, 1, decltype(u_c)::value, W, TYPE>), dim3(static_cast<unsigned>((p.N + 15) / 16)), dim3(64 * W), 0, s, p);
+        };
+        // as many waves of a workgroup as leave all of its panels in flight and two (four) workgroups on a CU
+        auto waves = [&](auto mt_c, auto u_c, auto most_c) {
+            if (p.panels > 4) go(mt_c, u_c, most_c);
+            else if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{});
+            else go(mt_c, IC<1>{}, IC<1>{});
+        };
+        if (p.M <= 16) waves(IC<1>{}, IC<4>{}, IC<8>{});
+        else if (p.M <= 32) waves(IC<2>{}, IC<2>{}, IC<4>{});
+        else if (p.M <= 48) waves(IC<3>{}, IC<2>{}, IC<4>{});
+        else waves(IC<4>{}, IC<2>{}, IC<4>{});
+    });
+    return launch_status();
+}
+
+bool mx4_is_fused(int64_t M) { return M <= kTokens; }
+// Y = X B^T for X as it is, up to kTokens rows of it: one launch, no workspace
+int mx4_fused_launch(int type, const void* x, int64_t ldx, int64_t M, const fxp_mx4& B, void* y, int64_t ldy, hipStream_t s) {
+    const Mx4Vector g{{B.data, B.scales, static_cast<int>(B.rows)}, static_cast<int>(M), static_cast<int>(B.rows), static_cast<int>(B.cols), static_cast<int>(mx_panels(B.cols)),
+                      aligned(x, 4 * static_cast<size_t>(elem_size(type))) && (M == 1 || ldx % 4 == 0), x, ldx, y, ldy};
+    by_type(type, [&](auto type_c) {
+        auto go = [&](auto mr_c, auto u_c, auto w_c) {
+            constexpr int W = decltype(w_c)::value;
+            hipLaunchKernelGGL((k_mx4_vector<decltype(mr_c)::value, decltype(u_c)::value, W, decltype(type_c)::value>), dim3(static_cast<unsigned>((g.N + 15) / 16)), dim3(64 * W), 0, s,
+                               g);
+        };
+        auto sized = [&](auto mr_c) {
+            if (g.panels > 16) go(mr_c, IC<4>{}, IC<8>{});
+            else if (g.panels > 8) go(mr_c, IC<2>{}, IC<8>{});
+            else if (g.panels > 4) go(mr_c, IC<1>{}, IC<8>{});
+            else go(mr_c, IC<1>{}, IC<4>{});
+        };
+        if (M == 1) sized(IC<1>{});
+        else if (M == 2) sized(IC<2>{});
+        else sized(IC<4>{});
+    });
+    return launch_status();
+}
+
 int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s) {
     const int64_t M = A.rows, N = B.rows, K = A.cols;
     const Mx4Plan plan = mx4_plan(M, N, K);
@@ -422,29 +583,7 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.per_split = plan.per_split;
     p.c = C;
     p.ldc = ldc;
-    auto typed = [&](int t, auto go) {
-        if (t == FXP_F32) go(IC<FXP_F32>{});
-        else if (t == FXP_BF16) go(IC<FXP_BF16>{});
-        else go(IC<FXP_F16>{});
-    };
-    if (plan.rows) {
-        typed(type, [&](auto type_c) {
-            constexpr int TYPE = decltype(type_c)::value;
-            auto go = [&](auto mt_c, auto nt_c, auto w_c) {
-                constexpr int NT = decltype(nt_c)::value, W = decltype(w_c)::value;
-                hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, NT, W, TYPE>), dim3(static_cast<unsigned>((N + 16 * NT - 1) / (16 * NT))), dim3(64 * W), 0, s, p);
-            };
-            auto waves = [&](auto mt_c, auto nt_c) {
-                if (p.panels >= 8) go(mt_c, nt_c, IC<8>{});
-                else if (p.panels >= 3) go(mt_c, nt_c, IC<4>{});
-                else go(mt_c, nt_c, IC<1>{});
-            };
-            if (M <= 16) waves(IC<1>{}, IC<1>{});
-            else if (M <= 32) waves(IC<2>{}, IC<1>{});
-            else waves(IC<4>{}, IC<1>{});
-        });
-        return launch_status();
-    }
+    if (plan.rows) return rows_launch(p, type, s);
     const bool parts = plan.splits > 1;
     if (parts) {
         p.c = ws;
@@ -456,14 +595,14 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.tiles_n = static_cast<int>((N + t - 1) / t);
     p.group_m = 8;
     const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
-    typed(parts ? FXP_F32 : type, [&](auto type_c) {
+    by_type(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
         if (t == 256) hipLaunchKernelGGL((k_mx4_large<64, 128, TYPE>), grid, dim3(512), 0, s, p);
         else if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
         else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
     });
     if (parts)
-        typed(type, [&](auto type_c) {
+        by_type(type, [&](auto type_c) {
             hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(static_cast<unsigned>((M * N + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(ws), plan.splits,
                                p.split_stride, p.M, p.N, C, ldc);
         });

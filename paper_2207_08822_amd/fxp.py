@@ -1145,9 +1145,10 @@ def mx4_linear(x, w, out=None, ws=None):
             raise FxpError("out shares elements with x")
     if ws is not None:
         _index(ws, "ws", dtype=torch.uint8)
-    else:
+    elif M > 4:
         ws = x.new_empty(int(lib().fxp_mx4_linear_workspace_bytes(M, w.rows, K)), dtype=torch.uint8)
-    _check(lib().fxp_mx4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, w.ref, out.data_ptr(), ldy, ws.data_ptr(), ws.numel(), _stream()), "fxp_mx4_linear")
+    _check(lib().fxp_mx4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, w.ref, out.data_ptr(), ldy, _p(ws), ws.numel() if ws is not None else 0, _stream()),
+           "fxp_mx4_linear")
     return out
 
 

@@ -88,7 +88,7 @@ def test_the_ends_of_the_scales(fxp):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("M,K,N", [(1, 100, 64), (5, 256, 300), (31, 1000, 77), (130, 520, 260), (700, 64, 300)])
+@pytest.mark.parametrize("M,K,N", [(1, 100, 64), (1, 3000, 77), (2, 255, 40), (3, 2500, 33), (4, 1030, 50), (5, 256, 300), (31, 1000, 77), (130, 520, 260), (700, 64, 300)])
 def test_linear(fxp, M, K, N, kind):
     say("mx4_linear", M, K, N, kind)
     rng = np.random.default_rng(M * K + N)

@@ -213,7 +213,9 @@ def test_mx4_products(L):
     assert need > 0 and f(**big) == -4 and f(**big, ws=BIG, n=need - 1) == -4 and f(**big, ws=BIG + 8, n=need) == -3
     assert L.fxp_mx4_gemm_workspace_bytes(-1, 4, 4) == 0 and L.fxp_mx4_linear_workspace_bytes(4, 4, 1 << 24) == 0 and L.fxp_mx4_layer_workspace_bytes(1, -1, 1) == 0
 
-    def g(type=0, X=BIG, ldx=70, M=4, W=mx4(rows=9), Y=BIG, ldy=9, ws=BIG, n=1 << 20):
+    assert L.fxp_mx4_linear_workspace_bytes(4, 9, 70) == 0
+
+    def g(type=0, X=BIG, ldx=70, M=5, W=mx4(rows=9), Y=BIG, ldy=9, ws=BIG, n=1 << 20):
         return L.fxp_mx4_linear(type, X, ldx, M, W, Y, ldy, ws, n, None)
 
     assert g(W=None) == -1 and g(type=3) == -9 and g(X=None) == -1 and g(Y=None) == -1 and g(ldx=69) == -2 and g(ldy=8) == -2 and g(M=-1) == -2
