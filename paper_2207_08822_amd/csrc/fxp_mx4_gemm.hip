@@ -320,58 +320,131 @@ __global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts
 
 // ---- a few rows ----
 //
-// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up in LDS.  B is read once, straight into the instruction's registers, U panels
-// of a wave at a time.
-template <int MT, int NT, int U, int WAVES, int TYPE>
-__global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
-    __shared__ v4f sums[WAVES > 1 ? WAVES : 1][MT * NT][64];
+// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up at the end.  A wave has U panels in flight, straight to LDS and out of it
+// again: a load of its own registers would have neighbouring lanes in different rows, 64 accesses of a cache line where 1024 bytes in a row are eight (37 x 4096 x 8192
+// 9.5 us, 8192 x 8192 by one row 8.3 us so).  Bound by B's bytes where all of its panels are in flight.
+// FUSED: A is not mapped yet; up to four rows of it.  A wave maps the panels that it takes, a row at a time, four elements a lane: less than a launch of its own.
+constexpr int kTokens = 4;
+
+struct Mx4Rows {
+    Mx4Product p;
+    const void* x;          // FUSED: A as it is
+    int64_t ldx;
+    int K, vec;
+};
+
+template <int MT, int NT, int U, int WAVES, int TYPE, int FUSED>         // FUSED: 0, or the rows of A
+__global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
+    const Mx4Product& p = g.p;
+    constexpr int RA = FUSED ? FUSED : 16 * MT, RB = 16 * NT;
+    constexpr int kScalesB = (RB * kMxRowScales + 255) / 256 * 256, kScalesA = FUSED ? (RA * kMxRowScales + 15) / 16 * 16 : (RA * kMxRowScales + 255) / 256 * 256;
+    constexpr int kSlot = (RA + RB) * kMxRowBytes + kScalesA + kScalesB, kAtA = RB * kMxRowBytes, kAtSB = kAtA + RA * kMxRowBytes, kAtSA = kAtSB + kScalesB;
+    constexpr int kBytes = WAVES * U * kSlot, kSums = WAVES * MT * NT * 64 * 16;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kBytes > kSums ? kBytes : kSums];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = static_cast<int>(blockIdx.x) * NT * 16, r = lane & 15, kb = lane >> 4;
+    const int n0 = static_cast<int>(blockIdx.x) * RB, r = lane & 15, kb = lane >> 4;
+    using T = typename Elem<TYPE>::T;
     v4f acc[MT][NT];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[m][n] = {};
-    // block 4 h + kb of a panel: 16 bytes at 64 h + 16 kb, its scale in byte kb / 2 + 2 h of word kb % 2
-    const int code_at = r * kMxRowBytes + kb * 16, scale_at = r * kMxRowScales + 4 * (kb & 1), shift = 8 * (kb >> 1);
+    // lane l of a load has 16 bytes of row l / 8 of eight, exchanged by the row as in the tiles
+    int from[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) from[i] = lane / 8 * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(8 * i + lane / 8)) * 16;
+    // block 4 h + kb of a panel: its scale is byte kb / 2 + 2 h of word kb % 2
+    const int shift = 8 * (kb >> 1), swz = swizzle_of_row<kMxRowBytes>(r);
+    uint8_t* const mine = lds + wave * U * kSlot;
     for (int t0 = wave; t0 < p.panels; t0 += WAVES * U) {
-        v4i b[U][NT][2], a[U][MT][2];
-        int eb[U][NT], ea[U][MT];
+        float x[U][FUSED ? FUSED : 1][4];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int t = t0 + u * WAVES;
             const bool there = t < p.panels;                        // past the last: no memory access, zeros
-            const auto rb = records(p.b.data + int64_t{t} * p.b.rows * kMxRowBytes, there ? p.b.rows * kMxRowBytes : 0);
-            const auto re = records(p.b.scales + int64_t{t} * p.b.rows * kMxRowScales, there ? p.b.rows * kMxRowScales : 0);
-            const auto ra = records(p.a.data + int64_t{t} * p.a.rows * kMxRowBytes, there ? p.a.rows * kMxRowBytes : 0);
-            const auto rs = records(p.a.scales + int64_t{t} * p.a.rows * kMxRowScales, there ? p.a.rows * kMxRowScales : 0);
+            uint8_t* const slot = mine + u * kSlot;
+            if constexpr (FUSED) {                                  // these first: they are waited for first
+                const int c = t * kMxPanel + 4 * lane;
+#pragma unroll
+                for (int m = 0; m < FUSED; ++m) {
+                    const T* const row = static_cast<const T*>(g.x) + m * g.ldx + c;
+                    if (g.vec && c + 4 <= g.K && m < p.M) {
+                        load_elems<TYPE, 4>(row, 0, true, x[u][m]);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[u][m][j] = c + j < g.K && m < p.M ? static_cast<float>(row[j]) : 0.0f;
+                    }
+                }
+            }
+            const uint8_t* const b = p.b.data + int64_t{t} * p.b.rows * kMxRowBytes;
+#pragma unroll
+            for (int i = 0; i < 2 * NT; ++i)
+                load_to_lds<16>(b, there ? p.b.rows * kMxRowBytes : 0, (n0 + 8 * i) * kMxRowBytes + from[i % 2], slot + i * 1024);
+            const uint8_t* const sb = p.b.scales + int64_t{t} * p.b.rows * kMxRowScales;
+#pragma unroll
+            for (int i = 0; i < kScalesB / 256; ++i) load_to_lds<4>(sb, there ? p.b.rows * kMxRowScales : 0, (n0 + 32 * i) * kMxRowScales + 4 * lane, slot + kAtSB + 256 * i);
+            if constexpr (!FUSED) {
+                const uint8_t* const a = p.a.data + int64_t{t} * p.a.rows * kMxRowBytes;
+#pragma unroll
+                for (int i = 0; i < 2 * MT; ++i)
+                    load_to_lds<16>(a, there ? p.a.rows * kMxRowBytes : 0, 8 * i * kMxRowBytes + from[i % 2], slot + kAtA + i * 1024);
+                const uint8_t* const sa = p.a.scales + int64_t{t} * p.a.rows * kMxRowScales;
+#pragma unroll
+                for (int i = 0; i < kScalesA / 256; ++i) load_to_lds<4>(sa, there ? p.a.rows * kMxRowScales : 0, 32 * i * kMxRowScales + 4 * lane, slot + kAtSA + 256 * i);
+            }
+        }
+        if constexpr (FUSED) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int m = 0; m < FUSED; ++m) {
+                    uint8_t* const slot = mine + u * kSlot;
+                    const int s = mx_scale_of(mx_max_of_8(x[u][m]));
+                    const float f = mx_inverse(s);
+                    const float y[4] = {x[u][m][0] * f, x[u][m][1] * f, x[u][m][2] * f, x[u][m][3] * f};
+                    *reinterpret_cast<uint16_t*>(slot + kAtA + m * kMxRowBytes + 2 * lane) = static_cast<uint16_t>(mx_nearest(y));
+                    if ((lane & 7) == 0) slot[kAtSA + m * kMxRowScales + mx_scale_place(lane >> 3)] = static_cast<uint8_t>(s);
+                }
+        }
+        wait_loads_and_lds<0>();
+        wave_barrier();                                             // a wave's own slots
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint8_t* const slot = mine + u * kSlot;
+            v4i b[NT][2], a[MT][2];
+            int eb[NT], ea[MT];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int at = (n0 + 16 * n) * kMxRowBytes + code_at;
-                b[u][n][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at, 0, kNonTemporal));
-                b[u][n][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, at + 64, 0, kNonTemporal));
-                eb[u][n] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, (n0 + 16 * n) * kMxRowScales + scale_at, 0, 0));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) b[n][h] = *reinterpret_cast<const v4i*>(slot + (16 * n + r) * kMxRowBytes + ((4 * h + kb) ^ swz) * 16);
+                eb[n] = *reinterpret_cast<const int*>(slot + kAtSB + (16 * n + r) * kMxRowScales + 4 * (kb & 1)) >> shift;
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const int at = 16 * m * kMxRowBytes + code_at;
-                a[u][m][0] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at, 0, 0));
-                a[u][m][1] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(ra, at + 64, 0, 0));
-                ea[u][m] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(rs, 16 * m * kMxRowScales + scale_at, 0, 0));
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);                          // all loads first: the compiler would hold few registers and wait more often
+                // rows of X that are not there: FUSED has zeros where it has a slot, and reads its last row again, as zeros, where it has none
+                const int row = FUSED ? min(r, FUSED - 1) : 16 * m + r;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+                for (int h = 0; h < 2; ++h) {
+                    a[m][h] = *reinterpret_cast<const v4i*>(slot + kAtA + row * kMxRowBytes + (FUSED ? 4 * h + kb : (4 * h + kb) ^ swz) * 16);
+                    if (FUSED && r >= FUSED) a[m][h] = v4i{};
+                }
+                ea[m] = *reinterpret_cast<const int*>(slot + kAtSA + row * kMxRowScales + 4 * (kb & 1)) >> shift;
+                if (FUSED && r >= FUSED) ea[m] = 0;
+            }
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                    acc[m][n] = mfma16<0, 0>(b[u][n][0], a[u][m][0], acc[m][n], eb[u][n] >> shift, ea[u][m] >> shift);
-                    acc[m][n] = mfma16<2, 2>(b[u][n][1], a[u][m][1], acc[m][n], eb[u][n] >> shift, ea[u][m] >> shift);
+                    acc[m][n] = mfma16<0, 0>(b[n][0], a[m][0], acc[m][n], eb[n], ea[m]);
+                    acc[m][n] = mfma16<2, 2>(b[n][1], a[m][1], acc[m][n], eb[n], ea[m]);
                 }
+        }
+        wait_loads_and_lds<0>();
+        wave_barrier();                                             // before the slots are loaded again
     }
+    v4f(*const sums)[MT * NT][64] = reinterpret_cast<v4f(*)[MT * NT][64]>(lds);
     if constexpr (WAVES > 1) {
+        __syncthreads();                                            // the slots of other waves
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -395,99 +468,6 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Product p) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (col + j < p.N) store_one<TYPE>(p.c, row * p.ldc + col + j, s[j]);
-    }
-}
-
-// ---- single tokens ----
-//
-// Up to four rows that are not mapped yet.  A wave maps the panels that it takes, a row at a time, four elements a lane, and passes the codes on in LDS: less than a launch of
-// its own.  16 rows of B a workgroup, a panel of eight of them a load, so that every load is 1024 bytes in a row: lane (r, kb) of the instruction (r < 16, kb < 4) has
-// block 2 kb + r / 8 of row r % 8 - rows 8 to 15 of the product are the odd blocks - and of X alike, so that the sum of an output's even blocks is at (n, m)
-// and that of its odd ones at (n + 8, m + 8); the other half of the product is not used.
-// Bound by B's bytes, in flight all at once.
-constexpr int kTokens = 4;
-
-struct Mx4Vector {
-    Mx4Operand b;
-    int M, N, K, panels, vec;
-    const void* x;
-    int64_t ldx;
-    void* y;
-    int64_t ldy;
-};
-
-template <int MR, int U, int WAVES, int TYPE>
-__global__ __launch_bounds__(WAVES * 64) void k_mx4_vector(Mx4Vector g) {
-    __shared__ v4f sums[WAVES][2][64];
-    __shared__ __attribute__((aligned(16))) uint8_t codes[WAVES * U * MR][kMxRowBytes], scales[WAVES * U * MR][kMxRowScales];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = static_cast<int>(blockIdx.x) * 16, r = lane & 15, kb = lane >> 4, half = r >> 3, m_of = r & 7;
-    const int code_at = (n0 + m_of) * kMxRowBytes + (2 * kb + half) * 16, scale_at = (n0 + m_of) * kMxRowScales + 4 * half, shift = 8 * kb;
-    using T = typename Elem<TYPE>::T;
-    v4f acc[2] = {{}, {}};
-    for (int t0 = wave; t0 < g.panels; t0 += WAVES * U) {
-        v4i b[U][2];
-        int e[U][2];
-        float x[U][MR][4];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int t = t0 + u * WAVES;
-            const bool there = t < g.panels;                        // past the last: no memory access, zeros
-            const auto rb = records(g.b.data + int64_t{t} * g.b.rows * kMxRowBytes, there ? g.b.rows * kMxRowBytes : 0);
-            const auto re = records(g.b.scales + int64_t{t} * g.b.rows * kMxRowScales, there ? g.b.rows * kMxRowScales : 0);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                b[u][i] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rb, code_at + i * 8 * kMxRowBytes, 0, kNonTemporal));
-                e[u][i] = static_cast<int>(__builtin_amdgcn_raw_buffer_load_b32(re, scale_at + i * 8 * kMxRowScales, 0, 0));
-            }
-            const int c = t * kMxPanel + 4 * lane;
-#pragma unroll
-            for (int m = 0; m < MR; ++m) {
-                const T* const row = static_cast<const T*>(g.x) + m * g.ldx + c;
-                if (g.vec && c + 4 <= g.K && m < g.M) {
-                    load_elems<TYPE, 4>(row, 0, true, x[u][m]);
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[u][m][j] = c + j < g.K && m < g.M ? static_cast<float>(row[j]) : 0.0f;
-                }
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);                          // all loads first
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int m = 0; m < MR; ++m) {
-                const int slot = (wave * U + u) * MR + m, s = mx_scale_of(mx_max_of_8(x[u][m]));
-                const float f = mx_inverse(s);
-                const float y[4] = {x[u][m][0] * f, x[u][m][1] * f, x[u][m][2] * f, x[u][m][3] * f};
-                *reinterpret_cast<uint16_t*>(&codes[slot][2 * lane]) = static_cast<uint16_t>(mx_nearest(y));
-                if ((lane & 7) == 0) scales[slot][mx_scale_place(lane >> 3)] = static_cast<uint8_t>(s);
-            }
-        wave_barrier();                                             // a wave's own slots
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int slot = (wave * U + u) * MR + min(m_of, MR - 1);
-            const v4i code = *reinterpret_cast<const v4i*>(&codes[slot][(2 * kb + half) * 16]);
-            const int scale = *reinterpret_cast<const int*>(&scales[slot][4 * half]) >> shift;
-            const v4i a = m_of < MR ? code : v4i{};
-#pragma unroll
-            for (int i = 0; i < 2; ++i) acc[i] = mfma16<0, 0>(b[u][i], a, acc[i], e[u][i] >> shift, scale);
-        }
-        wave_barrier();
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i) sums[wave][i][lane] = acc[i];
-    __syncthreads();
-    // lane (m, q, i): outputs 8 i + 4 q + j of row m
-    if (threadIdx.x >= 32) return;
-    const int m = lane & 7, q = lane >> 3 & 1, i = lane >> 4;
-    if (m >= g.M) return;
-    v4f s = {};
-    for (int w = 0; w < WAVES; ++w) s += sums[w][i][16 * q + m] + sums[w][i][16 * (q + 2) + m + 8];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + 8 * i + 4 * q + j;
-        if (n < g.N) store_one<TYPE>(g.y, m * g.ldy + n, s[j]);
     }
 }
 
@@ -526,23 +506,29 @@ static void by_type(int type, F go) {
     else go(IC<FXP_F16>{});
 }
 
-static int rows_launch(const Mx4Product& p, int type, hipStream_t s) {
+// as many panels of a workgroup in flight as leave room for two workgroups on a CU, where there are so many
+static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
+    const Mx4Product& p = g.p;
     by_type(type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
-        auto go = [&](auto mt_c, auto u_c, auto w_c) {
+        auto go = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
             constexpr int W = decltype(w_c)::value;
-            hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, 1, decltype(u_c)::value, W, TYPE>), dim3(static_cast<unsigned>((p.N + 15) / 16)), dim3(64 * W), 0, s, p);
+            hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, 1, decltype(u_c)::value, W, TYPE, decltype(fused_c)::value>), dim3(static_cast<unsigned>((p.N + 15) / 16)),
+                               dim3(64 * W), 0, s, g);
         };
-        // as many waves of a workgroup as leave all of its panels in flight and two (four) workgroups on a CU
-        auto waves = [&](auto mt_c, auto u_c, auto most_c) {
-            if (p.panels > 4) go(mt_c, u_c, most_c);
-            else if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{});
-            else go(mt_c, IC<1>{}, IC<1>{});
+        auto sized = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
+            if (p.panels > 8 * decltype(u_c)::value / 2) go(mt_c, u_c, w_c, fused_c);
+            else if (p.panels > 4) go(mt_c, IC<1>{}, IC<8>{}, fused_c);
+            else if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{}, fused_c);
+            else go(mt_c, IC<1>{}, IC<1>{}, fused_c);
         };
-        if (p.M <= 16) waves(IC<1>{}, IC<4>{}, IC<8>{});
-        else if (p.M <= 32) waves(IC<2>{}, IC<2>{}, IC<4>{});
-        else if (p.M <= 48) waves(IC<3>{}, IC<2>{}, IC<4>{});
-        else waves(IC<4>{}, IC<2>{}, IC<4>{});
+        if (fused && p.M == 1) sized(IC<1>{}, IC<4>{}, IC<8>{}, IC<1>{});
+        else if (fused && p.M == 2) sized(IC<1>{}, IC<3>{}, IC<8>{}, IC<2>{});
+        else if (fused) sized(IC<1>{}, IC<3>{}, IC<8>{}, IC<4>{});
+        else if (p.M <= 16) sized(IC<1>{}, IC<2>{}, IC<8>{}, IC<0>{});
+        else if (p.M <= 32) sized(IC<2>{}, IC<2>{}, IC<4>{}, IC<0>{});
+        else if (p.M <= 48) sized(IC<3>{}, IC<2>{}, IC<4>{}, IC<0>{});
+        else sized(IC<4>{}, IC<1>{}, IC<4>{}, IC<0>{});
     });
     return launch_status();
 }
@@ -550,25 +536,18 @@ static int rows_launch(const Mx4Product& p, int type, hipStream_t s) {
 bool mx4_is_fused(int64_t M) { return M <= kTokens; }
 // Y = X B^T for X as it is, up to kTokens rows of it: one launch, no workspace
 int mx4_fused_launch(int type, const void* x, int64_t ldx, int64_t M, const fxp_mx4& B, void* y, int64_t ldy, hipStream_t s) {
-    const Mx4Vector g{{B.data, B.scales, static_cast<int>(B.rows)}, static_cast<int>(M), static_cast<int>(B.rows), static_cast<int>(B.cols), static_cast<int>(mx_panels(B.cols)),
-                      aligned(x, 4 * static_cast<size_t>(elem_size(type))) && (M == 1 || ldx % 4 == 0), x, ldx, y, ldy};
-    by_type(type, [&](auto type_c) {
-        auto go = [&](auto mr_c, auto u_c, auto w_c) {
-            constexpr int W = decltype(w_c)::value;
-            hipLaunchKernelGGL((k_mx4_vector<decltype(mr_c)::value, decltype(u_c)::value, W, decltype(type_c)::value>), dim3(static_cast<unsigned>((g.N + 15) / 16)), dim3(64 * W), 0, s,
-                               g);
-        };
-        auto sized = [&](auto mr_c) {
-            if (g.panels > 16) go(mr_c, IC<4>{}, IC<8>{});
-            else if (g.panels > 8) go(mr_c, IC<2>{}, IC<8>{});
-            else if (g.panels > 4) go(mr_c, IC<1>{}, IC<8>{});
-            else go(mr_c, IC<1>{}, IC<4>{});
-        };
-        if (M == 1) sized(IC<1>{});
-        else if (M == 2) sized(IC<2>{});
-        else sized(IC<4>{});
-    });
-    return launch_status();
+    Mx4Rows g{};
+    g.p.b = {B.data, B.scales, static_cast<int>(B.rows)};
+    g.p.M = static_cast<int>(M);
+    g.p.N = static_cast<int>(B.rows);
+    g.p.panels = static_cast<int>(mx_panels(B.cols));
+    g.p.c = y;
+    g.p.ldc = ldy;
+    g.x = x;
+    g.ldx = ldx;
+    g.K = static_cast<int>(B.cols);
+    g.vec = aligned(x, 4 * static_cast<size_t>(elem_size(type))) && (M == 1 || ldx % 4 == 0);
+    return rows_launch(g, true, type, s);
 }
 
 int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s) {
@@ -583,7 +562,7 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.per_split = plan.per_split;
     p.c = C;
     p.ldc = ldc;
-    if (plan.rows) return rows_launch(p, type, s);
+    if (plan.rows) return rows_launch({p, nullptr, 0, 0, 0}, false, type, s);
     const bool parts = plan.splits > 1;
     if (parts) {
         p.c = ws;
