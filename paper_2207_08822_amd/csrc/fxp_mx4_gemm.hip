@@ -59,6 +59,7 @@ struct Mx4Product {
     void* c;
     int64_t ldc, split_stride;          // of partial sums, in elements: 0 where there is one part
     int tiles_m, tiles_n, group_m;
+    int vec;                            // rows of C of two bytes begin and end on multiples of 16 bytes
 };
 
 template <int TYPE>
@@ -66,35 +67,26 @@ __device__ inline void store_one(void* c, int64_t at, float v) {
     static_cast<typename Elem<TYPE>::T*>(c)[at] = static_cast<typename Elem<TYPE>::T>(v);
 }
 
-// The fragments of a wave to C from row row0, column col0 on: register r of a lane is row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32 of its fragment.
-template <int TYPE, int FM, int FN>
-__device__ inline void store_tile(const Mx4Product& p, const v16f (&acc)[FM][FN], int row0, int col0, int fhalf, int frow) {
-    const int64_t base = static_cast<int64_t>(blockIdx.y) * p.split_stride + (row0 + 4 * fhalf) * p.ldc + col0 + frow;
-    const bool inside = row0 + 32 * FM <= p.M && col0 + 32 * FN <= p.N;              // uniform
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int dr = 32 * i + 8 * (r >> 2) + (r & 3);
-            if (!inside && row0 + 4 * fhalf + dr >= p.M) continue;
-            const int64_t at = base + dr * p.ldc;
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-                if (inside || col0 + 32 * j + frow < p.N) store_one<TYPE>(p.c, at + 32 * j, acc[i][j][r]);
-        }
-}
-
 // ---- tiles ----
 //
-// BM x BN outputs a workgroup, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's bound).  16-byte pieces of a row
-// of 128 bytes are exchanged by the row, so that a fragment's reads spread over all banks.
+// BM x BN outputs a workgroup in waves of WM x WN, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's
+// bound).  16-byte pieces of a row of 128 bytes are exchanged by the row, so that a fragment's reads spread over all banks.
+//
+// A wave holds the fragments of two quarters of a panel: those of the next quarter are read while one is multiplied, across the barrier too, which stands before a
+// panel's last quarter.  Behind it the slot of this panel is free: the next one's loads into it are spread over the multiplications of that quarter and of the first of the
+// next panel.  (Reading a quarter and then multiplying it, a workgroup alone on its CU took 1600 clocks a panel of 128 x 128 where its products are 512.)
+//
+// Outputs of two bytes: the operands change places, so that a lane has four neighbouring columns, and the wave's tile goes through LDS to leave in 16-byte pieces of whole
+// rows.  fp32 leaves directly, 128 bytes in a row of C a store.
 template <int BM, int BN, int WM, int WN, int STAGES, int TYPE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Product p) {
     constexpr int NW = (BM / WM) * (BN / WN), FM = WM / 32, FN = WN / 32;
-    constexpr int kCodes = (BM + BN) * kMxRowBytes, kScales = (BM + BN) * kMxRowScales, kStage = kCodes + kScales;
+    constexpr int kCodesA = BM * kMxRowBytes, kCodes = (BM + BN) * kMxRowBytes, kStage = kCodes + (BM + BN) * kMxRowScales;
     constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LS = (BM + BN) / 32 / NW, kLoads = LA + LB + LS;       // loads of a wave a panel
+    constexpr bool kTwoBytes = TYPE != FXP_F32;
+    constexpr int kOutStride = WN * 2 + 16, kOut = WM * kOutStride;                                          // a wave's outputs of two bytes
     static_assert(LA * 8 * NW == BM && LB * 8 * NW == BN && LS * 32 * NW == BM + BN, "waves load as much");
-    static_assert(kLoads * (STAGES - 1) < 64, "loads in flight");
+    static_assert(kLoads * (STAGES - 1) < 64 && NW * kOut <= STAGES * kStage, "loads in flight, room for outputs");
     __shared__ __attribute__((aligned(1024))) uint8_t lds[STAGES * kStage];
 
     int tm, tn;
@@ -115,110 +107,28 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
         const int row = (wave + j * NW) * 8 + lane / 8;
         off_b[j] = (n0 + row) * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
     }
-    auto issue = [&](int t) {
+    auto slot_of = [&](int t) { return lds + (t % STAGES) * kStage; };
+    // past the last panel: no memory access, zeros
+    auto issue_a = [&](int t) {
         const int64_t panel = first + t;
-        const bool there = t < panels;                              // past the last: no memory access, zeros
-        uint8_t* const stage = lds + (t % STAGES) * kStage;
-        const int size_a = there ? p.a.rows * kMxRowBytes : 0, size_b = there ? p.b.rows * kMxRowBytes : 0;
-        const uint8_t* const a = p.a.data + panel * p.a.rows * kMxRowBytes;
-        const uint8_t* const b = p.b.data + panel * p.b.rows * kMxRowBytes;
 #pragma unroll
-        for (int j = 0; j < LA; ++j) load_to_lds<16>(a, size_a, off_a[j], stage + (wave + j * NW) * 1024);
+        for (int j = 0; j < LA; ++j)
+            load_to_lds<16>(p.a.data + panel * p.a.rows * kMxRowBytes, t < panels ? p.a.rows * kMxRowBytes : 0, off_a[j], slot_of(t) + (wave + j * NW) * 1024);
+    };
+    auto issue_b = [&](int t) {
+        const int64_t panel = first + t;
 #pragma unroll
-        for (int j = 0; j < LB; ++j) load_to_lds<16>(b, size_b, off_b[j], stage + BM * kMxRowBytes + (wave + j * NW) * 1024);
+        for (int j = 0; j < LB; ++j)
+            load_to_lds<16>(p.b.data + panel * p.b.rows * kMxRowBytes, t < panels ? p.b.rows * kMxRowBytes : 0, off_b[j], slot_of(t) + kCodesA + (wave + j * NW) * 1024);
 #pragma unroll
         for (int j = 0; j < LS; ++j) {
-            const int i = wave + j * NW;                            // 256 bytes: 32 rows
+            const int i = wave + j * NW;                            // 256 bytes: 32 rows of scales
             const bool of_a = i < BM / 32;
             const Mx4Operand& o = of_a ? p.a : p.b;
-            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, there ? o.rows * kMxRowScales : 0,
-                           (of_a ? m0 + 32 * i : n0 + 32 * (i - BM / 32)) * kMxRowScales + 4 * lane, stage + kCodes + 256 * i);
+            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, t < panels ? o.rows * kMxRowScales : 0,
+                           (of_a ? m0 + 32 * i : n0 + 32 * (i - BM / 32)) * kMxRowScales + 4 * lane, slot_of(t) + kCodes + 256 * i);
         }
     };
-
-    v16f acc[FM][FN];
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = {};
-    const int frow = lane & 31, fhalf = lane >> 5, fswz = swizzle_of_row<kMxRowBytes>(frow);
-#pragma unroll
-    for (int t = 0; t < STAGES - 1; ++t) issue(t);
-    for (int t = 0; t < panels; ++t) {
-        wait_loads_and_lds<(STAGES - 2) * kLoads>();
-        barrier();
-        issue(t + STAGES - 1);
-        const uint8_t* const stage = lds + (t % STAGES) * kStage;
-        const uint8_t* const sa = stage + (wm0 + frow) * kMxRowBytes;
-        const uint8_t* const sb = stage + (BM + wn0 + frow) * kMxRowBytes;
-        const uint8_t* const se = stage + kCodes + 4 * fhalf;
-        int ea[FM], eb[FN];
-#pragma unroll
-        for (int i = 0; i < FM; ++i) ea[i] = *reinterpret_cast<const int*>(se + (wm0 + 32 * i + frow) * kMxRowScales);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) eb[j] = *reinterpret_cast<const int*>(se + (BM + wn0 + 32 * j + frow) * kMxRowScales);
-        auto quarter = [&](auto ks_c) {
-            constexpr int KS = decltype(ks_c)::value;
-            const int piece = ((2 * KS + fhalf) ^ fswz) * 16;
-            v4i fa[FM], fb[FN];
-#pragma unroll
-            for (int i = 0; i < FM; ++i) fa[i] = *reinterpret_cast<const v4i*>(sa + i * 32 * kMxRowBytes + piece);
-#pragma unroll
-            for (int j = 0; j < FN; ++j) fb[j] = *reinterpret_cast<const v4i*>(sb + j * 32 * kMxRowBytes + piece);
-#pragma unroll
-            for (int i = 0; i < FM; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mfma32<KS, KS>(fa[i], fb[j], acc[i][j], ea[i], eb[j]);
-        };
-        quarter(IC<0>{});
-        quarter(IC<1>{});
-        quarter(IC<2>{});
-        quarter(IC<3>{});
-    }
-    wait_loads_and_lds<0>();                                        // none into LDS may outlive the workgroup
-
-    store_tile<TYPE, FM, FN>(p, acc, m0 + wm0, n0 + wn0, fhalf, frow);
-}
-
-// ---- large tiles ----
-//
-// 256 x 256 outputs, eight waves of 64 x 128, two panels in LDS.  A wave holds the fragments of two quarters of a panel: those of the next quarter are read while
-// one is multiplied, across the barrier too, which stands before a panel's last quarter.  Behind it the panel after next goes where this one was: its loads are spread
-// over the multiplications of that quarter and the next and have most of a panel's time.
-template <int WM, int WN, int TYPE>
-__global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4Product p) {
-    constexpr int B = 256, NW = (B / WM) * (B / WN), FM = WM / 32, FN = WN / 32;
-    constexpr int kCodes = 2 * B * kMxRowBytes, kStage = kCodes + 2 * B * kMxRowScales, L = B / 8 / NW, LS = B / 32 / NW;
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[2 * kStage];
-
-    int tm, tn;
-    tile_of_block(static_cast<int>(blockIdx.x), p.tiles_m, p.tiles_n, p.group_m, &tm, &tn);
-    const int m0 = tm * B, n0 = tn * B;
-    const int first = static_cast<int>(blockIdx.y) * p.per_split, panels = min(p.per_split, p.panels - first);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wm0 = (wave / (B / WN)) * WM, wn0 = (wave % (B / WN)) * WN;
-
-    int off_a[L], off_b[L];
-#pragma unroll
-    for (int j = 0; j < L; ++j) {
-        const int row = (wave + j * NW) * 8 + lane / 8, piece = ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
-        off_a[j] = (m0 + row) * kMxRowBytes + piece;
-        off_b[j] = (n0 + row) * kMxRowBytes + piece;
-    }
-    const int off_sa = (m0 + 32 * wave) * kMxRowScales + 4 * lane, off_sb = (n0 + 32 * wave) * kMxRowScales + 4 * lane;       // 32 rows of scales a load
-    auto issue = [&](const Mx4Operand& o, int t, const int (&off)[L], int off_s, int at, int at_s) {
-        const int64_t panel = first + t;
-        const bool there = t < panels;                              // past the last: no memory access, zeros
-        uint8_t* const stage = lds + (t & 1) * kStage;
-        const uint8_t* const codes = o.data + panel * o.rows * kMxRowBytes;
-#pragma unroll
-        for (int j = 0; j < L; ++j) load_to_lds<16>(codes, there ? o.rows * kMxRowBytes : 0, off[j], stage + at + (wave + j * NW) * 1024);
-#pragma unroll
-        for (int j = 0; j < LS; ++j)
-            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, there ? o.rows * kMxRowScales : 0, off_s + j * NW * 256, stage + at_s + (wave + j * NW) * 256);
-    };
-    auto issue_a = [&](int t) { issue(p.a, t, off_a, off_sa, 0, kCodes); };
-    auto issue_b = [&](int t) { issue(p.b, t, off_b, off_sb, B * kMxRowBytes, kCodes + B * kMxRowScales); };
 
     v16f acc[FM][FN];
 #pragma unroll
@@ -230,19 +140,19 @@ __global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4P
     int ea[FM], eb[FN], next_a[FM], next_b[FN];
     auto read = [&](auto buf_c, int t, auto ks_c) {
         constexpr int BUF = decltype(buf_c)::value, KS = decltype(ks_c)::value;
-        const uint8_t* const stage = lds + (t & 1) * kStage;
+        const uint8_t* const stage = slot_of(t);
         const int piece = ((2 * KS + fhalf) ^ fswz) * 16;
 #pragma unroll
         for (int i = 0; i < FM; ++i) fa[BUF][i] = *reinterpret_cast<const v4i*>(stage + (wm0 + 32 * i + frow) * kMxRowBytes + piece);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[BUF][j] = *reinterpret_cast<const v4i*>(stage + (B + wn0 + 32 * j + frow) * kMxRowBytes + piece);
+        for (int j = 0; j < FN; ++j) fb[BUF][j] = *reinterpret_cast<const v4i*>(stage + (BM + wn0 + 32 * j + frow) * kMxRowBytes + piece);
     };
     auto read_scales = [&](int t) {
-        const uint8_t* const at = lds + (t & 1) * kStage + kCodes + 4 * fhalf;
+        const uint8_t* const at = slot_of(t) + kCodes + 4 * fhalf;
 #pragma unroll
         for (int i = 0; i < FM; ++i) next_a[i] = *reinterpret_cast<const int*>(at + (wm0 + 32 * i + frow) * kMxRowScales);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) next_b[j] = *reinterpret_cast<const int*>(at + (B + wn0 + 32 * j + frow) * kMxRowScales);
+        for (int j = 0; j < FN; ++j) next_b[j] = *reinterpret_cast<const int*>(at + (BM + wn0 + 32 * j + frow) * kMxRowScales);
     };
     auto take_scales = [&] {
 #pragma unroll
@@ -251,29 +161,35 @@ __global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4P
         for (int j = 0; j < FN; ++j) eb[j] = next_b[j];
     };
     auto multiply = [&](auto buf_c, auto ks_c, auto reads_c, auto loads_c) {
-        constexpr int BUF = decltype(buf_c)::value, KS = decltype(ks_c)::value, reads = decltype(reads_c)::value, loads = decltype(loads_c)::value;
+        constexpr int BUF = decltype(buf_c)::value, KS = decltype(ks_c)::value;
+        constexpr int reads = decltype(reads_c)::value / 2, loads = decltype(loads_c)::value, rest = FM * FN - reads - loads;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
 #pragma unroll
-            for (int j = 0; j < FN; ++j) acc[i][j] = mfma32<KS, KS>(fa[BUF][i], fb[BUF][j], acc[i][j], ea[i], eb[j]);
-        // one multiplication, then two reads of LDS or a load, and so on
+            for (int j = 0; j < FN; ++j)
+                acc[i][j] = kTwoBytes ? mfma32<KS, KS>(fb[BUF][j], fa[BUF][i], acc[i][j], eb[j], ea[i]) : mfma32<KS, KS>(fa[BUF][i], fb[BUF][j], acc[i][j], ea[i], eb[j]);
+        if constexpr (rest >= 0) {                                  // one multiplication, then two reads of LDS or a load, and so on
 #pragma unroll
-        for (int n = 0; n < reads / 2; ++n) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        }
+            for (int n = 0; n < reads; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
 #pragma unroll
-        for (int n = 0; n < loads; ++n) {
-            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            for (int n = 0; n < loads; ++n) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
+            if constexpr (rest > 0) __builtin_amdgcn_sched_group_barrier(0x008, rest, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - reads / 2 - loads, 0);
     };
 
-    issue_a(0);
-    issue_b(0);
-    issue_a(1);
-    wait_loads_and_lds<L + LS>();
+#pragma unroll
+    for (int t = 0; t + 1 < STAGES; ++t) {
+        issue_a(t);
+        issue_b(t);
+    }
+    issue_a(STAGES - 1);
+    wait_loads_and_lds<(STAGES - 2) * kLoads + LA>();
     barrier();
     if (panels > 0) {
         read_scales(0);
@@ -282,18 +198,18 @@ __global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4P
         int t = 0;
         for (; t + 1 < panels; ++t) {
             read(IC<1>{}, t, IC<1>{});
-            issue_b(t + 1);
-            multiply(IC<0>{}, IC<0>{}, IC<FM + FN>{}, IC<L + LS>{});
+            issue_b(t + STAGES - 1);
+            multiply(IC<0>{}, IC<0>{}, IC<FM + FN>{}, IC<LB + LS>{});
             read(IC<0>{}, t, IC<2>{});
             multiply(IC<1>{}, IC<1>{}, IC<FM + FN>{}, IC<0>{});
             read(IC<1>{}, t, IC<3>{});
             multiply(IC<0>{}, IC<2>{}, IC<FM + FN>{}, IC<0>{});
-            wait_loads_and_lds<0>();
+            wait_loads_and_lds<(STAGES - 2) * kLoads>();            // the next panel is there, and this one read
             barrier();
             read_scales(t + 1);
             read(IC<0>{}, t + 1, IC<0>{});
-            issue_a(t + 2);
-            multiply(IC<1>{}, IC<3>{}, IC<FM + FN>{}, IC<L + LS>{});
+            issue_a(t + STAGES);
+            multiply(IC<1>{}, IC<3>{}, IC<FM + FN>{}, IC<LA>{});
             take_scales();
         }
         read(IC<1>{}, t, IC<1>{});
@@ -305,17 +221,85 @@ __global__ __launch_bounds__((256 / WM) * (256 / WN) * 64) void k_mx4_large(Mx4P
         multiply(IC<1>{}, IC<3>{}, IC<0>{}, IC<0>{});
     }
     wait_loads_and_lds<0>();                                        // none into LDS may outlive the workgroup
-    store_tile<TYPE, FM, FN>(p, acc, m0 + wm0, n0 + wn0, fhalf, frow);
+
+    const int row0 = m0 + wm0, col0 = n0 + wn0;
+    if constexpr (!kTwoBytes) {
+        // register r of a lane: row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32 of its fragment
+        const int64_t base = static_cast<int64_t>(blockIdx.y) * p.split_stride + (row0 + 4 * fhalf) * p.ldc + col0 + frow;
+        const bool inside = row0 + WM <= p.M && col0 + WN <= p.N;              // uniform
+        float* const c = static_cast<float*>(p.c) + base;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int dr = 32 * i + 8 * (r >> 2) + (r & 3);
+                if (!inside && row0 + 4 * fhalf + dr >= p.M) continue;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    if (inside || col0 + 32 * j + frow < p.N) c[dr * p.ldc + 32 * j] = acc[i][j][r];
+            }
+    } else {
+        // row lane % 32, column 8 (r / 4) + 4 (lane / 32) + r % 4
+        using T = typename Elem<TYPE>::T;
+        typedef T Four __attribute__((ext_vector_type(4)));
+        if (!p.vec) {
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+                const int row = row0 + 32 * i + frow;
+                if (row >= p.M) continue;
+                T* const c = static_cast<T*>(p.c) + row * p.ldc;
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int col = col0 + 32 * j + 8 * (r >> 2) + 4 * fhalf + (r & 3);
+                        if (col < p.N) c[col] = static_cast<T>(acc[i][j][r]);
+                    }
+            }
+            return;
+        }
+        barrier();                                                  // every wave is done with the panels
+        uint8_t* const mine = lds + wave * kOut;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    Four v;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) v[k] = static_cast<T>(acc[i][j][4 * q + k]);
+                    *reinterpret_cast<Four*>(mine + (32 * i + frow) * kOutStride + (32 * j + 8 * q + 4 * fhalf) * 2) = v;
+                }
+        wave_barrier();
+        constexpr int kPieces = WN / 8;                             // of 16 bytes in a row
+#pragma unroll
+        for (int n = 0; n < WM * kPieces / 64; ++n) {
+            const int row = (n * 64 + lane) / kPieces, piece = lane % kPieces;
+            if (row0 + row < p.M && col0 + 8 * piece < p.N)         // whole pieces: N is a multiple of eight
+                *reinterpret_cast<v4i*>(static_cast<T*>(p.c) + (row0 + row) * p.ldc + col0 + 8 * piece) = *reinterpret_cast<const v4i*>(mine + row * kOutStride + piece * 16);
+        }
+    }
 }
 
-// partial sums [parts][M * N] added in order
+// Partial sums added in order: rows of `cols` elements, the parts' without gaps, four elements a thread where rows begin on a multiple of four.
 template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts, int count, int64_t stride, int M, int N, void* c, int64_t ldc) {
-    const int64_t i = int64_t{blockIdx.x} * 256 + threadIdx.x;
-    if (i >= int64_t{M} * N) return;
-    float s = 0.0f;
-    for (int n = 0; n < count; ++n) s += parts[n * stride + i];
-    store_one<TYPE>(c, i / N * ldc + i % N, s);
+__global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts, int count, int64_t stride, int cols, int vec, void* c, int64_t ldc) {
+    const int i = static_cast<int>(blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= cols) return;
+    const int64_t from = static_cast<int64_t>(blockIdx.y) * cols + i, to = static_cast<int64_t>(blockIdx.y) * ldc + i;
+    if (vec && i + 4 <= cols) {
+        v4f s = {};
+#pragma unroll 4
+        for (int n = 0; n < count; ++n) s += *reinterpret_cast<const v4f*>(parts + n * stride + from);
+        store4<TYPE>(c, to, vec > 1, {s[0], s[1], s[2], s[3]});
+    } else {
+        for (int j = 0; j < 4 && i + j < cols; ++j) {
+            float s = 0.0f;
+            for (int n = 0; n < count; ++n) s += parts[n * stride + from + j];
+            store_one<TYPE>(c, to + j, s);
+        }
+    }
 }
 
 // ---- a few rows ----
@@ -480,11 +464,10 @@ struct Mx4Plan {
 };
 static Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K) {
     const int64_t panels = mx_panels(K);
-    Mx4Plan p{M <= kRowsMost, 128, 1, static_cast<int>(panels)};
+    Mx4Plan p{M <= kRowsMost, 256, 1, static_cast<int>(panels)};
     if (p.rows) return p;
     auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-    if (tiles(256) >= 512) p.tile = 256;
-    else if (tiles(128) < 256) p.tile = 64;
+    if (tiles(256) < 128) p.tile = tiles(128) < 256 ? 64 : 128;
     const int64_t count = tiles(p.tile);
     if (count < 256 && panels >= 8) {
         const int64_t want = std::min<int64_t>(panels / 4, (512 + count - 1) / count);
@@ -493,10 +476,12 @@ static Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K) {
     }
     return p;
 }
+// of one part: parts begin on 16 bytes
+static int64_t part_elements(int64_t M, int64_t N) { return (M * N + 3) / 4 * 4; }
 
 size_t mx4_gemm_bytes(int64_t M, int64_t N, int64_t K) {
     const Mx4Plan p = mx4_plan(M, N, K);
-    return p.splits > 1 ? round_up(static_cast<size_t>(p.splits) * M * N * sizeof(float), 256) : 0;
+    return p.splits > 1 ? round_up(static_cast<size_t>(p.splits) * part_elements(M, N) * sizeof(float), 256) : 0;
 }
 
 template <typename F>
@@ -567,24 +552,29 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     if (parts) {
         p.c = ws;
         p.ldc = N;
-        p.split_stride = M * N;
+        p.split_stride = part_elements(M, N);
     }
     const int t = plan.tile;
     p.tiles_m = static_cast<int>((M + t - 1) / t);
     p.tiles_n = static_cast<int>((N + t - 1) / t);
     p.group_m = 8;
+    p.vec = aligned(C, 16) && ldc % 8 == 0 && N % 8 == 0;
     const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
     by_type(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
-        if (t == 256) hipLaunchKernelGGL((k_mx4_large<64, 128, TYPE>), grid, dim3(512), 0, s, p);
+        if (t == 256) hipLaunchKernelGGL((k_mx4_tiles<256, 256, 64, 128, 2, TYPE>), grid, dim3(512), 0, s, p);
         else if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
         else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
     });
-    if (parts)
+    if (parts) {
+        const bool flat = ldc == N && M * N < int64_t{1} << 31;          // one row
+        const int64_t rows = flat ? 1 : M, cols = flat ? M * N : N;
         by_type(type, [&](auto type_c) {
-            hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(static_cast<unsigned>((M * N + 255) / 256)), dim3(256), 0, s, static_cast<const float*>(ws), plan.splits,
-                               p.split_stride, p.M, p.N, C, ldc);
+            const int vec = cols % 4 == 0 || flat ? (aligned(C, 4 * static_cast<size_t>(elem_size(type))) && (flat || ldc % 4 == 0) ? 2 : 1) : 0;
+            hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(static_cast<unsigned>((cols + 1023) / 1024), static_cast<unsigned>(rows)), dim3(256), 0, s,
+                               static_cast<const float*>(ws), plan.splits, p.split_stride, static_cast<int>(cols), vec, C, ldc);
         });
+    }
     return launch_status();
 }
 
