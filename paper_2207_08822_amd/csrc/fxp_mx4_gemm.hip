@@ -96,36 +96,28 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm0 = (wave / (BN / WN)) * WM, wn0 = (wave % (BN / WN)) * WN;
 
-    int off_a[LA], off_b[LB];
-#pragma unroll
-    for (int j = 0; j < LA; ++j) {
-        const int row = (wave + j * NW) * 8 + lane / 8;
-        off_a[j] = (m0 + row) * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
-    }
-#pragma unroll
-    for (int j = 0; j < LB; ++j) {
-        const int row = (wave + j * NW) * 8 + lane / 8;
-        off_b[j] = (n0 + row) * kMxRowBytes + ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row)) * 16;
-    }
+    // a wave's loads are NW x 8 rows apart (the exchange of pieces has a period of 16): one offset for all, the steps in the base
+    const int row_l = wave * 8 + lane / 8, piece_l = ((lane % 8) ^ swizzle_of_row<kMxRowBytes>(row_l)) * 16;
+    const int off_a = (m0 + row_l) * kMxRowBytes + piece_l, off_b = (n0 + row_l) * kMxRowBytes + piece_l;
     auto slot_of = [&](int t) { return lds + (t % STAGES) * kStage; };
+    auto codes = [&](const Mx4Operand& o, int t, int j, int off, uint8_t* to) {
+        const int size = o.rows * kMxRowBytes, step = j * NW * 1024;
+        load_to_lds<16>(o.data + static_cast<int64_t>(first + t) * size + step, t < panels ? max(size - step, 0) : 0, off, to + wave * 1024 + step);
+    };
     // past the last panel: no memory access, zeros
     auto issue_a = [&](int t) {
-        const int64_t panel = first + t;
 #pragma unroll
-        for (int j = 0; j < LA; ++j)
-            load_to_lds<16>(p.a.data + panel * p.a.rows * kMxRowBytes, t < panels ? p.a.rows * kMxRowBytes : 0, off_a[j], slot_of(t) + (wave + j * NW) * 1024);
+        for (int j = 0; j < LA; ++j) codes(p.a, t, j, off_a, slot_of(t));
     };
     auto issue_b = [&](int t) {
-        const int64_t panel = first + t;
 #pragma unroll
-        for (int j = 0; j < LB; ++j)
-            load_to_lds<16>(p.b.data + panel * p.b.rows * kMxRowBytes, t < panels ? p.b.rows * kMxRowBytes : 0, off_b[j], slot_of(t) + kCodesA + (wave + j * NW) * 1024);
+        for (int j = 0; j < LB; ++j) codes(p.b, t, j, off_b, slot_of(t) + kCodesA);
 #pragma unroll
         for (int j = 0; j < LS; ++j) {
             const int i = wave + j * NW;                            // 256 bytes: 32 rows of scales
             const bool of_a = i < BM / 32;
             const Mx4Operand& o = of_a ? p.a : p.b;
-            load_to_lds<4>(o.scales + panel * o.rows * kMxRowScales, t < panels ? o.rows * kMxRowScales : 0,
+            load_to_lds<4>(o.scales + static_cast<int64_t>(first + t) * o.rows * kMxRowScales, t < panels ? o.rows * kMxRowScales : 0,
                            (of_a ? m0 + 32 * i : n0 + 32 * (i - BM / 32)) * kMxRowScales + 4 * lane, slot_of(t) + kCodes + 256 * i);
         }
     };
