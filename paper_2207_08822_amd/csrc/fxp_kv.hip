@@ -417,6 +417,7 @@ struct RotaryWriter {
     void* out;
     int64_t q_token, q_head, out_token, out_head;
     int group, vec_q;       // query heads of a head of the cache; 0: no queries
+    uint32_t by_group;      // ceil(2^32 / group)
 };
 
 // Item i of a head: eight elements, four pairs of them or eight that stay.  Element j is `first` + j, or `second` + j - 4 from the fourth on.
@@ -435,9 +436,9 @@ __device__ inline bool has_element(const Piece& p, int j) {
     return p.pairs ? (NEAR ? j / 2 : j % 4) < p.pairs : j < p.elements;
 }
 
-// the elements of an item, turned; at: of the head's first element
-template <int TYPE, typename F, bool NEAR>
-__device__ inline void turned_piece(const RotaryWriter& r, const void* x, int64_t at, int position, bool vec, F amplitude, int i, const Piece& p, F (&y)[8]) {
+// the elements of an item; at: of the head's first element
+template <int TYPE, bool NEAR>
+__device__ inline void load_piece(const RotaryWriter& r, const void* x, int64_t at, bool vec, const Piece& p, float (&y)[8]) {
     if (r.whole) {
         float a[4], b[4];
         load_elems<TYPE, 4>(x, at + p.first, vec, a);
@@ -450,9 +451,13 @@ __device__ inline void turned_piece(const RotaryWriter& r, const void* x, int64_
     } else {
         const typename Elem<TYPE>::T* const row = static_cast<const typename Elem<TYPE>::T*>(x) + at;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = has_element<NEAR>(p, j) ? static_cast<F>(static_cast<float>(row[j < 4 ? p.first + j : p.second + j - 4])) : F(0);
+        for (int j = 0; j < 8; ++j) y[j] = has_element<NEAR>(p, j) ? static_cast<float>(row[j < 4 ? p.first + j : p.second + j - 4]) : 0.0f;
     }
-    if (p.pairs == 0) return;
+}
+// turned, if it is one of pairs
+template <typename F, bool NEAR>
+__device__ inline void turn_piece(const RotaryWriter& r, int position, F amplitude, int i, F (&y)[8]) {
+    if (i >= r.turned) return;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         F c, s;
@@ -476,23 +481,43 @@ __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& 
     constexpr int kKept = THREADS == 64 ? 2 : 4;         // items that a thread keeps; others are turned again
     double kept[kKept][8];
     uint32_t m = 0;
-    auto fetch = [&](int n, double (&y)[8]) {
-        const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces)), i = n - t * pieces;
-        turned_piece<TYPE, double, NEAR>(r, x, row0 + t * token, r.positions[run.first + t], vec, r.amplitude, i, piece_of<NEAR>(r, i), y);
+    struct Place {
+        int t, i;
+    };
+    auto place_of = [&](int n) {
+        const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces));
+        return Place{t, n - t * pieces};
+    };
+    auto fetch = [&](int n, float (&x8)[8], int& position) {
+        const Place at = place_of(n);
+        load_piece<TYPE, NEAR>(r, x, row0 + at.t * token, vec, piece_of<NEAR>(r, at.i), x8);
+        position = r.positions[run.first + at.t];
+    };
+    auto turn = [&](int n, const float (&x8)[8], int position, double (&y)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x8[j];
+        turn_piece<double, NEAR>(r, position, r.amplitude, place_of(n).i, y);
     };
     auto largest = [&](const double (&y)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = max(m, high_word(y[j]));
     };
+    // what is kept is loaded all at once
+    float raw[kKept][8];
+    int positions[kKept];
+#pragma unroll
+    for (int n = 0; n < kKept; ++n)
+        if (static_cast<int>(threadIdx.x) + n * THREADS < work) fetch(threadIdx.x + n * THREADS, raw[n], positions[n]);
 #pragma unroll
     for (int n = 0; n < kKept; ++n)
         if (static_cast<int>(threadIdx.x) + n * THREADS < work) {
-            fetch(threadIdx.x + n * THREADS, kept[n]);
+            turn(threadIdx.x + n * THREADS, raw[n], positions[n], kept[n]);
             largest(kept[n]);
         }
-    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+    for (int n = threadIdx.x + kKept * THREADS; n < work; n += THREADS) {
         double y[8];
-        fetch(i, y);
+        fetch(n, raw[0], positions[0]);
+        turn(n, raw[0], positions[0], y);
         largest(y);
     }
     m = THREADS == 64 ? wave_max(m) : block_max<THREADS / 64>(m, lds);
@@ -501,8 +526,8 @@ __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& 
     if (threadIdx.x == 0) *scale = e;
     const double unit = ldexp(1.0, 125 + c.bits - e), most = static_cast<double>((1 << (c.bits - 1)) - 1);
     auto write = [&](int n, const double (&y)[8]) {
-        const int t = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces));
-        const Piece p = piece_of<NEAR>(r, n - t * pieces);
+        const Place at = place_of(n);
+        const Piece p = piece_of<NEAR>(r, at.i);
         uint32_t b[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -510,7 +535,7 @@ __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& 
             const int v = static_cast<int>(z > most ? most : z);         // NaN: 0
             b[j] = static_cast<uint32_t>(y[j] < 0 ? -v : v);
         }
-        uint32_t* const row = page + (run.offset + t) * (dim / 4);
+        uint32_t* const row = page + (run.offset + at.t) * (dim / 4);
         if (r.whole) {
             row[p.first / 4] = perm(perm(b[3], b[2], 0x0c0c0400u), perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
             row[p.second / 4] = perm(perm(b[7], b[6], 0x0c0c0400u), perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
@@ -523,36 +548,53 @@ __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& 
 #pragma unroll
     for (int n = 0; n < kKept; ++n)
         if (static_cast<int>(threadIdx.x) + n * THREADS < work) write(threadIdx.x + n * THREADS, kept[n]);
-    for (int i = threadIdx.x + kKept * THREADS; i < work; i += THREADS) {
+    for (int n = threadIdx.x + kKept * THREADS; n < work; n += THREADS) {
         double y[8];
-        fetch(i, y);
-        write(i, y);
+        fetch(n, raw[0], positions[0]);
+        turn(n, raw[0], positions[0], y);
+        write(n, y);
     }
     if (grown && run.offset)
         for (int i = threadIdx.x; i < run.offset * (dim / 4); i += THREADS) page[i] = remap_nearest4(page[i], grown);
 }
 
-// the queries of a run's tokens, of the heads that read one head of the cache
+// The queries of a run's tokens, of the heads that read one head of the cache; a thread's loads of four items go out together (one after the other, a chunk of
+// 64 tokens took the way of one item sixteen times: 9000 tokens of 16 + 4 + 4 heads of 128 46 us).
 template <int TYPE, int THREADS, bool NEAR>
 __device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int head, uint32_t by_pieces) {
     const int rows = run.count * r.group, work = rows * r.pieces;
-    for (int n = threadIdx.x; n < work; n += THREADS) {
-        // heads inside tokens: a step of one token has its heads beside each other
-        const int row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces)), i = n - row * r.pieces;
-        const int t = row / r.group, h = head * r.group + row - t * r.group;
-        const Piece p = piece_of<NEAR>(r, i);
-        float y[8];
-        turned_piece<TYPE, float, NEAR>(r, r.q, (int64_t{run.first} + t) * r.q_token + h * r.q_head, r.positions[run.first + t], r.vec_q,
-                                        static_cast<float>(r.amplitude), i, p, y);
-        const int64_t to = (int64_t{run.first} + t) * r.out_token + h * r.out_head;
-        if (r.whole) {
-            store4<TYPE>(r.out, to + p.first, r.vec_q, {y[0], y[1], y[2], y[3]});
-            store4<TYPE>(r.out, to + p.second, r.vec_q, {y[4], y[5], y[6], y[7]});
-        } else {
-            typename Elem<TYPE>::T* const out = static_cast<typename Elem<TYPE>::T*>(r.out) + to;
+    constexpr int kAhead = 4;
+    for (int n0 = threadIdx.x; n0 < work; n0 += kAhead * THREADS) {
+        float y[kAhead][8];
+        int position[kAhead], t[kAhead], h[kAhead], i[kAhead];
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (has_element<NEAR>(p, j)) out[j < 4 ? p.first + j : p.second + j - 4] = static_cast<typename Elem<TYPE>::T>(y[j]);
+        for (int k = 0; k < kAhead; ++k) {
+            const int n = n0 + k * THREADS;
+            // heads inside tokens: a step of one token has its heads beside each other
+            const int row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces));
+            i[k] = n - row * r.pieces;
+            t[k] = r.group == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), r.by_group));
+            h[k] = head * r.group + row - t[k] * r.group;
+            if (n < work) {
+                load_piece<TYPE, NEAR>(r, r.q, (int64_t{run.first} + t[k]) * r.q_token + h[k] * r.q_head, r.vec_q, piece_of<NEAR>(r, i[k]), y[k]);
+                position[k] = r.positions[run.first + t[k]];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (n0 + k * THREADS >= work) break;
+            turn_piece<float, NEAR>(r, position[k], static_cast<float>(r.amplitude), i[k], y[k]);
+            const Piece p = piece_of<NEAR>(r, i[k]);
+            const int64_t to = (int64_t{run.first} + t[k]) * r.out_token + h[k] * r.out_head;
+            if (r.whole) {
+                store4<TYPE>(r.out, to + p.first, r.vec_q, {y[k][0], y[k][1], y[k][2], y[k][3]});
+                store4<TYPE>(r.out, to + p.second, r.vec_q, {y[k][4], y[k][5], y[k][6], y[k][7]});
+            } else {
+                typename Elem<TYPE>::T* const out = static_cast<typename Elem<TYPE>::T*>(r.out) + to;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (has_element<NEAR>(p, j)) out[j < 4 ? p.first + j : p.second + j - 4] = static_cast<typename Elem<TYPE>::T>(y[k][j]);
+            }
         }
     }
 }
@@ -748,6 +790,7 @@ extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step
         r.q_token = q_token; r.q_head = q_head;
         r.out_token = out_token; r.out_head = out_head;
         r.group = static_cast<int>(q_heads / cache->heads);
+        r.by_group = r.group > 1 ? fxp::inverse_of(r.group) : 0;
         r.vec_q = fxp::multiple_of_4(q, q_token, q_head, type) && fxp::multiple_of_4(out, out_token, out_head, type);
     }
     const int vk = fxp::multiple_of_4(k, k_token, k_head, type), vv = fxp::multiple_of_4(v, v_token, v_head, type);
