@@ -8,6 +8,8 @@
 // Writer.  q = floor(|x| 2^(125 + bits - e) + 1/2) with e the largest exponent of the block.  A workgroup has one run of one
 // head, keys or values; a thread has blocks of 4 tokens x 4 elements, which is one dword each way for keys (a token's four
 // elements) and, transposed in registers, for values (an element's four tokens).
+#include <algorithm>
+
 #include "fxp_rotary_device.h"
 #include "fxp_serve_device.h"
 
@@ -417,7 +419,8 @@ struct RotaryWriter {
     void* out;
     int64_t q_token, q_head, out_token, out_head;
     int group, vec_q;       // query heads of a head of the cache; 0: no queries
-    uint32_t by_group;      // ceil(2^32 / group)
+    uint32_t by_group, by_sixteens;         // ceil(2^32 / group); of dim / 16 where queries go by items of sixteen, 0 elsewhere
+    int shares;             // workgroups that a run's queries of one head of the cache are shared out to
 };
 
 // Item i of a head: eight elements, four pairs of them or eight that stay.  Element j is `first` + j, or `second` + j - 4 from the fourth on.
@@ -438,8 +441,10 @@ __device__ inline bool has_element(const Piece& p, int j) {
 
 // the elements of an item; at: of the head's first element
 template <int TYPE, bool NEAR>
-__device__ inline void load_piece(const RotaryWriter& r, const void* x, int64_t at, bool vec, const Piece& p, float (&y)[8]) {
-    if (r.whole) {
+__device__ inline void load_piece(const RotaryWriter& r, const void* x, int64_t at, int vec, const Piece& p, float (&y)[8]) {
+    if (vec > 1 && p.second == p.first + 4) {
+        load_elems<TYPE, 8>(x, at + p.first, true, y);
+    } else if (r.whole) {
         float a[4], b[4];
         load_elems<TYPE, 4>(x, at + p.first, vec, a);
         load_elems<TYPE, 4>(x, at + p.second, vec, b);
@@ -471,7 +476,7 @@ __device__ inline uint32_t high_word(double x) { return static_cast<uint32_t>(__
 
 template <int TYPE, int THREADS, bool NEAR>
 __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& r, const void* __restrict__ x, int64_t token, int64_t head_step, const Run& run,
-                                     int head, bool vec, uint32_t by_pieces, uint32_t* lds) {
+                                     int head, int vec, uint32_t by_pieces, uint32_t* lds) {
     const int dim = static_cast<int>(c.dim), pieces = r.pieces, work = run.count * pieces;
     const int64_t row0 = int64_t{run.first} * token + head * head_step;
     const int64_t block = int64_t{run.page} * c.heads + head;
@@ -558,13 +563,13 @@ __device__ inline void append_turned(const fxp_kv_cache& c, const RotaryWriter& 
         for (int i = threadIdx.x; i < run.offset * (dim / 4); i += THREADS) page[i] = remap_nearest4(page[i], grown);
 }
 
-// The queries of a run's tokens, of the heads that read one head of the cache; a thread's loads of four items go out together (one after the other, a chunk of
-// 64 tokens took the way of one item sixteen times: 9000 tokens of 16 + 4 + 4 heads of 128 46 us).
+// A share of the queries of a run's tokens, of the heads that read one head of the cache: four items a thread, whose loads go out together.
+constexpr int kQueryAhead = 4;
 template <int TYPE, int THREADS, bool NEAR>
-__device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int head, uint32_t by_pieces) {
+__device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int head, int share, uint32_t by_pieces) {
     const int rows = run.count * r.group, work = rows * r.pieces;
-    constexpr int kAhead = 4;
-    for (int n0 = threadIdx.x; n0 < work; n0 += kAhead * THREADS) {
+    constexpr int kAhead = kQueryAhead;
+    for (int n0 = share * kAhead * THREADS + threadIdx.x; n0 < work; n0 += r.shares * kAhead * THREADS) {
         float y[kAhead][8];
         int position[kAhead], t[kAhead], h[kAhead], i[kAhead];
 #pragma unroll
@@ -586,7 +591,9 @@ __device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int h
             turn_piece<float, NEAR>(r, position[k], static_cast<float>(r.amplitude), i[k], y[k]);
             const Piece p = piece_of<NEAR>(r, i[k]);
             const int64_t to = (int64_t{run.first} + t[k]) * r.out_token + h[k] * r.out_head;
-            if (r.whole) {
+            if (r.vec_q > 1 && p.second == p.first + 4) {
+                store_elems<TYPE, 8>(r.out, to + p.first, y[k]);
+            } else if (r.whole) {
                 store4<TYPE>(r.out, to + p.first, r.vec_q, {y[k][0], y[k][1], y[k][2], y[k][3]});
                 store4<TYPE>(r.out, to + p.second, r.vec_q, {y[k][4], y[k][5], y[k][6], y[k][7]});
             } else {
@@ -595,6 +602,49 @@ __device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int h
                 for (int j = 0; j < 8; ++j)
                     if (has_element<NEAR>(p, j)) out[j < 4 ? p.first + j : p.second + j - 4] = static_cast<typename Elem<TYPE>::T>(y[k][j]);
             }
+        }
+    }
+}
+
+// The same for elements of two bytes, pairs half of the rotated part apart and everything on multiples of 16 bytes: items of sixteen elements, whose two runs of eight are
+// 16 bytes each (8650 tokens, 16 + 4 + 4 heads of 128: 28 us, with 8-byte accesses 38).
+template <int TYPE, int THREADS>
+__device__ inline void turn_queries_wide(const RotaryWriter& r, const Run& run, int head, int share) {
+    const int pieces = r.dim / 16, turned = r.pairs / 8, rows = run.count * r.group, work = rows * pieces;
+    constexpr int kAhead = kQueryAhead / 2;
+    for (int n0 = share * kAhead * THREADS + threadIdx.x; n0 < work; n0 += r.shares * kAhead * THREADS) {
+        float u[kAhead][8], w[kAhead][8];
+        int position[kAhead], i[kAhead], first[kAhead], second[kAhead];
+        int64_t to[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int n = n0 + k * THREADS, row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), r.by_sixteens));
+            i[k] = n - row * pieces;
+            const int t = r.group == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), r.by_group)), h = head * r.group + row - t * r.group;
+            first[k] = i[k] < turned ? 8 * i[k] : r.rot + 16 * (i[k] - turned);
+            second[k] = i[k] < turned ? r.pairs + 8 * i[k] : first[k] + 8;
+            to[k] = (int64_t{run.first} + t) * r.out_token + h * r.out_head;
+            if (n < work) {
+                const int64_t at = (int64_t{run.first} + t) * r.q_token + h * r.q_head;
+                load_elems<TYPE, 8>(r.q, at + first[k], true, u[k]);
+                load_elems<TYPE, 8>(r.q, at + second[k], true, w[k]);
+                position[k] = r.positions[run.first + t];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (n0 + k * THREADS >= work) break;
+            if (i[k] < turned) {
+                const float amplitude = static_cast<float>(r.amplitude);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float c, s;
+                    cos_sin(angle_of(r.turns[8 * i[k] + j], position[k]), c, s);
+                    turn_pair(u[k][j], w[k][j], c * amplitude, s * amplitude);
+                }
+            }
+            store_elems<TYPE, 8>(r.out, to[k] + first[k], u[k]);
+            store_elems<TYPE, 8>(r.out, to[k] + second[k], w[k]);
         }
     }
 }
@@ -609,7 +659,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_append_rotary(fxp_kv_cache c, Ro
     if (!run_ok(run, tokens, c.pages)) return;
     if (blockIdx.z == 0) append_turned<TYPE, THREADS, NEAR>(c, r, k, k_token, k_head, run, blockIdx.y, vec_k, by_pieces, lds);
     else if (blockIdx.z == 1) append_run<TYPE, THREADS>(c, v, v_token, v_head, run, blockIdx.y, true, vec_v, inverse, lds);
-    else turn_queries<TYPE, THREADS, NEAR>(r, run, blockIdx.y, by_pieces);
+    else if (TYPE != FXP_F32 && !NEAR && r.by_sixteens) turn_queries_wide<TYPE, THREADS>(r, run, blockIdx.y, static_cast<int>(blockIdx.z) - 2);
+    else turn_queries<TYPE, THREADS, NEAR>(r, run, blockIdx.y, static_cast<int>(blockIdx.z) - 2, by_pieces);
 }
 
 // ---- inverse mapping: a thread has blocks of 4 tokens x 4 elements ----
@@ -771,9 +822,15 @@ extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step
     if (tokens == 0) return FXP_OK;
     if (!k || !v || !step->runs || !step->positions || (q && !out)) return FXP_ERR_NULL;
     const size_t size = static_cast<size_t>(fxp::elem_size(type));
+    const bool r_whole = rotation->rot % 8 == 0;
     if (!fxp::aligned(k, size) || !fxp::aligned(v, size) || !fxp::aligned(q, size) || !fxp::aligned(out, size) || !fxp::aligned(step->runs, 16) ||
         !fxp::aligned(step->positions, 4))
         return FXP_ERR_ALIGN;
+    // accesses of single elements, of four, of eight
+    auto width = [&](const void* p, int64_t token, int64_t head) {
+        if (!fxp::multiple_of_4(p, token, head, type)) return 0;
+        return r_whole && fxp::aligned(p, 16) && token * static_cast<int64_t>(size) % 16 == 0 && head * static_cast<int64_t>(size) % 16 == 0 ? 2 : 1;
+    };
     fxp::RotaryWriter r{};
     r.turns = rotation->turns;
     r.positions = step->positions;
@@ -783,7 +840,7 @@ extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step
     r.dim = static_cast<int>(cache->dim);
     r.turned = (r.pairs + 3) / 4;
     r.pieces = r.turned + (r.dim - r.rot + 7) / 8;
-    r.whole = r.rot % 8 == 0;                       // and so is the rest of a head
+    r.whole = r_whole;                              // and so is the rest of a head
     if (q) {
         r.q = q;
         r.out = out;
@@ -791,12 +848,18 @@ extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step
         r.out_token = out_token; r.out_head = out_head;
         r.group = static_cast<int>(q_heads / cache->heads);
         r.by_group = r.group > 1 ? fxp::inverse_of(r.group) : 0;
-        r.vec_q = fxp::multiple_of_4(q, q_token, q_head, type) && fxp::multiple_of_4(out, out_token, out_head, type);
+        r.by_sixteens = 0;
+        r.vec_q = std::min(width(q, q_token, q_head), width(out, out_token, out_head));
     }
-    const int vk = fxp::multiple_of_4(k, k_token, k_head, type), vv = fxp::multiple_of_4(v, v_token, v_head, type);
-    const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), q ? 3 : 2);
+    if (r.vec_q > 1 && r.rot % 16 == 0 && cache->dim > 16) r.by_sixteens = fxp::inverse_of(cache->dim / 16);
+    const int vk = width(k, k_token, k_head), vv = fxp::multiple_of_4(v, v_token, v_head, type);
     const uint32_t inverse = fxp::inverse_of(cache->dim / 4), by_pieces = fxp::inverse_of(r.pieces);
     const bool few = tokens <= 4 * n_runs;          // the rule of fxp_kv_append
+    // Queries of a whole page are shared out so that a thread has one turn of loads (8650 tokens, 16 + 4 + 4 heads of 128
+    // in fp16, neighbouring pairs: 31 us; one workgroup for a run and head of the cache 45, of which the keys and values are 17); those of
+    // single tokens are one workgroup's.
+    r.shares = !q ? 0 : few ? 1 : std::max(1, std::min(64, FXP_KV_PAGE * r.group * r.pieces / (fxp::kQueryAhead * 256)));
+    const dim3 grid(static_cast<unsigned>(n_runs), static_cast<unsigned>(cache->heads), static_cast<unsigned>(2 + r.shares));
     auto launch = [&](auto type_c, auto threads_c, auto near_c) {
         constexpr int TYPE = decltype(type_c)::value, THREADS = decltype(threads_c)::value;
         hipLaunchKernelGGL((fxp::k_kv_append_rotary<TYPE, THREADS, decltype(near_c)::value>), grid, dim3(THREADS), 0, static_cast<hipStream_t>(stream), *cache,

@@ -41,7 +41,7 @@ def step_of(fxp, rng, spans, pages, more=()):
 # heads, query heads, dim, rot, type, bits, runs as (count, offset)
 CASES = [(1, 1, 16, 16, "fp32", 8, [(1, 0)]), (8, 32, 128, 128, "bf16", 8, [(1, 5), (1, 63), (1, 0), (1, 17)]), (3, 21, 80, 40, "fp16", 8, [(64, 0), (3, 61), (33, 2)]),
          (2, 4, 256, 256, "fp32", 8, [(64, 0), (1, 1), (63, 1), (5, 30)]), (2, 0, 256, 64, "bf16", 5, [(1, 62), (1, 3)]), (4, 4, 64, 2, "fp16", 2, [(10, 0), (20, 9)]),
-         (12, 12, 64, 46, "fp32", 7, [(1, i) for i in range(64)]), (2, 2, 48, 12, "bf16", 8, [(2, 2), (3, 1), (4, 4), (6, 0)]), (1, 16, 160, 30, "bf16", 8, [(64, 0), (40, 3)])]
+         (12, 12, 64, 46, "fp32", 7, [(1, i) for i in range(64)]), (2, 2, 48, 12, "bf16", 8, [(2, 2), (3, 1), (4, 4), (6, 0)]), (1, 16, 160, 30, "bf16", 8, [(64, 0), (40, 3)]), (2, 6, 96, 32, "fp16", 8, [(64, 0), (5, 3)]), (2, 2, 16, 16, "bf16", 8, [(7, 0), (30, 20)])]
 
 
 @pytest.mark.parametrize("near", [False, True])
