@@ -447,21 +447,32 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
     }
 }
 
+// Rows of A that go by workgroups of 16 rows of B: 64 x 4096 x 9008 9.1 us (by tiles 14.3), 37 x 4096 x 2048 3.8 (6.2); 65 rows are two such
+// workgroups' work and 10.3 us by tiles.
 constexpr int kRowsMost = 64;
 
 // How a product is cut: tiles, and parts of the contraction where the tiles alone leave CUs idle.
+//
+// Tiles run in rounds of as many as are resident on 256 CUs: one a CU of 256 x 256, two of 128 x 128, three of 64 x 64.  A round of the smaller ones takes 0.57 and 0.38 of the
+// time of one of the large (2048^3 14.7 / 8.5 / 11.0 us by 256, 128 and two rounds of 64; 768 x 12608 x 2304 62.8 / 38.6 / 26.6; 3000 x 1024 x 5000 15.6 / 16.4 in two rounds /
+// 22.5 in five; 11000 x 300 x 500 11.9 / 9.1 / 9.6 in two): the tile with the shortest rounds in all is taken.
+// Fewer than 256 tiles of 64 x 64 with eight panels or more: parts of at least four panels, about two workgroups a CU (768 x 12608 x 768 19.1 us in one part, 16.3 in four,
+// 18.2 in eight; 192 x 9000 x 64 13.3 / 7.9 / 6.8; 300 x 4096 x 4096, 320 tiles, 10.2 in one, 15.2 in two).
 struct Mx4Plan {
     bool rows;
     int tile, splits, per_split;
 };
 static Mx4Plan mx4_plan(int64_t M, int64_t N, int64_t K) {
     const int64_t panels = mx_panels(K);
-    Mx4Plan p{M <= kRowsMost, 256, 1, static_cast<int>(panels)};
+    Mx4Plan p{M <= kRowsMost, 64, 1, static_cast<int>(panels)};
     if (p.rows) return p;
     auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-    if (tiles(256) < 128) p.tile = tiles(128) < 256 ? 64 : 128;
+    auto rounds = [&](int64_t t, int64_t resident) { return (tiles(t) + resident - 1) / resident; };
+    const int64_t by_64 = 38 * rounds(64, 768), by_128 = 57 * rounds(128, 512), by_256 = 100 * rounds(256, 256);
+    if (by_256 <= std::min(by_64, by_128)) p.tile = 256;
+    else if (by_128 <= by_64) p.tile = 128;
     const int64_t count = tiles(p.tile);
-    if (count < 256 && panels >= 8) {
+    if (p.tile == 64 && count < 256 && panels >= 8) {
         const int64_t want = std::min<int64_t>(panels / 4, (512 + count - 1) / count);
         p.per_split = static_cast<int>((panels + want - 1) / want);
         p.splits = static_cast<int>((panels + p.per_split - 1) / p.per_split);
