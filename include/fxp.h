@@ -495,7 +495,7 @@ typedef struct fxp_rotation {
  * heads, dim] of `type` at any strides >= 0 of the first three (fastest where bases, strides, rot / 2 and dim - rot are multiples of 16 bytes);
  * positions: int32, sequence b's at p_batch * b (0: the same for all).  Rows at negative positions are left as they are in y.  y may be x (with
  * x's strides) and shares no elements with it otherwise; y's rows may not overlap.  Cosines and sums are fp32, rounded once to `type`.
- * batch * ceil(tokens / 64) < 2^31, heads <= 65535, dim <= 65536. */
+ * heads <= 65535, dim <= 65536; fewer than 2^24 workgroups (of at least one token of one sequence, some 16 KiB of x where a sequence has them). */
 int fxp_rotary(const fxp_rotation* rotation, int backward, int type, int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
                const void* x, int64_t x_batch, int64_t x_token, int64_t x_head, const int32_t* positions, int64_t p_batch, void* y,
                int64_t y_batch, int64_t y_token, int64_t y_head, void* stream);
@@ -547,14 +547,15 @@ size_t fxp_mx4_scale_bytes(int64_t rows, int64_t cols);
 /* Maps x [rows, cols] of `type`, row stride ldx >= cols: q [rows, cols] with blocks along the rows and / or qT [cols, rows], x transposed, with blocks
  * along x's columns (either may be NULL), in one pass.  rounding: FXP_ROUND_NEAREST is to nearest, ties to even; FXP_ROUND_STOCHASTIC up with the
  * probability of what is cut off, in units of 2^-22: where the top 22 bits of the element's random word are less than the top 22 bits behind the code.
- * Words as in fxp_map: element i of x (row-major, without gaps) has word i % 4 of Philox block i / 4, in both copies. */
+ * Words as in fxp_map: element i of x (row-major, without gaps) has word i % 4 of Philox block i / 4, in both copies.  Fewer than 2^24 tiles of 32 x 256
+ * elements; q, qT and x share no memory. */
 int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT, uint64_t seed,
                 uint64_t stream_id, int rounding, void* stream);
 /* The values [rows, cols] that q stands for, rounded once to `type` (exact in fp32; in bf16 but for underflow). */
 int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream);
 
 /* C[M,N] of `type` = A B^T for mapped A [M,K] and B [N,K], row stride ldc >= N: products are exact, sums fp32 in no stated order (the same order on every call
- * of a size), rounded once to `type`.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
+ * of a size), rounded once to `type`.  Fewer than 2^23 tiles of 64 x 64 to 256 x 256 outputs.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
 size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream);
 
@@ -566,7 +567,7 @@ int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx
 /* A layer's training step, as fxp_linear_fwd / _bwd with blocks of 4-bit floats in place of int8 tensors: Y = X W, dX = dY W^T, dW = X^T dY, dense
  * row-major of one `type`, every operand mapped along the contraction that it is used in (the same random words in both copies).  The mapped operands belong to the
  * caller: fwd fills X [M,K], WT [N,K], XT [K,M] and W [K,N] (the last two may have data NULL where no backward call follows), bwd reads XT for dW and W for dX, and
- * fills dY [M,N] for dX and dYT [N,M] for dW.  dX or dW may be NULL.  Streams: (step << 8) | 0, 1, 2 for X, W, dY; step < 2^56.
+ * fills dY [M,N] for dX and dYT [N,M] for dW.  dX or dW may be NULL.  The mapped operands share no memory.  Streams: (step << 8) | 0, 1, 2 for X, W, dY; step < 2^56.
  * ws: fxp_mx4_layer_workspace_bytes bytes (at least 256), 256-byte aligned. */
 typedef struct fxp_mx4_layer {
     fxp_mx4 X, XT, W, WT, dY, dYT;

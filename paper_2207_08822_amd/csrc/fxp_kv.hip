@@ -419,7 +419,11 @@ struct RotaryWriter {
     void* out;
     int64_t q_token, q_head, out_token, out_head;
     int group, vec_q;       // query heads of a head of the cache; 0: no queries
-    uint32_t by_group, by_sixteens;         // ceil(2^32 / group); of dim / 16 where queries go by items of sixteen, 0 elsewhere
+    uint32_t by_group;      // ceil(2^32 / group) where 64 tokens of the group's heads are divided exactly with it, 0 elsewhere
+    uint32_t by_sixteens;   // the same of dim / 16 where queries go by items of sixteen, 0 elsewhere
+    __device__ int token_of(int row) const {
+        return group == 1 ? row : by_group ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), by_group)) : row / group;
+    }
     int shares;             // workgroups that a run's queries of one head of the cache are shared out to
 };
 
@@ -578,7 +582,7 @@ __device__ inline void turn_queries(const RotaryWriter& r, const Run& run, int h
             // heads inside tokens: a step of one token has its heads beside each other
             const int row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), by_pieces));
             i[k] = n - row * r.pieces;
-            t[k] = r.group == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), r.by_group));
+            t[k] = r.token_of(row);
             h[k] = head * r.group + row - t[k] * r.group;
             if (n < work) {
                 load_piece<TYPE, NEAR>(r, r.q, (int64_t{run.first} + t[k]) * r.q_token + h[k] * r.q_head, r.vec_q, piece_of<NEAR>(r, i[k]), y[k]);
@@ -620,7 +624,7 @@ __device__ inline void turn_queries_wide(const RotaryWriter& r, const Run& run, 
         for (int k = 0; k < kAhead; ++k) {
             const int n = n0 + k * THREADS, row = static_cast<int>(__umulhi(static_cast<uint32_t>(n), r.by_sixteens));
             i[k] = n - row * pieces;
-            const int t = r.group == 1 ? row : static_cast<int>(__umulhi(static_cast<uint32_t>(row), r.by_group)), h = head * r.group + row - t * r.group;
+            const int t = r.token_of(row), h = head * r.group + row - t * r.group;
             first[k] = i[k] < turned ? 8 * i[k] : r.rot + 16 * (i[k] - turned);
             second[k] = i[k] < turned ? r.pairs + 8 * i[k] : first[k] + 8;
             to[k] = (int64_t{run.first} + t) * r.out_token + h * r.out_head;
@@ -847,7 +851,7 @@ extern "C" int fxp_kv_append_rotary(const fxp_kv_cache* cache, const fxp_kv_step
         r.q_token = q_token; r.q_head = q_head;
         r.out_token = out_token; r.out_head = out_head;
         r.group = static_cast<int>(q_heads / cache->heads);
-        r.by_group = r.group > 1 ? fxp::inverse_of(r.group) : 0;
+        r.by_group = r.group > 1 && r.group < 8192 ? fxp::inverse_of(r.group) : 0;          // rows * group < 2^32
         r.by_sixteens = 0;
         r.vec_q = std::min(width(q, q_token, q_head), width(out, out_token, out_head));
     }

@@ -217,7 +217,7 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
             j.vec = vec_of(m);
             tiles += j.tiles_c * ((R + TR - 1) / TR);
         }
-        if (tiles >= int64_t{1} << 31) return static_cast<int>(FXP_ERR_DIMS);
+        if (tiles >= int64_t{1} << 24) return static_cast<int>(FXP_ERR_DIMS);          // 2^32 threads
         if (tiles == 0) return static_cast<int>(FXP_OK);
         hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value, SR, SC>), dim3(static_cast<unsigned>(tiles)), dim3(64 * std::min(SR * SC, 4)), 0, s,
                            jobs, key0, key1);
@@ -225,9 +225,8 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
     };
     auto sized = [&](auto type_c, auto stoch_c) {
         using std::integral_constant;
-        if (count == 1 && !maps[0].t) {
-            const int64_t pieces = maps[0].rows * mx_panels(maps[0].cols), blocks = (pieces * 32 + kMxThreads - 1) / kMxThreads;
-            if (blocks >= int64_t{1} << 31) return static_cast<int>(FXP_ERR_DIMS);
+        const int64_t pieces = maps[0].rows * mx_panels(maps[0].cols), blocks = (pieces * 32 + kMxThreads - 1) / kMxThreads;
+        if (count == 1 && !maps[0].t && blocks < int64_t{1} << 24) {                   // 2^32 threads
             if (blocks == 0) return static_cast<int>(FXP_OK);
             hipLaunchKernelGGL((k_mx4_map_rows<decltype(type_c)::value, decltype(stoch_c)::value>), dim3(static_cast<unsigned>(blocks)), dim3(kMxThreads), 0, s, maps[0],
                                static_cast<int>(mx_panels(maps[0].cols)), vec_of(maps[0]), key0, key1);
@@ -281,6 +280,17 @@ static Mx4Map map_of(const void* x, int64_t ld, int64_t rows, int64_t cols, cons
     return m;
 }
 
+// whether two buffers share bytes
+static bool meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes > 0 && b_bytes > 0 && x < y + static_cast<uintptr_t>(b_bytes) && y < x + static_cast<uintptr_t>(a_bytes);
+}
+static bool meet(const fxp_mx4& a, const fxp_mx4& b) {
+    const int64_t na = mx_panels(a.cols) * a.rows, nb = mx_panels(b.cols) * b.rows;
+    return meet(a.data, na * kMxRowBytes, b.data, nb * kMxRowBytes) || meet(a.data, na * kMxRowBytes, b.scales, nb * kMxRowScales) ||
+           meet(a.scales, na * kMxRowScales, b.data, nb * kMxRowBytes) || meet(a.scales, na * kMxRowScales, b.scales, nb * kMxRowScales);
+}
+
 static int check_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT) {
     if (!known_type(type)) return FXP_ERR_TYPE;
     if (rows < 0 || cols < 0 || rows > kMxMost || cols > kMxMost || ldx < cols || ldx >= int64_t{1} << 40) return FXP_ERR_DIMS;
@@ -293,6 +303,7 @@ static int check_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t
         const int rc = check_mx4(qT);
         if (rc) return rc;
         if (qT->rows != cols || qT->cols != rows) return FXP_ERR_DIMS;
+        if (q && meet(*q, *qT)) return FXP_ERR_VALUE;
     }
     if (rows && cols) {
         if (!x) return FXP_ERR_NULL;
@@ -424,6 +435,9 @@ static int check_layer(const fxp_mx4_layer* l, int64_t M, int64_t K, int64_t N, 
         if (w.q->rows != w.rows || w.q->cols != w.cols) return FXP_ERR_DIMS;
         const int rc = check_mx4(w.q);
         if (rc) return rc;
+        // no two of the call's operands are one
+        for (const Want& o : backward ? back : forward)
+            if (o.q != w.q && o.q->data && meet(*w.q, *o.q)) return FXP_ERR_VALUE;
     }
     return FXP_OK;
 }

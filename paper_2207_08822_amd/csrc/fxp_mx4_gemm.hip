@@ -49,6 +49,11 @@ __device__ inline void wave_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// 16 bytes at any address
+struct __attribute__((packed, aligned(1))) Sixteen {
+    v4i v;
+};
+
 struct Mx4Operand {
     const uint8_t *data, *scales;
     int rows;
@@ -59,7 +64,6 @@ struct Mx4Product {
     void* c;
     int64_t ldc, split_stride;          // of partial sums, in elements: 0 where there is one part
     int tiles_m, tiles_n, group_m;
-    int vec;                            // rows of C of two bytes begin and end on multiples of 16 bytes
 };
 
 template <int TYPE>
@@ -77,7 +81,7 @@ __device__ inline void store_one(void* c, int64_t at, float v) {
 // next panel.  (Reading a quarter and then multiplying it, a workgroup alone on its CU took 1600 clocks a panel of 128 x 128 where its products are 512.)
 //
 // Outputs of two bytes: the operands change places, so that a lane has four neighbouring columns, and the wave's tile goes through LDS to leave in 16-byte pieces of whole
-// rows.  fp32 leaves directly, 128 bytes in a row of C a store.
+// rows, wherever these begin (1263 x 1016 x 7053 with its input's mapping: single elements 43 us, so 18).  fp32 leaves directly, 128 bytes in a row of C a store.
 template <int BM, int BN, int WM, int WN, int STAGES, int TYPE>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Product p) {
     constexpr int NW = (BM / WM) * (BN / WN), FM = WM / 32, FN = WN / 32;
@@ -234,22 +238,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
         // row lane % 32, column 8 (r / 4) + 4 (lane / 32) + r % 4
         using T = typename Elem<TYPE>::T;
         typedef T Four __attribute__((ext_vector_type(4)));
-        if (!p.vec) {
-#pragma unroll
-            for (int i = 0; i < FM; ++i) {
-                const int row = row0 + 32 * i + frow;
-                if (row >= p.M) continue;
-                T* const c = static_cast<T*>(p.c) + row * p.ldc;
-#pragma unroll
-                for (int j = 0; j < FN; ++j)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int col = col0 + 32 * j + 8 * (r >> 2) + 4 * fhalf + (r & 3);
-                        if (col < p.N) c[col] = static_cast<T>(acc[i][j][r]);
-                    }
-            }
-            return;
-        }
         barrier();                                                  // every wave is done with the panels
         uint8_t* const mine = lds + wave * kOut;
 #pragma unroll
@@ -267,9 +255,19 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
         constexpr int kPieces = WN / 8;                             // of 16 bytes in a row
 #pragma unroll
         for (int n = 0; n < WM * kPieces / 64; ++n) {
-            const int row = (n * 64 + lane) / kPieces, piece = lane % kPieces;
-            if (row0 + row < p.M && col0 + 8 * piece < p.N)         // whole pieces: N is a multiple of eight
-                *reinterpret_cast<v4i*>(static_cast<T*>(p.c) + (row0 + row) * p.ldc + col0 + 8 * piece) = *reinterpret_cast<const v4i*>(mine + row * kOutStride + piece * 16);
+            const int row = (n * 64 + lane) / kPieces, piece = lane % kPieces, col = col0 + 8 * piece;
+            if (row0 + row >= p.M) continue;
+            T* const c = static_cast<T*>(p.c) + (row0 + row) * p.ldc + col;
+            const v4i v = *reinterpret_cast<const v4i*>(mine + row * kOutStride + piece * 16);
+            if (col + 8 <= p.N) {
+                reinterpret_cast<Sixteen*>(c)->v = v;
+            } else {
+                typedef T Eight __attribute__((ext_vector_type(8)));
+                const Eight e = __builtin_bit_cast(Eight, v);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (col + k < p.N) c[k] = e[k];
+            }
         }
     }
 }
@@ -561,7 +559,7 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.tiles_m = static_cast<int>((M + t - 1) / t);
     p.tiles_n = static_cast<int>((N + t - 1) / t);
     p.group_m = 8;
-    p.vec = aligned(C, 16) && ldc % 8 == 0 && N % 8 == 0;
+    if (static_cast<int64_t>(p.tiles_m) * p.tiles_n >= int64_t{1} << 23) return FXP_ERR_DIMS;          // 2^32 threads
     const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
     by_type(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;

@@ -131,6 +131,13 @@ extern "C" int fxp_rotary(const fxp_rotation* rotation, int backward, int type, 
         return FXP_ERR_DIMS;
     if (batch == 0 || tokens == 0 || heads == 0) return FXP_OK;
     if (!x || !y || !positions) return FXP_ERR_NULL;
+    // single tokens of many sequences are the tokens of one
+    if (tokens == 1 && (batch == 1 || p_batch == 1)) {
+        tokens = batch;
+        x_token = x_batch;
+        y_token = y_batch;
+        batch = 1;
+    }
     // steps that are never taken
     if (batch == 1) x_batch = y_batch = p_batch = 0;
     if (tokens == 1) x_token = y_token = 0;
@@ -169,7 +176,7 @@ extern "C" int fxp_rotary(const fxp_rotation* rotation, int backward, int type, 
     a.hb = static_cast<int>(std::min<int64_t>(heads, std::max(1, target / a.pieces)));
     a.tb = std::max(1, std::min({target / (a.hb * a.pieces), kRotTable / a.pairs, kRotTokens, static_cast<int>(std::min<int64_t>(tokens, kRotTokens))}));
     const int64_t blocks = (tokens + a.tb - 1) / a.tb;
-    if (blocks * batch >= kMost) return FXP_ERR_DIMS;
+    if (blocks * batch >= int64_t{1} << 24) return FXP_ERR_DIMS;           // 2^32 threads
     a.token_blocks = static_cast<int>(blocks);
     a.by_pieces = inverse_of(a.pieces);
     a.by_inner = inverse_of(a.heads_inside ? a.hb : a.tb);

@@ -1049,23 +1049,59 @@ class Mx4:
     def __init__(self, rows, cols, device="cuda"):
         if min(rows, cols) < 0 or max(rows, cols) > 2 ** 24 - 2 ** 16:
             raise FxpError("rows and cols must be between 0 and 2^24 - 2^16")
-        panels = -(-cols // MX4_PANEL)
-        self._set(torch.empty((panels, rows, 128), dtype=torch.uint8, device=device), torch.empty((panels, rows, 8), dtype=torch.uint8, device=device), rows, cols)
+        self._own(rows, cols, torch.empty(_mx4_bytes(rows, cols), dtype=torch.uint8, device=device))
 
     @classmethod
     def of(cls, data, scales, rows, cols):
         """The matrix that two tensors of these shapes are; codes and scales behind the last column have to be zeros."""
         self = cls.__new__(cls)
-        self._set(data, scales, rows, cols)
-        return self
-
-    def _set(self, data, scales, rows, cols):
         panels = -(-cols // MX4_PANEL)
         _index(data, "data", (panels, rows, 128), torch.uint8)
         _index(scales, "scales", (panels, rows, 8), torch.uint8)
-        self.data, self.scales, self.rows, self.cols, self.index = data, scales, rows, cols, data.get_device()
-        self.c = _Mx4(data.data_ptr(), scales.data_ptr(), rows, cols)
+        self._set(rows, cols, data.data_ptr(), scales.data_ptr(), data.get_device())
+        self._data, self._scales = data, scales
+        return self
+
+    def _own(self, rows, cols, buf):
+        """Codes and scales in one buffer; the tensors of them are made when they are asked for."""
+        at = buf.data_ptr()
+        self._set(rows, cols, at, at + -(-cols // MX4_PANEL) * rows * 128, buf.get_device())
+        self._buf, self._data, self._scales = buf, None, None
+        if self.index < 0:
+            raise FxpError("a mapped matrix must be on a GPU: libfxp has no CPU path")
+        return self
+
+    def _set(self, rows, cols, data, scales, index):
+        self.rows, self.cols, self.index = rows, cols, index
+        self.c = _Mx4(data, scales, rows, cols)
         self.ref = ctypes.byref(self.c)
+
+    def _split(self):
+        panels = -(-self.cols // MX4_PANEL)
+        n = panels * self.rows * 128
+        self._data, self._scales = self._buf[:n].view(panels, self.rows, 128), self._buf[n:].view(panels, self.rows, 8)
+
+    @property
+    def data(self):
+        if self._data is None:
+            self._split()
+        return self._data
+
+    @property
+    def scales(self):
+        if self._scales is None:
+            self._split()
+        return self._scales
+
+
+def _mx4_bytes(rows, cols):
+    return -(-cols // MX4_PANEL) * rows * 136
+
+
+def _mx4_like(x, rows, cols):
+    if rows > 2 ** 24 - 2 ** 16 or cols > 2 ** 24 - 2 ** 16:
+        raise FxpError("rows and cols must be at most 2^24 - 2^16")
+    return Mx4.__new__(Mx4)._own(rows, cols, x.new_empty(_mx4_bytes(rows, cols), dtype=torch.uint8))
 
 
 def mx4_map(x, rounding=STOCHASTIC, seed=0, stream_id=0, want_q=True, want_qT=False, out=None):
@@ -1075,7 +1111,7 @@ def mx4_map(x, rounding=STOCHASTIC, seed=0, stream_id=0, want_q=True, want_qT=Fa
     code = _served(x, "x", 2)
     rows, cols = x.shape
     if out is None:
-        q, qT = Mx4(rows, cols, x.device) if want_q else None, Mx4(cols, rows, x.device) if want_qT else None
+        q, qT = _mx4_like(x, rows, cols) if want_q else None, _mx4_like(x, cols, rows) if want_qT else None
     else:
         q, qT = out
         for t, shape in ((q, (rows, cols)), (qT, (cols, rows))):
@@ -1096,7 +1132,7 @@ def mx4_unmap(q, dtype=torch.float32, out=None):
     if out is None:
         if dtype not in _TYPES:
             raise FxpError("dtype must be float32, bfloat16 or float16")
-        out = q.data.new_empty((q.rows, q.cols), dtype=dtype)
+        out = torch.empty((q.rows, q.cols), dtype=dtype, device=q.index)
     code = _served(out, "out", 2)
     if out.shape != (q.rows, q.cols):
         raise FxpError("out must be [rows, cols] of q")
@@ -1113,7 +1149,7 @@ def mx4_gemm(A, B, dtype=torch.float32, out=None, ws=None):
     if out is None:
         if dtype not in _TYPES:
             raise FxpError("dtype must be float32, bfloat16 or float16")
-        out = A.data.new_empty((A.rows, B.rows), dtype=dtype)
+        out = torch.empty((A.rows, B.rows), dtype=dtype, device=A.index)
     code = _served(out, "out", 2)
     if out.shape != (A.rows, B.rows):
         raise FxpError("out must be [A.rows, B.rows]")
@@ -1121,7 +1157,7 @@ def mx4_gemm(A, B, dtype=torch.float32, out=None, ws=None):
         _index(ws, "ws", dtype=torch.uint8)
     else:
         nbytes = int(lib().fxp_mx4_gemm_workspace_bytes(A.rows, B.rows, A.cols))
-        ws = A.data.new_empty(nbytes) if nbytes else None
+        ws = out.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
     _check(lib().fxp_mx4_gemm(A.ref, B.ref, code, out.data_ptr(), _row_stride(out, "out"), _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_mx4_gemm")
     return out
 

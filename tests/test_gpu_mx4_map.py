@@ -128,3 +128,11 @@ def test_out_and_refusals(fxp):
         with pytest.raises(fxp.FxpError):
             f()
             pytest.fail(str(i))
+
+
+def test_two_copies_in_one_place_are_refused(fxp):
+    x = torch.randn((64, 64), device="cuda")
+    q = fxp.Mx4(64, 64)
+    for other in (q, fxp.Mx4.of(q.data, torch.zeros_like(q.scales), 64, 64), fxp.Mx4.of(torch.zeros_like(q.data), q.scales, 64, 64)):
+        with pytest.raises(fxp.FxpError):
+            fxp.mx4_map(x, out=(q, other))

@@ -173,3 +173,28 @@ def test_replayed_and_on_another_stream(fxp):
         graph.replay()
         assert torch.equal(out, fxp.rotary(x, positions, rope))
         torch.cuda.synchronize()
+
+
+def test_single_tokens_of_many_sequences(fxp):
+    """[batch, 1, heads, dim] with positions of their own and shared ones, more sequences than a grid has rows."""
+    rope = fxp.Rotary(8)
+    for B in (1, 3, 70000):
+        x = normal((B, 1, 2, 8), torch.float32, B)
+        positions = torch.arange(B, dtype=torch.int32, device="cuda")[:, None]
+        check(fxp, x, positions, rope)
+        check(fxp, x, positions[B // 2], rope, backward=True)
+
+
+def test_elements_past_32_bits(fxp):
+    """Rows that begin more than 2^32 elements behind the tensor's first."""
+    rope = fxp.Rotary(128)
+    big = torch.empty((1 << 17) + 3, 1 << 15, dtype=torch.bfloat16, device="cuda")
+    x = big.unflatten(1, (256, 128))[-2:]
+    x.copy_(normal(x.shape, x.dtype, 1))
+    whole = big.unflatten(1, (256, 128))
+    positions = torch.full((whole.shape[0],), -1, dtype=torch.int32, device="cuda")
+    positions[-2:] = torch.tensor([5, 70000])
+    want = ref.turn(host(x.float()), np.array([5, 70000]), rope)
+    before = host(x.double())
+    assert fxp.rotary(whole, positions, rope, out=whole) is whole
+    assert ref.within(host(x.double()), want, before, rope, 2.0 ** -7)

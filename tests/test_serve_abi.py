@@ -179,7 +179,7 @@ def test_append_rotary(L):
 
 
 def mx4(**over):
-    a = dict(data=BIG, scales=BIG, rows=5, cols=70) | over
+    a = dict(data=BIG, scales=BIG << 4, rows=5, cols=70) | over
     return c.byref(fxp._Mx4(*[a[n] for n, _ in fxp._Mx4._fields_]))
 
 
@@ -189,13 +189,15 @@ def test_mx4_sizes(L):
 
 
 def test_mx4_map_and_unmap(L):
-    def f(type=0, x=BIG, ld=70, rows=5, cols=70, q=mx4(), t=mx4(rows=70, cols=5), rounding=0):
+    def f(type=0, x=BIG, ld=70, rows=5, cols=70, q=mx4(), t=mx4(data=BIG << 1, scales=BIG << 5, rows=70, cols=5), rounding=0):
         return L.fxp_mx4_map(type, x, ld, rows, cols, q, t, 0, 0, rounding, None)
 
     assert f(q=None, t=None) == -1 and f(type=5) == -9 and f(rounding=2) == -5 and f(x=None) == -1 and f(x=BIG + 2) == -3 and f(ld=69) == -2
     assert f(rows=-1) == -2 and f(cols=1 << 24, ld=1 << 24) == -2 and f(q=mx4(rows=6)) == -2 and f(t=mx4()) == -2
+    for same in (dict(data=BIG + 512), dict(scales=BIG + 16), dict(scales=(BIG << 4) + 32)):          # in q's bytes
+        assert f(t=mx4(**(dict(data=BIG << 1, scales=BIG << 5, rows=70, cols=5) | same))) == -10
     for bad, rc in ((dict(data=None), -1), (dict(scales=None), -1), (dict(data=BIG + 8), -3), (dict(scales=BIG + 4), -3), (dict(rows=-1), -2)):
-        assert f(q=mx4(**bad)) == rc and f(t=mx4(**(dict(rows=70, cols=5) | bad))) == rc
+        assert f(q=mx4(**bad)) == rc and f(t=mx4(**(dict(data=BIG << 1, scales=BIG << 5, rows=70, cols=5) | bad))) == rc
         assert L.fxp_mx4_unmap(mx4(**bad), 0, BIG, 70, None) == rc
     assert L.fxp_mx4_unmap(None, 0, BIG, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 3, BIG, 70, None) == -9 and L.fxp_mx4_unmap(mx4(), 0, BIG, 69, None) == -2
     assert L.fxp_mx4_unmap(mx4(), 0, None, 70, None) == -1 and L.fxp_mx4_unmap(mx4(), 0, BIG + 2, 70, None) == -3
@@ -227,8 +229,8 @@ def test_mx4_layers(L):
     shapes = dict(X=(M, K), XT=(K, M), W=(K, N), WT=(N, K), dY=(M, N), dYT=(N, M))
 
     def layer(**over):
-        make = lambda n, s: fxp._Mx4(*(over.get(n) or (BIG, BIG, *s)))  # noqa: E731
-        return c.byref(fxp._Mx4Layer(*[make(n, s) for n, s in shapes.items()]))
+        make = lambda i, n, s: fxp._Mx4(*(over.get(n) or (BIG << i, BIG << (6 + i), *s)))  # noqa: E731
+        return c.byref(fxp._Mx4Layer(*[make(i, n, s) for i, (n, s) in enumerate(shapes.items())]))
 
     def fwd(type=0, X=BIG, W=BIG, M=M, K=K, N=N, Y=BIG, l=layer(), rounding=0, ws=BIG, n=1 << 20):
         return L.fxp_mx4_linear_fwd(type, X, W, M, K, N, Y, l, 0, 0, rounding, ws, n, None)
@@ -241,6 +243,7 @@ def test_mx4_layers(L):
         assert f(M=M + 1) == -2 and f(**{first: None}) == -1 and f(**{first: BIG + 2}) == -3
     assert fwd(W=None) == -1 and fwd(Y=None) == -1 and fwd(Y=BIG + 2) == -3 and bwd(dX=BIG + 2) == -3 and bwd(dW=BIG + 1) == -3 and bwd(dX=None, dW=None) == 0
     for name in ("X", "WT"):
-        assert fwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and fwd(l=layer(**{name: (BIG + 8, BIG, *shapes[name])})) == -3
+        assert fwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and fwd(l=layer(**{name: ((BIG << 21) + 8, BIG << 22, *shapes[name])})) == -3
+    assert fwd(l=layer(W=(BIG, BIG << 20, *shapes["W"]))) == -10 and bwd(l=layer(dYT=(BIG << 2, BIG << 20, *shapes["dYT"]))) == -10          # two in one place
     for name in ("dY", "W", "dYT", "XT"):
-        assert bwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and bwd(l=layer(**{name: (BIG, BIG + 4, *shapes[name])})) == -3
+        assert bwd(l=layer(**{name: (None, None, *shapes[name])})) == -1 and bwd(l=layer(**{name: (BIG << 21, (BIG << 22) + 4, *shapes[name])})) == -3
