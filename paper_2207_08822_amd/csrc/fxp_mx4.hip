@@ -486,6 +486,7 @@ extern "C" int fxp_mx4_linear_bwd(int type, const void* dY, const fxp_mx4_layer*
     const Mx4Map m = map_of(dY, N, M, N, dX ? &layer->dY : nullptr, dW ? &layer->dYT : nullptr, (step << 8) | 2);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     rc = mx4_map_launch(type, &m, 1, seed, rounding, s);
+    if (!rc && dW && dX && M && K && N) return mx4_gemm_launch2(layer->XT, layer->dYT, dW, layer->dY, layer->W, dX, type, ws, s);
     if (!rc && dW && K && N) rc = mx4_gemm_launch(layer->XT, layer->dYT, type, dW, N, ws, s);
     if (!rc && dX && M && K) rc = mx4_gemm_launch(layer->dY, layer->W, type, dX, K, ws, s);
     return rc;

@@ -95,5 +95,7 @@ size_t mx4_gemm_bytes(int64_t M, int64_t N, int64_t K);
 bool mx4_is_fused(int64_t M);
 int mx4_fused_launch(int type, const void* x, int64_t ldx, int64_t M, const fxp_mx4& B, void* y, int64_t ldy, hipStream_t s);
 int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s);
+// two of them with outputs without gaps, in a workspace that is enough for each
+int mx4_gemm_launch2(const fxp_mx4& A0, const fxp_mx4& B0, void* C0, const fxp_mx4& A1, const fxp_mx4& B1, void* C1, int type, void* ws, hipStream_t s);
 
 }  // namespace fxp

@@ -71,6 +71,44 @@ __device__ inline void store_one(void* c, int64_t at, float v) {
     static_cast<typename Elem<TYPE>::T*>(c)[at] = static_cast<typename Elem<TYPE>::T>(v);
 }
 
+// ---- partial sums ----
+//
+// Added in order: rows of `cols` elements, the parts' without gaps, four elements a thread where rows begin on a multiple of four.  A launch of its own, or the last workgroups
+// of the product that follows (a layer's weight gradient before its input gradient: 4.8 us as a launch, 0.4 so).
+struct Mx4Sum {
+    const float* parts;
+    int count, rows, cols, vec;         // vec: 0, 1 where parts are read by four, 2 where the result is written so too
+    int64_t stride;
+    void* c;
+    int64_t ldc;
+    int tiles;                          // riding: workgroups before the first of these
+};
+inline unsigned sum_blocks(const Mx4Sum& r, int threads) {
+    return r.count == 0 ? 0u : static_cast<unsigned>(r.rows) * static_cast<unsigned>((r.cols + 4 * threads - 1) / (4 * threads));
+}
+template <int TYPE, int THREADS>
+__device__ inline void sum_parts(const Mx4Sum& r, int block) {
+    const int in_row = (r.cols + 4 * THREADS - 1) / (4 * THREADS), row = block / in_row, i = (block - row * in_row) * 4 * THREADS + static_cast<int>(threadIdx.x) * 4;
+    if (i >= r.cols) return;
+    const int64_t from = static_cast<int64_t>(row) * r.cols + i, to = static_cast<int64_t>(row) * r.ldc + i;
+    if (r.vec && i + 4 <= r.cols) {
+        v4f s = {};
+#pragma unroll 4
+        for (int n = 0; n < r.count; ++n) s += *reinterpret_cast<const v4f*>(r.parts + n * r.stride + from);
+        store4<TYPE>(r.c, to, r.vec > 1, {s[0], s[1], s[2], s[3]});
+    } else {
+        for (int j = 0; j < 4 && i + j < r.cols; ++j) {
+            float s = 0.0f;
+            for (int n = 0; n < r.count; ++n) s += r.parts[n * r.stride + from + j];
+            store_one<TYPE>(r.c, to + j, s);
+        }
+    }
+}
+template <int TYPE>
+__global__ __launch_bounds__(256) void k_mx4_sum(Mx4Sum r) {
+    sum_parts<TYPE, 256>(r, static_cast<int>(blockIdx.x));
+}
+
 // ---- tiles ----
 //
 // BM x BN outputs a workgroup in waves of WM x WN, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's
@@ -83,7 +121,11 @@ __device__ inline void store_one(void* c, int64_t at, float v) {
 // Outputs of two bytes: the operands change places, so that a lane has four neighbouring columns, and the wave's tile goes through LDS to leave in 16-byte pieces of whole
 // rows, wherever these begin (1263 x 1016 x 7053 with its input's mapping: single elements 43 us, so 18).  fp32 leaves directly, 128 bytes in a row of C a store.
 template <int BM, int BN, int WM, int WN, int STAGES, int TYPE>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Product p) {
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Product p, Mx4Sum rider) {
+    if (rider.count != 0 && static_cast<int>(blockIdx.x) >= rider.tiles) {
+        sum_parts<TYPE, (BM / WM) * (BN / WN) * 64>(rider, static_cast<int>(blockIdx.x) - rider.tiles);
+        return;
+    }
     constexpr int NW = (BM / WM) * (BN / WN), FM = WM / 32, FN = WN / 32;
     constexpr int kCodesA = BM * kMxRowBytes, kCodes = (BM + BN) * kMxRowBytes, kStage = kCodes + (BM + BN) * kMxRowScales;
     constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LS = (BM + BN) / 32 / NW, kLoads = LA + LB + LS;       // loads of a wave a panel
@@ -268,26 +310,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
                 for (int k = 0; k < 8; ++k)
                     if (col + k < p.N) c[k] = e[k];
             }
-        }
-    }
-}
-
-// Partial sums added in order: rows of `cols` elements, the parts' without gaps, four elements a thread where rows begin on a multiple of four.
-template <int TYPE>
-__global__ __launch_bounds__(256) void k_mx4_sum(const float* __restrict__ parts, int count, int64_t stride, int cols, int vec, void* c, int64_t ldc) {
-    const int i = static_cast<int>(blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= cols) return;
-    const int64_t from = static_cast<int64_t>(blockIdx.y) * cols + i, to = static_cast<int64_t>(blockIdx.y) * ldc + i;
-    if (vec && i + 4 <= cols) {
-        v4f s = {};
-#pragma unroll 4
-        for (int n = 0; n < count; ++n) s += *reinterpret_cast<const v4f*>(parts + n * stride + from);
-        store4<TYPE>(c, to, vec > 1, {s[0], s[1], s[2], s[3]});
-    } else {
-        for (int j = 0; j < 4 && i + j < cols; ++j) {
-            float s = 0.0f;
-            for (int n = 0; n < count; ++n) s += parts[n * stride + from + j];
-            store_one<TYPE>(c, to + j, s);
         }
     }
 }
@@ -492,6 +514,11 @@ static void by_type(int type, F go) {
     else go(IC<FXP_F16>{});
 }
 
+static int sum_launch(const Mx4Sum& r, int type, hipStream_t s) {
+    by_type(type, [&](auto type_c) { hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(sum_blocks(r, 256)), dim3(256), 0, s, r); });
+    return launch_status();
+}
+
 // as many panels of a workgroup in flight as leave room for two workgroups on a CU, where there are so many
 static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
     const Mx4Product& p = g.p;
@@ -503,7 +530,7 @@ static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
                                dim3(64 * W), 0, s, g);
         };
         auto sized = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
-            if (p.panels > 8 * decltype(u_c)::value / 2) go(mt_c, u_c, w_c, fused_c);
+            if (p.panels > std::max(4, 8 * decltype(u_c)::value / 2)) go(mt_c, u_c, w_c, fused_c);
             else if (p.panels > 4) go(mt_c, IC<1>{}, IC<8>{}, fused_c);
             else if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{}, fused_c);
             else go(mt_c, IC<1>{}, IC<1>{}, fused_c);
@@ -513,7 +540,7 @@ static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
         else if (fused) sized(IC<1>{}, IC<3>{}, IC<8>{}, IC<4>{});
         else if (p.M <= 16) sized(IC<1>{}, IC<2>{}, IC<8>{}, IC<0>{});
         else if (p.M <= 32) sized(IC<2>{}, IC<2>{}, IC<4>{}, IC<0>{});
-        else if (p.M <= 48) sized(IC<3>{}, IC<2>{}, IC<4>{}, IC<0>{});
+        else if (p.M <= 48) sized(IC<3>{}, IC<1>{}, IC<4>{}, IC<0>{});          // 37 x 4100 x 9001 9.4 us, two panels a wave 10.8
         else sized(IC<4>{}, IC<1>{}, IC<4>{}, IC<0>{});
     });
     return launch_status();
@@ -536,7 +563,8 @@ int mx4_fused_launch(int type, const void* x, int64_t ldx, int64_t M, const fxp_
     return rows_launch(g, true, type, s);
 }
 
-int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s) {
+// rider: a sum to be done in this launch; rest: receives the product's own sum, if it has one, in place of a launch of it
+static int gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, Mx4Sum rider, Mx4Sum* rest, hipStream_t s) {
     const int64_t M = A.rows, N = B.rows, K = A.cols;
     const Mx4Plan plan = mx4_plan(M, N, K);
     Mx4Product p{};
@@ -548,8 +576,13 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.per_split = plan.per_split;
     p.c = C;
     p.ldc = ldc;
-    if (plan.rows) return rows_launch({p, nullptr, 0, 0, 0}, false, type, s);
     const bool parts = plan.splits > 1;
+    if (rider.count && (plan.rows || parts)) {                                           // no tiles, or several parts of them
+        const int rc = sum_launch(rider, type, s);
+        if (rc) return rc;
+        rider.count = 0;
+    }
+    if (plan.rows) return rows_launch({p, nullptr, 0, 0, 0}, false, type, s);
     if (parts) {
         p.c = ws;
         p.ldc = N;
@@ -559,24 +592,40 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     p.tiles_m = static_cast<int>((M + t - 1) / t);
     p.tiles_n = static_cast<int>((N + t - 1) / t);
     p.group_m = 8;
-    if (static_cast<int64_t>(p.tiles_m) * p.tiles_n >= int64_t{1} << 23) return FXP_ERR_DIMS;          // 2^32 threads
-    const dim3 grid(static_cast<unsigned>(p.tiles_m) * static_cast<unsigned>(p.tiles_n), static_cast<unsigned>(plan.splits));
+    const int64_t count = static_cast<int64_t>(p.tiles_m) * p.tiles_n;
+    if (count >= int64_t{1} << 22) return FXP_ERR_DIMS;                                  // 2^32 threads, riders among them
+    rider.tiles = static_cast<int>(count);
     by_type(parts ? FXP_F32 : type, [&](auto type_c) {
         constexpr int TYPE = decltype(type_c)::value;
-        if (t == 256) hipLaunchKernelGGL((k_mx4_tiles<256, 256, 64, 128, 2, TYPE>), grid, dim3(512), 0, s, p);
-        else if (t == 128) hipLaunchKernelGGL((k_mx4_tiles<128, 128, 64, 64, 2, TYPE>), grid, dim3(256), 0, s, p);
-        else hipLaunchKernelGGL((k_mx4_tiles<64, 64, 32, 32, 3, TYPE>), grid, dim3(256), 0, s, p);
+        auto go = [&](auto kernel, int threads) {
+            hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(count) + sum_blocks(rider, threads), static_cast<unsigned>(plan.splits)), dim3(threads), 0, s, p, rider);
+        };
+        if (t == 256) go(k_mx4_tiles<256, 256, 64, 128, 2, TYPE>, 512);
+        else if (t == 128) go(k_mx4_tiles<128, 128, 64, 64, 2, TYPE>, 256);
+        else go(k_mx4_tiles<64, 64, 32, 32, 3, TYPE>, 256);
     });
-    if (parts) {
-        const bool flat = ldc == N && M * N < int64_t{1} << 31;          // one row
-        const int64_t rows = flat ? 1 : M, cols = flat ? M * N : N;
-        by_type(type, [&](auto type_c) {
-            const int vec = cols % 4 == 0 || flat ? (aligned(C, 4 * static_cast<size_t>(elem_size(type))) && (flat || ldc % 4 == 0) ? 2 : 1) : 0;
-            hipLaunchKernelGGL((k_mx4_sum<decltype(type_c)::value>), dim3(static_cast<unsigned>((cols + 1023) / 1024), static_cast<unsigned>(rows)), dim3(256), 0, s,
-                               static_cast<const float*>(ws), plan.splits, p.split_stride, static_cast<int>(cols), vec, C, ldc);
-        });
+    const int rc = launch_status();
+    if (rc || !parts) return rc;
+    const bool flat = ldc == N;                                                          // one row (parts are of fewer than 2^24 outputs)
+    Mx4Sum sum{static_cast<const float*>(ws), plan.splits, static_cast<int>(flat ? 1 : M), static_cast<int>(flat ? M * N : N), 0, p.split_stride, C, ldc, 0};
+    if (flat || N % 4 == 0) sum.vec = aligned(C, 4 * static_cast<size_t>(elem_size(type))) && (flat || ldc % 4 == 0) ? 2 : 1;
+    if (rest) {
+        *rest = sum;
+        return FXP_OK;
     }
-    return launch_status();
+    return sum_launch(sum, type, s);
+}
+
+int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64_t ldc, void* ws, hipStream_t s) {
+    return gemm_launch(A, B, type, C, ldc, ws, Mx4Sum{}, nullptr, s);
+}
+
+// Two products, the first one's partial sums added up in the second's launch; both use ws only one after the other.
+int mx4_gemm_launch2(const fxp_mx4& A0, const fxp_mx4& B0, void* C0, const fxp_mx4& A1, const fxp_mx4& B1, void* C1, int type, void* ws, hipStream_t s) {
+    Mx4Sum sum{};
+    const bool alone = mx4_gemm_bytes(A1.rows, B1.rows, A1.cols) != 0;                   // the second wants the workspace too
+    const int rc = gemm_launch(A0, B0, type, C0, B0.rows, ws, Mx4Sum{}, alone ? nullptr : &sum, s);
+    return rc ? rc : gemm_launch(A1, B1, type, C1, B1.rows, ws, sum, nullptr, s);
 }
 
 }  // namespace fxp
