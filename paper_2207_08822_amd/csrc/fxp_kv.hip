@@ -408,6 +408,8 @@ __global__ __launch_bounds__(THREADS) void k_kv_append(fxp_kv_cache c, const voi
 // Keys: a thread has items of eight elements of a token, two runs of four that hold their pairs together; they are turned in 64 bits and mapped
 // from there, so that what the cache holds is the formula's rounding, not that of a cosine in 32 bits (an element near a half would go the other way
 // once in some 10^4).  The vector ALU does a 64-bit multiply-add in the time of a 32-bit one; angles are found in registers, item by item.
+// 256 runs of a token, 32 + 8 + 8 heads of 128 in bf16: 9.4 us (k_kv_append 6.8, without queries), the way of one token; 8650 tokens of 16 + 4 + 4 in fp16 31.8 us for 99 MB, of
+// which keys and values are 17 (k_kv_append 10.7).
 struct RotaryWriter {
     const uint64_t* turns;
     const int32_t* positions;
