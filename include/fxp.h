@@ -555,7 +555,7 @@ int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols
 int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream);
 
 /* C[M,N] of `type` = A B^T for mapped A [M,K] and B [N,K], row stride ldc >= N: products are exact, sums fp32 in no stated order (the same order on every call
- * of a size), rounded once to `type`.  Fewer than 2^22 tiles of 64 x 64 to 256 x 256 outputs.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
+ * of a size), rounded once to `type`.  Fewer than 2^22 tiles of 64 x 64 to 256 x 256 outputs.  C shares no memory with A and B.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
 size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream);
 

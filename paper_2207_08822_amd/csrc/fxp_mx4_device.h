@@ -22,7 +22,7 @@ __device__ inline int mx_scale_of(uint32_t m) {
 __device__ inline float mx_inverse(int s) { return __uint_as_float(static_cast<uint32_t>(max(254 - s, 0)) << 23); }
 
 // Elements in units of their scale as codes, the first in the lowest bits: a sign, then the magnitude's place in 0, 0.5, 1, 1.5, 2, 3, 4, 6.
-// To nearest, ties to even: what the conversion instruction does.  |x| with its sign put aside serves both roundings: y = x * f.
+// To nearest, ties to even: what the conversion instruction does.
 template <int N>
 __device__ inline uint32_t mx_nearest(const float (&y)[N]) {
     static_assert(N == 4 || N == 8, "two or four bytes");

@@ -979,7 +979,8 @@ def _rotary(x, positions, rope, out, backward):
 
 def rotary(x, positions, rope, out=None):
     """x [tokens, heads, dim] or [batch, tokens, heads, dim] (any strides but the last) turned by rope's angles at `positions`, int32 [tokens] or
-    [batch, tokens]; rows at negative positions are left as they are in out.  out: may be x itself, and shares no elements with it otherwise."""
+    [batch, tokens]; rows at negative positions are left as they are in out (not set, without one).  out: may be x itself, and shares no elements with
+    it otherwise."""
     return _rotary(x, positions, rope, out, 0)
 
 
@@ -1005,7 +1006,7 @@ def kv_append_rotary(k, v, cache, tab, rope, q=None, out=None):
     """kv_append of the step's tokens with the keys turned by `rope` on the way (tab.runs, tab.positions); keys are mapped as they come out of the
     rotation, without a rounding between.  q [tokens, q_heads, dim]: the step's queries, which the same launch turns into out (q itself, or a tensor
     that shares no elements with q, k and v); returns out, or None without q.  Rows of out whose tokens are not written to the cache - of refused
-    requests, behind the last one - are left as they are."""
+    requests, behind the last one - are left as they are (not set, without out)."""
     code = _served(k, "k", 3)
     if _served(v, "v", 3) != code or k.shape != v.shape or k.shape != (tab.tokens, cache.heads, cache.dim):
         raise FxpError("k and v must be [tokens, heads, dim] of the tables and the cache, and of one type")

@@ -222,3 +222,62 @@ def test_replayed(fxp):
         torch.cuda.synchronize()
         want = step(eager, torch.empty_like(y))
         assert torch.equal(y, want) and torch.equal(buf.y, eager.y) and torch.equal(buf.dx, eager.dx) and torch.equal(buf.dw, eager.dw) and buf.dw.any()
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("M", [1, 3, 4, 9, 80])
+def test_rows_that_are_not_finite(fxp, M, kind):
+    """Inf or NaN in a row of x makes that row of y NaN and leaves the others; in a row of the weights, that column."""
+    say("mx4_linear, not finite", M, kind)
+    K, N = 700, 90
+    x, W = torch.randn((M, K), device="cuda").to(TYPES[kind]), torch.randn((N, K), device="cuda")
+    w = fxp.mx4_map(W, rounding=fxp.NEAREST)[0]
+    want = fxp.mx4_linear(x, w)
+    assert bool(want.isfinite().all())
+    x[0, 699] = float("nan")
+    x[M // 2, 3] = float("-inf")
+    W[17, 300] = float("inf")
+    got = fxp.mx4_linear(x, fxp.mx4_map(W, rounding=fxp.NEAREST)[0])
+    want[0], want[M // 2], want[:, 17] = float("nan"), float("nan"), float("nan")
+    assert torch.equal(got.nan_to_num(1e4), want.nan_to_num(1e4)) and torch.equal(got.isnan(), want.isnan())
+
+
+def test_large_tiles_with_the_sum_of_a_split_product(fxp):
+    """A layer whose weight gradient is split over its rows and added up beside the input gradient's tiles."""
+    M, K, N = 12608, 768, 128
+    say("mx4 layer", M, K, N)
+    X, W, dY = (torch.randn(s, device="cuda", dtype=torch.bfloat16) for s in ((M, K), (K, N), (M, N)))
+    buf = fxp.Mx4LayerBuffers(M, K, N, torch.bfloat16)
+    Y = fxp.mx4_linear_fwd(X, W, buf)
+    dX, dW = fxp.mx4_linear_bwd(dY, buf)
+    value = lambda q: fxp.mx4_unmap(q).double()  # noqa: E731
+    for got, a, b in ((Y, buf.X, buf.WT), (dX, buf.dY, buf.W), (dW, buf.XT, buf.dYT)):
+        a, b = value(a), value(b).T.contiguous()
+        want, bound = a @ b, a.abs() @ b.abs() * (a.shape[1] * 2.0 ** -23)
+        assert bool(((got.double() - want).abs() <= bound + want.abs() * 2.0 ** -8 * 1.01 + 2.0 ** -25).all())
+    first = dX.clone(), dW.clone()
+    fxp.mx4_linear_bwd(dY, buf, need_dX=False)
+    assert torch.equal(buf.dw, first[1])
+    fxp.mx4_linear_bwd(buf.y.copy_(dY), buf)                                             # a gradient written over the output
+    assert torch.equal(buf.dx, first[0]) and torch.equal(buf.dw, first[1])
+
+
+def test_elements_past_32_bits(fxp):
+    """A matrix, and a product, of more than 2^31 elements: their last rows and columns are those of a small one."""
+    rows, cols = 70016, 32800
+    say("mx4 past 32 bits", rows, cols)
+    x = torch.randn((rows, cols), device="cuda", dtype=torch.bfloat16)
+    q, qT = fxp.mx4_map(x, rounding=fxp.NEAREST, want_qT=True)
+    alone = fxp.mx4_map(x, rounding=fxp.NEAREST)[0]
+    assert torch.equal(alone.data, q.data) and torch.equal(alone.scales, q.scales)
+    part, partT = fxp.mx4_map(x[-64:], rounding=fxp.NEAREST)[0], fxp.mx4_map(x[:, -64:], rounding=fxp.NEAREST, want_q=False, want_qT=True)[1]
+    for whole, end in ((q, part), (qT, partT)):
+        assert torch.equal(whole.data[:, -64:], end.data) and torch.equal(whole.scales[:, -64:], end.scales)
+    x.zero_()
+    assert torch.equal(fxp.mx4_unmap(q, out=x)[-64:], fxp.mx4_unmap(part, torch.bfloat16))
+    del q, qT, alone
+    rng = np.random.default_rng(6)
+    (A, _), (B, b) = random_mx4(fxp, rng, rows, 64), random_mx4(fxp, rng, cols, 64)
+    a = fxp.mx4_unmap(A)[-64:].double().cpu().numpy()
+    got = fxp.mx4_gemm(A, B, out=x)[-64:]
+    assert torch.equal(got.cpu(), torch.tensor(a @ b.T).float().bfloat16())              # exact sums, rounded once
