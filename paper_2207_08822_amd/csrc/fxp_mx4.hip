@@ -246,32 +246,49 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
     return typed(std::integral_constant<int, FXP_F16>{});
 }
 
-// ---- inverse mapping: a thread has eight elements of a row; bound by its stores (8192 x 8192 to bf16 30 us, 5.8 TB/s) ----
+// ---- inverse mapping ----
+//
+// A thread has 16 bytes of its output, neighbouring lanes beside each other, of one row or of two.  Bound by its stores (8192 x 8192 to bf16 30 us, 5.8 TB/s; 12608 x 768 to
+// fp32 8.5, where eight elements a thread, in two stores that leave every other 16 bytes to each other, take 10.5; 8192 x 8192 to fp32 54 and 62.5).
+constexpr int kUnmapRows = 8;           // of a workgroup
+
 template <int TYPE>
 __global__ __launch_bounds__(kMxThreads) void k_mx4_unmap(const uint8_t* __restrict__ data, const uint8_t* __restrict__ scales, int64_t rows, int64_t cols, void* y, int64_t ld,
                                                           int vec) {
-    const int64_t piece = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) % (kMxRowBytes / 4), row = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) / (kMxRowBytes / 4);
-    const int64_t c = int64_t{blockIdx.y} * kMxPanel + piece * 8;
-    if (row >= rows || c >= cols) return;
-    const int64_t line = blockIdx.y * rows + row;
-    const uint32_t codes = *reinterpret_cast<const uint32_t*>(data + line * kMxRowBytes + piece * 4);
-    const int s = scales[line * kMxRowScales + mx_scale_place(static_cast<int>(piece) / 4)];
-    // 2^-127 is a sub-normal number, and there is no number for 255
-    const float unit = s == 255 ? __uint_as_float(0x7fc00000u) : s == 0 ? __uint_as_float(0x400000u) : __uint_as_float(static_cast<uint32_t>(s) << 23);
-    float v[8];
+    constexpr int N = 16 / static_cast<int>(sizeof(typename Elem<TYPE>::T)), kThreads = kMxPanel / N, kStep = kMxThreads / kThreads, kMine = kUnmapRows / kStep;
+    const int piece = threadIdx.x % kThreads;
+    const int64_t row = int64_t{blockIdx.x} * kUnmapRows + threadIdx.x / kThreads, c = int64_t{blockIdx.y} * kMxPanel + piece * N;
+    if (c >= cols) return;
+    uint32_t codes[kMine];
+    int s[kMine];
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
-        const float2 two = mx_values(codes, b);
-        v[2 * b] = two.x * unit;
-        v[2 * b + 1] = two.y * unit;
+    for (int n = 0; n < kMine; ++n) {
+        if (row + n * kStep >= rows) break;
+        const int64_t line = blockIdx.y * rows + row + n * kStep;
+        const uint8_t* const p = data + line * kMxRowBytes + piece * (N / 2);
+        codes[n] = N == 4 ? *reinterpret_cast<const uint16_t*>(p) : *reinterpret_cast<const uint32_t*>(p);
+        s[n] = scales[line * kMxRowScales + mx_scale_place(piece * N / kMxBlock)];
     }
-    const int64_t at = row * ld + c;
-    if (vec && c + 8 <= cols) {
-        store_elems<TYPE, 8>(y, at, v);
-    } else {
-        typename Elem<TYPE>::T* const p = static_cast<typename Elem<TYPE>::T*>(y) + at;
-        for (int j = 0; j < 8; ++j)
-            if (c + j < cols) p[j] = static_cast<typename Elem<TYPE>::T>(v[j]);
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+        if (row + n * kStep >= rows) break;
+        // 2^-127 is a sub-normal number, and there is no number for 255
+        const float unit = s[n] == 255 ? __uint_as_float(0x7fc00000u) : s[n] == 0 ? __uint_as_float(0x400000u) : __uint_as_float(static_cast<uint32_t>(s[n]) << 23);
+        float v[N];
+#pragma unroll
+        for (int b = 0; b < N / 2; ++b) {
+            const float2 two = mx_values(codes[n], b);
+            v[2 * b] = two.x * unit;
+            v[2 * b + 1] = two.y * unit;
+        }
+        const int64_t at = (row + n * kStep) * ld + c;
+        if (vec && c + N <= cols) {
+            store_elems<TYPE, N>(y, at, v);
+        } else {
+            typename Elem<TYPE>::T* const p = static_cast<typename Elem<TYPE>::T*>(y) + at;
+            for (int j = 0; j < N; ++j)
+                if (c + j < cols) p[j] = static_cast<typename Elem<TYPE>::T>(v[j]);
+        }
     }
 }
 
@@ -344,8 +361,7 @@ extern "C" int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, v
     if (q->rows == 0 || q->cols == 0) return FXP_OK;
     if (!y) return FXP_ERR_NULL;
     if (!aligned(y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
-    constexpr int kRows = kMxThreads / (kMxRowBytes / 4);
-    const dim3 grid(static_cast<unsigned>((q->rows + kRows - 1) / kRows), static_cast<unsigned>(mx_panels(q->cols)));
+    const dim3 grid(static_cast<unsigned>((q->rows + kUnmapRows - 1) / kUnmapRows), static_cast<unsigned>(mx_panels(q->cols)));
     const int vec = aligned(y, 16) && ldy * elem_size(type) % 16 == 0;
     auto go = [&](auto type_c) {
         hipLaunchKernelGGL((k_mx4_unmap<decltype(type_c)::value>), grid, dim3(kMxThreads), 0, static_cast<hipStream_t>(stream), q->data, q->scales, q->rows, q->cols, y, ldy, vec);
