@@ -48,7 +48,7 @@ typedef enum fxp_status {
     FXP_ERR_OVERFLOW = -8,  /* contraction longer than an int32 sum is sure to hold (> 133144 terms) where the call has no
                                64-bit path for it: int32 output, a batched product, or no room in ws for the slices */
     FXP_ERR_TYPE = -9,      /* unknown element type */
-    FXP_ERR_VALUE = -10     /* a scalar argument outside its range */
+    FXP_ERR_VALUE = -10     /* a scalar argument outside its range, or operands that share memory where they must not */
 } fxp_status;
 
 /* Rounding of the 24-bit shifted mantissa to bits-1 magnitude bits. */
@@ -548,26 +548,27 @@ size_t fxp_mx4_scale_bytes(int64_t rows, int64_t cols);
  * along x's columns (either may be NULL), in one pass.  rounding: FXP_ROUND_NEAREST is to nearest, ties to even; FXP_ROUND_STOCHASTIC up with the
  * probability of what is cut off, in units of 2^-22: where the top 22 bits of the element's random word are less than the top 22 bits behind the code.
  * Words as in fxp_map: element i of x (row-major, without gaps) has word i % 4 of Philox block i / 4, in both copies.  Fewer than 2^24 tiles of 32 x 256
- * elements; q, qT and x share no memory. */
+ * elements; q, qT and x share no memory (FXP_ERR_VALUE). */
 int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT, uint64_t seed,
                 uint64_t stream_id, int rounding, void* stream);
-/* The values [rows, cols] that q stands for, rounded once to `type` (exact in fp32; in bf16 but for underflow). */
+/* The values [rows, cols] that q stands for, rounded once to `type` (exact in fp32; in bf16 but for underflow).  y shares no memory with q (FXP_ERR_VALUE). */
 int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, void* stream);
 
 /* C[M,N] of `type` = A B^T for mapped A [M,K] and B [N,K], row stride ldc >= N: products are exact, sums fp32 in no stated order (the same order on every call
- * of a size), rounded once to `type`.  Fewer than 2^22 tiles of 64 x 64 to 256 x 256 outputs.  C shares no memory with A and B.  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
+ * of a size), rounded once to `type`.  Fewer than 2^22 tiles of 64 x 64 to 256 x 256 outputs.  C shares no memory with A and B (FXP_ERR_VALUE).  ws: fxp_mx4_gemm_workspace_bytes bytes (may be 0), 256-byte aligned. */
 size_t fxp_mx4_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* C, int64_t ldc, void* ws, size_t ws_bytes, void* stream);
 
 /* Y[M,N] = X[M,K] W of `type`, W = [N,K] mapped (W^T with blocks along the contraction: fxp_mx4_map's qT of W[K,N]); X is mapped to nearest on the way.  Row strides
- * ldx >= K, ldy >= N.  Any M, one row to many.  Y must not overlap X.  ws: fxp_mx4_linear_workspace_bytes bytes (0, and NULL allowed, for M <= 4), 256-byte aligned. */
+ * ldx >= K, ldy >= N.  Any M, one row to many.  Y must not overlap X, and shares no memory with W (FXP_ERR_VALUE).  ws: fxp_mx4_linear_workspace_bytes bytes (0, and NULL allowed, for M <= 4), 256-byte aligned. */
 size_t fxp_mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, const fxp_mx4* W, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
 
 /* A layer's training step, as fxp_linear_fwd / _bwd with blocks of 4-bit floats in place of int8 tensors: Y = X W, dX = dY W^T, dW = X^T dY, dense
  * row-major of one `type`, every operand mapped along the contraction that it is used in (the same random words in both copies).  The mapped operands belong to the
  * caller: fwd fills X [M,K], WT [N,K], XT [K,M] and W [K,N] (the last two may have data NULL where no backward call follows), bwd reads XT for dW and W for dX, and
- * fills dY [M,N] for dX and dYT [N,M] for dW.  dX or dW may be NULL.  The mapped operands share no memory.  Streams: (step << 8) | 0, 1, 2 for X, W, dY; step < 2^56.
+ * fills dY [M,N] for dX and dYT [N,M] for dW.  dX or dW may be NULL.  The mapped operands of a call share no memory
+ * with each other or with its dense matrices, nor does dX with dW (FXP_ERR_VALUE); Y may lie over X or W, dX and dW over dY, which are mapped before.  Streams: (step << 8) | 0, 1, 2 for X, W, dY; step < 2^56.
  * ws: fxp_mx4_layer_workspace_bytes bytes (at least 256), 256-byte aligned. */
 typedef struct fxp_mx4_layer {
     fxp_mx4 X, XT, W, WT, dY, dYT;

@@ -3,6 +3,7 @@
 // A mapped matrix serves products that contract over its columns; a training step contracts every operand along both of its axes and therefore maps it twice,
 // with blocks of 32 along the rows and of 32 along the columns.  Both copies come out of one pass: 32 x 32 elements hold whole blocks of both.
 #include <algorithm>
+#include <initializer_list>
 
 #include "fxp_mx4_device.h"
 
@@ -309,6 +310,18 @@ static bool meet(const fxp_mx4& a, const fxp_mx4& b) {
     return meet(a.data, na * kMxRowBytes, b.data, nb * kMxRowBytes) || meet(a.data, na * kMxRowBytes, b.scales, nb * kMxRowScales) ||
            meet(a.scales, na * kMxRowScales, b.data, nb * kMxRowBytes) || meet(a.scales, na * kMxRowScales, b.scales, nb * kMxRowScales);
 }
+// whether rows of a matrix, `stride` bytes from each other, share bytes with a mapped matrix
+static bool meet(const void* m, int64_t rows, int64_t row_bytes, int64_t stride, const void* b, int64_t bytes) {
+    if (rows <= 0 || row_bytes <= 0 || bytes <= 0) return false;
+    // the first row that ends behind b's first byte: does it begin before b's end?
+    const int64_t from = static_cast<int64_t>(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(m));
+    const int64_t row = from < row_bytes ? 0 : (from - row_bytes) / stride + 1;
+    return row < rows && row * stride < from + bytes;
+}
+static bool meet(int type, const void* m, int64_t rows, int64_t cols, int64_t ld, const fxp_mx4& q) {
+    const int64_t size = elem_size(type), n = mx_panels(q.cols) * q.rows;
+    return meet(m, rows, cols * size, ld * size, q.data, n * kMxRowBytes) || meet(m, rows, cols * size, ld * size, q.scales, n * kMxRowScales);
+}
 
 static int check_map(int type, const void* x, int64_t ldx, int64_t rows, int64_t cols, const fxp_mx4* q, const fxp_mx4* qT) {
     if (!known_type(type)) return FXP_ERR_TYPE;
@@ -348,6 +361,8 @@ extern "C" int fxp_mx4_map(int type, const void* x, int64_t ldx, int64_t rows, i
     const int rc = fxp::check_map(type, x, ldx, rows, cols, q, qT);
     if (rc) return rc;
     if (!fxp::known_rounding(rounding)) return FXP_ERR_ROUNDING;
+    for (const fxp_mx4* t : {q, qT})
+        if (t && fxp::meet(type, x, rows, cols, ldx, *t)) return FXP_ERR_VALUE;
     const fxp::Mx4Map m = fxp::map_of(x, ldx, rows, cols, q, qT, stream_id);
     return fxp::mx4_map_launch(type, &m, 1, seed, rounding, static_cast<hipStream_t>(stream));
 }
@@ -361,6 +376,7 @@ extern "C" int fxp_mx4_unmap(const fxp_mx4* q, int type, void* y, int64_t ldy, v
     if (q->rows == 0 || q->cols == 0) return FXP_OK;
     if (!y) return FXP_ERR_NULL;
     if (!aligned(y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
+    if (meet(type, y, q->rows, q->cols, ldy, *q)) return FXP_ERR_VALUE;
     const dim3 grid(static_cast<unsigned>((q->rows + kUnmapRows - 1) / kUnmapRows), static_cast<unsigned>(mx_panels(q->cols)));
     const int vec = aligned(y, 16) && ldy * elem_size(type) % 16 == 0;
     auto go = [&](auto type_c) {
@@ -394,6 +410,8 @@ extern "C" int fxp_mx4_gemm(const fxp_mx4* A, const fxp_mx4* B, int type, void* 
     const size_t need = mx4_gemm_bytes(A->rows, B->rows, A->cols);
     if (need && (!ws || ws_bytes < need)) return FXP_ERR_WORKSPACE;
     if (need && !aligned(ws, 256)) return FXP_ERR_ALIGN;
+    for (const fxp_mx4* q : {A, B})
+        if (meet(type, C, A->rows, B->rows, ldc, *q)) return FXP_ERR_VALUE;
     return mx4_gemm_launch(*A, *B, type, C, ldc, ws, static_cast<hipStream_t>(stream));
 }
 
@@ -421,11 +439,13 @@ extern "C" int fxp_mx4_linear(int type, const void* X, int64_t ldx, int64_t M, c
     if (M == 0 || N == 0) return FXP_OK;
     if (!Y) return FXP_ERR_NULL;
     if (!aligned(Y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
-    if (mx4_is_fused(M)) return mx4_fused_launch(type, X, ldx, M, *W, Y, ldy, static_cast<hipStream_t>(stream));
+    const bool shared = meet(type, Y, M, N, ldy, *W);
+    if (mx4_is_fused(M)) return shared ? static_cast<int>(FXP_ERR_VALUE) : mx4_fused_launch(type, X, ldx, M, *W, Y, ldy, static_cast<hipStream_t>(stream));
     const size_t codes = round_up(static_cast<size_t>(mx_panels(K) * M * kMxRowBytes), 256), mapped = mapped_bytes(M, K);
     const size_t need = fxp_mx4_linear_workspace_bytes(M, N, K);               // 0: a few rows, or a contraction of nothing
     if (need && (!ws || ws_bytes < need)) return FXP_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    if (shared) return FXP_ERR_VALUE;
     uint8_t* const at = static_cast<uint8_t*>(ws);
     const fxp_mx4 q{at, at + codes, M, K};
     const Mx4Map m = map_of(X, ldx, M, K, &q, nullptr, 0);
@@ -459,6 +479,12 @@ static int check_layer(const fxp_mx4_layer* l, int64_t M, int64_t K, int64_t N, 
     }
     return FXP_OK;
 }
+// Whether a dense matrix shares bytes with one of the operands that are there.
+static bool meets_one(int type, const void* m, int64_t rows, int64_t cols, std::initializer_list<const fxp_mx4*> operands) {
+    for (const fxp_mx4* q : operands)
+        if (m && q->data && meet(type, m, rows, cols, cols, *q)) return true;
+    return false;
+}
 static const fxp_mx4* if_there(const fxp_mx4& q) { return q.data ? &q : nullptr; }
 }  // namespace fxp
 
@@ -481,6 +507,8 @@ extern "C" int fxp_mx4_linear_fwd(int type, const void* X, const void* W, int64_
     if (!aligned(Y, static_cast<size_t>(elem_size(type)))) return FXP_ERR_ALIGN;
     if (!ws || ws_bytes < fxp_mx4_layer_workspace_bytes(M, K, N)) return FXP_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
+    const std::initializer_list<const fxp_mx4*> operands = {&layer->X, &layer->XT, &layer->W, &layer->WT};
+    if (meets_one(type, X, M, K, operands) || meets_one(type, W, K, N, operands) || meets_one(type, Y, M, N, operands)) return FXP_ERR_VALUE;
     const Mx4Map maps[2] = {map_of(X, K, M, K, &layer->X, if_there(layer->XT), step << 8), map_of(W, N, K, N, if_there(layer->W), &layer->WT, (step << 8) | 1)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
     rc = mx4_map_launch(type, maps, 2, seed, rounding, s);
@@ -501,6 +529,12 @@ extern "C" int fxp_mx4_linear_bwd(int type, const void* dY, const fxp_mx4_layer*
     if (!ws || ws_bytes < fxp_mx4_layer_workspace_bytes(M, K, N)) return FXP_ERR_WORKSPACE;
     if (!aligned(ws, 256)) return FXP_ERR_ALIGN;
     if (!dX && !dW) return FXP_OK;
+    // what a call does not use may lie anywhere
+    const fxp_mx4 none{};
+    const std::initializer_list<const fxp_mx4*> operands = {dX ? &layer->dY : &none, dX ? &layer->W : &none, dW ? &layer->dYT : &none, dW ? &layer->XT : &none};
+    if (meets_one(type, dY, M, N, {dX ? &layer->dY : &none, dW ? &layer->dYT : &none}) || meets_one(type, dX, M, K, operands) || meets_one(type, dW, K, N, operands) ||
+        (dX && dW && meet(dX, M * K * elem_size(type), dW, K * N * elem_size(type))))
+        return FXP_ERR_VALUE;
     const Mx4Map m = map_of(dY, N, M, N, dX ? &layer->dY : nullptr, dW ? &layer->dYT : nullptr, (step << 8) | 2);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     rc = mx4_map_launch(type, &m, 1, seed, rounding, s);

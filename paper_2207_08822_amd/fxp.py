@@ -1043,6 +1043,12 @@ def kv_append_rotary(k, v, cache, tab, rope, q=None, out=None):
 MX4_PANEL = 256         # columns of a panel of a mapped matrix
 
 
+def _check_mx4(rc, what):
+    if rc == -10:                         # FXP_ERR_VALUE: of these calls' arguments only shared memory has it
+        raise FxpError(f"{what}: operands share memory")
+    _check(rc, what)
+
+
 class Mx4:
     """A matrix [rows, cols] in 4-bit floats with a scale for each 32 elements of a row (the layout of include/fxp.h), for products that contract over cols:
     data uint8 [panels, rows, 128], scales uint8 [panels, rows, 8]."""
@@ -1108,7 +1114,7 @@ def _mx4_like(x, rows, cols):
 def mx4_map(x, rounding=STOCHASTIC, seed=0, stream_id=0, want_q=True, want_qT=False, out=None):
     """(q, qT): x [rows, cols] mapped with blocks along its rows, for products that contract over cols, and x transposed with blocks along its columns, for
     products that contract over rows; None where not wanted.  rounding: NEAREST (ties to even) or STOCHASTIC (Philox words as in map).  out: the pair of
-    Mx4 to fill, None where not wanted."""
+    Mx4 to fill, None where not wanted; they share no memory with x or each other."""
     code = _served(x, "x", 2)
     rows, cols = x.shape
     if out is None:
@@ -1122,13 +1128,13 @@ def mx4_map(x, rounding=STOCHASTIC, seed=0, stream_id=0, want_q=True, want_qT=Fa
                     raise FxpError("out must be the mapped matrix of x's shape, and of the transposed one")
     if q is None and qT is None:
         raise FxpError("neither copy is wanted")
-    _check(lib().fxp_mx4_map(code, x.data_ptr(), _row_stride(x, "x"), rows, cols, q.ref if q else None, qT.ref if qT else None, seed, stream_id, rounding, _stream()),
-           "fxp_mx4_map")
+    _check_mx4(lib().fxp_mx4_map(code, x.data_ptr(), _row_stride(x, "x"), rows, cols, q.ref if q else None, qT.ref if qT else None, seed, stream_id, rounding, _stream()),
+               "fxp_mx4_map")
     return q, qT
 
 
 def mx4_unmap(q, dtype=torch.float32, out=None):
-    """The values [rows, cols] that q stands for, in `dtype` or out's type."""
+    """The values [rows, cols] that q stands for, in `dtype` or out's type; out shares no memory with q."""
     _here(q, "q")
     if out is None:
         if dtype not in _TYPES:
@@ -1137,12 +1143,12 @@ def mx4_unmap(q, dtype=torch.float32, out=None):
     code = _served(out, "out", 2)
     if out.shape != (q.rows, q.cols):
         raise FxpError("out must be [rows, cols] of q")
-    _check(lib().fxp_mx4_unmap(q.ref, code, out.data_ptr(), _row_stride(out, "out"), _stream()), "fxp_mx4_unmap")
+    _check_mx4(lib().fxp_mx4_unmap(q.ref, code, out.data_ptr(), _row_stride(out, "out"), _stream()), "fxp_mx4_unmap")
     return out
 
 
 def mx4_gemm(A, B, dtype=torch.float32, out=None, ws=None):
-    """C [A.rows, B.rows] = A B^T of two mapped matrices, in `dtype` or out's type."""
+    """C [A.rows, B.rows] = A B^T of two mapped matrices, in `dtype` or out's type; out shares no memory with them."""
     _here(A, "A")
     _here(B, "B")
     if A.cols != B.cols:
@@ -1159,13 +1165,13 @@ def mx4_gemm(A, B, dtype=torch.float32, out=None, ws=None):
     else:
         nbytes = int(lib().fxp_mx4_gemm_workspace_bytes(A.rows, B.rows, A.cols))
         ws = out.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-    _check(lib().fxp_mx4_gemm(A.ref, B.ref, code, out.data_ptr(), _row_stride(out, "out"), _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_mx4_gemm")
+    _check_mx4(lib().fxp_mx4_gemm(A.ref, B.ref, code, out.data_ptr(), _row_stride(out, "out"), _p(ws), ws.numel() if ws is not None else 0, _stream()), "fxp_mx4_gemm")
     return out
 
 
 def mx4_linear(x, w, out=None, ws=None):
     """y [M, N] = x [M, K] W of x's type; w: W transposed and mapped, [N, K] (mx4_map(W, want_q=False, want_qT=True)[1] of W [K, N]).  x is mapped to nearest on the way.  Any M,
-    one token to many.  out: may not share elements with x."""
+    one token to many.  out: may not share elements with x, or memory with w."""
     code = _served(x, "x", 2)
     M, K = x.shape
     if K != w.cols:
@@ -1184,8 +1190,8 @@ def mx4_linear(x, w, out=None, ws=None):
         _index(ws, "ws", dtype=torch.uint8)
     elif M > 4:
         ws = x.new_empty(int(lib().fxp_mx4_linear_workspace_bytes(M, w.rows, K)), dtype=torch.uint8)
-    _check(lib().fxp_mx4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, w.ref, out.data_ptr(), ldy, _p(ws), ws.numel() if ws is not None else 0, _stream()),
-           "fxp_mx4_linear")
+    _check_mx4(lib().fxp_mx4_linear(code, x.data_ptr(), _row_stride(x, "x"), M, w.ref, out.data_ptr(), ldy, _p(ws), ws.numel() if ws is not None else 0, _stream()),
+               "fxp_mx4_linear")
     return out
 
 
@@ -1218,8 +1224,8 @@ def mx4_linear_fwd(X, W, buf, seed=0, step=0, rounding=STOCHASTIC):
     _here(buf, "buf")
     _layer_operand(X, (buf.M, buf.K), buf, "X")
     _layer_operand(W, (buf.K, buf.N), buf, "W")
-    _check(lib().fxp_mx4_linear_fwd(_TYPES[buf.dtype], X.data_ptr(), W.data_ptr(), buf.M, buf.K, buf.N, buf.y.data_ptr(), buf.ref, seed, step, rounding,
-                                    buf.ws.data_ptr(), buf.ws.numel(), _stream()), "fxp_mx4_linear_fwd")
+    _check_mx4(lib().fxp_mx4_linear_fwd(_TYPES[buf.dtype], X.data_ptr(), W.data_ptr(), buf.M, buf.K, buf.N, buf.y.data_ptr(), buf.ref, seed, step, rounding,
+                                       buf.ws.data_ptr(), buf.ws.numel(), _stream()), "fxp_mx4_linear_fwd")
     return buf.y
 
 
@@ -1228,6 +1234,6 @@ def mx4_linear_bwd(dY, buf, seed=0, step=0, rounding=STOCHASTIC, need_dX=True, n
     _here(buf, "buf")
     _layer_operand(dY, (buf.M, buf.N), buf, "dY")
     dX, dW = buf.dx if need_dX else None, buf.dw if need_dW else None
-    _check(lib().fxp_mx4_linear_bwd(_TYPES[buf.dtype], dY.data_ptr(), buf.ref, buf.M, buf.K, buf.N, _p(dX), _p(dW), seed, step, rounding, buf.ws.data_ptr(),
-                                    buf.ws.numel(), _stream()), "fxp_mx4_linear_bwd")
+    _check_mx4(lib().fxp_mx4_linear_bwd(_TYPES[buf.dtype], dY.data_ptr(), buf.ref, buf.M, buf.K, buf.N, _p(dX), _p(dW), seed, step, rounding, buf.ws.data_ptr(),
+                                       buf.ws.numel(), _stream()), "fxp_mx4_linear_bwd")
     return dX, dW

@@ -1,0 +1,82 @@
+"""Matrices in 4-bit floats beside the tensors that they are made from and that are made from them, in one buffer: right up to the last byte, refused past it."""
+import pytest
+
+from tests.gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def fxp():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a GPU: there is no CPU path in libfxp")
+    from paper_2207_08822_amd import fxp as binding
+    binding.lib()
+    return binding
+
+
+def refused(fxp, f):
+    with pytest.raises(fxp.FxpError, match="share memory"):
+        f()
+
+
+def test_neighbours_in_one_buffer(fxp):
+    """A mapped matrix between a tensor's rows, which are 1024 bytes apart, and its tensor behind it."""
+    say("mx4, one buffer")
+    rows, cols = 3, 64                                          # 384 bytes of codes, 24 of scales
+    room = torch.zeros(8192, dtype=torch.uint8, device="cuda")
+    x = room[:3072].view(torch.float32).view(3, 256)[:, :cols]
+    x.copy_(torch.randn((rows, cols), device="cuda"))
+    value = x.clone()
+    want = fxp.mx4_map(value, rounding=fxp.NEAREST)[0]
+    at = lambda codes, scales: fxp.Mx4.of(room[codes:codes + 384].view(1, 3, 128), room[scales:scales + 24].view(1, 3, 8), rows, cols)  # noqa: E731
+    for codes, scales in ((256, 640), (640, 256), (1280, 2304), (4096, 1000)):
+        q = at(codes, scales)
+        assert fxp.mx4_map(x, rounding=fxp.NEAREST, out=(q, None))[0] is q
+        assert torch.equal(q.data, want.data) and torch.equal(q.scales, want.scales) and torch.equal(x, value)
+        y = room[:3072].view(torch.float32).view(3, 256)[:, 192:] if codes == 256 else room[5120:5888].view(torch.float32).view(3, 64)
+        assert torch.equal(fxp.mx4_unmap(q, out=y), fxp.mx4_unmap(want)) and torch.equal(q.data, want.data) and torch.equal(q.scales, want.scales)
+    for codes, scales in ((240, 640), (256, 1000 + 16), (656, 256), (2048, 4096), (4096, 2296)):
+        q = at(codes, scales)
+        refused(fxp, lambda: fxp.mx4_map(x, out=(q, None)))
+        refused(fxp, lambda: fxp.mx4_unmap(q, out=x))
+    assert torch.equal(x, value)
+
+
+def test_outputs_over_operands_are_refused(fxp):
+    x = torch.randn((70, 64), device="cuda")
+    room = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
+    w = fxp.Mx4.of(room[:64 * 128].view(1, 64, 128), room[8192:8192 + 512].view(1, 64, 8), 64, 64)
+    fxp.mx4_map(x[:64], rounding=fxp.NEAREST, out=(w, None))
+    codes = w.data.clone()
+    for M in (1, 3, 40, 70):
+        inside = room[8192 + 508:8192 + 508 + M * 256].view(torch.float32).view(M, 64)
+        beside = room[8192 + 512:8192 + 512 + M * 256].view(torch.float32).view(M, 64)
+        refused(fxp, lambda: fxp.mx4_linear(x[:M], w, out=inside))
+        refused(fxp, lambda: fxp.mx4_gemm(w, w, out=room[:64 * 256].view(torch.float32).view(64, 64)))
+        assert torch.equal(fxp.mx4_linear(x[:M], w, out=beside), fxp.mx4_linear(x[:M], w))
+        q = fxp.mx4_map(x[:M], rounding=fxp.NEAREST)[0]
+        refused(fxp, lambda: fxp.mx4_gemm(q, w, out=inside))
+        assert torch.equal(fxp.mx4_gemm(q, w, out=beside), fxp.mx4_gemm(q, w))
+    assert torch.equal(w.data, codes)
+
+
+def test_a_layer_whose_gradients_are_one_buffer(fxp):
+    M, K, N = 40, 64, 30
+    X, W, dY = (torch.randn(s, device="cuda") for s in ((M, K), (K, N), (M, N)))
+    buf = fxp.Mx4LayerBuffers(M, K, N)
+    fxp.mx4_linear_fwd(X, W, buf)
+    dX, dW = (g.clone() for g in fxp.mx4_linear_bwd(dY, buf))
+    own = buf.dx, buf.dw
+    room = torch.zeros(M * K + K * N, device="cuda")
+    buf.dx, buf.dw = room[:M * K].view(M, K), room[M * K - 1:M * K - 1 + K * N].view(K, N)
+    refused(fxp, lambda: fxp.mx4_linear_bwd(dY, buf))
+    buf.dw = room[M * K:].view(K, N)
+    assert all(torch.equal(a, b) for a, b in zip(fxp.mx4_linear_bwd(dY, buf), (dX, dW)))
+    buf.dx, buf.dw = own
+    # the output over the input, a gradient over the upstream gradient: both are mapped before
+    Y = fxp.mx4_linear_fwd(X, W, buf).clone()
+    buf.y = X.view(-1)[:M * N].view(M, N)
+    assert torch.equal(fxp.mx4_linear_fwd(X, W, buf), Y)
