@@ -484,6 +484,7 @@ int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int typ
  * on stay as they are.  turns[i] is f_i as a fraction of a turn in units of 2^-64, modulo one turn: the angle of every 31-bit position is
  * exact to 2^-34 turns.  Host struct; rot even, 2 .. min(dim, FXP_ROTARY_MOST), 0 < amplitude < 1e30; turns [rot / 2] on the device, 8-byte aligned. */
 #define FXP_ROTARY_MOST 1024
+#define FXP_ROTARY_ZERO 0x100       /* of fxp_rotary's `backward` */
 typedef struct fxp_rotation {
     const uint64_t* turns;
     int64_t rot;
@@ -493,8 +494,9 @@ typedef struct fxp_rotation {
 
 /* y = x turned by its positions, or with `backward` by the opposite angles (and stretched alike): the gradient of that.  x and y: [batch, tokens,
  * heads, dim] of `type` at any strides >= 0 of the first three (fastest where bases, strides, rot / 2 and dim - rot are multiples of 16 bytes);
- * positions: int32, sequence b's at p_batch * b (0: the same for all).  Rows at negative positions are left as they are in y.  y may be x (with
- * x's strides) and shares no elements with it otherwise; y's rows may not overlap.  Cosines and sums are fp32, rounded once to `type`.
+ * positions: int32, sequence b's at p_batch * b (0: the same for all).  Rows at negative positions are left as they are in y; with FXP_ROTARY_ZERO
+ * added to `backward` (0 or 1) they become zeros, every element of them.  y may be x (with x's strides) and shares no elements with it otherwise; y's
+ * rows may not overlap.  Cosines and sums are fp32, rounded once to `type`.
  * heads <= 65535, dim <= 65536; fewer than 2^24 workgroups (of at least one token of one sequence, some 16 KiB of x where a sequence has them). */
 int fxp_rotary(const fxp_rotation* rotation, int backward, int type, int64_t batch, int64_t tokens, int64_t heads, int64_t dim,
                const void* x, int64_t x_batch, int64_t x_token, int64_t x_head, const int32_t* positions, int64_t p_batch, void* y,

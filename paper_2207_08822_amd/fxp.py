@@ -966,6 +966,7 @@ def _rotary(x, positions, rope, out, backward):
         raise FxpError("the rotated part is larger than a head")
     if out is None:
         out = x.new_empty(x.shape)
+        backward |= 0x100                 # FXP_ROTARY_ZERO: no row of it holds what was in the memory before
     elif _served(out, "out", x.dim()) != code or out.shape != x.shape or _rows_overlap(out):
         raise FxpError("out must have the shape and type of x, and rows that do not overlap")
     elif not _same_rows(out, x) and _share(x, out):
@@ -979,7 +980,7 @@ def _rotary(x, positions, rope, out, backward):
 
 def rotary(x, positions, rope, out=None):
     """x [tokens, heads, dim] or [batch, tokens, heads, dim] (any strides but the last) turned by rope's angles at `positions`, int32 [tokens] or
-    [batch, tokens]; rows at negative positions are left as they are in out (not set, without one).  out: may be x itself, and shares no elements with
+    [batch, tokens]; rows at negative positions are left as they are in out (zeros, without one).  out: may be x itself, and shares no elements with
     it otherwise."""
     return _rotary(x, positions, rope, out, 0)
 
