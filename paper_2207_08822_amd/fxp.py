@@ -991,16 +991,18 @@ def rotary_bwd(dy, positions, rope, out=None):
 
 
 def _meet(a, b):
-    """Whether tensors [tokens, heads, dim] of one type share elements; exact where a token's heads lie together and tokens are as far apart in both."""
+    """Whether tensors [tokens, heads, dim] of one type share elements; exact where a token's heads lie together and tokens are as far apart in both, and
+    where both have as many heads, tokens and heads as far apart in both."""
     (a0, a1), (b0, b1) = _span(a), _span(b)
     if a1 <= b0 or b1 <= a0 or not a.numel() or not b.numel():
         return False
     step = a.stride(0)
     reach = [(t.shape[1] - 1) * t.stride(1) + t.shape[2] for t in (a, b)]
-    if a.shape[0] <= 1 or b.shape[0] <= 1 or step != b.stride(0) or max(reach) > step:
-        return True
-    at = (b0 - a0) // a.element_size() % step           # of a token of b behind one of a
-    return at < reach[0] or at + reach[1] > step
+    if a.shape[0] > 1 and b.shape[0] > 1 and step == b.stride(0) and max(reach) <= step:
+        at = (b0 - a0) // a.element_size() % step       # of a token of b behind one of a
+        if at >= reach[0] and at + reach[1] <= step:
+            return False
+    return a.shape[:2] != b.shape[:2] or _share(a, b)
 
 
 def kv_append_rotary(k, v, cache, tab, rope, q=None, out=None):
