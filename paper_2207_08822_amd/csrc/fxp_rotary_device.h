@@ -64,7 +64,7 @@ inline int check_rotation(const fxp_rotation* r, int64_t dim) {
     if (!r || !r->turns) return FXP_ERR_NULL;
     if (r->rot < 2 || r->rot > dim || r->rot % 2 || r->rot > FXP_ROTARY_MOST) return FXP_ERR_DIMS;
     if (!aligned(r->turns, 8)) return FXP_ERR_ALIGN;
-    if (!(r->amplitude > 0.0 && r->amplitude < 1e30)) return FXP_ERR_VALUE;
+    if (!(r->amplitude >= 0x1p-126 && r->amplitude < 1e30)) return FXP_ERR_VALUE;           // below, fp32 has fewer digits of it, or none
     return FXP_OK;
 }
 

@@ -925,8 +925,8 @@ class Rotary:
                  device="cuda"):
         if dim < 2 or dim % 2 or dim > 1024:
             raise FxpError("dim must be even, 2 to 1024")
-        if not base > 0 or not factor > 0 or not 0 < amplitude < 1e30:
-            raise FxpError("base, factor and amplitude must be positive")
+        if not base > 0 or not factor > 0 or not 2.0 ** -126 <= amplitude < 1e30:
+            raise FxpError("base, factor and amplitude must be positive, amplitude from 2^-126 to 1e30")
         if frequencies is None:
             if scaling == "base" and dim > 2:
                 base = base * factor ** (dim / (dim - 2))
