@@ -533,9 +533,11 @@ static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
                                dim3(64 * W), 0, s, g);
         };
         auto sized = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
-            if (p.panels > std::max(4, 8 * decltype(u_c)::value / 2)) go(mt_c, u_c, w_c, fused_c);
-            else if (p.panels > 4) go(mt_c, IC<1>{}, IC<8>{}, fused_c);
-            else if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{}, fused_c);
+            constexpr int U = decltype(u_c)::value;
+            if (p.panels > 4 * U) return go(mt_c, u_c, w_c, fused_c);
+            if constexpr (U > 1)
+                if (p.panels > 4) return go(mt_c, IC<1>{}, IC<8>{}, fused_c);
+            if (p.panels > 1) go(mt_c, IC<1>{}, IC<4>{}, fused_c);
             else go(mt_c, IC<1>{}, IC<1>{}, fused_c);
         };
         if (fused && p.M == 1) sized(IC<1>{}, IC<4>{}, IC<8>{}, IC<1>{});
