@@ -319,7 +319,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_mx4_tiles(Mx4Pro
 
 // ---- a few rows ----
 //
-// A workgroup has NT x 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up at the end.  A wave has U panels in flight, straight to LDS and out of it
+// A workgroup has 16 rows of B (outputs) and all of A's; its waves take panels in turn and add up at the end.  A wave has U panels in flight, straight to LDS and out of it
 // again: a load of its own registers would have neighbouring lanes in different rows, 64 accesses of a cache line where 1024 bytes in a row are eight (37 x 4096 x 8192
 // 9.5 us, so 5.3).  Bound by B's bytes where all of its panels are in flight (one row by 8192 x 8192 8.6 us, 36 MB at 4.4 TB/s; 37 x 4100 x 9001 8.5).
 // FUSED: A is not mapped yet; up to four rows of it.  A wave maps the panels that it takes, a row at a time, four elements a lane: less than a launch of its own.
@@ -332,22 +332,20 @@ struct Mx4Rows {
     int K, vec;
 };
 
-template <int MT, int NT, int U, int WAVES, int TYPE, int FUSED>         // FUSED: 0, or the rows of A
+template <int MT, int U, int WAVES, int TYPE, int FUSED>         // FUSED: 0, or the rows of A
 __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
     const Mx4Product& p = g.p;
-    constexpr int RA = FUSED ? FUSED : 16 * MT, RB = 16 * NT;
+    constexpr int RA = FUSED ? FUSED : 16 * MT, RB = 16;
     constexpr int kScalesB = (RB * kMxRowScales + 255) / 256 * 256, kScalesA = FUSED ? (RA * kMxRowScales + 15) / 16 * 16 : (RA * kMxRowScales + 255) / 256 * 256;
     constexpr int kSlot = (RA + RB) * kMxRowBytes + kScalesA + kScalesB, kAtA = RB * kMxRowBytes, kAtSB = kAtA + RA * kMxRowBytes, kAtSA = kAtSB + kScalesB;
-    constexpr int kBytes = WAVES * U * kSlot, kSums = WAVES * MT * NT * 64 * 16;
+    constexpr int kBytes = WAVES * U * kSlot, kSums = WAVES * MT * 64 * 16;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[kBytes > kSums ? kBytes : kSums];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = static_cast<int>(blockIdx.x) * RB, r = lane & 15, kb = lane >> 4;
     using T = typename Elem<TYPE>::T;
-    v4f acc[MT][NT];
+    v4f acc[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) acc[m][n] = {};
+    for (int m = 0; m < MT; ++m) acc[m] = {};
     // lane l of a load has 16 bytes of row l / 8 of eight, exchanged by the row as in the tiles
     int from[2];
 #pragma unroll
@@ -377,11 +375,10 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
             }
             const uint8_t* const b = p.b.data + int64_t{t} * p.b.rows * kMxRowBytes;
 #pragma unroll
-            for (int i = 0; i < 2 * NT; ++i)
+            for (int i = 0; i < 2; ++i)
                 load_to_lds<16>(b, there ? p.b.rows * kMxRowBytes : 0, (n0 + 8 * i) * kMxRowBytes + from[i % 2], slot + i * 1024);
             const uint8_t* const sb = p.b.scales + int64_t{t} * p.b.rows * kMxRowScales;
-#pragma unroll
-            for (int i = 0; i < kScalesB / 256; ++i) load_to_lds<4>(sb, there ? p.b.rows * kMxRowScales : 0, (n0 + 32 * i) * kMxRowScales + 4 * lane, slot + kAtSB + 256 * i);
+            load_to_lds<4>(sb, there ? p.b.rows * kMxRowScales : 0, n0 * kMxRowScales + 4 * lane, slot + kAtSB);
             if constexpr (!FUSED) {
                 const uint8_t* const a = p.a.data + int64_t{t} * p.a.rows * kMxRowBytes;
 #pragma unroll
@@ -410,14 +407,11 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const uint8_t* const slot = mine + u * kSlot;
-            v4i b[NT][2], a[MT][2];
-            int eb[NT], ea[MT];
+            v4i b[2], a[MT][2];
+            int ea[MT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) b[n][h] = *reinterpret_cast<const v4i*>(slot + (16 * n + r) * kMxRowBytes + ((4 * h + kb) ^ swz) * 16);
-                eb[n] = *reinterpret_cast<const int*>(slot + kAtSB + (16 * n + r) * kMxRowScales + 4 * (kb & 1)) >> shift;
-            }
+            for (int h = 0; h < 2; ++h) b[h] = *reinterpret_cast<const v4i*>(slot + r * kMxRowBytes + ((4 * h + kb) ^ swz) * 16);
+            const int eb = *reinterpret_cast<const int*>(slot + kAtSB + r * kMxRowScales + 4 * (kb & 1)) >> shift;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 // rows of X that are not there: FUSED has zeros where it has a slot, and reads its last row again, as zeros, where it has none
@@ -431,38 +425,34 @@ __global__ __launch_bounds__(WAVES * 64) void k_mx4_rows(Mx4Rows g) {
                 if (FUSED && r >= FUSED) ea[m] = 0;
             }
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    acc[m][n] = mfma16<0, 0>(b[n][0], a[m][0], acc[m][n], eb[n], ea[m]);
-                    acc[m][n] = mfma16<2, 2>(b[n][1], a[m][1], acc[m][n], eb[n], ea[m]);
-                }
+            for (int m = 0; m < MT; ++m) {
+                acc[m] = mfma16<0, 0>(b[0], a[m][0], acc[m], eb, ea[m]);
+                acc[m] = mfma16<2, 2>(b[1], a[m][1], acc[m], eb, ea[m]);
+            }
         }
         wait_loads_and_lds<0>();
         wave_barrier();                                             // before the slots are loaded again
     }
-    v4f(*const sums)[MT * NT][64] = reinterpret_cast<v4f(*)[MT * NT][64]>(lds);
+    v4f(*const sums)[MT][64] = reinterpret_cast<v4f(*)[MT][64]>(lds);
     if constexpr (WAVES > 1) {
         __syncthreads();                                            // the slots of other waves
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) sums[wave][m * NT + n][lane] = acc[m][n];
+        for (int m = 0; m < MT; ++m) sums[wave][m][lane] = acc[m];
         __syncthreads();
     }
-    // outputs 4 kb .. 4 kb + 3 of a tile of B's rows, row r of A's
-    for (int tile = wave; tile < MT * NT; tile += WAVES) {
+    // outputs 4 kb .. 4 kb + 3 of B's rows, row r of a tile of A's
+    for (int tile = wave; tile < MT; tile += WAVES) {
         v4f s;
         if constexpr (WAVES > 1) {
             s = sums[0][tile][lane];
             for (int w = 1; w < WAVES; ++w) s += sums[w][tile][lane];
         } else {
-            s = acc[0][0];
+            s = acc[0];
 #pragma unroll
-            for (int i = 1; i < MT * NT; ++i)
-                if (i == tile) s = acc[i / NT][i % NT];
+            for (int i = 1; i < MT; ++i)
+                if (i == tile) s = acc[i];
         }
-        const int row = 16 * (tile / NT) + r, col = n0 + 16 * (tile % NT) + 4 * kb;
+        const int row = 16 * tile + r, col = n0 + 4 * kb;
         if (row >= p.M) continue;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -529,7 +519,7 @@ static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
         constexpr int TYPE = decltype(type_c)::value;
         auto go = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
             constexpr int W = decltype(w_c)::value;
-            hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, 1, decltype(u_c)::value, W, TYPE, decltype(fused_c)::value>), dim3(static_cast<unsigned>((p.N + 15) / 16)),
+            hipLaunchKernelGGL((k_mx4_rows<decltype(mt_c)::value, decltype(u_c)::value, W, TYPE, decltype(fused_c)::value>), dim3(static_cast<unsigned>((p.N + 15) / 16)),
                                dim3(64 * W), 0, s, g);
         };
         auto sized = [&](auto mt_c, auto u_c, auto w_c, auto fused_c) {
