@@ -572,11 +572,7 @@ static int gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, in
     p.c = C;
     p.ldc = ldc;
     const bool parts = plan.splits > 1;
-    if (rider.count && (plan.rows || parts)) {                                           // no tiles, or several parts of them
-        const int rc = sum_launch(rider, type, s);
-        if (rc) return rc;
-        rider.count = 0;
-    }
+    if (rider.count && (plan.rows || parts)) return FXP_ERR_DIMS;                        // cannot be: see mx4_gemm_launch2
     if (plan.rows) return rows_launch({p, nullptr, 0, 0, 0}, false, type, s);
     if (parts) {
         p.c = ws;
@@ -615,7 +611,8 @@ int mx4_gemm_launch(const fxp_mx4& A, const fxp_mx4& B, int type, void* C, int64
     return gemm_launch(A, B, type, C, ldc, ws, Mx4Sum{}, nullptr, s);
 }
 
-// Two products, the first one's partial sums added up in the second's launch; both use ws only one after the other.
+// Two products, the first one's partial sums added up in the second's launch; both use ws only one after the other.  The second goes by whole tiles
+// then: where it has parts the first one's sum is a launch of its own, and a first contraction that is split has 1793 rows or more, which are the second's.
 int mx4_gemm_launch2(const fxp_mx4& A0, const fxp_mx4& B0, void* C0, const fxp_mx4& A1, const fxp_mx4& B1, void* C1, int type, void* ws, hipStream_t s) {
     Mx4Sum sum{};
     const bool alone = mx4_gemm_bytes(A1.rows, B1.rows, A1.cols) != 0;                   // the second wants the workspace too
