@@ -9,7 +9,7 @@
 
 namespace fxp {
 
-constexpr int kMxThreads = 256;
+constexpr int kMxThreads = 256, kMxTileRows = 32;       // of a tile of both copies, which is a panel wide
 
 struct Mx4Job {
     Mx4Map m;
@@ -64,17 +64,19 @@ __device__ inline uint32_t codes_of(const float (&x)[N], float f, const uint32_t
     }
 }
 
-// A wave's step is 32 rows x 64 columns, whole blocks of both copies; a lane has 4 x 8 elements of it.  A workgroup maps STEPS_R x STEPS_C steps; codes are put
-// together in LDS and leave in 16-byte pieces.
-// Bound by memory for nearest (8192 x 8192 in bf16: 54 us, 206 MB at 3.8 TB/s), by the vector ALU for stochastic rounding (12608 x 768 in fp32: 16.7 us, 44 instructions an element, 14 of
-// them Philox's, three quarters of the time).
-template <int TYPE, bool STOCH, int STEPS_R, int STEPS_C>
-__global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4)) void k_mx4_map(Mx4Jobs jobs, uint32_t key0, uint32_t key1) {
-    constexpr int BR = STEPS_R, BC = 2 * STEPS_C, TR = 32 * BR, TC = 32 * BC, kPad = 16, SQ = TC / 2 + kPad, ST = TR / 2 + kPad;
-    constexpr int kWaves = STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4, kMine = STEPS_R * STEPS_C / kWaves, kAll = 64 * kWaves;
-    static_assert(kMine * kWaves == STEPS_R * STEPS_C && kMxPanel % TR == 0 && kMxPanel % TC == 0, "tiles lie in one panel, waves have as many steps");
+// A wave has 32 rows x 64 columns, whole blocks of both copies, a lane 4 x 8 elements of it; the four waves of a workgroup lie side by side along a panel, so that lines of
+// q leave whole.  Codes are put together in LDS and leave in 16-byte pieces.
+// Bound by memory for nearest: 8192 x 8192 in bf16 43.5 us (206 MB at 4.7 TB/s) over six sets of tensors in turn, back to back; 36 over one set, which stays in the
+// Infinity Cache in part; 54 where each call is followed by the inverses of both copies, 268 MB of stores.  By the vector ALU for stochastic
+// rounding (12608 x 768 in fp32: 15.7 us over two sets, 17.5 over sixteen; 44 instructions an element, 14 of them Philox's and the rest the scales and codes of two copies,
+// are three quarters of the time).
+// Other tiles, over six sets and sixteen: the waves below each other 61.5 us and 17.4, two by two 47.8 and 17.4; two steps a wave 47.7 and 23.4, eight 55.8 and 31.9.
+template <int TYPE, bool STOCH>
+__global__ __launch_bounds__(kMxThreads) void k_mx4_map(Mx4Jobs jobs, uint32_t key0, uint32_t key1) {
+    constexpr int TR = kMxTileRows, TC = kMxPanel, BC = TC / kMxBlock, kPad = 16, SQ = TC / 2 + kPad, ST = TR / 2 + kPad;
+    static_assert(TR == kMxBlock && TC == kMxThreads, "a block of rows, a panel");
     __shared__ __attribute__((aligned(16))) uint8_t lq[TR * SQ], lt[TC * ST];
-    __shared__ uint8_t eq[TR * BC], et[TC * BR];
+    __shared__ uint8_t eq[TR * BC], et[TC];
     const Mx4Job& J = jobs.job[jobs.count > 1 && blockIdx.x >= jobs.job[1].first ? 1 : 0];
     const int tile = static_cast<int>(blockIdx.x - J.first);
     const int r0 = tile / J.tiles_c * TR, c0 = tile % J.tiles_c * TC;
@@ -85,8 +87,9 @@ __global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4
     using T = typename Elem<TYPE>::T;
     const T* const corner = static_cast<const T*>(J.m.x) + r0 * J.m.ld + c0;
 
-    auto load = [&](int n, float (&x)[4][8]) {
-        const int step = wave + kWaves * n, r = step / STEPS_C * 32 + 4 * rb, c = step % STEPS_C * 64 + 8 * cb;
+    const int r = 4 * rb, c = wave * 64 + 8 * cb;
+    float x[4][8];
+    auto load = [&] {           // a scope of its own: in line, loads and words are scheduled worse (12608 x 768 in fp32, stochastic, over sixteen sets 17.9 us, so 17.5)
         const T* const p = corner + r * J.m.ld + c;
         if (inside) {
 #pragma unroll
@@ -103,49 +106,36 @@ __global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4
             }
         }
     };
-    float x[4][8];
-    load(0, x);
+    load();
+    uint32_t add[4][8], sign[4][8];
+    if constexpr (STOCH) {
+        const uint64_t at = static_cast<uint64_t>(r0 + r) * static_cast<uint32_t>(cols) + static_cast<uint32_t>(c0 + c);
 #pragma unroll
-    for (int n = 0; n < kMine; ++n) {
-        float next[4][8];
-        if (n + 1 < kMine) load(n + 1, next);
-        const int step = wave + kWaves * n, br = step / STEPS_C, sc = step % STEPS_C;
-        uint32_t add[4][8], sign[4][8];
-        if constexpr (STOCH) {
-            const uint64_t at = static_cast<uint64_t>(r0 + br * 32 + 4 * rb) * static_cast<uint32_t>(cols) + static_cast<uint32_t>(c0 + sc * 64 + 8 * cb);
+        for (int i = 0; i < 4; ++i) {
+            adds_of_8(at + static_cast<uint64_t>(i) * static_cast<uint32_t>(cols), (cols & 3) == 0, sid0, sid1, key0, key1, add[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                adds_of_8(at + static_cast<uint64_t>(i) * static_cast<uint32_t>(cols), (cols & 3) == 0, sid0, sid1, key0, key1, add[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) sign[i][j] = __float_as_uint(x[i][j]) >> 28 & 8u;
-            }
+            for (int j = 0; j < 8; ++j) sign[i][j] = __float_as_uint(x[i][j]) >> 28 & 8u;
         }
-        if (want_q) {
+    }
+    if (want_q) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t m = 0;
+        for (int i = 0; i < 4; ++i) {
+            uint32_t m = 0;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m = max(m, magnitude(x[i][j]));
-                const int s = mx_scale_of(max_of_4(m)), row = br * 32 + 4 * rb + i;
-                *reinterpret_cast<uint32_t*>(&lq[row * SQ + sc * 32 + 4 * cb]) = codes_of<STOCH>(x[i], mx_inverse(s), add[i], sign[i]);
-                if ((cb & 3) == 0) eq[row * BC + 2 * sc + (cb >> 2)] = static_cast<uint8_t>(s);
-            }
+            for (int j = 0; j < 8; ++j) m = max(m, magnitude(x[i][j]));
+            const int s = mx_scale_of(max_of_4(m));
+            *reinterpret_cast<uint32_t*>(&lq[(r + i) * SQ + wave * 32 + 4 * cb]) = codes_of<STOCH>(x[i], mx_inverse(s), add[i], sign[i]);
+            if ((cb & 3) == 0) eq[(r + i) * BC + 2 * wave + (cb >> 2)] = static_cast<uint8_t>(s);
         }
-        if (want_t) {
+    }
+    if (want_t) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
-                const uint32_t a[4] = {add[0][j], add[1][j], add[2][j], add[3][j]}, g[4] = {sign[0][j], sign[1][j], sign[2][j], sign[3][j]};
-                const int s = mx_scale_of(max_over_8(max(max(magnitude(y[0]), magnitude(y[1])), max(magnitude(y[2]), magnitude(y[3]))))), col = sc * 64 + 8 * cb + j;
-                *reinterpret_cast<uint16_t*>(&lt[col * ST + br * 16 + 2 * rb]) = static_cast<uint16_t>(codes_of<STOCH>(y, mx_inverse(s), a, g));
-                if (rb == 0) et[col * BR + br] = static_cast<uint8_t>(s);
-            }
-        }
-        if (n + 1 < kMine) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[i][j] = next[i][j];
+        for (int j = 0; j < 8; ++j) {
+            const float y[4] = {x[0][j], x[1][j], x[2][j], x[3][j]};
+            const uint32_t a[4] = {add[0][j], add[1][j], add[2][j], add[3][j]}, g[4] = {sign[0][j], sign[1][j], sign[2][j], sign[3][j]};
+            const int s = mx_scale_of(max_over_8(max(max(magnitude(y[0]), magnitude(y[1])), max(magnitude(y[2]), magnitude(y[3])))));
+            *reinterpret_cast<uint16_t*>(&lt[(c + j) * ST + 2 * rb]) = static_cast<uint16_t>(codes_of<STOCH>(y, mx_inverse(s), a, g));
+            if (rb == 0) et[c + j] = static_cast<uint8_t>(s);
         }
     }
     __syncthreads();
@@ -157,7 +147,7 @@ __global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4
         out_scales += line * kMxRowScales;
         const int at = b0 % kMxPanel / kMxBlock, here = min(height, lines - l0) * width;
 #pragma unroll
-        for (int i0 = 0; i0 < height * width; i0 += kAll) {
+        for (int i0 = 0; i0 < height * width; i0 += kMxThreads) {
             const int i = i0 + static_cast<int>(threadIdx.x), l = i / width, p = i % width;
             if (i >= here) break;
             *reinterpret_cast<uint4*>(data + l * kMxRowBytes + (at + p) * 16) = *reinterpret_cast<const uint4*>(&codes[l * stride + p * 16]);
@@ -166,11 +156,12 @@ __global__ __launch_bounds__(64 * (STEPS_R * STEPS_C < 4 ? STEPS_R * STEPS_C : 4
     };
     using std::integral_constant;
     if (want_q) leave(lq, eq, SQ, integral_constant<int, TR>{}, integral_constant<int, BC>{}, r0, rows, c0, J.m.q, J.m.q_scales);
-    if (want_t) leave(lt, et, ST, integral_constant<int, TC>{}, integral_constant<int, BR>{}, c0, cols, r0, J.m.t, J.m.t_scales);
+    if (want_t) leave(lt, et, ST, integral_constant<int, TC>{}, integral_constant<int, 1>{}, c0, cols, r0, J.m.t, J.m.t_scales);
 }
 
-// Rows alone: a lane has eight elements of a row, a block is four lanes, a panel of a row half a wave; nothing goes through LDS (8192 x 8192 in bf16: 39 us, 172 MB at 4.4 TB/s;
-// through the tiles of both copies 52).
+// Rows alone: a lane has eight elements of a row, a block is four lanes, a panel of a row half a wave; nothing goes through LDS.  8192 x 8192 in bf16, nearest, over six sets of
+// tensors in turn 33.7 us, 172 MB at 5.1 TB/s, through the tiles of both copies 33.8; 12608 x 768 in fp32, stochastic, over sixteen sets 11.0 and 12.8; 3001 x 1003 in bf16,
+// stochastic 7.7 and 11.2.
 template <int TYPE, bool STOCH>
 __global__ __launch_bounds__(kMxThreads) void k_mx4_map_rows(Mx4Map m, int panels, int vec, uint32_t key0, uint32_t key1) {
     const int64_t piece = (int64_t{blockIdx.x} * kMxThreads + threadIdx.x) >> 5;        // a panel of a row, panel after panel of a row
@@ -204,8 +195,8 @@ __global__ __launch_bounds__(kMxThreads) void k_mx4_map_rows(Mx4Map m, int panel
 int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int rounding, hipStream_t s) {
     const uint32_t key0 = static_cast<uint32_t>(seed), key1 = static_cast<uint32_t>(seed >> 32);
     auto vec_of = [&](const Mx4Map& m) { return aligned(m.x, 16) && m.ld * elem_size(type) % 16 == 0; };
-    auto launch = [&](auto type_c, auto stoch_c, auto r_c, auto c_c) {
-        constexpr int SR = decltype(r_c)::value, SC = decltype(c_c)::value, TR = 32 * SR, TC = 64 * SC;
+    auto launch = [&](auto type_c, auto stoch_c) {
+        constexpr int TR = kMxTileRows, TC = kMxPanel;
         Mx4Jobs jobs{};
         int64_t tiles = 0;
         for (int i = 0; i < count; ++i) {
@@ -222,12 +213,10 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
         }
         if (tiles >= int64_t{1} << 24) return static_cast<int>(FXP_ERR_DIMS);          // 2^32 threads
         if (tiles == 0) return static_cast<int>(FXP_OK);
-        hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value, SR, SC>), dim3(static_cast<unsigned>(tiles)), dim3(64 * std::min(SR * SC, 4)), 0, s,
-                           jobs, key0, key1);
+        hipLaunchKernelGGL((k_mx4_map<decltype(type_c)::value, decltype(stoch_c)::value>), dim3(static_cast<unsigned>(tiles)), dim3(kMxThreads), 0, s, jobs, key0, key1);
         return launch_status();
     };
     auto sized = [&](auto type_c, auto stoch_c) {
-        using std::integral_constant;
         const int64_t pieces = maps[0].rows * mx_panels(maps[0].cols), blocks = (pieces * 32 + kMxThreads - 1) / kMxThreads;
         if (count == 1 && !maps[0].t && blocks < int64_t{1} << 24) {                   // 2^32 threads
             if (blocks == 0) return static_cast<int>(FXP_OK);
@@ -235,9 +224,7 @@ int mx4_map_launch(int type, const Mx4Map* maps, int count, uint64_t seed, int r
                                static_cast<int>(mx_panels(maps[0].cols)), vec_of(maps[0]), key0, key1);
             return launch_status();
         }
-        // One step a wave, side by side along a row: lines of q leave whole.  8192 x 8192 in bf16 to nearest 35.6 us and 12608 x 768 in fp32, stochastic 16.8, where four
-        // steps below each other take 40.2 / 16.4, two by two 37.4 / 16.7, two steps a wave 38.8 / 21.2, eight 45.7 / 32.2.
-        return launch(type_c, stoch_c, integral_constant<int, 1>{}, integral_constant<int, 4>{});
+        return launch(type_c, stoch_c);
     };
     auto typed = [&](auto type_c) {
         return rounding == FXP_ROUND_STOCHASTIC ? sized(type_c, std::true_type{}) : sized(type_c, std::false_type{});
