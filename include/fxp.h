@@ -481,8 +481,9 @@ int fxp_kv_attention(const fxp_kv_cache* cache, const fxp_kv_step* step, int typ
 /* ---- rotary positions ----
  * Pair i < rot / 2 of a head's elements stands for a point of the plane that is turned by position * f_i and stretched by `amplitude`:
  * (u, w) -> amplitude * (u cos - w sin, u sin + w cos).  Pairs are elements 2 i and 2 i + 1 (interleaved) or i and i + rot / 2; elements from rot
- * on stay as they are.  turns[i] is f_i as a fraction of a turn in units of 2^-64, modulo one turn: the angle of every 31-bit position is
- * exact to 2^-34 turns.  Host struct; rot even, 2 .. min(dim, FXP_ROTARY_MOST), 2^-126 <= amplitude < 1e30; turns [rot / 2] on the device, 8-byte aligned. */
+ * on stay as they are.  turns[i] is f_i as a fraction of a turn in units of 2^-64, modulo one turn: its product with a 31-bit position, modulo one turn, is
+ * the angle to 2^-34 turns.  fxp_rotary and the writer's queries take the 32 top bits of it (to 2^-32 turns), the writer's keys all.  Host struct; rot
+ * even, 2 .. min(dim, FXP_ROTARY_MOST), 2^-126 <= amplitude < 1e30; turns [rot / 2] on the device, 8-byte aligned. */
 #define FXP_ROTARY_MOST 1024
 #define FXP_ROTARY_ZERO 0x100       /* of fxp_rotary's `backward` */
 typedef struct fxp_rotation {

@@ -512,7 +512,17 @@ static int sum_launch(const Mx4Sum& r, int type, hipStream_t s) {
     return launch_status();
 }
 
-// as many panels of a workgroup in flight as leave room for two workgroups on a CU, where there are so many
+// U panels of a wave in flight, as many as leave room for two workgroups on a CU, where the contraction has more than 4 U (half of what a workgroup of eight waves holds then);
+// else one, of eight waves, of four up to four panels (one row by 1024 x 16384 4.6 us, of eight 4.8), of one for a single panel.  us, launches back to back, weights out of memory
+// (600 MB of them in turn), bf16, U in flight / one of eight waves; * what the rule takes:
+//             N = 4096, K = 4096  8192          16384         N = 16384, K = 4096  8192  16384
+//   1 row     5.5 / 5.2*   7.0* / 8.0    11.1* / 13.8  12.3 / 9.7*   18.5* / 17.7  33.3* / 31.6
+//   2 rows    6.0* / 5.5   9.5* / 9.1    15.1* / 16.8  13.0* / 10.4  23.6* / 18.4  39.1* / 33.2
+//   4 rows    7.6* / 6.3   12.6* / 10.7  21.2* / 21.3  16.7* / 11.7  31.2* / 21.2  50.2* / 38.7
+//   9 rows    4.4* / 4.5   6.0* / 6.3    9.3* / 10.0   10.0* / 9.1   17.8* / 18.0  33.4* / 33.0
+//   32 rows   5.5* / 5.0   8.3* / 7.2    14.1* / 11.7  13.0* / 12.3  22.5* / 22.2  40.9* / 41.4
+// So U in flight is worth it for one row, and up to 16, where B has few rows; for 2 to 4 and for 17 to 32 rows, and where B's rows alone make four workgroups a CU, one panel of
+// eight waves is as fast or faster.
 static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
     const Mx4Product& p = g.p;
     by_type(type, [&](auto type_c) {
@@ -535,7 +545,7 @@ static int rows_launch(const Mx4Rows& g, bool fused, int type, hipStream_t s) {
         else if (fused) sized(IC<1>{}, IC<3>{}, IC<8>{}, IC<4>{});
         else if (p.M <= 16) sized(IC<1>{}, IC<2>{}, IC<8>{}, IC<0>{});
         else if (p.M <= 32) sized(IC<2>{}, IC<2>{}, IC<4>{}, IC<0>{});
-        else if (p.M <= 48) sized(IC<3>{}, IC<1>{}, IC<4>{}, IC<0>{});          // 37 x 4100 x 9001 9.4 us, two panels a wave 10.8
+        else if (p.M <= 48) sized(IC<3>{}, IC<1>{}, IC<4>{}, IC<0>{});          // 37 x 4100 x 9001 back to back 9.2 us, two panels a wave 10.4; 37 x 4096 x 4096 4.4 and 4.2
         else sized(IC<4>{}, IC<1>{}, IC<4>{}, IC<0>{});
     });
     return launch_status();

@@ -2,7 +2,8 @@
 //
 // The angle of pair i at position p is p * f_i, f_i a fixed-point fraction of a turn with 64 bits behind the point: the product modulo 2^64 is the angle
 // modulo one turn, with an error of p * 2^-65 turns (2^-34 at the largest position), so that far positions cost no argument reduction and lose
-// nothing.  Its two top bits (after half a quarter is added) are the quarter, the rest an angle r in [-pi/4, pi/4), for which the Taylor series of
+// nothing.  In 32 bits the angle's lower half is cut off, up to 2^-32 turns: 1.5e-9 of the pair's length, where half a step of a cosine near one is 3e-8.  Its two top bits
+// (after half a quarter is added) are the quarter, the rest an angle r in [-pi/4, pi/4), for which the Taylor series of
 // sine and cosine are summed as far as their terms reach the last place: x^9 and x^10 in 32 bits (next terms 1.8e-9 and 1.2e-10 at pi/4, half a
 // step is 3e-8), x^15 and x^16 in 64 (next terms 4.6e-17 and 2e-18, half a step 5.6e-17).
 #pragma once

@@ -919,7 +919,8 @@ class Rotary:
     or elements dim / 2 apart; a head's elements from `dim` on stay.  scaling, for contexts longer than a model was trained with: "linear" (f / factor), "base"
     (base * factor ** (dim / (dim - 2)): the slowest pair becomes `factor` times slower) or "parts" (f where a pair makes `high` turns or more over the
     `original` tokens, f / factor where it makes `low` or fewer, in between in proportion).  amplitude: what turned elements are multiplied by.
-    frequencies: f itself, in place of all that."""
+    frequencies: f itself, in place of all that.  Made once a model: exact fractions and a copy to the device, under a millisecond for 64 pairs; rotary,
+    rotary_bwd and kv_append_rotary take as many positions and tensors with it as there are."""
 
     def __init__(self, dim, base=10000.0, interleaved=False, scaling=None, factor=1.0, original=0, low=1.0, high=32.0, amplitude=1.0, frequencies=None,
                  device="cuda"):
