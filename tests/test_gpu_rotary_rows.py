@@ -72,3 +72,21 @@ def test_weight_gradient_over_a_padded_batch(fxp):
     got, want = X.flatten(0, 1).T @ dq.flatten(0, 1), X[there].T @ dq[there]
     bound = X[there].abs().T @ dq[there].abs() * (40 * 2.0 ** -23)
     assert bool(((got - want).abs() <= bound + 2.0 ** -60).all())
+
+
+@pytest.mark.parametrize("outside", [False, True])
+@pytest.mark.parametrize("B, T, heads, dim, rot, kind", [(2, 301, 4, 128, 128, "bf16"), (1, 3, 300, 20, 12, "fp32"), (3, 70, 40, 64, 32, "fp16"), (70, 1, 7, 258, 64, "bf16"), (1, 9, 2, 4000, 1024, "fp32")])
+def test_many_rows_and_heads(fxp, B, T, heads, dim, rot, kind, outside):
+    """Several workgroups along tokens and heads: rows with a token are those of a call whose rows all have one, the others zeros."""
+    say("rotary, many rows", B, T, heads, dim, rot, kind, outside)
+    rope = fxp.Rotary(rot)
+    g = torch.Generator("cuda").manual_seed(T)
+    x = torch.randn((B, heads, T, dim) if outside else (B, T, heads, dim), device="cuda", generator=g).to(TYPES[kind])
+    x = x.transpose(1, 2) if outside else x
+    positions = torch.randint(0, 5000, (B, T), dtype=torch.int32, device="cuda", generator=g)
+    want = fxp.rotary_bwd(x, positions, rope)
+    gone = torch.rand((B, T), device="cuda", generator=g) < 0.4
+    want[gone] = 0
+    x = torch.where(gone[:, :, None, None], float("nan"), x)                # what such a row holds is not looked at
+    leave_nan(x.shape, x.dtype)
+    assert torch.equal(fxp.rotary_bwd(x, torch.where(gone, -1 - positions, positions), rope), want)
