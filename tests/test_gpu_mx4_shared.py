@@ -27,7 +27,7 @@ def test_neighbours_in_one_buffer(fxp):
     say("mx4, one buffer")
     rows, cols = 3, 64                                          # 384 bytes of codes, 24 of scales
     room = torch.zeros(8192, dtype=torch.uint8, device="cuda")
-    x = room[:3072].view(torch.float32).view(3, 256)[:, :cols]
+    x = room.view(torch.float32).as_strided((rows, cols), (256, 1))
     x.copy_(torch.randn((rows, cols), device="cuda"))
     value = x.clone()
     want = fxp.mx4_map(value, rounding=fxp.NEAREST)[0]
@@ -36,7 +36,7 @@ def test_neighbours_in_one_buffer(fxp):
         q = at(codes, scales)
         assert fxp.mx4_map(x, rounding=fxp.NEAREST, out=(q, None))[0] is q
         assert torch.equal(q.data, want.data) and torch.equal(q.scales, want.scales) and torch.equal(x, value)
-        y = room[:3072].view(torch.float32).view(3, 256)[:, 192:] if codes == 256 else room[5120:5888].view(torch.float32).view(3, 64)
+        y = room.view(torch.float32).as_strided((rows, cols), (256, 1), 192) if codes == 256 else room[5120:5888].view(torch.float32).view(3, 64)
         assert torch.equal(fxp.mx4_unmap(q, out=y), fxp.mx4_unmap(want)) and torch.equal(q.data, want.data) and torch.equal(q.scales, want.scales)
     for codes, scales in ((240, 640), (256, 1000 + 16), (656, 256), (2048, 4096), (4096, 2296)):
         q = at(codes, scales)
